@@ -1,7 +1,7 @@
 // Host side of the C ABI: configuration checks, the stash allocator, the per-micro-batch state machine
 // and the kernel sequence of forward / backward-p1 / backward-p2 for a LLaMa-like decoder stage.
-#include "../../include/tbp.h"
 #include "kernels.h"
+#include "entry.h"
 
 #include <algorithm>
 #include <atomic>
@@ -11,11 +11,9 @@
 #include <new>
 #include <vector>
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-tbp_status fail(tbp_status code, const char* fmt, ...) {
+tbp_status tbp::fail(tbp_status code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -23,13 +21,10 @@ tbp_status fail(tbp_status code, const char* fmt, ...) {
   return code;
 }
 
-#define TBP_HIP(expr)                                                                        \
-  do {                                                                                       \
-    hipError_t e__ = (expr);                                                                 \
-    if (e__ != hipSuccess) return fail(TBP_EDEVICE, "%s: %s", #expr, hipGetErrorString(e__)); \
-  } while (0)
+namespace {
 
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+using tbp::align_up;
+using tbp::fail;
 
 // ---- stash layout ------------------------------------------------------------------------------------
 // Tensors that backward-p2 consumes ("W" class: inputs and output derivatives of the linear layers) live in
