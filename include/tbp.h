@@ -286,6 +286,114 @@ tbp_status tbp_attention_p1(int dtype, int batch, int n_heads, int seq, int head
                             int ld_qkv, const void* out, const void* d_out, int ld_out, const float* lse, void* dqkv,
                             int ld_dqkv, void* scratch, void* stream);
 
+/* ---- operators for long contexts, the last stage and serving ----------------------------------------------------------
+ * Sliding-window attention with sinks (over a batch, and for one new token over a cache), rotary positions, log
+ * probabilities of tokens, the norm of all gradients with clipping.  They follow the rules at the top of this file; sizes
+ * here need not be multiples of anything unless said. */
+
+/* Attention in which query i of a sequence sees key j when j <= i and (j > i - window or j < sinks): the last `window`
+ * tokens, itself among them, and the first `sinks`.  window >= seq is plain causal attention.  bf16 storage, head_dim 64 or
+ * 128, n_kv_heads divides n_heads: query heads h * n_heads / n_kv_heads .. of key head h follow each other.
+ * qkv: device [batch*seq, ld_qkv], column blocks q [n_heads*head_dim] | k | v [n_kv_heads*head_dim each], q and k already
+ * rotated; out: device [batch*seq, ld_out]; lse: device [batch, n_heads, seq] fp32, as for tbp_attention_fwd.
+ * lengths: device [batch] int32 or NULL: tokens of each sequence (taken as 0 .. seq); rows behind them are padding, never
+ * read, and come out as zeros (lse: -infinity).  A token's row has to be finite: in a tile of 32 keys with one that a query
+ * sees, an infinite or NaN value row reaches that query.
+ * Limits: 0 <= seq <= 2^20, window >= 1, sinks >= 0; leading dimensions multiples of 8 below 2^22, tensors 16-byte aligned. */
+tbp_status tbp_window_attention_fwd(int dtype, int batch, int n_heads, int n_kv_heads, int seq, int head_dim, int window,
+                                    int sinks, const int32_t* lengths, const void* qkv, int ld_qkv, void* out, int ld_out,
+                                    float* lse, void* stream);
+/* Its backward-p1 (Section 3.1): dq | dk | dv into dqkv [batch*seq, ld_dqkv] (not rotated back; dk and dv are summed over the
+ * query heads that share them) from the forward's out and lse and d_out, which has out's leading dimension.  scratch: device,
+ * 256-byte aligned, >= tbp_window_attention_p1_scratch_bytes of the same sizes.  Results do not depend on timing. */
+size_t tbp_window_attention_p1_scratch_bytes(int batch, int n_heads, int n_kv_heads, int seq, int head_dim, int window, int sinks);
+tbp_status tbp_window_attention_p1(int dtype, int batch, int n_heads, int n_kv_heads, int seq, int head_dim, int window,
+                                   int sinks, const int32_t* lengths, const void* qkv, int ld_qkv, const void* out,
+                                   const void* d_out, int ld_out, const float* lse, void* dqkv, int ld_dqkv, void* scratch,
+                                   void* stream);
+
+/* A cache keeps the keys (and another one the values) of a batch of sequences: [batch, capacity, ld_cache] with
+ * n_kv_heads*head_dim columns.  Position p lies in row p when p < sinks and in row sinks + (p - sinks) % (capacity - sinks)
+ * otherwise: a cache that is long enough is a plain array, a shorter one keeps the sinks and the last capacity - sinks tokens.
+ *
+ * One new token per sequence: q [batch, ld_q] (rotated) against the keys that the token at position lengths[b] - 1 sees, itself
+ * among them (its key and value are in the cache already); of a window longer than capacity - sinks, what the cache keeps.
+ * out [batch, ld_out], lse [batch, n_heads] fp32.  lengths[b] <= 0: zeros, lse -infinity.  capacity > sinks.
+ * workspace: device, 256-byte aligned, >= tbp_window_decode_workspace_bytes of the same sizes (may be 0: NULL); nothing in it
+ * has to be initialised.  Types, head rules and alignment as above. */
+size_t tbp_window_decode_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks);
+tbp_status tbp_window_decode(int dtype, int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks,
+                             int capacity, const int32_t* lengths, const void* q, int ld_q, const void* cache_k,
+                             const void* cache_v, int ld_cache, void* out, int ld_out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Rotary positions.  Of every head the first rot_dim columns are turned in pairs, (i, i + rot_dim/2) or (2i, 2i + 1), by the
+ * angle position * theta_i; the others are passed on.  The table [n_pos, rot_dim/2] of (cos, sin) pairs fp32 has the format of
+ * tbp_rope_table's; theta_i = base^(-2i/rot_dim), scaled for contexts longer than those trained on:
+ *   LINEAR  theta_i / factor;
+ *   BASE    the base times factor^(rot_dim / (rot_dim - 2)): the slowest pair as with LINEAR, the fastest unchanged
+ *           (rot_dim > 2);
+ *   RAMP    theta_i ((1 - g) / factor + g) with g = clamp((n - low) / (high - low), 0, 1), n = original * theta_i / 2 pi the
+ *           turns of the pair over the original context: fast pairs stay, slow ones are interpolated.
+ * magnitude (0 stands for 1) scales cosines and sines. */
+typedef enum { TBP_ROTARY_PLAIN = 0, TBP_ROTARY_LINEAR = 1, TBP_ROTARY_BASE = 2, TBP_ROTARY_RAMP = 3 } tbp_rotary_scaling;
+typedef enum { TBP_ROTARY_HALF = 0, TBP_ROTARY_INTERLEAVED = 1 } tbp_rotary_layout;
+typedef struct {
+  int32_t scaling;          /* tbp_rotary_scaling */
+  float factor;             /* > 0 (not read for PLAIN) */
+  float low, high;          /* RAMP: turns, low < high */
+  float original;           /* RAMP: the original context's tokens, > 0 */
+  float magnitude;
+} tbp_rotary_scale;
+size_t tbp_rotary_table_bytes(int n_pos, int rot_dim);
+/* scale: host, NULL for PLAIN. */
+tbp_status tbp_rotary_table(int n_pos, int rot_dim, float base, const tbp_rotary_scale* scale, void* table, void* stream);
+/* y = the rotation of x, or its derivative (backward != 0: dx from dy, the transposed rotation).  x [rows, ld_x], y [rows, ld_y],
+ * the first n_heads*head_dim columns; y may be x itself (other overlaps not).  positions: device [rows] int32, or NULL: row % seq.
+ * A position outside the table makes the rotated columns NaN.  Any alignment of the element type; 16-byte alignment of rows
+ * and pieces is faster. */
+tbp_status tbp_rotary(int dtype, int rows, int n_heads, int head_dim, int rot_dim, int layout, const void* table, int n_pos,
+                      const int32_t* positions, int seq, int backward, const void* x, int ld_x, void* y, int ld_y, void* stream);
+/* n_new new tokens per sequence, at positions lengths[b] - n_new .. lengths[b] - 1 (lengths: device [batch] int32, the new ones
+ * counted): qkv [batch*n_new, ld_qkv] as for tbp_window_attention_fwd, not rotated; q leaves rotated in q_out [batch*n_new, ld_q], k
+ * rotated and v as it is go to the tokens' rows of the caches (of tokens that share a row, the last one's).  Tokens at negative positions
+ * do not exist: zeros in q_out, nothing stored.  The caches have qkv's type. */
+tbp_status tbp_rotary_append(int dtype, int batch, int n_new, int n_heads, int n_kv_heads, int head_dim, int rot_dim, int layout,
+                             const void* table, int n_pos, const int32_t* lengths, const void* qkv, int ld_qkv, void* q_out,
+                             int ld_q, void* cache_k, void* cache_v, int ld_cache, int capacity, int sinks, void* stream);
+
+/* Log probabilities over rows of logits [rows, vocab] (ld_logits, storage type): of the target token of every row, logp = x[target] -
+ * lse; entropy = -sum p log p; lse = log sum exp x; and the `top` (0 .. 64, at most vocab) most likely tokens in order, ties by the lower
+ * index: top_logp, top_ids [rows, top].  targets: device [rows] int32; one outside 0 .. vocab-1 is left out: logp 0.  logp, entropy, lse:
+ * device [rows] fp32.  A logit of -infinity has probability zero; a row of nothing else has lse = logp = -infinity, entropy 0, derivatives
+ * 0.  A NaN or +infinity makes its row's results NaN (top_ids -1).  workspace: device, 256-byte aligned, at least
+ * tbp_logprobs_workspace_bytes(rows, vocab, top) bytes (may be 0: NULL); nothing in it has to be initialised. */
+size_t tbp_logprobs_workspace_bytes(int rows, int vocab, int top);
+tbp_status tbp_logprobs(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets, float* logp,
+                        float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* workspace,
+                        size_t workspace_bytes, void* stream);
+/* The derivative of the logits, d_logits [rows, ld_d] in the storage type, from lse and entropy of the forward and the derivatives of
+ * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits. */
+tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
+                           const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
+                           int64_t ld_d, void* stream);
+/* Both in one pass, for derivatives that are known beforehand (a mean over the tokens: d_logp = -1 / tokens). */
+tbp_status tbp_logprobs_step(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
+                             const float* d_logp, const float* d_entropy, float* logp, float* entropy, float* lse, void* d_logits,
+                             int64_t ld_d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm over n gradient tensors (host arrays of device pointers and element counts; contiguous tensors of one dtype; counts may be 0)
+ * and the gradients scaled by max_norm / norm where norm > max_norm.  Sums of squares are fp64 and do not depend on timing.
+ * tbp_grad_sumsq leaves the sum of squares, device fp64: stages of a pipeline add theirs up and hand the total to tbp_grad_clip, which
+ * computes it itself when sumsq is NULL.  outs[i] (out_dtype) may be grads[i] itself: clipped in place, not touched where nothing is to be
+ * clipped.  norm (may be NULL): device fp32.  A norm that is not finite is reported and scales nothing.
+ * workspace: device, 256-byte aligned, >= tbp_grad_workspace_bytes(n). */
+size_t tbp_grad_workspace_bytes(int n);
+tbp_status tbp_grad_sumsq(int dtype, int n, const void* const* grads, const int64_t* counts, double* sumsq, void* workspace,
+                          void* stream);
+tbp_status tbp_grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,
+                         const double* sumsq, float max_norm, float* norm, void* workspace, void* stream);
+
 /* Measurement aid (no paper passage: it prices the hardware, not the method): a register-resident loop of
  * 32x32x16 bf16 MFMAs, blocks x 4 wavefronts x iters x 16 instructions = blocks*iters*2^21 FLOP, touching no memory
  * inside the loop.  What it sustains is the practical ceiling of the matrix pipes under the chip's power management,

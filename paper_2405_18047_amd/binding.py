@@ -111,6 +111,23 @@ def lib() -> C.CDLL:
         L.tbp_rmsnorm_p1_scratch_bytes.argtypes = [C.c_int]
         L.tbp_rmsnorm_gain_p2.argtypes = [C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 3
         L.tbp_rope_table_bytes.argtypes = [C.c_int, C.c_int]
+        i32, f32, i64, ptr, size = C.c_int, C.c_float, C.c_int64, C.c_void_p, C.c_size_t
+        L.tbp_window_attention_fwd.argtypes = [i32] * 8 + [ptr, ptr, i32, ptr, i32, ptr, ptr]
+        L.tbp_window_attention_p1_scratch_bytes.argtypes, L.tbp_window_attention_p1_scratch_bytes.restype = [i32] * 7, size
+        L.tbp_window_attention_p1.argtypes = [i32] * 8 + [ptr, ptr, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, ptr]
+        L.tbp_window_decode_workspace_bytes.argtypes, L.tbp_window_decode_workspace_bytes.restype = [i32] * 6, size
+        L.tbp_window_decode.argtypes = [i32] * 8 + [ptr, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, size, ptr]
+        L.tbp_rotary_table_bytes.argtypes, L.tbp_rotary_table_bytes.restype = [i32] * 2, size
+        L.tbp_rotary_table.argtypes = [i32, i32, f32, ptr, ptr, ptr]
+        L.tbp_rotary.argtypes = [i32] * 6 + [ptr, i32, ptr, i32, i32, ptr, i32, ptr, i32, ptr]
+        L.tbp_rotary_append.argtypes = [i32] * 8 + [ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]
+        L.tbp_logprobs_workspace_bytes.argtypes, L.tbp_logprobs_workspace_bytes.restype = [i32] * 3, size
+        L.tbp_logprobs.argtypes = [i32] * 3 + [ptr, i64, ptr, ptr, ptr, ptr, i32, ptr, ptr, ptr, size, ptr]
+        L.tbp_logprobs_p1.argtypes = [i32] * 3 + [ptr, i64] + [ptr] * 6 + [i64, ptr]
+        L.tbp_logprobs_step.argtypes = [i32] * 3 + [ptr, i64] + [ptr] * 7 + [i64, ptr, size, ptr]
+        L.tbp_grad_workspace_bytes.argtypes, L.tbp_grad_workspace_bytes.restype = [i32], size
+        L.tbp_grad_sumsq.argtypes = [i32, i32] + [ptr] * 5
+        L.tbp_grad_clip.argtypes = [i32] * 3 + [ptr] * 4 + [f32, ptr, ptr, ptr]
         _lib = L
     return _lib
 

@@ -221,6 +221,78 @@ inline int run_end(const int* mbs, int n, int i, int tokens) {
   return j;
 }
 
+// ---- sliding-window attention with sinks (bf16 storage, head_dim 64 or 128), see include/tbp.h ----------------------------------
+struct WindowShape { int batch, heads, kv_heads, seq, head_dim, window, sinks; };      // window, sinks at most seq (decode: at most capacity)
+// How the pass over the queries cuts the lists of (query head, query step) pairs of its key blocks of 128: those of the sinks into
+// sink_parts each, the others into other_parts; a block of more than one part leaves partial sums.
+struct WindowParts {
+  int blocks, sink_blocks, sink_parts, other_parts;
+  __host__ __device__ int workgroups() const { return sink_blocks * sink_parts + (blocks - sink_blocks) * other_parts; }
+  __host__ __device__ int cut_blocks() const { return (sink_parts > 1 ? sink_blocks : 0) + (other_parts > 1 ? blocks - sink_blocks : 0); }
+  __host__ __device__ int partials() const { return (sink_parts > 1 ? sink_blocks * sink_parts : 0) + (other_parts > 1 ? (blocks - sink_blocks) * other_parts : 0); }
+  __host__ __device__ int partial_of(int kb, int part) const {
+    if (kb < sink_blocks) return kb * sink_parts + part;
+    return (sink_parts > 1 ? sink_blocks * sink_parts : 0) + (kb - sink_blocks) * other_parts + part;
+  }
+};
+WindowParts window_parts(const WindowShape& w);
+size_t window_attention_p1_partial_bytes(const WindowShape& w);
+hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, void* out, long ld_out,
+                                float* lse, hipStream_t s);
+hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, const void* out,
+                               const void* d_out, long ld_out, const float* lse, void* dqkv, long ld_dqkv, float* delta,
+                               float* partial, hipStream_t s);
+int window_decode_splits(int batch, int kv_heads, int most_seen);
+hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths, const void* q, long ld_q, const void* cache_k,
+                         const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, float* part_o,
+                         float2* part_ml, hipStream_t s);
+
+// ---- rotary positions, see include/tbp.h ---------------------------------------------------------------------------------------
+enum { ROTARY_PLAIN = 0, ROTARY_LINEAR = 1, ROTARY_BASE = 2, ROTARY_RAMP = 3 };      // tbp_rotary_scaling
+struct RotaryScale { int kind; float factor, low, high, original, magnitude; };
+hipError_t rotary_table(int n_pos, int rot_dim, float base, const RotaryScale& sc, float2* table, hipStream_t s);
+struct RotaryParams {
+  const void* x; long ld_x; void* y; long ld_y;      // rows of heads of dh columns; y may be x
+  const float2* table; int n_pos;
+  const int* positions; int seq;                     // position of row r: positions[r], or r % seq
+  int rows, heads, dh, half, interleaved;            // half: rotated pairs of a head
+  float sgn;                                         // of the sines: -1 for the derivative
+  // append only: x's heads are q_heads of q, kv_heads of k, kv_heads of v
+  const int* lengths; int tokens_new, q_heads, kv_heads;
+  void* cache_k; void* cache_v; long ld_c; int capacity, sinks;
+  int units, groups; long items;                     // set by the launch
+};
+hipError_t rotary(int dtype, const RotaryParams& p, hipStream_t s);
+hipError_t rotary_append(int dtype, const RotaryParams& p, hipStream_t s);
+
+// ---- log probabilities of tokens, see include/tbp.h ------------------------------------------------------------------------------
+struct LogprobParams {
+  const void* logits; long ld; int rows, vocab;
+  const int* targets;
+  float* logp; float* entropy; float* lse;           // [rows]; written by the forward, read by p1 (entropy, lse)
+  int top; float* top_logp; int* top_ids;            // [rows, top]
+  const float* d_logp; const float* d_entropy;       // [rows]; d_entropy may be null
+  void* d_logits; long ld_d;
+};
+constexpr int kMaxTop = 64;
+hipError_t logprobs(int dtype, const LogprobParams& p, hipStream_t s);
+hipError_t logprobs_p1(int dtype, const LogprobParams& p, hipStream_t s);
+hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s);
+
+// ---- the norm over gradient tensors and clipping, see include/tbp.h --------------------------------------------------------------
+constexpr int kGradTable = 96;                       // tensors per launch (the table travels as a kernel argument)
+constexpr int kGradSums = 2048;                      // sums (workgroups) per launch
+struct GradTable {
+  int n, pieces;
+  const void* src[kGradTable]; void* dst[kGradTable];
+  int64_t count[kGradTable];
+  int first[kGradTable];                             // the tensor's first piece
+};
+hipError_t grad_sumsq(int dtype, int n, const void* const* grads, const int64_t* counts, double* sums, int* n_sums, hipStream_t s);
+hipError_t grad_sum(const double* sums, int n, double* out, hipStream_t s);
+hipError_t grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,
+                     const double* sums, int n_sums, float max_norm, float* norm, hipStream_t s);
+
 // Limits enforced by the host before any launch.
 inline int max_d_model(int dtype) { return dtype == 1 ? 8192 : 4096; }
 constexpr int kMaxSeq = 4096;

@@ -1,0 +1,1187 @@
+// Sliding-window attention with sinks for gfx950 (bf16 storage, fp32 accumulation, head_dim 64 or 128, grouped heads): forward,
+// backward-p1, and the form for one new token per sequence over a cache.
+//
+// Query i of a sequence of n tokens sees key j when j <= i and (j > i - window or j < sinks); tokens n .. S - 1 of a row of the
+// batch are padding: never read, zeros in every result (lse: -inf).  H query heads share KV key heads, H / KV = G each.
+// The orientation of the products, the row order that feeds the accumulators of one product into the next, and the LDS images are
+// those of the fused attention (attention.hip); what differs is which key blocks a query block meets (the blocks of the
+// sinks, then those of the window) and, in the pass over the queries, which (query head, query block) pairs a key block meets.
+#include "kernels.h"
+#include "gfx950.h"
+#include "head_tile.h"
+#include "rows.h"
+
+namespace tbp {
+
+// Rows at which sequence b ends.
+__device__ __forceinline__ int seq_end(const int* __restrict__ lengths, int b, int S) {
+  if (!lengths) return S;
+  const int n = __builtin_amdgcn_readfirstlane(lengths[b]);
+  return n < 0 ? 0 : n < S ? n : S;
+}
+
+// The 64-key blocks that the queries first .. last (last < n) meet: those of the sinks that lie before the window, then the window's.
+struct KeyBlocks {
+  int n_sink, win0, count;
+  __device__ __forceinline__ KeyBlocks(int first, int last, int window, int sinks) {
+    const int lo = first - window + 1;
+    win0 = lo > 0 ? lo >> 6 : 0;
+    const int seen_sinks = sinks < last + 1 ? sinks : last + 1;
+    const int js = (seen_sinks + 63) >> 6;
+    n_sink = js < win0 ? js : win0;
+    count = n_sink + (last >> 6) - win0 + 1;
+  }
+  __device__ __forceinline__ int key0(int j) const { return (j < n_sink ? j : win0 + j - n_sink) << 6; }
+};
+
+struct WinParams {
+  const bf16_t* qkv; long ld_qkv;      // [B*S, >= (H + 2 KV) DH]: q | k | v column blocks
+  bf16_t* out; long ld_out;            // [B*S, >= H*DH]
+  float* lse;                          // [B, H, S]: log2 of the row's sum of exp2(score * scale * log2 e)
+  const int* lengths;                  // [B] or nullptr
+  int B, H, KV, G, S, window, sinks;
+  float scale_log2e;
+};
+
+// Workgroup ids run over (sequence, key head) fastest, then over the query heads of the key head, query blocks slowest: the heads
+// that read the same keys then sit on one XCD (ids go round the 8 XCDs) wherever the number of key heads is a multiple of 8.
+struct HeadOf {
+  int b, h, hk;
+  __device__ __forceinline__ HeadOf(int x, int B, int KV, int G) {
+    const int u = x % (B * KV), gq = x / (B * KV);
+    b = u / KV;
+    hk = u - b * KV;
+    h = hk * G + gq;
+  }
+};
+
+// ------------------------------------------------------------------------------------------ forward
+// One workgroup = 4 waves x 32 queries of one (sequence, head); keys and values stream through LDS in blocks of 64, double-buffered,
+// K one block ahead of V, the scores of the next block computed beside the exponentials of this one in a pinned order.
+template <int DH, bool AHEAD, int SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_fwd_kernel(WinParams p) {
+  using HT = HeadTile<DH>;
+  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT, NT = 2 / SPLIT;
+  constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
+  constexpr int NCH = IMG / 1024 / 4;                 // copies per wave per operand per block
+
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  lds_u8* const lds = LDS_PTR(unsigned char, smem_raw);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+
+  const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qb = (int)gridDim.y - 1 - (int)blockIdx.y;             // last query blocks first: the first ones may have short windows
+  const HeadOf at((int)blockIdx.x, p.B, p.KV, p.G);
+  const int b = at.b, h = at.h;
+  const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
+  const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
+  const long tok0 = (long)b * p.S;
+  const int n = seq_end(p.lengths, b, p.S);
+  constexpr int LPR = DH / 8, RPI = 64 / LPR;                       // lanes per row and rows per wave-wide store
+  const int rl = lane / LPR, piece = lane % LPR;
+
+  if (q0 >= n) {                                                    // (uniform) nothing but padding
+    if (wk == 0) {
+      for (int r0 = 0; r0 < 32; r0 += RPI)
+        if (qw0 + r0 + rl < p.S) *reinterpret_cast<u32x4*>(p.out + (tok0 + qw0 + r0 + rl) * p.ld_out + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
+      if (g == 0 && query < p.S) p.lse[((long)b * p.H + h) * p.S + query] = -INFINITY;
+    }
+    return;
+  }
+  const int q_last = (q0 + BQ < n ? q0 + BQ : n) - 1;
+  const KeyBlocks kbs(q0, q_last, p.window, p.sinks);
+
+  const typename HT::Offsets fo = HT::offsets(lane);
+  // rows r0 .. of the sequence, at most `rows` of them and none from n on, as seen from column `col`
+  auto rows_desc = [&](int r0, int rows, long col) {
+    const int left = n - r0 < rows ? n - r0 : rows;
+    return make_desc(p.qkv + (tok0 + r0) * p.ld_qkv + col, (uint32_t)((left > 0 ? left : 0) * p.ld_qkv * 2));
+  };
+  // ---- the block's query rows: copied (coalesced) into the second slot, which nothing else uses until they have been read
+  {
+    const u32x4 dq = rows_desc(q0, BQ, (long)h * DH);
+#pragma unroll
+    for (int i = 0; i < 2 * NCH / SPLIT; i++) {
+      int row; unsigned go;
+      HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
+      dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dq, q0 + row < n ? go : kOob);
+    }
+  }
+  int c_row[NCH];
+  unsigned c_off[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; i++) HT::plan(wave + 4 * i, lane, p.ld_qkv, c_row[i], c_off[i]);
+  const int nblk = kbs.count;
+  const long kcol = (long)(p.H + at.hk) * DH, vcol = kcol + (long)p.KV * DH;
+  auto issue = [&](int j, int which) {      // which: 0 the K image, 1 the V image of block j
+    const int kv0 = kbs.key0(j);
+    const u32x4 desc = rows_desc(kv0, BKV, which ? vcol : kcol);
+    const uint32_t base = lds0 + (j & 1) * SLOT + which * IMG + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < NCH; i++) dma16(base + i * 4096, desc, (kv0 + c_row[i] < n) ? c_off[i] : kOob);
+  };
+
+  f32x16 ot[DT];
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) ot[t][e] = 0.f;
+  // m: reference point of the row's exponentials (the same in both lane halves); l: this lane half's share of the row sum
+  float m = -INFINITY, l[2] = {0.f, 0.f};
+
+  issue(0, 0);
+  issue(0, 1);
+  wait_vmem<0>();
+  __syncthreads();
+  bf16x8 qf[KS];                       // this lane's query row as B operand of S^T = K Q^T
+#pragma unroll
+  for (int s = 0; s < KS; s++) qf[s] = HT::rows_frag(lds + SLOT, fo, 32 * wq, s);
+  f32x16 sa[NT], sb[NT];               // S^T of the block whose softmax is in work, and of the next one
+  const int wk_rows = 32 * wk * HT::RB;          // (SPLIT 2: this wave's tile of the K and V images)
+  auto scores = [&](f32x16 (&st)[NT], lds_u8* kimg) {
+#pragma unroll
+    for (int kt = 0; kt < NT; kt++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) st[kt][e] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; s++)
+#pragma unroll
+      for (int kt = 0; kt < NT; kt++)
+        st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(HT::rows_frag(kimg, fo, 32 * kt, s), qf[s], st[kt], 0, 0, 0);
+  };
+  if constexpr (AHEAD) {
+    scores(sa, lds + wk_rows);
+    __syncthreads();                   // every wave has its query row: the second slot is free
+    if (nblk > 1) issue(1, 0);
+  }
+
+  auto block = [&](f32x16 (&st)[NT], f32x16 (&nx)[NT], int j) {
+    wait_vmem<0>();
+    __syncthreads();                   // K of block j + 1 and V of block j have landed; every wave is done with block j - 1
+    if (AHEAD ? j + 2 < nblk : j + 1 < nblk) issue(AHEAD ? j + 2 : j + 1, 0);      // (not AHEAD: K of block j has landed)
+    if (j + 1 < nblk) issue(j + 1, 1);
+    const int kv0 = kbs.key0(j) + 32 * wk;
+    if (kv0 > qw0 + 31) return;        // every key of the block is after every query of this wave
+    lds_u8* const kimg = lds + ((j + 1) & 1) * SLOT + wk_rows;   // (after the last block: an older one, whose scores nobody uses)
+    lds_u8* const vimg = lds + (j & 1) * SLOT + IMG + wk_rows;
+    const bool low = kv0 < qw0 + 32 - p.window && kv0 + 32 * NT > p.sinks;         // some query of this wave is past the window of some key
+    if (!AHEAD && low && kv0 >= p.sinks && kv0 + 32 * NT <= qw0 + 1 - p.window) return;      // ... and every query past that of every key
+    bf16x8 kf[2][NT];
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int s = 0; s < 2; s++)
+#pragma unroll
+        for (int kt = 0; kt < NT; kt++) kf[s][kt] = HT::rows_frag(kimg, fo, 32 * kt, s);
+    } else {
+      scores(st, lds + (j & 1) * SLOT + wk_rows);
+    }
+    if (low || kv0 + 32 * NT - 1 > qw0) {
+      const int hi = query - kv0 - 4 * g, lo = hi - p.window, sk = p.sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
+#pragma unroll
+      for (int kt = 0; kt < NT; kt++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const int r = 32 * kt + 8 * (e >> 2) + (e & 3);
+          st[kt][e] = (r > hi || (r <= lo && r >= sk)) ? -INFINITY : st[kt][e];
+        }
+    }
+    // The reference point m of the exponentials has to stay within a safe distance of the running maximum, not on it: it is moved
+    // (and what is accumulated rescaled) only when some query's maximum has risen by more than kSlack octaves above it.
+    constexpr float kSlack = 8.f;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < NT; kt++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) mx = fmaxf(mx, st[kt][e]);
+    mx *= p.scale_log2e;
+    if (__any(mx > m + kSlack)) {
+      const float mnew = fmaxf(m, fmaxf(mx, xor32(mx)));
+      // (a lane that is here because of its neighbours, while its own query has seen no key yet: -inf - -inf would make NaN of its zeros)
+      const float alpha = __builtin_amdgcn_exp2f(m - (mnew == -INFINITY ? 0.f : mnew));
+      l[0] *= alpha;
+      l[1] *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) ot[t][e] *= alpha;
+      m = mnew;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;         // (no key seen yet: zeros)
+    bf16x8 pb[2 * NT], vf[DT];
+    auto elements = [&](int e0, int e1) {               // exponentials of elements e0 .. e1 - 1 of the lane's 16 NT
+#pragma unroll
+      for (int e = e0; e < e1; e++) {
+        const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e >> 4][e & 15], p.scale_log2e, -ref));
+        st[e >> 4][e & 15] = pe;
+        l[e & 1] += pe;
+        if (e % 8 == 7) pb[e >> 3] = pack8(st[e >> 4], (e >> 3) & 1);
+      }
+    };
+    // MFMAs of the scores; elements done beside them, the rest beside all PV k-steps but the last
+    constexpr int NA = NT * KS, NE = 16 * NT, EA = NT == 2 ? 18 : 10, PK = 2 * NT, PE = PK - 1;
+    static_assert(EA >= 8 && EA + (NE - EA) / PE >= 16 && (NT == 1 || EA + (NE - EA) * 2 / PE >= 24), "P must be ready in time");
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int kt = 0; kt < NT; kt++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) nx[kt][e] = 0.f;
+    }
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < NA; i++) {
+        const int s = i / NT, kt = i % NT;
+        nx[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s & 1][kt], qf[s], nx[kt], 0, 0, 0);
+        if (s + 2 < KS) kf[s & 1][kt] = HT::rows_frag(kimg, fo, 32 * kt, s + 2);
+        if (i >= NA - DT) vf[i - (NA - DT)] = HT::cols_frag(vimg, fo, 0, 0, i - (NA - DT));
+        elements(EA * i / NA, EA * (i + 1) / NA);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < DT; t++) vf[t] = HT::cols_frag(vimg, fo, 0, 0, t);
+      elements(0, EA);
+    }
+#pragma unroll
+    for (int i = 0; i < PK * DT; i++) {
+      const int ku = i / DT, t = i % DT;
+      ot[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t], pb[ku], ot[t], 0, 0, 0);
+      if (ku < PE) vf[t] = HT::cols_frag(vimg, fo, 32 * ((ku + 1) >> 1), (ku + 1) & 1, t);
+      if (ku < PE) elements(EA + (NE - EA) * i / (PE * DT), EA + (NE - EA) * (i + 1) / (PE * DT));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  for (int j = 0; j < nblk; j += 2) {
+    block(sa, sb, j);
+    if (j + 1 < nblk) block(sb, sa, j + 1);
+  }
+
+  // ---- o = O^T / l, transposed back through LDS (rows padded against bank conflicts) and written as whole rows
+  __syncthreads();
+  constexpr int EROW = DH * 2 + 16;
+  static_assert(BQ * EROW <= 2 * SLOT, "the output tile must fit in the ring");
+  lds_u8* const erow = lds + 32 * wq * EROW;
+  float lq = (l[0] + l[1]) + xor32(l[0] + l[1]);
+  if constexpr (SPLIT == 2) {
+    // the two waves of a query: what the second one summed, brought to the common reference point, joins the first one's
+    static_assert(BQ * EROW + 1024 <= SLOT && QW * DT * 4096 <= SLOT, "output tile, statistics and partial sums side by side");
+    LDS_AS float* const part = reinterpret_cast<LDS_AS float*>(lds + SLOT) + wq * (DT * 1024);
+    LDS_AS float* const stat = reinterpret_cast<LDS_AS float*>(lds + BQ * EROW) + wq * 128;
+    if (wk == 1) {
+#pragma unroll
+      for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) part[(t * 16 + e) * 64 + lane] = ot[t][e];
+      stat[lane] = m;
+      stat[64 + lane] = lq;
+    }
+    __syncthreads();
+    if (wk == 1) return;
+    const float m1 = stat[lane], mc = fmaxf(m, m1);
+    const float f0 = __builtin_amdgcn_exp2f(m - mc), f1 = __builtin_amdgcn_exp2f(m1 - mc);
+    m = mc;
+    lq = lq * f0 + stat[64 + lane] * f1;
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) ot[t][e] = ot[t][e] * f0 + part[(t * 16 + e) * 64 + lane] * f1;
+  }
+  {
+    const bool live = query < n;                        // (padding: zeros, whatever the lane holds)
+    const float inv = 1.f / lq;
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+      for (int e4 = 0; e4 < 4; e4++) {
+        bf16x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = (bf16_t)(live ? ot[t][4 * e4 + r] * inv : 0.f);
+        *reinterpret_cast<LDS_AS bf16x4*>(erow + ql * EROW + (32 * t + 8 * e4 + 4 * g) * 2) = v;
+      }
+    if (g == 0 && query < p.S) p.lse[((long)b * p.H + h) * p.S + query] = live ? m + __builtin_amdgcn_logf(lq) : -INFINITY;
+  }
+  // (LDS operations of a wave execute in order: the reads below see this wave's own writes above)
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += RPI) {
+    const int qrow = qw0 + r0 + rl;
+    if (qrow < p.S)
+      *reinterpret_cast<u32x4*>(p.out + (tok0 + qrow) * p.ld_out + h * DH + 8 * piece) =
+          *reinterpret_cast<const LDS_AS u32x4*>(erow + (r0 + rl) * EROW + 16 * piece);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ backward-p1: dQ and delta
+// dQ = scale * dS K: oriented like the forward, per 32-key tile S^T and dP^T = V dO^T are rebuilt, dS^T = P^T (dP^T - delta) is fed into
+// dQ^T += K^T dS^T.  delta = rowsum(dout * out) of its queries is computed first and left for the pass over the queries.
+struct WinDqParams {
+  const bf16_t* qkv; long ld_qkv;
+  const bf16_t* dout; const bf16_t* out; long ld_do;
+  const float* lse;                    // [B, H, S]
+  float* delta;                        // [B*S, H]: written here for the tokens that are there
+  const int* lengths;
+  bf16_t* dqkv; long ld_dqkv;
+  int B, H, KV, G, S, window, sinks;
+  float scale, scale_log2e;
+};
+
+template <int DH, int SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_bwd_dq_kernel(WinDqParams p) {
+  using HT = HeadTile<DH>;
+  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT;
+  constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
+  constexpr int NCH = IMG / 1024 / 4;
+
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  lds_u8* const lds = LDS_PTR(unsigned char, smem_raw);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+
+  const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qb = (int)gridDim.y - 1 - (int)blockIdx.y;
+  const HeadOf at((int)blockIdx.x, p.B, p.KV, p.G);
+  const int b = at.b, h = at.h;
+  const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;
+  const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
+  const long tok0 = (long)b * p.S;
+  const int n = seq_end(p.lengths, b, p.S);
+  constexpr int LPR = DH / 8, RPI = 64 / LPR;
+  const int rl = lane / LPR, piece = lane % LPR;
+
+  if (q0 >= n) {
+    if (wk == 0)
+      for (int r0 = 0; r0 < 32; r0 += RPI)
+        if (qw0 + r0 + rl < p.S) *reinterpret_cast<u32x4*>(p.dqkv + (tok0 + qw0 + r0 + rl) * p.ld_dqkv + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
+    return;
+  }
+  const int q_last = (q0 + BQ < n ? q0 + BQ : n) - 1;
+  const KeyBlocks kbs(q0, q_last, p.window, p.sinks);
+
+  const typename HT::Offsets fo = HT::offsets(lane);
+  auto rows_desc = [&](const bf16_t* base, long ld, int r0, int rows, long col) {
+    const int left = n - r0 < rows ? n - r0 : rows;
+    return make_desc(base + (tok0 + r0) * ld + col, (uint32_t)((left > 0 ? left : 0) * ld * 2));
+  };
+  // ---- the block's query rows into the second slot and their output derivatives into the first (coalesced copies)
+  {
+    const u32x4 dq = rows_desc(p.qkv, p.ld_qkv, q0, BQ, (long)h * DH), dd = rows_desc(p.dout, p.ld_do, q0, BQ, (long)h * DH);
+#pragma unroll
+    for (int i = 0; i < 2 * NCH / SPLIT; i++) {
+      int row; unsigned go, gd;
+      HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
+      HT::plan(wave + 4 * i, lane, p.ld_do, row, gd);
+      const bool ok = q0 + row < n;
+      dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dq, ok ? go : kOob);
+      dma16(lds0 + (wave + 4 * i) * 1024, dd, ok ? gd : kOob);
+    }
+  }
+  int c_row[NCH];
+  unsigned c_off[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; i++) HT::plan(wave + 4 * i, lane, p.ld_qkv, c_row[i], c_off[i]);
+  const int nblk = kbs.count;
+  const long kcol = (long)(p.H + at.hk) * DH, vcol = kcol + (long)p.KV * DH;
+  auto issue = [&](int j) {
+    const int kv0 = kbs.key0(j);
+    const u32x4 dk = rows_desc(p.qkv, p.ld_qkv, kv0, BKV, kcol), dv = rows_desc(p.qkv, p.ld_qkv, kv0, BKV, vcol);
+    const uint32_t base = lds0 + (j & 1) * SLOT + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < NCH; i++) {
+      const unsigned off = (kv0 + c_row[i] < n) ? c_off[i] : kOob;
+      dma16(base + i * 4096, dk, off);
+      dma16(base + IMG + i * 4096, dv, off);
+    }
+  };
+  const bool qlive = query < n;
+  const float lse_q = qlive ? p.lse[((long)b * p.H + h) * p.S + query] : 0.f;
+
+  f32x16 dqt[DT];
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) dqt[t][e] = 0.f;
+
+  wait_vmem<0>();
+  __syncthreads();
+  bf16x8 qf[KS], dof[KS];            // this lane's query row and output-derivative row as B operands
+#pragma unroll
+  for (int s = 0; s < KS; s++) {
+    qf[s] = HT::rows_frag(lds + SLOT, fo, 32 * wq, s);
+    dof[s] = HT::rows_frag(lds, fo, 32 * wq, s);
+  }
+  __syncthreads();                   // every wave has its rows: both slots are free for the key blocks
+  issue(0);
+  // ---- delta: the block's rows of the output arrive in the second slot beside the first key block
+  {
+    const u32x4 dr = rows_desc(p.out, p.ld_do, q0, BQ, (long)h * DH);
+#pragma unroll
+    for (int i = 0; i < 2 * NCH / SPLIT; i++) {
+      int row; unsigned go;
+      HT::plan(wave + 4 * i, lane, p.ld_do, row, go);
+      dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dr, q0 + row < n ? go : kOob);
+    }
+  }
+  wait_vmem<0>();
+  __syncthreads();
+  float dl_q = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; s++) {
+    const bf16x8 o = HT::rows_frag(lds + SLOT, fo, 32 * wq, s);
+#pragma unroll
+    for (int i = 0; i < 8; i++) dl_q += (float)o[i] * (float)dof[s][i];
+  }
+  dl_q += xor32(dl_q);
+  if (qlive && g == 0 && wk == 0) p.delta[(tok0 + query) * p.H + h] = dl_q;
+  __syncthreads();                   // the second slot is free again
+  for (int j = 0; j < nblk; j++) {
+    wait_vmem<0>();
+    __syncthreads();                 // block j has landed; every wave is done with the other slot
+    if (j + 1 < nblk) issue(j + 1);
+    const int kv0 = kbs.key0(j);
+    lds_u8* const kimg = lds + (j & 1) * SLOT;
+    lds_u8* const vimg = kimg + IMG;
+    const int hi = query - kv0 - 4 * g, lo = hi - p.window, sk = p.sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
+#pragma unroll 1
+    for (int kt = SPLIT == 2 ? wk : 0; kt < (SPLIT == 2 ? wk + 1 : 2); kt++) {
+      const int t0 = kv0 + 32 * kt;  // (uniform over the wave) tiles that none of its queries sees a key of
+      if (t0 > qw0 + 31 || (t0 >= p.sinks && t0 + 32 <= qw0 + 1 - p.window)) continue;
+      const bool edge = t0 + 31 > qw0 || (t0 < qw0 + 32 - p.window && t0 + 32 > p.sinks);
+      f32x16 st, dp;
+#pragma unroll
+      for (int e = 0; e < 16; e++) { st[e] = 0.f; dp[e] = 0.f; }
+      // (the order is pinned: the compiler would fetch each fragment right before its MFMA)
+      constexpr int PF = 3;
+      bf16x8 kf[PF], vf[PF], ktf[DT];
+#pragma unroll
+      for (int s = 0; s < PF; s++) { kf[s] = HT::rows_frag(kimg, fo, 32 * kt, s); vf[s] = HT::rows_frag(vimg, fo, 32 * kt, s); }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; s++) {
+        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s % PF], qf[s], st, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s % PF], dof[s], dp, 0, 0, 0);
+        if (s + PF < KS) { kf[s % PF] = HT::rows_frag(kimg, fo, 32 * kt, s + PF); vf[s % PF] = HT::rows_frag(vimg, fo, 32 * kt, s + PF); }
+        if (s >= KS - DT) ktf[s - (KS - DT)] = HT::cols_frag(kimg, fo, 32 * kt, 0, s - (KS - DT));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e++) st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], p.scale_log2e, -lse_q));
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const int r = 32 * kt + 8 * (e >> 2) + (e & 3);
+          st[e] = (r > hi || (r <= lo && r >= sk)) ? 0.f : st[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e++) st[e] *= dp[e] - dl_q;    // dS^T
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+        const bf16x8 sb = pack8(st, u);
+#pragma unroll
+        for (int t = 0; t < DT; t++) {
+          dqt[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ktf[t], sb, dqt[t], 0, 0, 0);
+          if (u == 0) ktf[t] = HT::cols_frag(kimg, fo, 32 * kt, 1, t);     // the second k-step's fragment, behind the MFMA that used the first
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+
+  __syncthreads();
+  if constexpr (SPLIT == 2) {        // the two waves of a query add up, first the wave of the first tiles
+    LDS_AS float* const part = reinterpret_cast<LDS_AS float*>(lds) + wq * (DT * 1024);
+    static_assert(QW * DT * 4096 <= 2 * SLOT, "the partial sums must fit in the ring");
+    if (wk == 1) {
+#pragma unroll
+      for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) part[(t * 16 + e) * 64 + lane] = dqt[t][e];
+    }
+    __syncthreads();
+    if (wk == 0) {
+#pragma unroll
+      for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) dqt[t][e] += part[(t * 16 + e) * 64 + lane];
+    }
+    __syncthreads();
+    if (wk == 1) return;
+  }
+  constexpr int EROW = DH * 2 + 16;
+  static_assert(BQ * EROW <= 2 * SLOT, "the output tile must fit in the ring");
+  lds_u8* const erow = lds + 32 * wq * EROW;
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; e4++) {
+      bf16x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; r++) v[r] = (bf16_t)(qlive ? dqt[t][4 * e4 + r] * p.scale : 0.f);
+      *reinterpret_cast<LDS_AS bf16x4*>(erow + ql * EROW + (32 * t + 8 * e4 + 4 * g) * 2) = v;
+    }
+  // (LDS operations of a wave execute in order: the reads below see this wave's own writes above)
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += RPI) {
+    const int qrow = qw0 + r0 + rl;
+    if (qrow < p.S)
+      *reinterpret_cast<u32x4*>(p.dqkv + (tok0 + qrow) * p.ld_dqkv + h * DH + 8 * piece) =
+          *reinterpret_cast<const LDS_AS u32x4*>(erow + (r0 + rl) * EROW + 16 * piece);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ backward-p1: dK and dV
+// One workgroup = 128 keys of one (sequence, key head) and a part of the (query head of the group, 64-query step) pairs that see them,
+// walked as one list, so that dK and dV of shared heads add up in the accumulators.  The key blocks of the sinks are seen by every
+// later query, not just by a window of them: their lists are longer, and cut into parts of about the length of the
+// others'.  Lists are also cut where the key blocks alone are too few to fill the chip.  A key block of one part is written as it is;
+// the parts of others leave fp32 partial sums that a second launch adds up in order.
+// Roles of the waves as in the fused attention's pass: 4 "left" waves compute P and dS of their 32 keys and hand them over through
+// LDS, 4 "right" waves issue all copies and accumulate dV^T += dO^T P, dK^T += Q^T dS of one 32-query tile later.
+struct WinKvParams {
+  const bf16_t* qkv; long ld_qkv;
+  const bf16_t* dout; long ld_do;
+  const float* lse;
+  const float* delta;
+  const int* lengths;
+  bf16_t* dqkv; long ld_dqkv;
+  float* partial;                      // [B KV][sum of parts over the key blocks that are cut][2][128][DH]
+  int B, H, KV, G, S, window, sinks;
+  WindowParts parts;
+  float scale, scale_log2e;
+};
+
+template <int DH>
+__global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
+  using HT = HeadTile<DH>;
+  constexpr int KEYS = 128, KS = DH / 16, DT = DH / 32, BQ = 64, KB = KEYS / 32;
+  constexpr int IMG = BQ * HT::RB, SLOT = 2 * IMG + 1024;     // Q image, dO image, 64 x (lse, delta); three slots
+  constexpr int NCH = IMG / 1024 / 4;                         // copies per right wave and image
+  constexpr int OPS = 2 * NCH + 1;                            // vector-memory operations of one issue(), per right wave
+  constexpr int HAND = 4 * 4096;                              // one hand-over buffer: 4 wave pairs x 64 lanes x 64 bytes
+  constexpr int HALF = 32 * HT::RB;                           // the second tile's rows inside an image
+
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  lds_u8* const lds = LDS_PTR(unsigned char, smem_raw);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  lds_u8* const hand = lds + 3 * SLOT;
+
+  const int tid = threadIdx.x, lane = tid & 63, kl = lane & 31, g = lane >> 5;
+  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int right = wave8 >> 2, wave = wave8 & 3;             // role, and which 32 keys of the block
+  const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
+  const int y = (int)blockIdx.y;
+  const bool sink_block = y < p.parts.sink_blocks * p.parts.sink_parts;
+  const int np = sink_block ? p.parts.sink_parts : p.parts.other_parts;
+  const int yy = sink_block ? y : y - p.parts.sink_blocks * p.parts.sink_parts;
+  const int kb = yy / np + (sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
+  const int kv0 = kb * KEYS, kw0 = kv0 + 32 * wave, key = kw0 + kl;
+  const long tok0 = (long)b * p.S;
+  const int n = seq_end(p.lengths, b, p.S);
+  const typename HT::Offsets fo = HT::offsets(lane);
+  // steps of 64 queries that see the block, for each of the G query heads; this part's share of the G * nst pairs
+  const int step0 = kv0 / BQ, nq = (n + BQ - 1) / BQ;
+  int step1 = nq;
+  if (kv0 >= p.sinks && (long)kv0 + KEYS + p.window - 2 < n) step1 = (kv0 + KEYS + p.window - 2) / BQ + 1;
+  const int nst = step1 > step0 ? step1 - step0 : 0;
+  const int total = p.G * nst, share = (total + np - 1) / np;
+  const int i0 = part * share < total ? part * share : total, i1 = i0 + share < total ? i0 + share : total;
+  const int nt = 2 * (i1 - i0);                               // 32-query tiles
+  const int hq0 = nst ? i0 / nst : 0, sq0 = nst ? step0 + i0 - hq0 * nst : 0;      // the first pair
+  typedef LDS_AS float lds_f32;
+  lds_u8* const my_hand = hand + wave * 4096 + lane * 16;     // + buffer * HAND + 1024 * {p0, p1, s0, s1}
+  constexpr int KVIMG = KEYS * HT::RB;                        // image of the block's K (then V) rows
+  lds_u8* const kvimg = lds + 2 * SLOT;
+  static_assert(2 * KVIMG <= SLOT + 2 * HAND, "K and V images must fit in the third slot plus the hand-over area");
+  // 32 x 32 tiles of queries from q and keys from k of which no pair is seen; and of which every pair is
+  auto unseen = [&](int q, int k) { return q + 31 < k || (q - (k + 31) >= p.window && k >= p.sinks); };
+  auto whole = [&](int q, int k) { return q >= k + 31 && (q + 31 - k < p.window || k + 32 <= p.sinks); };
+
+  if (!right) {
+    // ------------------------------------------------------------------ left: S, dP, P, dS
+    bf16x8 kfb[KS], vfb[KS];
+    __syncthreads();                                          // the first two steps and the K / V rows have landed
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      kfb[s] = HT::rows_frag(kvimg, fo, 32 * wave, s);
+      vfb[s] = HT::rows_frag(kvimg + KVIMG, fo, 32 * wave, s);
+    }
+    __syncthreads();                                          // every left wave has its rows: the area is free again
+    int st_at = sq0;                                          // the step that tile `it` lies in
+    const int past = key >= p.sinks ? key + p.window : 0x7fffffff;      // the first query past the lane's key's window
+    for (int it = 0; it <= nt; it++) {
+      const int qt0 = st_at * BQ + 32 * (it & 1);
+      lds_u8* const out = my_hand + (it & 1) * HAND;
+      if (it < nt && unseen(qt0, kw0)) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) *reinterpret_cast<LDS_AS u32x4*>(out + 1024 * i) = u32x4{0, 0, 0, 0};
+      } else if (it < nt) {
+        lds_u8* const slot = lds + ((it >> 1) % 3) * SLOT;
+        lds_u8* const qimg = slot + (it & 1) * HALF;
+        lds_u8* const dimg = qimg + IMG;
+        const lds_f32* const stat = reinterpret_cast<const lds_f32*>(slot + 2 * IMG) + 32 * (it & 1);
+        f32x16 sa, da;
+#pragma unroll
+        for (int e = 0; e < 16; e++) { sa[e] = 0.f; da[e] = 0.f; }
+        constexpr int PF = KS < 4 ? KS : 4;
+        bf16x8 fq[KS], fd[KS];
+        f32x4 ls[4], dl[4];
+#pragma unroll
+        for (int s = 0; s < PF; s++) { fq[s] = HT::rows_frag(qimg, fo, 0, s); fd[s] = HT::rows_frag(dimg, fo, 0, s); }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+          if (s + PF < KS) { fq[s + PF] = HT::rows_frag(qimg, fo, 0, s + PF); fd[s + PF] = HT::rows_frag(dimg, fo, 0, s + PF); }
+          if (s >= KS - 4) {
+            const int e4 = s - (KS - 4);
+            ls[e4] = *reinterpret_cast<const LDS_AS f32x4*>(stat + 8 * e4 + 4 * g);
+            dl[e4] = *reinterpret_cast<const LDS_AS f32x4*>(stat + BQ + 8 * e4 + 4 * g);
+          }
+          sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[s], kfb[s], sa, 0, 0, 0);
+          da = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[s], vfb[s], da, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        // register e of the tile is query qt0 + 8 (e / 4) + 4 g + e % 4
+        float pv[16], sv[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++) pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[e], p.scale_log2e, -ls[e >> 2][e & 3]));
+        if (!whole(qt0, kw0)) {
+          const int lo = key - qt0 - 4 * g, hi = past - qt0 - 4 * g;
+#pragma unroll
+          for (int e = 0; e < 16; e++) {
+            const int r = 8 * (e >> 2) + (e & 3);
+            pv[e] = (r < lo || r >= hi) ? 0.f : pv[e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e++) sv[e] = pv[e] * (da[e] - dl[e >> 2][e & 3]);
+        bf16x8 kp[2], ks[2];
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+          for (int t = 0; t < 8; t++) { kp[u][t] = (bf16_t)pv[8 * u + t]; ks[u][t] = (bf16_t)sv[8 * u + t]; }
+        *reinterpret_cast<LDS_AS bf16x8*>(out) = kp[0];
+        *reinterpret_cast<LDS_AS bf16x8*>(out + 1024) = kp[1];
+        *reinterpret_cast<LDS_AS bf16x8*>(out + 2048) = ks[0];
+        *reinterpret_cast<LDS_AS bf16x8*>(out + 3072) = ks[1];
+      }
+      if (it & 1) st_at = st_at + 1 == step1 ? step0 : st_at + 1;
+      __syncthreads();
+    }
+    __syncthreads();                                          // every right wave's copies have landed: the ring is free
+    __syncthreads();                                          // the right waves have put dK and dV into LDS (below)
+    return;
+  }
+
+  // -------------------------------------------------------------------- right: copies, dV^T, dK^T
+  int c_row[NCH];
+  unsigned cq_off[NCH], cd_off[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; i++) {
+    HT::plan(wave + 4 * i, lane, p.ld_qkv, c_row[i], cq_off[i]);
+    HT::plan(wave + 4 * i, lane, p.ld_do, c_row[i], cd_off[i]);
+  }
+  // Called once for every pair in order.  Every call issues exactly OPS operations per wave (pairs past the end write zeros into their
+  // slot and fetch nothing), so a wait for "all but the last issue" is a fixed count.
+  int is_i = i0, is_h = hq0, is_st = sq0;
+  auto issue = [&] {
+    const bool live = is_i < i1;
+    const int q0 = live ? is_st * BQ : 0, h = hk * p.G + (live ? is_h : 0);
+    const uint32_t slot = lds0 + ((is_i - i0) % 3) * SLOT;
+    const int left = live ? (n - q0 < BQ ? n - q0 : BQ) : 0;
+    const u32x4 dq = make_desc(p.qkv + (tok0 + q0) * p.ld_qkv + (long)h * DH, (uint32_t)(left * p.ld_qkv * 2));
+    const u32x4 dd = make_desc(p.dout + (tok0 + q0) * p.ld_do + (long)h * DH, (uint32_t)(left * p.ld_do * 2));
+#pragma unroll
+    for (int c = 0; c < NCH; c++) {
+      const bool ok = c_row[c] < left;
+      dma16(slot + wave * 1024 + c * 4096, dq, ok ? cq_off[c] : kOob);
+      dma16(slot + IMG + wave * 1024 + c * 4096, dd, ok ? cd_off[c] : kOob);
+    }
+    // row statistics: wave 0 fetches lse[0..63], wave 1 delta[0..63]; waves 2 and 3 issue the same instruction out of range (nothing
+    // moves) to keep the count uniform.  (Rows past the end: zeros, which with zero rows of Q and dO add nothing.)
+    const u32x4 ds = (wave & 1) == 0 ? make_desc(p.lse + ((long)b * p.H + h) * p.S + q0, (uint32_t)(left * 4))
+                                     : make_desc(p.delta + (tok0 + q0) * p.H + h, (uint32_t)(left * p.H * 4));
+    const unsigned off = (wave < 2 && lane < left) ? (unsigned)((wave & 1) == 0 ? lane * 4 : lane * p.H * 4) : kOob;
+    dma4(slot + 2 * IMG + wave * 256, ds, off);
+    is_i++;
+    if (++is_st == step1) { is_st = step0; is_h++; }
+  };
+  // A right wave owns 32 head-dim columns (its index) of dV^T and dK^T for all four key blocks of the workgroup.  With head_dim 64 waves
+  // 2 and 3 have no columns and only copy.
+  f32x16 dvt[KB], dkt[KB];
+#pragma unroll
+  for (int t = 0; t < KB; t++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) { dvt[t][e] = 0.f; dkt[t][e] = 0.f; }
+  const bool has_cols = wave < DT;
+  int col0 = 0, col1 = 0;                                     // fragment offsets of this wave's column block
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+    if (t == wave) { col0 = fo.cols[t][0]; col1 = fo.cols[t][1]; }
+  auto my_cols = [&](lds_u8* img, int u) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_AS s16x4*>(img + col0 + 16 * u * HT::RB));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_AS s16x4*>(img + col1 + 16 * u * HT::RB));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  {  // the block's K and V rows, for the left waves
+    const int left = n - kv0 < KEYS ? n - kv0 : KEYS;         // (may be negative: no rows)
+    const bf16_t* kb0 = p.qkv + (tok0 + kv0) * p.ld_qkv + (long)(p.H + hk) * DH;
+    const uint32_t bytes = (uint32_t)((left > 0 ? left : 0) * p.ld_qkv * 2);
+    const u32x4 dk = make_desc(kb0, bytes), dv = make_desc(kb0 + (long)p.KV * DH, bytes);
+#pragma unroll
+    for (int i = 0; i < 2 * NCH; i++) {
+      int row; unsigned go;
+      HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
+      const unsigned off = row < left ? go : kOob;
+      dma16(lds0 + 2 * SLOT + (wave + 4 * i) * 1024, dk, off);
+      dma16(lds0 + 2 * SLOT + KVIMG + (wave + 4 * i) * 1024, dv, off);
+    }
+  }
+  issue();
+  issue();
+  wait_vmem<0>();
+  __syncthreads();
+  __syncthreads();                                            // the left waves have read their K and V rows
+  for (int it = 0; it <= nt; it++) {
+    if (it > 0) {
+      const int tile = it - 1;
+      if (has_cols) {
+        lds_u8* const qimg = lds + ((tile >> 1) % 3) * SLOT + (tile & 1) * HALF;
+        lds_u8* const dimg = qimg + IMG;
+        // this wave's 32 head-dim columns of dO^T and Q^T (two k-steps of 16 queries), then every key block's P and dS, each
+        // fetched one key block ahead of its MFMAs (pinned, as on the left)
+        bf16x8 fo_d[2], fo_q[2], kp[2][2], ks[2][2];
+        const lds_u8* const in = hand + (tile & 1) * HAND + lane * 16;
+        auto fetch = [&](int kbk) {
+#pragma unroll
+          for (int u = 0; u < 2; u++) {
+            kp[kbk & 1][u] = *reinterpret_cast<const LDS_AS bf16x8*>(in + kbk * 4096 + 1024 * u);
+            ks[kbk & 1][u] = *reinterpret_cast<const LDS_AS bf16x8*>(in + kbk * 4096 + 2048 + 1024 * u);
+          }
+        };
+#pragma unroll
+        for (int u = 0; u < 2; u++) { fo_d[u] = my_cols(dimg, u); fo_q[u] = my_cols(qimg, u); }
+        fetch(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kbk = 0; kbk < KB; kbk++) {
+          if (kbk + 1 < KB) fetch(kbk + 1);
+#pragma unroll
+          for (int u = 0; u < 2; u++) {
+            dvt[kbk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fo_d[u], kp[kbk & 1][u], dvt[kbk], 0, 0, 0);
+            dkt[kbk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fo_q[u], ks[kbk & 1][u], dkt[kbk], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    // Pair (it + 1) / 2 is what the left waves start at the next iteration, when `it` is odd: it was issued three barriers ago and only
+    // the issue after it may still be in flight
+    if (it & 1) wait_vmem<OPS>();
+    __syncthreads();
+    // after this barrier nobody reads the pair before it / 2 any more (it even): its slot takes pair it / 2 + 2
+    if (!(it & 1)) issue();
+  }
+  wait_vmem<0>();                                             // (copies past the end: zeros, no traffic)
+  __syncthreads();                                            // ... of every wave, before the ring is reused below
+
+  if (np > 1) {
+    // a part of the sums, dK unscaled: [2][128 keys][DH] fp32, 16 bytes per lane
+    const long idx = (long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, part);
+    float* const base = p.partial + idx * 2 * KEYS * DH;
+    if (has_cols) {
+#pragma unroll
+      for (int kbk = 0; kbk < KB; kbk++)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; e4++) {
+          float* const o = base + (long)(32 * kbk + kl) * DH + 32 * wave + 8 * e4 + 4 * g;
+          *reinterpret_cast<f32x4*>(o) = f32x4{dkt[kbk][4 * e4], dkt[kbk][4 * e4 + 1], dkt[kbk][4 * e4 + 2], dkt[kbk][4 * e4 + 3]};
+          *reinterpret_cast<f32x4*>(o + KEYS * DH) = f32x4{dvt[kbk][4 * e4], dvt[kbk][4 * e4 + 1], dvt[kbk][4 * e4 + 2], dvt[kbk][4 * e4 + 3]};
+        }
+    }
+    __syncthreads();                                          // (the left waves count two barriers behind the loop)
+    return;
+  }
+  // ---- dk = scale * dK^T transposed, dv = dV^T transposed, put together in LDS (the ring is free) and written as whole rows
+  constexpr int EROW = DH * 2 + 16;
+  lds_u8* const edk = lds;
+  lds_u8* const edv = lds + KEYS * EROW;
+  static_assert(2 * KEYS * EROW <= 3 * SLOT, "dK and dV tiles must fit in the ring");
+  if (has_cols) {
+#pragma unroll
+    for (int kbk = 0; kbk < KB; kbk++)
+#pragma unroll
+      for (int e4 = 0; e4 < 4; e4++) {
+        bf16x4 vk, vv;
+#pragma unroll
+        for (int r = 0; r < 4; r++) { vk[r] = (bf16_t)(dkt[kbk][4 * e4 + r] * p.scale); vv[r] = (bf16_t)dvt[kbk][4 * e4 + r]; }
+        const int off = (32 * kbk + kl) * EROW + (32 * wave + 8 * e4 + 4 * g) * 2;
+        *reinterpret_cast<LDS_AS bf16x4*>(edk + off) = vk;
+        *reinterpret_cast<LDS_AS bf16x4*>(edv + off) = vv;
+      }
+  }
+  __syncthreads();
+  {
+    constexpr int LPR = DH / 8, RPI = 64 / LPR;               // lanes per row, rows per wave-wide store
+    const int rl = lane / LPR, piece = lane % LPR;
+#pragma unroll
+    for (int r0 = 0; r0 < KEYS / 4; r0 += RPI) {
+      const int row = KEYS / 4 * wave + r0 + rl;              // this wave's quarter of the key rows
+      const int krow = kv0 + row;
+      if (krow < p.S) {
+        bf16_t* const out = p.dqkv + (tok0 + krow) * p.ld_dqkv + (long)(p.H + hk) * DH + 8 * piece;
+        *reinterpret_cast<u32x4*>(out) = *reinterpret_cast<const LDS_AS u32x4*>(edk + row * EROW + 16 * piece);
+        *reinterpret_cast<u32x4*>(out + (long)p.KV * DH) = *reinterpret_cast<const LDS_AS u32x4*>(edv + row * EROW + 16 * piece);
+      }
+    }
+  }
+}
+
+// dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 16 key rows of one of them; a thread has 8
+// columns of one row of dK or dV.
+template <int DH>
+__global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
+  constexpr int KEYS = 128, LPR = DH / 8, ROWS = 256 / (2 * LPR);
+  const int per = KEYS / ROWS, cut = (int)blockIdx.y / per;
+  const int kb = p.parts.sink_parts > 1 ? cut : cut + p.parts.sink_blocks;       // (blocks that are cut: the sinks', the others', or all)
+  const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
+  const int which = (int)threadIdx.x / (ROWS * LPR), t = (int)threadIdx.x % (ROWS * LPR);
+  const int row = ((int)blockIdx.y % per) * ROWS + t / LPR, col = 8 * (t % LPR);
+  const int np = kb < p.parts.sink_blocks ? p.parts.sink_parts : p.parts.other_parts;
+  const float* src = p.partial + ((long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, 0)) * 2 * KEYS * DH + (long)which * KEYS * DH + (long)row * DH + col;
+  float v[8] = {};
+  for (int i = 0; i < np; i++) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(src + (long)i * 2 * KEYS * DH), c = *reinterpret_cast<const f32x4*>(src + (long)i * 2 * KEYS * DH + 4);
+#pragma unroll
+    for (int k = 0; k < 4; k++) { v[k] += a[k]; v[4 + k] += c[k]; }
+  }
+  const int krow = kb * KEYS + row;
+  if (krow >= p.S) return;
+#pragma unroll
+  for (int k = 0; k < 8; k++) v[k] *= which ? 1.f : p.scale;
+  Vec<bf16_t>::store(p.dqkv + ((long)b * p.S + krow) * p.ld_dqkv + (long)(p.H + which * p.KV + hk) * DH + col, v);
+}
+
+// ------------------------------------------------------------------------------------------ one new token per sequence
+// Workgroup = one (sequence, key head, 32 query heads of its group) and a share of the keys that the new token sees, 4 waves that take
+// tiles of 32 keys in turn, each through a ring of its own in LDS: no barrier before the waves join.  S^T = K Q^T with the query heads
+// as columns (unused ones: zeros), then O^T += V^T P^T, as in the forward.  Bound by the reading of K and V: a tile is 16 KiB at
+// head_dim 128 and 16 MFMAs, a fifteenth of the time that it takes to arrive.
+// Seen keys are numbered v = 0 .. seen - 1: the sinks, then the window in order; number v lies in slot v (sinks) or
+// sinks + (first + v - n_sink) mod ring.
+struct WinDecodeParams {
+  const bf16_t* q; long ld_q;          // [B, >= H*DH]
+  const bf16_t* ck; const bf16_t* cv; long ld_c; long seq_stride;   // [B][capacity][>= KV*DH]
+  const int* lengths;
+  bf16_t* out; long ld_out;
+  float* lse;                          // [B, H]
+  float* part_o; float2* part_ml;      // [B, H, splits][DH], [B, H, splits] (splits > 1)
+  int B, H, KV, G, capacity, window, sinks, splits;
+  float scale_log2e;
+};
+
+// Asynchronous global -> LDS copy of 16 bytes per lane from a 64-bit address (a cache may be longer than a buffer descriptor's range).
+__device__ __forceinline__ void dma16_far(uint32_t lds_base, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(src) : "memory");
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
+  using HT = HeadTile<DH>;
+  constexpr int KS = DH / 16, DT = DH / 32, IMG = 32 * HT::RB, SLOT = 2 * IMG, NCH = IMG / 1024, RING = 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  lds_u8* const lds = LDS_PTR(unsigned char, smem_raw) + wave * (RING * SLOT);
+  const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)lds);
+  const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV, sp = (int)blockIdx.y, gq0 = (int)blockIdx.z * 32;
+  const int nh = p.G - gq0 < 32 ? p.G - gq0 : 32;              // query heads of this workgroup
+  const int h = hk * p.G + gq0 + ql;                           // this lane's (if ql < nh)
+  const int len = __builtin_amdgcn_readfirstlane(p.lengths[b]);
+  const int ring = p.capacity - p.sinks, reach = p.window < ring ? p.window : ring;
+  const int n_sink = len < p.sinks ? (len > 0 ? len : 0) : p.sinks;
+  const int first = len - reach > p.sinks ? len - reach : p.sinks;
+  const int seen = n_sink + (len > first ? len - first : 0);
+  const int r0 = (first - p.sinks) % ring;                     // ring place of the window's first key
+  const int tiles = (seen + 31) / 32, per = (tiles + p.splits - 1) / p.splits;
+  const int t0 = sp * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+
+  const typename HT::Offsets fo = HT::offsets(lane);
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; s++) {
+    qf[s] = bf16x8{};
+    if (ql < nh) qf[s] = *reinterpret_cast<const bf16x8*>(p.q + (long)b * p.ld_q + (long)h * DH + 16 * s + 8 * g);
+  }
+  const bf16_t* const kbase = p.ck + (long)b * p.seq_stride + (long)hk * DH;
+  const bf16_t* const vbase = p.cv + (long)b * p.seq_stride + (long)hk * DH;
+  // (numbers past the last read the last key's row: finite, and their probability is zero)
+  auto issue = [&](int t) {
+    const uint32_t base = lds0 + (((t - t0) >> 2) & (RING - 1)) * SLOT;
+#pragma unroll
+    for (int c = 0; c < NCH; c++) {
+      const int row = HT::RPC * c + lane / HT::GPRW, G16 = (lane % HT::GPRW) ^ HT::swz(row);
+      int v = 32 * t + row;
+      v = v < seen ? v : seen - 1;
+      int x = r0 + v - n_sink;
+      x = x >= ring ? x - ring : x;
+      const long off = (long)(v < n_sink ? v : p.sinks + x) * p.ld_c + 8 * G16;
+      dma16_far(base + c * 1024, kbase + off);
+      dma16_far(base + IMG + c * 1024, vbase + off);
+    }
+  };
+  f32x16 ot[DT];
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) ot[t][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  if (t0 + wave < t1) issue(t0 + wave);
+  for (int t = t0 + wave; t < t1; t += 4) {
+    if (t + 4 < t1) {
+      issue(t + 4);
+      wait_vmem<2 * NCH>();
+    } else {
+      wait_vmem<0>();
+    }
+    asm volatile("" ::: "memory");
+    lds_u8* const kimg = lds + (((t - t0) >> 2) & (RING - 1)) * SLOT;
+    lds_u8* const vimg = kimg + IMG;
+    f32x16 st;
+#pragma unroll
+    for (int e = 0; e < 16; e++) st[e] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; s++) st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(HT::rows_frag(kimg, fo, 0, s), qf[s], st, 0, 0, 0);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      if (32 * t + 32 > seen && 32 * t + 8 * (e >> 2) + (e & 3) + 4 * g >= seen) st[e] = -INFINITY;
+      mx = fmaxf(mx, st[e]);
+    }
+    mx *= p.scale_log2e;
+    const float mnew = fmaxf(m, fmaxf(mx, xor32(mx)));
+    const float ref = mnew == -INFINITY ? 0.f : mnew, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = mnew;
+    l *= alpha;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], p.scale_log2e, -ref));
+      l += st[e];
+    }
+#pragma unroll
+    for (int tt = 0; tt < DT; tt++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) ot[tt][e] *= alpha;
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      const bf16x8 pb = pack8(st, u);
+#pragma unroll
+      for (int tt = 0; tt < DT; tt++) ot[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(HT::cols_frag(vimg, fo, 0, u, tt), pb, ot[tt], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // every fragment of the slot has been read before copies into it start
+  }
+  l += xor32(l);
+  // ---- the four waves join (each leaves sums and statistics in its own part of the LDS, head by head)
+  constexpr int OROW = DH + 4;                                 // floats of a head's row
+  LDS_AS float* const mine = reinterpret_cast<LDS_AS float*>(lds);
+  static_assert(32 * OROW * 4 + 256 <= RING * SLOT, "a wave's sums must fit in its ring");
+#pragma unroll
+  for (int t = 0; t < DT; t++)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; e4++)
+      *reinterpret_cast<LDS_AS f32x4*>(mine + ql * OROW + 32 * t + 8 * e4 + 4 * g) = f32x4{ot[t][4 * e4], ot[t][4 * e4 + 1], ot[t][4 * e4 + 2], ot[t][4 * e4 + 3]};
+  if (g == 0) {
+    mine[32 * OROW + ql] = m;
+    mine[32 * OROW + 32 + ql] = l;
+  }
+  __syncthreads();
+  LDS_AS float* const all = reinterpret_cast<LDS_AS float*>(LDS_PTR(unsigned char, smem_raw));
+  constexpr int WSTRIDE = RING * SLOT / 4;
+  for (int i = (int)threadIdx.x; i < nh * (DH / 4); i += 256) {
+    const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
+    float mw[4], M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+      mw[w] = all[w * WSTRIDE + 32 * OROW + r];
+      M = fmaxf(M, mw[w]);
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+      const float f = __builtin_amdgcn_exp2f(mw[w] - (M == -INFINITY ? 0.f : M));
+      L += f * all[w * WSTRIDE + 32 * OROW + 32 + r];
+      const f32x4 x = *reinterpret_cast<LDS_AS f32x4*>(all + w * WSTRIDE + r * OROW + c);
+#pragma unroll
+      for (int k = 0; k < 4; k++) o[k] += f * x[k];
+    }
+    const long head = (long)b * p.H + hk * p.G + gq0 + r;
+    if (p.splits > 1) {
+      *reinterpret_cast<f32x4*>(p.part_o + (head * p.splits + sp) * DH + c) = o;
+      if (c == 0) p.part_ml[head * p.splits + sp] = make_float2(M, L);
+    } else {
+      const float inv = L > 0.f ? 1.f / L : 0.f;               // (no key seen: zeros)
+      bf16x4 v;
+#pragma unroll
+      for (int k = 0; k < 4; k++) v[k] = (bf16_t)(o[k] * inv);
+      *reinterpret_cast<bf16x4*>(p.out + (long)b * p.ld_out + (long)(hk * p.G + gq0 + r) * DH + c) = v;
+      if (c == 0) p.lse[head] = M + __builtin_amdgcn_logf(L);
+    }
+  }
+}
+
+// The shares of a head's keys join: one wave per head, 4 columns per lane (head_dim 64: lanes 0..15).
+template <int DH>
+__global__ __launch_bounds__(256) void window_decode_join_kernel(WinDecodeParams p) {
+  constexpr int LPH = DH / 4, HPB = 256 / LPH;
+  const long head = (long)blockIdx.x * HPB + threadIdx.x / LPH;
+  const int c = 4 * (threadIdx.x % LPH);
+  if (head >= (long)p.B * p.H) return;
+  float M = -INFINITY, L = 0.f;
+  for (int i = 0; i < p.splits; i++) M = fmaxf(M, p.part_ml[head * p.splits + i].x);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < p.splits; i++) {
+    const float2 ml = p.part_ml[head * p.splits + i];
+    const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
+    L += f * ml.y;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + (head * p.splits + i) * DH + c);
+#pragma unroll
+    for (int k = 0; k < 4; k++) o[k] += f * x[k];
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  bf16x4 v;
+#pragma unroll
+  for (int k = 0; k < 4; k++) v[k] = (bf16_t)(o[k] * inv);
+  *reinterpret_cast<bf16x4*>(p.out + head / p.H * p.ld_out + (head % p.H) * DH + c) = v;
+  if (c == 0) p.lse[head] = M + __builtin_amdgcn_logf(L);
+}
+
+// ------------------------------------------------------------------------------------------ launches
+template <int DH, bool AHEAD, int SPLIT>
+static hipError_t launch_fwd(const WinParams& p, hipStream_t s) {
+  constexpr size_t smem = 2 * 2 * 64 * DH * 2;
+  auto kern = window_fwd_kernel<DH, AHEAD, SPLIT>;
+  static AttrOnce once;
+  if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128)), dim3(256), smem, s, p);
+  return hipGetLastError();
+}
+
+hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, void* out, long ld_out,
+                                float* lse, hipStream_t s) {
+  WinParams p{};
+  p.qkv = (const bf16_t*)qkv; p.ld_qkv = ld_qkv; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.lengths = lengths;
+  p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.seq; p.window = w.window; p.sinks = w.sinks;
+  p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
+  const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
+  if (w.seq > 64 && groups <= 256) return w.head_dim == 128 ? launch_fwd<128, false, 2>(p, s) : launch_fwd<64, false, 2>(p, s);
+  if (w.seq <= 256) return w.head_dim == 128 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<64, false, 1>(p, s);
+  return w.head_dim == 128 ? launch_fwd<128, true, 1>(p, s) : launch_fwd<64, true, 1>(p, s);
+}
+
+template <int DH, int SPLIT>
+static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
+  constexpr size_t smem = 2 * 2 * 64 * DH * 2;
+  auto kern = window_bwd_dq_kernel<DH, SPLIT>;
+  static AttrOnce once;
+  if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128)), dim3(256), smem, s, p);
+  return hipGetLastError();
+}
+
+template <int DH>
+static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
+  constexpr size_t smem = 3 * (2 * 64 * DH * 2 + 1024) + 2 * 4 * 4096;       // three slots, two hand-over buffers
+  auto kern = window_bwd_kv_kernel<DH>;
+  static AttrOnce once;
+  if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.KV * p.B), (unsigned)p.parts.workgroups()), dim3(512), smem, s, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.parts.cut_blocks()) return e;
+  constexpr int per = 128 / (256 / (2 * (DH / 8)));
+  hipLaunchKernelGGL((window_bwd_join_kernel<DH>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+WindowParts window_parts(const WindowShape& w) {
+  WindowParts r{};
+  r.blocks = (w.seq + 127) / 128;
+  const int sinks = w.sinks < w.seq ? w.sinks : w.seq, G = w.heads / w.kv_heads;
+  r.sink_blocks = (sinks + 127) / 128;
+  const long all = (w.seq + 63) / 64, seen = ((long)w.window + 126 + 64) / 64 + 1;
+  const long sink_pairs = G * all, other_pairs = G * (seen < all ? seen : all);      // pairs of the longest lists
+  // parts: about 256 workgroups at least, where the lists are long enough for them (4 pairs a part)
+  const long groups = (long)w.batch * w.kv_heads * r.blocks;
+  long parts = groups < 256 ? (256 + groups - 1) / groups : 1;
+  if (parts > (other_pairs + 3) / 4) parts = (other_pairs + 3) / 4;
+  if (parts > 32) parts = 32;
+  r.other_parts = (int)parts;
+  const long share = (other_pairs + parts - 1) / parts;
+  long sp = (sink_pairs + share - 1) / share;
+  r.sink_parts = (int)(sp > 256 ? 256 : sp < 1 ? 1 : sp);
+  return r;
+}
+
+size_t window_attention_p1_partial_bytes(const WindowShape& w) {
+  const WindowParts r = window_parts(w);
+  return (size_t)w.batch * w.kv_heads * r.partials() * 2 * 128 * w.head_dim * sizeof(float);
+}
+
+hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, const void* out,
+                               const void* d_out, long ld_out, const float* lse, void* dqkv, long ld_dqkv, float* delta,
+                               float* partial, hipStream_t s) {
+  WinDqParams q{};
+  q.qkv = (const bf16_t*)qkv; q.ld_qkv = ld_qkv; q.dout = (const bf16_t*)d_out; q.out = (const bf16_t*)out; q.ld_do = ld_out;
+  q.lse = lse; q.delta = delta; q.lengths = lengths; q.dqkv = (bf16_t*)dqkv; q.ld_dqkv = ld_dqkv;
+  q.B = w.batch; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.seq; q.window = w.window; q.sinks = w.sinks;
+  q.scale = 1.f / sqrtf((float)w.head_dim);
+  q.scale_log2e = 1.4426950408889634f * q.scale;
+  const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
+  hipError_t e;
+  if (groups <= 256) e = w.head_dim == 128 ? launch_dq<128, 2>(q, s) : launch_dq<64, 2>(q, s);
+  else e = w.head_dim == 128 ? launch_dq<128, 1>(q, s) : launch_dq<64, 1>(q, s);
+  if (e != hipSuccess) return e;
+  WinKvParams p{};
+  p.qkv = q.qkv; p.ld_qkv = ld_qkv; p.dout = q.dout; p.ld_do = ld_out; p.lse = lse; p.delta = delta; p.lengths = lengths;
+  p.dqkv = q.dqkv; p.ld_dqkv = ld_dqkv; p.partial = partial;
+  p.B = q.B; p.H = q.H; p.KV = q.KV; p.G = q.G; p.S = q.S; p.window = q.window; p.sinks = q.sinks;
+  p.parts = window_parts(w);
+  p.scale = q.scale; p.scale_log2e = q.scale_log2e;
+  return w.head_dim == 128 ? launch_kv<128>(p, s) : launch_kv<64>(p, s);
+}
+
+int window_decode_splits(int batch, int kv_heads, int most_seen) {
+  const long groups = (long)batch * kv_heads;
+  long splits = (512 + groups - 1) / groups;
+  const long tiles = (most_seen + 31) / 32;
+  if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;      // two tiles per wave at least
+  return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+}
+
+template <int DH>
+static hipError_t launch_decode(const WinDecodeParams& p, hipStream_t s) {
+  constexpr size_t smem = 4 * 2 * 2 * 32 * DH * 2;
+  auto kern = window_decode_kernel<DH>;
+  static AttrOnce once;
+  if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.B * p.KV), (unsigned)p.splits, (unsigned)((p.G + 31) / 32)), dim3(256), smem, s, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
+  constexpr int HPB = 256 / (DH / 4);
+  hipLaunchKernelGGL((window_decode_join_kernel<DH>), dim3((unsigned)(((long)p.B * p.H + HPB - 1) / HPB)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths, const void* q, long ld_q, const void* cache_k,
+                         const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, float* part_o,
+                         float2* part_ml, hipStream_t s) {
+  WinDecodeParams p{};
+  p.q = (const bf16_t*)q; p.ld_q = ld_q; p.ck = (const bf16_t*)cache_k; p.cv = (const bf16_t*)cache_v; p.ld_c = ld_cache;
+  p.seq_stride = (long)capacity * ld_cache;
+  p.lengths = lengths; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.part_o = part_o; p.part_ml = part_ml;
+  p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.capacity = capacity; p.window = w.window;
+  p.sinks = w.sinks; p.splits = splits;
+  p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
+  return w.head_dim == 128 ? launch_decode<128>(p, s) : launch_decode<64>(p, s);
+}
+
+}  // namespace tbp
