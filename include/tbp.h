@@ -319,8 +319,9 @@ tbp_status tbp_window_attention_p1(int dtype, int batch, int n_heads, int n_kv_h
  * One new token per sequence: q [batch, ld_q] (rotated) against the keys that the token at position lengths[b] - 1 sees, itself
  * among them (its key and value are in the cache already); of a window longer than capacity - sinks, what the cache keeps.
  * out [batch, ld_out], lse [batch, n_heads] fp32.  lengths[b] <= 0: zeros, lse -infinity.  capacity > sinks.
- * workspace: device, 256-byte aligned, >= tbp_window_decode_workspace_bytes of the same sizes (may be 0: NULL); nothing in it
- * has to be initialised.  Types, head rules and alignment as above. */
+ * workspace: device, 256-byte aligned, >= tbp_window_decode_workspace_bytes of the same sizes (may be 0: NULL), all zeros before the
+ * first call with it; every call leaves it fit for the next one of the same sizes.  Calls that share one must not overlap.  Types, head
+ * rules and alignment as above. */
 size_t tbp_window_decode_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks);
 tbp_status tbp_window_decode(int dtype, int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks,
                              int capacity, const int32_t* lengths, const void* q, int ld_q, const void* cache_k,
@@ -366,12 +367,9 @@ tbp_status tbp_rotary_append(int dtype, int batch, int n_new, int n_heads, int n
  * lse; entropy = -sum p log p; lse = log sum exp x; and the `top` (0 .. 64, at most vocab) most likely tokens in order, ties by the lower
  * index: top_logp, top_ids [rows, top].  targets: device [rows] int32; one outside 0 .. vocab-1 is left out: logp 0.  logp, entropy, lse:
  * device [rows] fp32.  A logit of -infinity has probability zero; a row of nothing else has lse = logp = -infinity, entropy 0, derivatives
- * 0.  A NaN or +infinity makes its row's results NaN (top_ids -1).  workspace: device, 256-byte aligned, at least
- * tbp_logprobs_workspace_bytes(rows, vocab, top) bytes (may be 0: NULL); nothing in it has to be initialised. */
-size_t tbp_logprobs_workspace_bytes(int rows, int vocab, int top);
+ * 0.  A NaN or +infinity makes its row's results NaN (top_ids -1). */
 tbp_status tbp_logprobs(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets, float* logp,
-                        float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* workspace,
-                        size_t workspace_bytes, void* stream);
+                        float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* stream);
 /* The derivative of the logits, d_logits [rows, ld_d] in the storage type, from lse and entropy of the forward and the derivatives of
  * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits. */
 tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
@@ -380,7 +378,7 @@ tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, i
 /* Both in one pass, for derivatives that are known beforehand (a mean over the tokens: d_logp = -1 / tokens). */
 tbp_status tbp_logprobs_step(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
                              const float* d_logp, const float* d_entropy, float* logp, float* entropy, float* lse, void* d_logits,
-                             int64_t ld_d, void* workspace, size_t workspace_bytes, void* stream);
+                             int64_t ld_d, void* stream);
 
 /* The norm over n gradient tensors (host arrays of device pointers and element counts; contiguous tensors of one dtype; counts may be 0)
  * and the gradients scaled by max_norm / norm where norm > max_norm.  Sums of squares are fp64 and do not depend on timing.

@@ -121,10 +121,9 @@ def lib() -> C.CDLL:
         L.tbp_rotary_table.argtypes = [i32, i32, f32, ptr, ptr, ptr]
         L.tbp_rotary.argtypes = [i32] * 6 + [ptr, i32, ptr, i32, i32, ptr, i32, ptr, i32, ptr]
         L.tbp_rotary_append.argtypes = [i32] * 8 + [ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]
-        L.tbp_logprobs_workspace_bytes.argtypes, L.tbp_logprobs_workspace_bytes.restype = [i32] * 3, size
-        L.tbp_logprobs.argtypes = [i32] * 3 + [ptr, i64, ptr, ptr, ptr, ptr, i32, ptr, ptr, ptr, size, ptr]
+        L.tbp_logprobs.argtypes = [i32] * 3 + [ptr, i64, ptr, ptr, ptr, ptr, i32, ptr, ptr, ptr]
         L.tbp_logprobs_p1.argtypes = [i32] * 3 + [ptr, i64] + [ptr] * 6 + [i64, ptr]
-        L.tbp_logprobs_step.argtypes = [i32] * 3 + [ptr, i64] + [ptr] * 7 + [i64, ptr, size, ptr]
+        L.tbp_logprobs_step.argtypes = [i32] * 3 + [ptr, i64] + [ptr] * 7 + [i64, ptr]
         L.tbp_grad_workspace_bytes.argtypes, L.tbp_grad_workspace_bytes.restype = [i32], size
         L.tbp_grad_sumsq.argtypes = [i32, i32] + [ptr] * 5
         L.tbp_grad_clip.argtypes = [i32] * 3 + [ptr] * 4 + [f32, ptr, ptr, ptr]
@@ -142,7 +141,9 @@ def tbp_version() -> str:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """torch's current stream of the current device (torch.cuda.current_stream().cuda_stream, without the Python object in
+    between: 0.2 us for 2.7)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dt(t: torch.Tensor) -> int:

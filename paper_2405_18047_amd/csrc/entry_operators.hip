@@ -87,14 +87,22 @@ tbp_status tbp_window_attention_p1(int dtype, int batch, int n_heads, int n_kv_h
   return TBP_OK;
 }
 
-static long most_seen(int window, int sinks) { return (long)window + sinks; }
+// The decode workspace: counters of finished shares (zero between calls), then the shares' sums and statistics.
+struct DecodeSpace { int splits; size_t part_o, part_ml, bytes; };
+static DecodeSpace decode_space(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks) {
+  DecodeSpace d{};
+  d.splits = tbp::window_decode_splits(batch, n_kv_heads, (long)window + sinks);
+  const size_t parts = (size_t)batch * n_heads * d.splits, groups = (n_heads / n_kv_heads + 31) / 32;
+  d.part_o = align_up((size_t)batch * n_kv_heads * groups * sizeof(unsigned), 256);
+  d.part_ml = d.part_o + align_up(parts * head_dim * sizeof(float), 256);
+  d.bytes = d.part_ml + parts * sizeof(float2);
+  return d;
+}
 
 size_t tbp_window_decode_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks) {
   if (batch < 1 || check_window(TBP_BF16, batch, n_heads, n_kv_heads, 0, head_dim, window, sinks) != TBP_OK) return 0;
-  const int splits = tbp::window_decode_splits(batch, n_kv_heads, most_seen(window, sinks));
-  if (splits == 1) return 0;
-  const size_t parts = (size_t)batch * n_heads * splits;
-  return align_up(parts * head_dim * sizeof(float), 256) + parts * sizeof(float2);
+  const DecodeSpace d = decode_space(batch, n_heads, n_kv_heads, head_dim, window, sinks);
+  return d.splits == 1 ? 0 : d.bytes;
 }
 
 tbp_status tbp_window_decode(int dtype, int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks,
@@ -111,15 +119,13 @@ tbp_status tbp_window_decode(int dtype, int batch, int n_heads, int n_kv_heads, 
   if (check_ld("ld_cache", ld_cache, (long)n_kv_heads * head_dim) != TBP_OK) return TBP_EINVAL;
   if (misaligned(q, 16) || misaligned(cache_k, 16) || misaligned(cache_v, 16) || misaligned(out, 16))
     return fail(TBP_EINVAL, "tensors must be 16-byte aligned");
-  const size_t need = tbp_window_decode_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, window, sinks);
-  if (need && (!workspace || misaligned(workspace, 256) || workspace_bytes < need))
-    return fail(TBP_EINVAL, "workspace must be 256-byte aligned and have %zu bytes", need);
-  const int splits = tbp::window_decode_splits(batch, n_kv_heads, most_seen(window, sinks));
-  float* const part_o = static_cast<float*>(workspace);
-  float2* const part_ml = need ? reinterpret_cast<float2*>(static_cast<char*>(workspace) +
-                                                           align_up((size_t)batch * n_heads * splits * head_dim * sizeof(float), 256)) : nullptr;
+  const DecodeSpace d = decode_space(batch, n_heads, n_kv_heads, head_dim, window, sinks);
+  if (d.splits > 1 && (!workspace || misaligned(workspace, 256) || workspace_bytes < d.bytes))
+    return fail(TBP_EINVAL, "workspace must be 256-byte aligned and have %zu bytes", d.bytes);
+  char* const ws = static_cast<char*>(d.splits > 1 ? workspace : nullptr);
   TBP_HIP(tbp::window_decode(tbp::WindowShape{batch, n_heads, n_kv_heads, 0, head_dim, window, sinks}, capacity, lengths, q, ld_q,
-                             cache_k, cache_v, ld_cache, out, ld_out, lse, splits, part_o, part_ml, stream_of(stream)));
+                             cache_k, cache_v, ld_cache, out, ld_out, lse, d.splits, reinterpret_cast<unsigned*>(ws),
+                             reinterpret_cast<float*>(ws + d.part_o), reinterpret_cast<float2*>(ws + d.part_ml), stream_of(stream)));
   return TBP_OK;
 }
 
@@ -209,25 +215,12 @@ static tbp_status check_logits(int dtype, int rows, int vocab, const void* logit
   return TBP_OK;
 }
 
-size_t tbp_logprobs_workspace_bytes(int rows, int vocab, int top) {
-  (void)rows; (void)vocab; (void)top;
-  return 0;
-}
-
-static tbp_status check_workspace(size_t need, const void* workspace, size_t bytes) {
-  if (need && (!workspace || misaligned(workspace, 256) || bytes < need))
-    return fail(TBP_EINVAL, "workspace must be 256-byte aligned and have %zu bytes", need);
-  return TBP_OK;
-}
-
 tbp_status tbp_logprobs(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets, float* logp,
-                        float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* workspace,
-                        size_t workspace_bytes, void* stream) {
+                        float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* stream) {
   if (check_logits(dtype, rows, vocab, logits, ld_logits) != TBP_OK) return TBP_EINVAL;
   if (top < 0 || top > tbp::kMaxTop || top > vocab) return fail(TBP_EINVAL, "top must be 0 .. %d and at most vocab", tbp::kMaxTop);
   if (rows == 0) return TBP_OK;
   if (!targets || !logp || !entropy || !lse || (top && (!top_logp || !top_ids))) return fail(TBP_EINVAL, "null pointer");
-  if (check_workspace(tbp_logprobs_workspace_bytes(rows, vocab, top), workspace, workspace_bytes) != TBP_OK) return TBP_EINVAL;
   tbp::LogprobParams p{};
   p.logits = logits; p.ld = ld_logits; p.rows = rows; p.vocab = vocab; p.targets = targets; p.logp = logp; p.entropy = entropy; p.lse = lse;
   p.top = top; p.top_logp = top_logp; p.top_ids = top_ids;
@@ -254,14 +247,13 @@ tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, i
 
 tbp_status tbp_logprobs_step(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
                              const float* d_logp, const float* d_entropy, float* logp, float* entropy, float* lse, void* d_logits,
-                             int64_t ld_d, void* workspace, size_t workspace_bytes, void* stream) {
+                             int64_t ld_d, void* stream) {
   if (check_logits(dtype, rows, vocab, logits, ld_logits) != TBP_OK) return TBP_EINVAL;
   if (ld_d < vocab) return fail(TBP_EINVAL, "leading dimension smaller than vocab");
   if (rows == 0) return TBP_OK;
   if (!targets || !lse || !entropy || !logp || !d_logp || !d_logits) return fail(TBP_EINVAL, "null pointer");
   if (misaligned(d_logits, dtype == TBP_BF16 ? 2 : 4)) return fail(TBP_EINVAL, "d_logits must be aligned to its elements");
   if (d_logits == logits && ld_d != ld_logits) return fail(TBP_EINVAL, "in place both leading dimensions must be the same");
-  if (check_workspace(tbp_logprobs_workspace_bytes(rows, vocab, 0), workspace, workspace_bytes) != TBP_OK) return TBP_EINVAL;
   tbp::LogprobParams p{};
   p.logits = logits; p.ld = ld_logits; p.rows = rows; p.vocab = vocab; p.targets = targets; p.logp = logp; p.entropy = entropy; p.lse = lse;
   p.d_logp = d_logp; p.d_entropy = d_entropy; p.d_logits = d_logits; p.ld_d = ld_d;

@@ -1,62 +1,194 @@
 // Log probabilities of given tokens over rows of logits, with the entropy of every row and its most likely tokens, and the
-// derivative of the logits.
-//   m = max x, s = sum e^(x - m), t = sum (x - m) e^(x - m):  lse = m + log s,  logp = x_target - lse,  H = log s - t / s,
-//   dx = dlogp (1[target] - p) - dH p (log p + H).
-// All of them are read (and written) once at the memory's rate in the end; statistics are fp32.
+// derivative of the logits.  In units of log 2, with a reference point r near the maximum:
+//   s = sum 2^d, t = sum d 2^d, d = x log2 e - r:   lse = (r + log2 s) ln 2,  logp = x_target - lse,  H = (log2 s - t / s) ln 2,
+//   dx = dlogp (1[target] - p) - dH p (log p + H),  p = 2^(x log2 e - lse / ln 2).
+// The products x log2 e go into d unrounded (fused multiply-add), so r may be any number: s, t and lse refer to the same one.
+//
+// A workgroup owns a row and holds it in registers (16 or 4 pieces of 16 bytes per thread) from the statistics to the ranking or to the
+// derivative: a row is read once.  Rows longer than that are walked in blocks and read a second time for the derivative (for the ranking
+// only by the few threads that hold a candidate).
 #include "kernels.h"
 #include "rows.h"
 
+#include <type_traits>
+
 namespace tbp {
 
-struct Stats { float m, s, t; };
-__device__ __forceinline__ Stats join(Stats a, Stats b) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == -INFINITY) return Stats{m, a.s + b.s, a.t + b.t};       // (nothing but -inf so far: zeros, or NaN that is passed on)
-  const float da = a.m - m, db = b.m - m, fa = __expf(da), fb = __expf(db);
-  return Stats{m, a.s * fa + b.s * fb, (a.m == -INFINITY ? 0.f : (a.t + da * a.s) * fa) + (b.m == -INFINITY ? 0.f : (b.t + db * b.s) * fb)};
-}
-__device__ __forceinline__ void add(Stats& a, float x) {
-  if (x == -INFINITY) return;
-  if (x > a.m) {
-    const float d = a.m - x, f = __expf(d);
-    a.t = a.m == -INFINITY ? a.t : (a.t + d * a.s) * f;
-    a.s = a.s * f;
-    a.m = x;
+// 2^d is zero below this: what it is multiplied with only has to be finite there (a logit of -infinity).  A NaN stays one by 2^d.
+constexpr float kFar = -300.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// 16 bytes at any address that an element may have (rows of odd length): one load or store all the same.
+typedef u32x4 Any4 __attribute__((aligned(4)));
+typedef u32x4 Any2 __attribute__((aligned(2)));
+template <typename T> struct Logits {
+  static constexpr int N = 16 / (int)sizeof(T);
+  typedef typename std::conditional<sizeof(T) == 4, Any4, Any2>::type Any;
+  static __device__ __forceinline__ u32x4 load(const T* p) { return *reinterpret_cast<const Any*>(p); }
+  static __device__ __forceinline__ void store(T* p, const float* v) {
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<Any*>(p) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+      bf16x8 o;
+#pragma unroll
+      for (int i = 0; i < 8; i++) o[i] = (bf16_t)v[i];
+      *reinterpret_cast<Any*>(p) = __builtin_bit_cast(u32x4, o);
+    }
   }
-  const float d = x - a.m, e = __expf(d);
-  a.s += e;
-  a.t += d * e;
+  static __device__ __forceinline__ float get(const u32x4& r, int i) {      // i is a constant after unrolling
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r[i]);
+    else return (i & 1) ? __uint_as_float(r[i >> 1] & 0xffff0000u) : __uint_as_float(r[i >> 1] << 16);
+  }
+  static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;      // -infinity
+};
+
+// Statistics of a part of a row; r = -infinity: no finite logit so far (s, t: zeros, or NaN that is passed on).
+struct Stats { float r, s, t; };
+__device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
+  const float r = fmaxf(a.r, b.r);
+  const float da = a.r == -INFINITY ? 0.f : a.r - r, db = b.r == -INFINITY ? 0.f : b.r - r;
+  const float fa = a.r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(da), fb = b.r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(db);
+  return Stats{r, a.s * fa + b.s * fb, (a.t + da * a.s) * fa + (b.t + db * b.s) * fb};
 }
 
 // a is ranked before b: larger value, or the same and a lower index
 __device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
-  __shared__ Stats red[4];
-  __shared__ float bv[4];
-  __shared__ int bi[4];
-  const long row = blockIdx.x;
-  const T* const x = (const T*)p.logits + row * p.ld;
-  Stats a{-INFINITY, 0.f, 0.f};
-  for (int i = threadIdx.x; i < p.vocab; i += 256) add(a, (float)x[i]);
-  for (int d = 1; d < 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
+constexpr int kCandidates = 1024;
+
+// What the threads of a row share.
+template <int NT> struct RowShared {
+  Stats red[NT / 64];
+  float lane_max[NT / 64][64];
+  int n;
+  float cv[kCandidates];
+  int ci[kCandidates];
+  float bv[NT / 64];
+  int bi[NT / 64];
+};
+
+// One row's pieces: piece c of the thread's block b is at element N (NT (CH b + c) + thread).
+template <typename T, int NT, int CH>
+struct Row {
+  using L = Logits<T>;
+  static constexpr int N = L::N;
+  u32x4 x[CH];
+  // The pieces as they are, but unknown to the compiler: what one pass has unpacked from them is not kept for the next (twice the registers).
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int c = 0; c < CH; c++) asm volatile("" : "+v"(x[c]));
+  }
+  static __device__ __forceinline__ int at(int blk, int c) { return N * (NT * (CH * blk + c) + (int)threadIdx.x); }
+  __device__ __forceinline__ void load(const T* row, int vocab, int blk) {
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const int i = at(blk, c);
+      if (i + N <= vocab) x[c] = L::load(row + i);
+      else x[c] = u32x4{L::kNone, L::kNone, L::kNone, L::kNone};
+    }
+    // the row's end, if it lies inside a piece
+    const int tail = vocab / N * N;
+    if (tail < vocab && tail / N % NT == (int)threadIdx.x && tail / N / NT / CH == blk) {
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+        if (at(blk, c) != tail) continue;
+#pragma unroll
+        for (int e = 0; e < N - 1; e++) {
+          if (tail + e >= vocab) continue;
+          if constexpr (sizeof(T) == 4) x[c][e] = reinterpret_cast<const uint32_t*>(row)[tail + e];
+          else {
+            const uint32_t v = reinterpret_cast<const uint16_t*>(row)[tail + e];
+            x[c][e >> 1] = (e & 1) ? (x[c][e >> 1] & 0xffffu) | v << 16 : (x[c][e >> 1] & 0xffff0000u) | v;
+          }
+        }
+      }
+    }
+  }
+};
+
+// The k-th largest of 64 numbers, one per lane.
+__device__ __forceinline__ float kth_largest(float v, int k) {
+  int rank = 0;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < 64; j++) {
+    const float o = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), j));
+    rank += before(o, j, v, lane) ? 1 : 0;
+  }
+  const uint64_t who = __ballot(rank == k - 1);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), who ? __builtin_ctzll(who) : 0));
+}
+
+// Ranking.  The row's maxima over 64 classes of threads are 64 of its logits, so the top-th largest of them is a lower bound of the top-th
+// largest logit, and hardly more logits than `top` reach it (their number is that of draws from 64 boxes until `top` are met: 24 for 20,
+// 90 for 48).  Those are collected and ranked among each other.  Rows with more than kCandidates of them (a great many ties) are ranked one place
+// at a time over the whole row.
+template <typename T, int NT, int CH>
+__device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const T* x, Row<T, NT, CH>& data, int nblk, float my_max, float lse,
+                                         RowShared<NT>& sh) {
+  using R = Row<T, NT, CH>;
+  const int tid = threadIdx.x;
+  float* const out_v = p.top_logp + row * p.top;
+  int* const out_i = p.top_ids + row * p.top;
+  if (!(lse == lse)) {                               // NaN or +infinity in the row
+    if (tid < p.top) { out_v[tid] = __builtin_nanf(""); out_i[tid] = -1; }
+    return;
+  }
+  sh.lane_max[tid >> 6][tid & 63] = my_max;
+  if (tid == 0) sh.n = 0;
   __syncthreads();
-  a = join(join(red[0], red[1]), join(red[2], red[3]));
-  const float ls = logf(a.s), lse = a.m == -INFINITY ? (a.s == a.s ? -INFINITY : a.s) : a.m + ls;
-  if (threadIdx.x == 0) {
-    const int t = p.targets ? p.targets[row] : -1;
-    if (p.logp) p.logp[row] = t >= 0 && t < p.vocab ? (lse == -INFINITY ? -INFINITY : (float)x[t] - lse) : 0.f;
-    if (p.entropy) p.entropy[row] = lse == -INFINITY ? 0.f : ls - a.t / a.s;
-    if (p.lse) p.lse[row] = lse;
+  float cls = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < NT / 64; w++) cls = fmaxf(cls, sh.lane_max[w][tid & 63]);
+  const float bar = kth_largest(cls, p.top);
+  // (bar -infinity: fewer than `top` classes hold a finite logit; the finite ones are collected and the rest of the places filled below)
+  if (my_max >= bar && my_max > -INFINITY) {
+    for (int b = 0; b < nblk; b++) {
+      if (nblk > 1) data.load(x, p.vocab, b);
+      data.forget();
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+#pragma unroll
+        for (int e = 0; e < R::N; e++) {
+          const float v = Logits<T>::get(data.x[c], e);
+          if (v >= bar && v > -INFINITY) {
+            const int at = atomicAdd(&sh.n, 1);
+            if (at < kCandidates) { sh.cv[at] = v; sh.ci[at] = R::at(b, c) + e; }
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int n = sh.n;
+  if (n <= kCandidates) {
+    for (int i = tid; i < n; i += NT) {
+      const float v = sh.cv[i];
+      const int id = sh.ci[i];
+      int rank = 0;
+      for (int j = 0; j < n; j++) rank += before(sh.cv[j], sh.ci[j], v, id) ? 1 : 0;
+      if (rank < p.top) { out_v[rank] = v - lse; out_i[rank] = id; }
+    }
+    // fewer finite logits than places: the others in order of their index, which are among the first n + top
+    if (n < p.top && tid < 64) {
+      int place = n;
+      for (int i0 = 0; place < p.top; i0 += 64) {
+        const bool none = i0 + tid < p.vocab && (float)x[i0 + tid] == -INFINITY;
+        const uint64_t who = __ballot(none);
+        const int at = place + __popcll(who & ((1ull << tid) - 1));
+        if (none && at < p.top) { out_v[at] = -INFINITY; out_i[at] = i0 + tid; }
+        place += __popcll(who);
+      }
+    }
+    return;
   }
   float pv = INFINITY;
   int pi = -1;
   for (int k = 0; k < p.top; k++) {
     float v = -INFINITY;
     int best = 0x7fffffff;
-    for (int i = threadIdx.x; i < p.vocab; i += 256) {
+    for (int i = tid; i < p.vocab; i += NT) {
       const float c = (float)x[i];
       if ((c < pv || (c == pv && i > pi)) && (best == 0x7fffffff || before(c, i, v, best))) { v = c; best = i; }
     }
@@ -66,51 +198,169 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobParams p) {
       if (before(ov, oi, v, best)) { v = ov; best = oi; }
     }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) { bv[threadIdx.x >> 6] = v; bi[threadIdx.x >> 6] = best; }
+    if ((tid & 63) == 0) { sh.bv[tid >> 6] = v; sh.bi[tid >> 6] = best; }
     __syncthreads();
-    v = bv[0]; best = bi[0];
-    for (int w = 1; w < 4; w++)
-      if (before(bv[w], bi[w], v, best)) { v = bv[w]; best = bi[w]; }
-    if (threadIdx.x == 0) {
-      const bool ok = lse == lse && best < p.vocab;
-      p.top_logp[row * p.top + k] = !ok ? __builtin_nanf("") : lse == -INFINITY ? -INFINITY : v - lse;
-      p.top_ids[row * p.top + k] = ok ? best : -1;
-    }
+    v = sh.bv[0]; best = sh.bi[0];
+    for (int w = 1; w < NT / 64; w++)
+      if (before(sh.bv[w], sh.bi[w], v, best)) { v = sh.bv[w]; best = sh.bi[w]; }
+    if (tid == 0) { out_v[k] = lse == -INFINITY ? -INFINITY : v - lse; out_i[k] = best; }
     pv = v; pi = best;
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
-  const long row = blockIdx.x;
-  const int i = (int)blockIdx.y * 256 + threadIdx.x;
-  if (i >= p.vocab) return;
-  const float lse = p.lse[row], x = (float)((const T*)p.logits)[row * p.ld + i];
+// The derivative of one piece of a row.
+struct RowWeights { float lse2, dl, inner, dh2; int target; };      // inner = dl + dH H, dh2 = dH ln 2
+__device__ __forceinline__ RowWeights row_weights(const LogprobParams& p, long row, float lse, float entropy) {
   const int t = p.targets[row];
-  const float dl = t >= 0 && t < p.vocab ? p.d_logp[row] : 0.f, dh = p.d_entropy ? p.d_entropy[row] : 0.f;
-  const float lp = x - lse, pr = __expf(lp);
-  float d = pr > 0.f ? -pr * (dl + dh * (lp + p.entropy[row])) : 0.f;
-  if (pr != pr) d = pr;
-  if (i == t) d += dl;
-  ((T*)p.d_logits)[row * p.ld_d + i] = (T)(lse == -INFINITY ? 0.f : d);
+  const bool given = t >= 0 && t < p.vocab, none = lse == -INFINITY;
+  const float dl = given && !none ? p.d_logp[row] : 0.f, dh = p.d_entropy && !none ? p.d_entropy[row] : 0.f;
+  return RowWeights{none ? 0.f : lse * kLog2e, dl, dl + dh * entropy, dh * kLn2, given ? t : -1};
+}
+template <typename T>
+__device__ __forceinline__ void derive(const u32x4& x, int i, const RowWeights& w, float* v) {
+  using L = Logits<T>;
+#pragma unroll
+  for (int e = 0; e < L::N; e++) {
+    const float d = __builtin_fmaf(L::get(x, e), kLog2e, -w.lse2);
+    v[e] = -__builtin_amdgcn_exp2f(d) * __builtin_fmaf(w.dh2, fmaxf(d, kFar), w.inner);
+  }
+  if ((unsigned)(w.target - i) < (unsigned)L::N) {
+#pragma unroll
+    for (int e = 0; e < L::N; e++) v[e] += w.target - i == e ? w.dl : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, int i, int vocab, const float* v) {
+  using L = Logits<T>;
+  if (i + L::N <= vocab) L::store(row + i, v);
+  else
+#pragma unroll
+    for (int e = 0; e < L::N - 1; e++)
+      if (i + e < vocab) row[i + e] = (T)v[e];
 }
 
-hipError_t logprobs(int dtype, const LogprobParams& p, hipStream_t s) {
-  if (dtype) hipLaunchKernelGGL((logprobs_kernel<bf16_t>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((logprobs_kernel<float>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
+template <typename T, int NT, int CH, bool STEP>
+__global__ __launch_bounds__(NT) void logprobs_kernel(LogprobParams p) {
+  using R = Row<T, NT, CH>;
+  __shared__ RowShared<NT> sh;
+  const int tid = threadIdx.x;
+  const long row = blockIdx.x;
+  const T* const x = (const T*)p.logits + row * p.ld;
+  const int nblk = (p.vocab + NT * CH * R::N - 1) / (NT * CH * R::N);
+  R data;
+  Stats a{-INFINITY, 0.f, 0.f};
+  float my_max = -INFINITY;
+  for (int b = 0; b < nblk; b++) {
+    data.load(x, p.vocab, b);
+    float mx = my_max;
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+      for (int e = 0; e < R::N; e++) mx = fmaxf(mx, Logits<T>::get(data.x[c], e));
+    if (mx > my_max) {                               // the reference point moves to the maximum
+      const float r = mx * kLog2e, d = a.r == -INFINITY ? 0.f : a.r - r, f = __builtin_amdgcn_exp2f(d);
+      a.t = (a.t + d * a.s) * f;
+      a.s *= f;
+      a.r = r;
+      my_max = mx;
+    }
+    data.forget();
+    const float ref = a.r == -INFINITY ? 0.f : a.r;
+    float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+      for (int e = 0; e < R::N; e++) {
+        const float d = __builtin_fmaf(Logits<T>::get(data.x[c], e), kLog2e, -ref), v = __builtin_amdgcn_exp2f(d);
+        s[e & 1] += v;
+        t[e & 1] = __builtin_fmaf(v, fmaxf(d, kFar), t[e & 1]);
+      }
+    a.s += s[0] + s[1];
+    a.t += t[0] + t[1];
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  if ((tid & 63) == 0) sh.red[tid >> 6] = a;
+  __syncthreads();
+  a = sh.red[tid & (NT / 64 - 1)];
+#pragma unroll
+  for (int d = 1; d < NT / 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  // (lane 0's sums for all: lanes may differ in the last bit)
+  auto first = [](float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); };
+  a = Stats{first(a.r), first(a.s), first(a.t)};
+  const bool none = a.r == -INFINITY && a.s == a.s;                 // nothing but -infinity
+  const float ls = __builtin_amdgcn_logf(a.s);
+  const float lse = none ? -INFINITY : a.r == -INFINITY ? a.s : (a.r + ls) * kLn2, entropy = none ? 0.f : (ls - a.t / a.s) * kLn2;
+  if (tid == 0) {
+    const int t = p.targets[row];
+    p.logp[row] = t >= 0 && t < p.vocab ? (none ? -INFINITY : (float)x[t] - lse) : 0.f;
+    p.entropy[row] = entropy;
+    p.lse[row] = lse;
+  }
+  if constexpr (STEP) {
+    __syncthreads();                                                // (in place: the target's logit has been read)
+    const RowWeights w = row_weights(p, row, lse, entropy);
+    T* const o = (T*)p.d_logits + row * p.ld_d;
+    for (int b = 0; b < nblk; b++) {
+      if (nblk > 1) data.load(x, p.vocab, b);
+      data.forget();
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+        const int i = R::at(b, c);
+        if (i >= p.vocab) break;
+        float v[R::N];
+        derive<T>(data.x[c], i, w, v);
+        store_piece<T>(o, i, p.vocab, v);
+      }
+    }
+  } else {
+    if (p.top) rank_top<T, NT, CH>(p, row, x, data, nblk, my_max, lse, sh);
+  }
+}
+
+// The derivative by itself: a workgroup takes 4 pieces per thread of one row.
+template <typename T>
+__global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
+  using R = Row<T, 256, 4>;
+  const long row = blockIdx.x;
+  R data;
+  data.load((const T*)p.logits + row * p.ld, p.vocab, blockIdx.y);
+  const RowWeights w = row_weights(p, row, p.lse[row], p.entropy[row]);
+  T* const o = (T*)p.d_logits + row * p.ld_d;
+#pragma unroll
+  for (int c = 0; c < 4; c++) {
+    const int i = R::at(blockIdx.y, c);
+    if (i >= p.vocab) break;
+    float v[R::N];
+    derive<T>(data.x[c], i, w, v);
+    store_piece<T>(o, i, p.vocab, v);
+  }
+}
+
+template <typename T, int NT, int CH, bool STEP>
+static hipError_t launch(const LogprobParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((logprobs_kernel<T, NT, CH, STEP>), dim3((unsigned)p.rows), dim3(NT), 0, s, p);
   return hipGetLastError();
 }
 
+template <typename T, bool STEP>
+static hipError_t launch_t(const LogprobParams& p, hipStream_t s) {
+  constexpr int N = Logits<T>::N;
+  if (p.vocab <= 256 * 4 * N) return launch<T, 256, 4, STEP>(p, s);
+  if (p.rows >= 512 && p.vocab <= 256 * 16 * N) return launch<T, 256, 16, STEP>(p, s);
+  if (p.vocab <= 1024 * 4 * N) return launch<T, 1024, 4, STEP>(p, s);
+  return launch<T, 1024, 16, STEP>(p, s);
+}
+
+hipError_t logprobs(int dtype, const LogprobParams& p, hipStream_t s) { return dtype ? launch_t<bf16_t, false>(p, s) : launch_t<float, false>(p, s); }
+hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s) { return dtype ? launch_t<bf16_t, true>(p, s) : launch_t<float, true>(p, s); }
+
 hipError_t logprobs_p1(int dtype, const LogprobParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.rows, (unsigned)((p.vocab + 255) / 256));
+  const int per = 256 * 4 * (dtype ? 8 : 4);
+  const dim3 grid((unsigned)p.rows, (unsigned)((p.vocab + per - 1) / per));
   if (dtype) hipLaunchKernelGGL((logprobs_p1_kernel<bf16_t>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((logprobs_p1_kernel<float>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
-}
-
-hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s) {
-  if (hipError_t e = logprobs(dtype, p, s); e != hipSuccess) return e;
-  return logprobs_p1(dtype, p, s);
 }
 
 }  // namespace tbp

@@ -867,7 +867,8 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
 // ------------------------------------------------------------------------------------------ one new token per sequence
 // Workgroup = one (sequence, key head, 32 query heads of its group) and a share of the keys that the new token sees, 4 waves that take
 // tiles of 32 keys in turn, each through a ring of its own in LDS: no barrier before the waves join.  S^T = K Q^T with the query heads
-// as columns (unused ones: zeros), then O^T += V^T P^T, as in the forward.  Bound by the reading of K and V: a tile is 16 KiB at
+// as columns (unused ones: zeros), then O^T += V^T P^T, as in the forward.  The share that is done last joins them all (a launch for it took
+// 3.8 us, and its host side as much again).  Bound by the reading of K and V: a tile is 16 KiB at
 // head_dim 128 and 16 MFMAs, a fifteenth of the time that it takes to arrive.
 // Seen keys are numbered v = 0 .. seen - 1: the sinks, then the window in order; number v lies in slot v (sinks) or
 // sinks + (first + v - n_sink) mod ring.
@@ -878,6 +879,7 @@ struct WinDecodeParams {
   bf16_t* out; long ld_out;
   float* lse;                          // [B, H]
   float* part_o; float2* part_ml;      // [B, H, splits][DH], [B, H, splits] (splits > 1)
+  unsigned* arrived;                   // [B, KV, 32-head groups]: shares that are done; zero before and after every call
   int B, H, KV, G, capacity, window, sinks, splits;
   float scale_log2e;
 };
@@ -998,6 +1000,15 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
   }
   __syncthreads();
   LDS_AS float* const all = reinterpret_cast<LDS_AS float*>(LDS_PTR(unsigned char, smem_raw));
+  auto finish = [&](int r, int c, f32x4 o, float M, float L) {  // columns c .. c + 3 of this workgroup's head r
+    const long head = (long)b * p.H + hk * p.G + gq0 + r;
+    const float inv = L > 0.f ? 1.f / L : 0.f;                 // (no key seen: zeros)
+    bf16x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; k++) v[k] = (bf16_t)(o[k] * inv);
+    *reinterpret_cast<bf16x4*>(p.out + (long)b * p.ld_out + (long)(hk * p.G + gq0 + r) * DH + c) = v;
+    if (c == 0) p.lse[head] = M + __builtin_amdgcn_logf(L);
+  };
   constexpr int WSTRIDE = RING * SLOT / 4;
   for (int i = (int)threadIdx.x; i < nh * (DH / 4); i += 256) {
     const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
@@ -1021,40 +1032,41 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
       *reinterpret_cast<f32x4*>(p.part_o + (head * p.splits + sp) * DH + c) = o;
       if (c == 0) p.part_ml[head * p.splits + sp] = make_float2(M, L);
     } else {
-      const float inv = L > 0.f ? 1.f / L : 0.f;               // (no key seen: zeros)
-      bf16x4 v;
-#pragma unroll
-      for (int k = 0; k < 4; k++) v[k] = (bf16_t)(o[k] * inv);
-      *reinterpret_cast<bf16x4*>(p.out + (long)b * p.ld_out + (long)(hk * p.G + gq0 + r) * DH + c) = v;
-      if (c == 0) p.lse[head] = M + __builtin_amdgcn_logf(L);
+      finish(r, c, o, M, L);
     }
   }
-}
-
-// The shares of a head's keys join: one wave per head, 4 columns per lane (head_dim 64: lanes 0..15).
-template <int DH>
-__global__ __launch_bounds__(256) void window_decode_join_kernel(WinDecodeParams p) {
-  constexpr int LPH = DH / 4, HPB = 256 / LPH;
-  const long head = (long)blockIdx.x * HPB + threadIdx.x / LPH;
-  const int c = 4 * (threadIdx.x % LPH);
-  if (head >= (long)p.B * p.H) return;
-  float M = -INFINITY, L = 0.f;
-  for (int i = 0; i < p.splits; i++) M = fmaxf(M, p.part_ml[head * p.splits + i].x);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < p.splits; i++) {
-    const float2 ml = p.part_ml[head * p.splits + i];
-    const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
-    L += f * ml.y;
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + (head * p.splits + i) * DH + c);
-#pragma unroll
-    for (int k = 0; k < 4; k++) o[k] += f * x[k];
+  if (p.splits == 1) return;
+  // ---- the share that is done last joins all of them, in their order.  (The partial sums are written through to memory that every XCD sees
+  // before the share is counted, and read behind the count.)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+  __syncthreads();
+  LDS_AS unsigned* const flag = reinterpret_cast<LDS_AS unsigned*>(all);
+  if (threadIdx.x == 0) {
+    unsigned* const count = p.arrived + ((long)blockIdx.z * gridDim.x + blockIdx.x);
+    const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = before + 1 == (unsigned)p.splits;
+    if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last ? 1u : 0u;
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
-  bf16x4 v;
+  __syncthreads();
+  if (!*flag) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  for (int i = (int)threadIdx.x; i < nh * (DH / 4); i += 256) {
+    const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
+    const long at = ((long)b * p.H + hk * p.G + gq0 + r) * p.splits;
+    float M = -INFINITY, L = 0.f;
+    for (int k = 0; k < p.splits; k++) M = fmaxf(M, p.part_ml[at + k].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < p.splits; k++) {
+      const float2 ml = p.part_ml[at + k];
+      const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
+      L += f * ml.y;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + (at + k) * DH + c);
 #pragma unroll
-  for (int k = 0; k < 4; k++) v[k] = (bf16_t)(o[k] * inv);
-  *reinterpret_cast<bf16x4*>(p.out + head / p.H * p.ld_out + (head % p.H) * DH + c) = v;
-  if (c == 0) p.lse[head] = M + __builtin_amdgcn_logf(L);
+      for (int e = 0; e < 4; e++) o[e] += f * x[e];
+    }
+    finish(r, c, o, M, L);
+  }
 }
 
 // ------------------------------------------------------------------------------------------ launches
@@ -1150,7 +1162,7 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   return w.head_dim == 128 ? launch_kv<128>(p, s) : launch_kv<64>(p, s);
 }
 
-int window_decode_splits(int batch, int kv_heads, int most_seen) {
+int window_decode_splits(int batch, int kv_heads, long most_seen) {
   const long groups = (long)batch * kv_heads;
   long splits = (512 + groups - 1) / groups;
   const long tiles = (most_seen + 31) / 32;
@@ -1165,19 +1177,16 @@ static hipError_t launch_decode(const WinDecodeParams& p, hipStream_t s) {
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.B * p.KV), (unsigned)p.splits, (unsigned)((p.G + 31) / 32)), dim3(256), smem, s, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
-  constexpr int HPB = 256 / (DH / 4);
-  hipLaunchKernelGGL((window_decode_join_kernel<DH>), dim3((unsigned)(((long)p.B * p.H + HPB - 1) / HPB)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
 hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths, const void* q, long ld_q, const void* cache_k,
-                         const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, float* part_o,
-                         float2* part_ml, hipStream_t s) {
+                         const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, unsigned* arrived,
+                         float* part_o, float2* part_ml, hipStream_t s) {
   WinDecodeParams p{};
   p.q = (const bf16_t*)q; p.ld_q = ld_q; p.ck = (const bf16_t*)cache_k; p.cv = (const bf16_t*)cache_v; p.ld_c = ld_cache;
   p.seq_stride = (long)capacity * ld_cache;
-  p.lengths = lengths; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.part_o = part_o; p.part_ml = part_ml;
+  p.lengths = lengths; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.part_o = part_o; p.part_ml = part_ml; p.arrived = arrived;
   p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.capacity = capacity; p.window = w.window;
   p.sinks = w.sinks; p.splits = splits;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);

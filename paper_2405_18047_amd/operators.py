@@ -2,7 +2,9 @@
 positions, log probabilities of tokens, the norm of all gradients with clipping.
 
 As in binding.py: argument marshalling only, on torch's current stream; outputs and workspaces are allocated where the caller
-passes none.  Index tensors (lengths, positions, targets) are int32 on the device.
+passes none.  Index tensors (lengths, positions, targets) are int32 on the device.  The checks here are those that the C entry
+points cannot make (types, shapes and strides of tensors); the single-token calls are bound by the host, which is why they
+are written out rather than shared by many small functions.
 """
 from __future__ import annotations
 
@@ -10,7 +12,7 @@ import ctypes as C
 
 import torch
 
-from .binding import _check, _dt, _ptr, _stream, lib
+from .binding import TBP_BF16, TBP_F32, _check, _stream, lib
 
 __all__ = [
     "TBP_ROTARY_HALF", "TBP_ROTARY_INTERLEAVED", "TBP_ROTARY_PLAIN", "TBP_ROTARY_LINEAR", "TBP_ROTARY_BASE", "TBP_ROTARY_RAMP",
@@ -21,105 +23,112 @@ __all__ = [
 TBP_ROTARY_HALF, TBP_ROTARY_INTERLEAVED = 0, 1
 TBP_ROTARY_PLAIN, TBP_ROTARY_LINEAR, TBP_ROTARY_BASE, TBP_ROTARY_RAMP = 0, 1, 2, 3
 
+_F32, _I32 = torch.float32, torch.int32
+_CODE = {torch.bfloat16: TBP_BF16, torch.float32: TBP_F32}
+
 
 class tbp_rotary_scale(C.Structure):
     _fields_ = [("scaling", C.c_int32), ("factor", C.c_float), ("low", C.c_float), ("high", C.c_float), ("original", C.c_float),
                 ("magnitude", C.c_float)]
 
 
-def _index(t, n, what):
-    """An int32 vector of n entries, or None."""
+def _dt(t):
+    try:
+        return _CODE[t.dtype]
+    except KeyError:
+        raise TypeError(f"unsupported tensor dtype {t.dtype}") from None
+
+
+def _vector(t, n, dtype, what):
+    """The address of a contiguous vector of n entries (None: null)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise TypeError(f"{what} must be a contiguous int32 tensor of {n} entries")
-    return _ptr(t)
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise TypeError(f"{what} must be a contiguous {dtype} tensor of {n} entries")
+    return t.data_ptr()
 
 
-def _floats(t, n, what):
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
-        raise TypeError(f"{what} must be a contiguous float32 tensor of {n} entries")
-    return _ptr(t)
+def _matrix(t, dtype, what):
+    """The leading dimension of a matrix whose rows are contiguous."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 2:
+        raise TypeError(f"{what} must be a matrix of type {dtype}")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise TypeError(f"{what} must have contiguous rows")
+    return ld if shape[0] > 1 or ld > shape[1] else shape[1]
 
 
-def _matrix(t, what):
-    """The leading dimension of a tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError(f"{what} must be a matrix with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _caches(k, v, dtype, batch, width):
+    """(capacity, distance of rows) of a pair of caches."""
+    shape, stride = k.shape, k.stride()
+    if len(shape) != 3 or shape[0] != batch or shape[2] != width or stride[2] != 1 or (batch > 1 and stride[0] != shape[1] * stride[1]):
+        raise TypeError("caches must be [batch, capacity, n_kv_heads*head_dim] with contiguous rows of one distance")
+    if v.shape != shape or v.stride() != stride or k.dtype is not dtype or v.dtype is not dtype:
+        raise TypeError("both caches must have one shape, one stride, and the tokens' type")
+    return shape[1], stride[1]
 
 
-def _like(t, ref, what):
-    if t.dtype != ref.dtype or t.device != ref.device:
-        raise TypeError(f"{what} must have type {ref.dtype} on {ref.device}")
-    return t
-
-
-def _workspace(nbytes, device):
-    """A uint8 tensor (256-byte aligned, as torch's allocations on the device are), or None for nothing."""
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-# ---- sliding-window attention ------------------------------------------------------------------------------------------
 def _sequences(rows, seq):
     if seq < 1 or rows % seq:
         raise ValueError(f"{rows} rows are no whole sequences of {seq}")
     return rows // seq
 
 
+# ---- sliding-window attention ------------------------------------------------------------------------------------------
 def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, sinks=0, lengths=None, out=None, lse=None):
     """qkv [batch*seq, (n_heads + 2 n_kv_heads) head_dim] (q | k | v, rotated) -> (out [batch*seq, n_heads*head_dim], lse2 [batch, heads, seq])."""
-    batch = _sequences(qkv.shape[0], seq)
-    out = torch.empty((qkv.shape[0], n_heads * head_dim), dtype=qkv.dtype, device=qkv.device) if out is None else _like(out, qkv, "out")
-    lse = torch.empty((batch, n_heads, seq), dtype=torch.float32, device=qkv.device) if lse is None else lse
-    _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _index(lengths, batch, "lengths"),
-                                          _ptr(qkv), _matrix(qkv, "qkv"), _ptr(out), _matrix(out, "out"), _floats(lse, batch * n_heads * seq, "lse"),
-                                          _stream()))
+    batch, dt = _sequences(qkv.shape[0], seq), qkv.dtype
+    if out is None:
+        out = qkv.new_empty((qkv.shape[0], n_heads * head_dim))
+    if lse is None:
+        lse = torch.empty((batch, n_heads, seq), dtype=_F32, device=qkv.device)
+    _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
+                                          qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), _matrix(out, dt, "out"),
+                                          _vector(lse, batch * n_heads * seq, _F32, "lse"), _stream()))
     return out, lse
 
 
 def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head_dim, window, sinks=0, lengths=None, dqkv=None, scratch=None):
     """-> dqkv [batch*seq, (n_heads + 2 n_kv_heads) head_dim] (dq | dk | dv, not rotated back)."""
-    batch = _sequences(qkv.shape[0], seq)
-    _like(out, qkv, "out"), _like(d_out, qkv, "d_out")
-    if _matrix(d_out, "d_out") != _matrix(out, "out") or d_out.shape != out.shape:
+    batch, dt = _sequences(qkv.shape[0], seq), qkv.dtype
+    ld_out = _matrix(out, dt, "out")
+    if _matrix(d_out, dt, "d_out") != ld_out or d_out.shape != out.shape:
         raise TypeError("d_out must have out's shape and leading dimension")
-    dqkv = torch.empty((qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim), dtype=qkv.dtype, device=qkv.device) if dqkv is None else _like(dqkv, qkv, "dqkv")
+    if dqkv is None:
+        dqkv = qkv.new_empty((qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim))
+    L = lib()
     if scratch is None:
-        scratch = _workspace(lib().tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks), qkv.device)
-    _check(lib().tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _index(lengths, batch, "lengths"),
-                                         _ptr(qkv), _matrix(qkv, "qkv"), _ptr(out), _ptr(d_out), _matrix(out, "out"),
-                                         _floats(lse, batch * n_heads * seq, "lse"), _ptr(dqkv), _matrix(dqkv, "dqkv"), _ptr(scratch), _stream()))
+        scratch = torch.empty(L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks),
+                              dtype=torch.uint8, device=qkv.device)
+    _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
+                                     qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), d_out.data_ptr(), ld_out,
+                                     _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), _matrix(dqkv, dt, "dqkv"),
+                                     scratch.data_ptr(), _stream()))
     return dqkv
 
 
 def tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks=0, device="cuda:0"):
     """The workspace of tbp_window_decode calls of these sizes (which must not overlap), or None where they need none."""
-    return _workspace(lib().tbp_window_decode_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, window, sinks), device)
-
-
-def _cache(t, batch, width, what):
-    if t.dim() != 3 or t.shape[0] != batch or t.shape[2] != width or t.stride(2) != 1 or t.stride(0) != t.shape[1] * t.stride(1):
-        raise TypeError(f"{what} must be [batch, capacity, n_kv_heads*head_dim] with contiguous rows of one distance")
-    return t
+    nbytes = lib().tbp_window_decode_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, window, sinks)
+    return torch.zeros(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_dim, window, sinks=0, out=None, lse=None, workspace=None):
     """q [batch, n_heads*head_dim] of the token at position lengths[b] - 1 over caches [batch, capacity, n_kv_heads*head_dim] ->
-    (out [batch, n_heads*head_dim], lse2 [batch, heads])."""
-    batch, width = q.shape[0], n_kv_heads * head_dim
-    _cache(_like(cache_k, q, "cache_k"), batch, width, "cache_k"), _cache(_like(cache_v, q, "cache_v"), batch, width, "cache_v")
-    if cache_k.shape != cache_v.shape or cache_k.stride() != cache_v.stride():
-        raise TypeError("cache_k and cache_v must have one shape and stride")
-    out = torch.empty((batch, n_heads * head_dim), dtype=q.dtype, device=q.device) if out is None else _like(out, q, "out")
-    lse = torch.empty((batch, n_heads), dtype=torch.float32, device=q.device) if lse is None else lse
+    (out [batch, n_heads*head_dim], lse2 [batch, heads]).  A program that decodes keeps a workspace (tbp_window_decode_workspace)."""
+    batch, dt = q.shape[0], q.dtype
+    capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
+    if out is None:
+        out = q.new_empty((batch, n_heads * head_dim))
+    if lse is None:
+        lse = torch.empty((batch, n_heads), dtype=_F32, device=q.device)
     if workspace is None:
         workspace = tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks, q.device)
-    _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, cache_k.shape[1], _index(lengths, batch, "lengths"),
-                                   _ptr(q), _matrix(q, "q"), _ptr(cache_k), _ptr(cache_v), cache_k.stride(1), _ptr(out), _matrix(out, "out"),
-                                   _floats(lse, batch * n_heads, "lse"), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
+                                   q.data_ptr(), _matrix(q, dt, "q"), cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
+                                   _matrix(out, dt, "out"), _vector(lse, batch * n_heads, _F32, "lse"),
+                                   None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()))
     return out, lse
 
 
@@ -127,27 +136,29 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
 def tbp_rotary_table(n_pos, rot_dim, base, scaling=TBP_ROTARY_PLAIN, factor=1.0, low=1.0, high=32.0, original=4096.0, magnitude=1.0,
                      device="cuda:0"):
     """-> table [n_pos, rot_dim/2, 2] of cosines and sines."""
-    t = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    t = torch.empty((n_pos, rot_dim // 2, 2), dtype=_F32, device=device)
     sc = tbp_rotary_scale(scaling, factor, low, high, original, magnitude)
-    _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), _ptr(t), _stream()))
+    _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), t.data_ptr(), _stream()))
     return t
 
 
 def _table(table):
-    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+    shape = table.shape
+    if table.dtype is not _F32 or len(shape) != 3 or shape[2] != 2 or not table.is_contiguous():
         raise TypeError("the table must be a contiguous float32 tensor [n_pos, rot_dim/2, 2]")
-    return table.shape[0], 2 * table.shape[1]
+    return shape[0], 2 * shape[1]
 
 
 def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP_ROTARY_HALF, backward=False, out=None):
     """The first n_heads*head_dim columns of x [rows, ld], turned (backward: the derivative).  seq: tokens per sequence, where no positions
     are given.  out: new [rows, n_heads*head_dim], or the tensor to write to (x itself: in place)."""
     n_pos, rot_dim = _table(table)
-    rows = x.shape[0]
-    out = torch.empty((rows, n_heads * head_dim), dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
-    _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, _ptr(table), n_pos, _index(positions, rows, "positions"),
-                            (seq or n_pos) if positions is None else 1, 1 if backward else 0, _ptr(x), _matrix(x, "x"), _ptr(out),
-                            _matrix(out, "out"), _stream()))
+    rows, dt = x.shape[0], x.dtype
+    if out is None:
+        out = x.new_empty((rows, n_heads * head_dim))
+    _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
+                            (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), _matrix(x, dt, "x"), out.data_ptr(),
+                            _matrix(out, dt, "out"), _stream()))
     return out
 
 
@@ -155,61 +166,57 @@ def tbp_rotary_append(qkv, n_heads, n_kv_heads, head_dim, table, lengths, cache_
     """New tokens qkv [batch*n_new, (n_heads + 2 n_kv_heads) head_dim], the last ones of sequences of `lengths`: k (rotated) and v into the
     caches [batch, capacity, n_kv_heads*head_dim]; -> q rotated [batch*n_new, n_heads*head_dim]."""
     n_pos, rot_dim = _table(table)
-    batch, width = lengths.shape[0], n_kv_heads * head_dim
-    n_new = 0 if batch == 0 else qkv.shape[0] // batch
-    if n_new * batch != qkv.shape[0]:
-        raise ValueError(f"{qkv.shape[0]} rows are no whole number of tokens for {batch} sequences")
-    _cache(_like(cache_k, qkv, "cache_k"), batch, width, "cache_k"), _cache(_like(cache_v, qkv, "cache_v"), batch, width, "cache_v")
-    if cache_k.shape != cache_v.shape or cache_k.stride() != cache_v.stride():
-        raise TypeError("cache_k and cache_v must have one shape and stride")
-    q_out = torch.empty((qkv.shape[0], n_heads * head_dim), dtype=qkv.dtype, device=qkv.device) if q_out is None else _like(q_out, qkv, "q_out")
-    _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, _ptr(table), n_pos,
-                                   _index(lengths, batch, "lengths"), _ptr(qkv), _matrix(qkv, "qkv"), _ptr(q_out), _matrix(q_out, "q_out"),
-                                   _ptr(cache_k), _ptr(cache_v), cache_k.stride(1), cache_k.shape[1], sinks, _stream()))
+    batch, rows, dt = lengths.shape[0], qkv.shape[0], qkv.dtype
+    n_new = 0 if batch == 0 else rows // batch
+    if n_new * batch != rows:
+        raise ValueError(f"{rows} rows are no whole number of tokens for {batch} sequences")
+    capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
+    if q_out is None:
+        q_out = qkv.new_empty((rows, n_heads * head_dim))
+    _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos,
+                                   _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), _matrix(qkv, dt, "qkv"), q_out.data_ptr(),
+                                   _matrix(q_out, dt, "q_out"), cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream()))
     return q_out
 
 
 # ---- log probabilities -----------------------------------------------------------------------------------------------------
-def _rows(n, device):
-    return torch.empty(n, dtype=torch.float32, device=device)
-
-
-def tbp_logprobs(logits, targets, top=0, workspace=None):
+def tbp_logprobs(logits, targets, top=0):
     """logits [rows, vocab], targets [rows] (int32; outside the vocabulary: left out) -> (logp, entropy, lse), each [rows] fp32, and with top > 0
     (top_logp [rows, top] fp32, top_ids [rows, top] int32) behind them."""
     rows, vocab = logits.shape
-    logp, entropy, lse = (_rows(rows, logits.device) for _ in range(3))
-    top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device) if top > 0 else None
-    top_ids = torch.empty((rows, top), dtype=torch.int32, device=logits.device) if top > 0 else None
-    if workspace is None:
-        workspace = _workspace(lib().tbp_logprobs_workspace_bytes(rows, vocab, top), logits.device)
-    _check(lib().tbp_logprobs(_dt(logits), rows, vocab, _ptr(logits), _matrix(logits, "logits"), _index(targets, rows, "targets"), _ptr(logp),
-                              _ptr(entropy), _ptr(lse), top, _ptr(top_logp), _ptr(top_ids), _ptr(workspace),
-                              0 if workspace is None else workspace.numel(), _stream()))
+    stats = torch.empty((3, rows), dtype=_F32, device=logits.device)
+    at = stats.data_ptr()
+    top_logp = top_ids = None
+    if top > 0:
+        top_logp = torch.empty((rows, top), dtype=_F32, device=logits.device)
+        top_ids = torch.empty((rows, top), dtype=_I32, device=logits.device)
+    _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits"), _vector(targets, rows, _I32, "targets"),
+                              at, at + 4 * rows, at + 8 * rows, top, None if top_logp is None else top_logp.data_ptr(),
+                              None if top_ids is None else top_ids.data_ptr(), _stream()))
+    logp, entropy, lse = stats.unbind()
     return (logp, entropy, lse, top_logp, top_ids) if top > 0 else (logp, entropy, lse)
 
 
 def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=None):
     """-> the derivative of the logits [rows, vocab] (out: the tensor to write to, logits itself allowed)."""
-    rows, vocab = logits.shape
-    out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device) if out is None else _like(out, logits, "out")
-    _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, _ptr(logits), _matrix(logits, "logits"), _index(targets, rows, "targets"),
-                                 _floats(lse, rows, "lse"), _floats(entropy, rows, "entropy"), _floats(d_logp, rows, "d_logp"),
-                                 _floats(d_entropy, rows, "d_entropy"), _ptr(out), _matrix(out, "out"), _stream()))
+    (rows, vocab), dt = logits.shape, logits.dtype
+    out = torch.empty((rows, vocab), dtype=dt, device=logits.device) if out is None else out
+    _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
+                                 _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
+                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), _matrix(out, dt, "out"), _stream()))
     return out
 
 
-def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None, workspace=None):
+def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
     """Forward and derivative in one pass -> (logp, entropy, lse, d_logits)."""
-    rows, vocab = logits.shape
-    logp, entropy, lse = (_rows(rows, logits.device) for _ in range(3))
-    out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device) if out is None else _like(out, logits, "out")
-    if workspace is None:
-        workspace = _workspace(lib().tbp_logprobs_workspace_bytes(rows, vocab, 0), logits.device)
-    _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, _ptr(logits), _matrix(logits, "logits"), _index(targets, rows, "targets"),
-                                   _floats(d_logp, rows, "d_logp"), _floats(d_entropy, rows, "d_entropy"), _ptr(logp), _ptr(entropy), _ptr(lse),
-                                   _ptr(out), _matrix(out, "out"), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
-    return logp, entropy, lse, out
+    (rows, vocab), dt = logits.shape, logits.dtype
+    stats = torch.empty((3, rows), dtype=_F32, device=logits.device)
+    at = stats.data_ptr()
+    out = torch.empty((rows, vocab), dtype=dt, device=logits.device) if out is None else out
+    _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
+                                   _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
+                                   out.data_ptr(), _matrix(out, dt, "out"), _stream()))
+    return (*stats.unbind(), out)
 
 
 # ---- the norm over gradient tensors, and clipping --------------------------------------------------------------------------
@@ -239,16 +246,12 @@ class GradList:
     def sumsq(self, out=None):
         """The sum of squares [1] float64 (stages of a pipeline add theirs up before they clip)."""
         out = torch.empty(1, dtype=torch.float64, device=self.device) if out is None else out
-        if out.dtype != torch.float64:
-            raise TypeError("out must be float64")
-        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _ptr(out), _ptr(self._ws), _stream()))
+        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream()))
         return out
 
     def clip(self, max_norm, sumsq=None, norm=None):
         """Writes the outputs; -> the norm [1] float32.  sumsq: [1] float64, computed here where none is given."""
-        norm = torch.empty(1, dtype=torch.float32, device=self.device) if norm is None else norm
-        if sumsq is not None and sumsq.dtype != torch.float64:
-            raise TypeError("sumsq must be float64")
-        _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _ptr(sumsq), max_norm, _floats(norm, 1, "norm"),
-                                   _ptr(self._ws), _stream()))
+        norm = torch.empty(1, dtype=_F32, device=self.device) if norm is None else norm
+        _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _vector(sumsq, 1, torch.float64, "sumsq"), max_norm,
+                                   _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream()))
         return norm

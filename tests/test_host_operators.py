@@ -28,11 +28,11 @@ ROTARY = dict(dtype=BF16, rows=4, n_heads=2, head_dim=64, rot_dim=32, layout=0, 
 APPEND = dict(dtype=BF16, batch=2, n_new=1, n_heads=4, n_kv_heads=2, head_dim=64, rot_dim=32, layout=0, table=P, n_pos=10, lengths=P, qkv=P,
               ld_qkv=512, q_out=P, ld_q=256, cache_k=P, cache_v=P, ld_cache=128, capacity=8, sinks=2, stream=None)
 LOGPROBS = dict(dtype=BF16, rows=3, vocab=50, logits=P, ld_logits=50, targets=P, logp=P, entropy=P, lse=P, top=3, top_logp=P, top_ids=P,
-                workspace=P, workspace_bytes=1 << 30, stream=None)
+                stream=None)
 LOGPROBS_P1 = dict(dtype=BF16, rows=3, vocab=50, logits=P, ld_logits=50, targets=P, lse=P, entropy=P, d_logp=P, d_entropy=None, d_logits=P,
                    ld_d=50, stream=None)
 LOGPROBS_STEP = dict(dtype=BF16, rows=3, vocab=50, logits=P, ld_logits=50, targets=P, d_logp=P, d_entropy=None, logp=P, entropy=P, lse=P,
-                     d_logits=P, ld_d=50, workspace=P, workspace_bytes=1 << 30, stream=None)
+                     d_logits=P, ld_d=50, stream=None)
 
 CASES = [("tbp_window_attention_fwd", WINDOW, change) for change in (
     {"dtype": F32}, {"dtype": 9}, {"head_dim": 96}, {"n_kv_heads": 3}, {"n_kv_heads": 0}, {"n_heads": 0}, {"batch": -1}, {"seq": -1},
