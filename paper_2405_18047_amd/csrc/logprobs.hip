@@ -55,18 +55,28 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
 // a is ranked before b: larger value, or the same and a lower index
 __device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
 
-constexpr int kCandidates = 1024;
-
-// What the threads of a row share.
-template <int NT> struct RowShared {
-  Stats red[NT / 64];
+// What the threads of a row share: for the statistics, and for the ranking.
+template <int NT> struct RowShared { Stats red[NT / 64]; };
+template <int NT> struct RankShared {
+  static constexpr int kCandidates = NT == 64 ? 256 : 1024;
   float lane_max[NT / 64][64];
+  float bar;
   int n;
-  float cv[kCandidates];
-  int ci[kCandidates];
+  uint64_t key[kCandidates];
   float bv[NT / 64];
   int bi[NT / 64];
 };
+
+// Value and index as one number: larger for what is ranked before.  (The value's bits as an unsigned number in the order of the values; no
+// NaN comes here, and -0 counts as 0.)
+__device__ __forceinline__ uint64_t rank_key(float v, int i) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~i;
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t u = (uint32_t)(k >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
 
 // One row's pieces: piece c of the thread's block b is at element N (NT (CH b + c) + thread).
 template <typename T, int NT, int CH>
@@ -78,6 +88,12 @@ struct Row {
   __device__ __forceinline__ void forget() {
 #pragma unroll
     for (int c = 0; c < CH; c++) asm volatile("" : "+v"(x[c]));
+  }
+  __device__ __forceinline__ float piece_max(int c) const {
+    float m = L::get(x[c], 0);
+#pragma unroll
+    for (int e = 1; e < N; e++) m = fmaxf(m, L::get(x[c], e));
+    return m;
   }
   static __device__ __forceinline__ int at(int blk, int c) { return N * (NT * (CH * blk + c) + (int)threadIdx.x); }
   __device__ __forceinline__ void load(const T* row, int vocab, int blk) {
@@ -107,41 +123,51 @@ struct Row {
   }
 };
 
-// The k-th largest of 64 numbers, one per lane.
-__device__ __forceinline__ float kth_largest(float v, int k) {
-  int rank = 0;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int j = 0; j < 64; j++) {
-    const float o = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), j));
-    rank += before(o, j, v, lane) ? 1 : 0;
-  }
-  const uint64_t who = __ballot(rank == k - 1);
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), who ? __builtin_ctzll(who) : 0));
-}
-
-// Ranking.  The row's maxima over 64 classes of threads are 64 of its logits, so the top-th largest of them is a lower bound of the top-th
-// largest logit, and hardly more logits than `top` reach it (their number is that of draws from 64 boxes until `top` are met: 24 for 20,
-// 90 for 48).  Those are collected and ranked among each other.  Rows with more than kCandidates of them (a great many ties) are ranked one place
-// at a time over the whole row.
+// Ranking.  The row's maxima over 64 (or 128) classes of threads are so many of its logits, so the top-th largest of them is a lower bound of
+// the top-th largest logit, and hardly more logits than `top` reach it: as many as draws from 64 boxes take until `top` have been
+// met, 24 for 20 and 44 for 32 (of 128 boxes 89 for 64).  Those are collected and ranked among each other.  Rows with more of them than there is
+// room for (a great many ties) are ranked one place at a time over the whole row.
 template <typename T, int NT, int CH>
-__device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const T* x, Row<T, NT, CH>& data, int nblk, float my_max, float lse,
-                                         RowShared<NT>& sh) {
+__device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const T* x, Row<T, NT, CH>& data, const float (&piece_max)[CH], int nblk, float my_max, float lse,
+                                         RankShared<NT>& sh) {
   using R = Row<T, NT, CH>;
-  const int tid = threadIdx.x;
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* const out_v = p.top_logp + row * p.top;
   int* const out_i = p.top_ids + row * p.top;
   if (!(lse == lse)) {                               // NaN or +infinity in the row
     if (tid < p.top) { out_v[tid] = __builtin_nanf(""); out_i[tid] = -1; }
     return;
   }
-  sh.lane_max[tid >> 6][tid & 63] = my_max;
+  // the bar: the waves rank the classes among them, 64 / NW (128 / NW) each, and whoever finds the one in place top - 1 says so
   if (tid == 0) sh.n = 0;
-  __syncthreads();
-  float cls = -INFINITY;
+  const int classes = NW > 1 && p.top > 32 ? 128 : 64;
+  if constexpr (NW > 1) {
+    sh.lane_max[wave][lane] = my_max;
+    __syncthreads();
+  }
+  float cls[2] = {my_max, -INFINITY};
+  if constexpr (NW > 1) {
+    cls[0] = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < NT / 64; w++) cls = fmaxf(cls, sh.lane_max[w][tid & 63]);
-  const float bar = kth_largest(cls, p.top);
+    for (int w = 0; w < NW; w++) cls[w & 1] = fmaxf(cls[w & 1], sh.lane_max[w][lane]);
+    if (classes == 64) cls[0] = fmaxf(cls[0], cls[1]);
+  }
+  if constexpr (NW == 1) {                           // one wave: every lane finds its own class's rank
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < 64; j++)
+      rank += before(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_max), j)), j, my_max, lane) ? 1 : 0;
+    if (rank == p.top - 1) sh.bar = my_max;
+  }
+  for (int j = wave; NW > 1 && j < classes; j += NW) {
+    const float mine = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, j < 64 ? cls[0] : cls[1]), j & 63));
+    int rank = __popcll(__ballot(before(cls[0], lane, mine, j)));
+    if (classes == 128) rank += __popcll(__ballot(before(cls[1], 64 + lane, mine, j)));
+    if (rank == p.top - 1) sh.bar = mine;
+  }
+  __syncthreads();
+  const float bar = sh.bar;
   // (bar -infinity: fewer than `top` classes hold a finite logit; the finite ones are collected and the rest of the places filled below)
   if (my_max >= bar && my_max > -INFINITY) {
     for (int b = 0; b < nblk; b++) {
@@ -149,35 +175,35 @@ __device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const
       data.forget();
 #pragma unroll
       for (int c = 0; c < CH; c++) {
+        if ((nblk > 1 ? data.piece_max(c) : piece_max[c]) < bar) continue;
 #pragma unroll
         for (int e = 0; e < R::N; e++) {
           const float v = Logits<T>::get(data.x[c], e);
           if (v >= bar && v > -INFINITY) {
             const int at = atomicAdd(&sh.n, 1);
-            if (at < kCandidates) { sh.cv[at] = v; sh.ci[at] = R::at(b, c) + e; }
+            if (at < sh.kCandidates) sh.key[at] = rank_key(v, R::at(b, c) + e);
           }
         }
       }
     }
   }
   __syncthreads();
-  const int n = sh.n;
-  if (n <= kCandidates) {
-    for (int i = tid; i < n; i += NT) {
-      const float v = sh.cv[i];
-      const int id = sh.ci[i];
+  const int n = __builtin_amdgcn_readfirstlane(sh.n);
+  if (n <= sh.kCandidates) {
+    for (int i = wave; i < n; i += NW) {             // a wave counts what is ranked before candidate i
+      const uint64_t mine = sh.key[i];
       int rank = 0;
-      for (int j = 0; j < n; j++) rank += before(sh.cv[j], sh.ci[j], v, id) ? 1 : 0;
-      if (rank < p.top) { out_v[rank] = v - lse; out_i[rank] = id; }
+      for (int j0 = 0; j0 < n; j0 += 64) rank += __popcll(__ballot(j0 + lane < n && sh.key[j0 + lane] > mine));
+      if (lane == 0 && rank < p.top) { out_v[rank] = key_value(mine) - lse; out_i[rank] = (int)~(uint32_t)mine; }
     }
     // fewer finite logits than places: the others in order of their index, which are among the first n + top
-    if (n < p.top && tid < 64) {
+    if (n < p.top && wave == 0) {
       int place = n;
       for (int i0 = 0; place < p.top; i0 += 64) {
-        const bool none = i0 + tid < p.vocab && (float)x[i0 + tid] == -INFINITY;
+        const bool none = i0 + lane < p.vocab && (float)x[i0 + lane] == -INFINITY;
         const uint64_t who = __ballot(none);
-        const int at = place + __popcll(who & ((1ull << tid) - 1));
-        if (none && at < p.top) { out_v[at] = -INFINITY; out_i[at] = i0 + tid; }
+        const int at = place + __popcll(who & ((1ull << lane) - 1));
+        if (none && at < p.top) { out_v[at] = -INFINITY; out_i[at] = i0 + lane; }
         place += __popcll(who);
       }
     }
@@ -240,7 +266,7 @@ __device__ __forceinline__ void store_piece(T* row, int i, int vocab, const floa
 }
 
 template <typename T, int NT, int CH, bool STEP>
-__global__ __launch_bounds__(NT) void logprobs_kernel(LogprobParams p) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void logprobs_kernel(LogprobParams p) {
   using R = Row<T, NT, CH>;
   __shared__ RowShared<NT> sh;
   const int tid = threadIdx.x;
@@ -249,14 +275,15 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobParams p) {
   const int nblk = (p.vocab + NT * CH * R::N - 1) / (NT * CH * R::N);
   R data;
   Stats a{-INFINITY, 0.f, 0.f};
-  float my_max = -INFINITY;
+  float my_max = -INFINITY, piece_max[CH];            // (of the last block)
   for (int b = 0; b < nblk; b++) {
     data.load(x, p.vocab, b);
     float mx = my_max;
 #pragma unroll
-    for (int c = 0; c < CH; c++)
-#pragma unroll
-      for (int e = 0; e < R::N; e++) mx = fmaxf(mx, Logits<T>::get(data.x[c], e));
+    for (int c = 0; c < CH; c++) {
+      piece_max[c] = data.piece_max(c);
+      mx = fmaxf(mx, piece_max[c]);
+    }
     if (mx > my_max) {                               // the reference point moves to the maximum
       const float r = mx * kLog2e, d = a.r == -INFINITY ? 0.f : a.r - r, f = __builtin_amdgcn_exp2f(d);
       a.t = (a.t + d * a.s) * f;
@@ -314,7 +341,8 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobParams p) {
       }
     }
   } else {
-    if (p.top) rank_top<T, NT, CH>(p, row, x, data, nblk, my_max, lse, sh);
+    __shared__ RankShared<NT> rank;
+    if (p.top) rank_top<T, NT, CH>(p, row, x, data, piece_max, nblk, my_max, lse, rank);
   }
 }
 
@@ -346,8 +374,12 @@ static hipError_t launch(const LogprobParams& p, hipStream_t s) {
 template <typename T, bool STEP>
 static hipError_t launch_t(const LogprobParams& p, hipStream_t s) {
   constexpr int N = Logits<T>::N;
+  const bool many = p.rows > 256;
+  if (p.vocab <= 64 * 4 * N && p.top <= 32) return launch<T, 64, 4, STEP>(p, s);
+  if (p.vocab <= 64 * 16 * N && many && p.top <= 32) return launch<T, 64, 16, STEP>(p, s);
   if (p.vocab <= 256 * 4 * N) return launch<T, 256, 4, STEP>(p, s);
-  if (p.rows >= 512 && p.vocab <= 256 * 16 * N) return launch<T, 256, 16, STEP>(p, s);
+  if (many && (p.vocab <= 256 * 16 * N || (!STEP && p.vocab > 512 * 16 * N))) return launch<T, 256, 16, STEP>(p, s);
+  if (many && p.vocab <= 512 * 16 * N) return launch<T, 512, 16, STEP>(p, s);
   if (p.vocab <= 1024 * 4 * N) return launch<T, 1024, 4, STEP>(p, s);
   return launch<T, 1024, 16, STEP>(p, s);
 }
