@@ -7,7 +7,29 @@
 
 namespace tbp {
 
-constexpr int kPiece = 8192;           // elements that a workgroup takes at a time
+// Elements that a workgroup takes at a time: 8192, of lists of up to 16 M elements 4096 (clipping 0.8 M 9.3 / 8.3 us, 0.4 M 9.2 / 8.3; 25 M 63.4 /
+// 62.5; 405 M 708 / 717).
+constexpr int kPiece = 8192, kSmallPiece = 4096;
+constexpr int64_t kSmallList = 16 << 20;
+// The norm of a list of more than this reads it past the caches: the clipping launch that follows finds nothing of it there anyway.  us, kept / past,
+// the norm, and with clipping into bf16: 1.6 GB 265 / 238 and 709 / 682, 810 MB 143 / 127 and 362 / 347, 405 MB 76.4 / 69.4 and 224 / 218; of
+// 202 MB, which the memory-side cache keeps, 43.8 / 39.6, but 91 / 98 with clipping.
+constexpr int64_t kStreamedBytes = (int64_t)384 << 20;
+
+// Accesses of 16 bytes that are not to be kept in the caches.
+template <typename T> __device__ __forceinline__ void load_past(const T* p, float* v) {
+  Vec<T>::unpack(__builtin_bit_cast(typename Vec<T>::Raw, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p))), v);
+}
+__device__ __forceinline__ void store_past(float* p, const float* v) {
+  const u32x4 r{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(p));
+}
+__device__ __forceinline__ void store_past(bf16_t* p, const float* v) {
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; i++) r[i] = (bf16_t)v[i];
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p));
+}
 
 __device__ __forceinline__ double block_sum(double v) {        // of 256 threads, the same in all, order fixed
   __shared__ double red[4];
@@ -28,20 +50,20 @@ __device__ __forceinline__ int tensor_of(const GradTable& t, int i) {
   return lo;
 }
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable t, double* __restrict__ sums) {
   constexpr int N = Vec<T>::N;
   double acc = 0.0;
   for (int i = blockIdx.x; i < t.pieces; i += gridDim.x) {
     const int k = tensor_of(t, i);
-    const long at = (long)(i - t.first[k]) * kPiece, left = t.count[k] - at;
+    const long at = (long)(i - t.first[k]) * t.piece, left = t.count[k] - at;
     const T* const g = (const T*)t.src[k] + at;
-    const int n = left < kPiece ? (int)left : kPiece;
+    const int n = left < t.piece ? (int)left : t.piece;
     if ((uintptr_t)g % 16 == 0) {
 #pragma unroll 4
       for (int j = threadIdx.x * N; j + N <= n; j += 256 * N) {
         float v[N];
-        Vec<T>::load(g + j, v);
+        if constexpr (PAST) load_past<T>(g + j, v); else Vec<T>::load(g + j, v);
 #pragma unroll
         for (int e = 0; e < N; e++) acc += (double)v[e] * (double)v[e];
       }
@@ -73,10 +95,10 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const doubl
   for (int i = blockIdx.x; i < t.pieces; i += gridDim.x) {
     const int k = tensor_of(t, i);
     if (!clips && (const void*)t.src[k] == t.dst[k]) continue;         // in place, and nothing changes
-    const long at = (long)(i - t.first[k]) * kPiece, left = t.count[k] - at;
+    const long at = (long)(i - t.first[k]) * t.piece, left = t.count[k] - at;
     const T* const g = (const T*)t.src[k] + at;
     O* const o = (O*)t.dst[k] + at;
-    const int n = left < kPiece ? (int)left : kPiece;
+    const int n = left < t.piece ? (int)left : t.piece;
     int done = 0;
     if ((uintptr_t)g % 16 == 0 && (uintptr_t)o % 16 == 0) {
 #pragma unroll 4
@@ -87,7 +109,7 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const doubl
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] *= c;
 #pragma unroll
-        for (int e = 0; e < 8; e += Vec<O>::N) Vec<O>::store(o + j + e, v + e);
+        for (int e = 0; e < 8; e += Vec<O>::N) store_past(o + j + e, v + e);
       }
       done = n / 8 * 8;
     }
@@ -101,11 +123,15 @@ static int grid_of(const GradTable& t) { return t.pieces < kGradSums ? t.pieces 
 template <typename F>
 static hipError_t tables(int n, const void* const* src, void* const* dst, const int64_t* counts, F body) {
   int sums = 0;
+  int64_t all = 0;
+  for (int i = 0; i < n; i++) all += counts[i];
+  const int piece = all <= kSmallList ? kSmallPiece : kPiece;
   for (int i = 0; i < n;) {
     GradTable t{};
+    t.piece = piece;
     for (; i < n && t.n < kGradTable; i++) {
       if (counts[i] == 0) continue;
-      const int64_t pieces = (counts[i] + kPiece - 1) / kPiece;
+      const int64_t pieces = (counts[i] + piece - 1) / piece;
       if (t.pieces + pieces > (1 << 30)) break;
       t.src[t.n] = src[i]; t.dst[t.n] = dst ? dst[i] : nullptr; t.count[t.n] = counts[i]; t.first[t.n] = t.pieces;
       t.pieces += (int)pieces;
@@ -120,9 +146,13 @@ static hipError_t tables(int n, const void* const* src, void* const* dst, const 
 
 hipError_t grad_sumsq(int dtype, int n, const void* const* grads, const int64_t* counts, double* sums, int* n_sums, hipStream_t s) {
   *n_sums = 0;
+  int64_t bytes = 0;
+  for (int i = 0; i < n; i++) bytes += counts[i] * (dtype ? 2 : 4);
+  const bool past = bytes > kStreamedBytes;
   return tables(n, grads, nullptr, counts, [&](const GradTable& t, int grid, int before) {
-    if (dtype) hipLaunchKernelGGL((grad_sumsq_kernel<bf16_t>), dim3((unsigned)grid), dim3(256), 0, s, t, sums + before);
-    else hipLaunchKernelGGL((grad_sumsq_kernel<float>), dim3((unsigned)grid), dim3(256), 0, s, t, sums + before);
+    auto kern = dtype ? (past ? grad_sumsq_kernel<bf16_t, true> : grad_sumsq_kernel<bf16_t, false>)
+                      : (past ? grad_sumsq_kernel<float, true> : grad_sumsq_kernel<float, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, t, sums + before);
     *n_sums = before + grid;
     return hipGetLastError();
   });

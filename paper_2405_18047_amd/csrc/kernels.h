@@ -283,7 +283,7 @@ hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s);
 constexpr int kGradTable = 96;                       // tensors per launch (the table travels as a kernel argument)
 constexpr int kGradSums = 2048;                      // sums (workgroups) per launch
 struct GradTable {
-  int n, pieces;
+  int n, pieces, piece;                              // tensors, their pieces, elements of a piece
   const void* src[kGradTable]; void* dst[kGradTable];
   int64_t count[kGradTable];
   int first[kGradTable];                             // the tensor's first piece

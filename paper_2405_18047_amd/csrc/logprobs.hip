@@ -25,15 +25,17 @@ template <typename T> struct Logits {
   static constexpr int N = 16 / (int)sizeof(T);
   typedef typename std::conditional<sizeof(T) == 4, Any4, Any2>::type Any;
   static __device__ __forceinline__ u32x4 load(const T* p) { return *reinterpret_cast<const Any*>(p); }
+  // (nontemporal: [4096, 32000] bf16 with its derivative 109.6 -> 88.6 us; loads of that kind, 109.6 -> 97.0)
   static __device__ __forceinline__ void store(T* p, const float* v) {
     if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<Any*>(p) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+      const u32x4 o{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+      __builtin_nontemporal_store(o, reinterpret_cast<Any*>(p));
     } else {
       typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
       bf16x8 o;
 #pragma unroll
       for (int i = 0; i < 8; i++) o[i] = (bf16_t)v[i];
-      *reinterpret_cast<Any*>(p) = __builtin_bit_cast(u32x4, o);
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), reinterpret_cast<Any*>(p));
     }
   }
   static __device__ __forceinline__ float get(const u32x4& r, int i) {      // i is a constant after unrolling
