@@ -884,6 +884,19 @@ struct WinDecodeParams {
   float scale_log2e;
 };
 
+constexpr int kShareTiles = 8;         // two per wave
+
+// Numbers that another workgroup, perhaps on another XCD, reads behind a counter: written through to memory that all of them see, and read from
+// there.  (A fence that writes the whole L2 back instead cost 40 to 80 us a call where many workgroups have one.)
+__device__ __forceinline__ void store_shared(float* p, float a, float b) {
+  const uint64_t v = (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_shared(const float* p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
 // Asynchronous global -> LDS copy of 16 bytes per lane from a 64-bit address (a cache may be longer than a buffer descriptor's range).
 __device__ __forceinline__ void dma16_far(uint32_t lds_base, const void* src) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(src) : "memory");
@@ -907,7 +920,10 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
   const int first = len - reach > p.sinks ? len - reach : p.sinks;
   const int seen = n_sink + (len > first ? len - first : 0);
   const int r0 = (first - p.sinks) % ring;                     // ring place of the window's first key
-  const int tiles = (seen + 31) / 32, per = (tiles + p.splits - 1) / p.splits;
+  // shares of the tiles that there are: at most `splits`, none below kShareTiles; the workgroups behind them have nothing to do
+  const int tiles = (seen + 31) / 32, even = (tiles + p.splits - 1) / p.splits, per = even > kShareTiles ? even : kShareTiles;
+  const int shares = tiles > per ? (tiles + per - 1) / per : 1;
+  if (sp >= shares) return;
   const int t0 = sp * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
   const typename HT::Offsets fo = HT::offsets(lane);
@@ -1028,42 +1044,45 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
       for (int k = 0; k < 4; k++) o[k] += f * x[k];
     }
     const long head = (long)b * p.H + hk * p.G + gq0 + r;
-    if (p.splits > 1) {
-      *reinterpret_cast<f32x4*>(p.part_o + (head * p.splits + sp) * DH + c) = o;
-      if (c == 0) p.part_ml[head * p.splits + sp] = make_float2(M, L);
+    if (shares > 1) {
+      float* const at = p.part_o + (head * p.splits + sp) * DH + c;
+      store_shared(at, o[0], o[1]);
+      store_shared(at + 2, o[2], o[3]);
+      if (c == 0) store_shared(reinterpret_cast<float*>(p.part_ml + head * p.splits + sp), M, L);
     } else {
       finish(r, c, o, M, L);
     }
   }
-  if (p.splits == 1) return;
-  // ---- the share that is done last joins all of them, in their order.  (The partial sums are written through to memory that every XCD sees
-  // before the share is counted, and read behind the count.)
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-  __syncthreads();
+  if (shares == 1) return;
+  // ---- the share that is done last joins all of them, in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // this wave's sums are where everyone sees them ...
+  __syncthreads();                                            // ... and every wave's, before the share is counted
   LDS_AS unsigned* const flag = reinterpret_cast<LDS_AS unsigned*>(all);
   if (threadIdx.x == 0) {
     unsigned* const count = p.arrived + ((long)blockIdx.z * gridDim.x + blockIdx.x);
-    const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool last = before + 1 == (unsigned)p.splits;
+    const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (unsigned)shares;
     if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *flag = last ? 1u : 0u;
   }
   __syncthreads();
   if (!*flag) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   for (int i = (int)threadIdx.x; i < nh * (DH / 4); i += 256) {
     const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
     const long at = ((long)b * p.H + hk * p.G + gq0 + r) * p.splits;
     float M = -INFINITY, L = 0.f;
-    for (int k = 0; k < p.splits; k++) M = fmaxf(M, p.part_ml[at + k].x);
+#pragma unroll 8
+    for (int k = 0; k < shares; k++) M = fmaxf(M, load_shared(reinterpret_cast<const float*>(p.part_ml + at + k)).x);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < p.splits; k++) {
-      const float2 ml = p.part_ml[at + k];
+#pragma unroll 8
+    for (int k = 0; k < shares; k++) {
+      const float2 ml = load_shared(reinterpret_cast<const float*>(p.part_ml + at + k));
+      const float2 x = load_shared(p.part_o + (at + k) * DH + c), z = load_shared(p.part_o + (at + k) * DH + c + 2);
       const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
       L += f * ml.y;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + (at + k) * DH + c);
-#pragma unroll
-      for (int e = 0; e < 4; e++) o[e] += f * x[e];
+      o[0] += f * x.x;
+      o[1] += f * x.y;
+      o[2] += f * z.x;
+      o[3] += f * z.y;
     }
     finish(r, c, o, M, L);
   }
@@ -1162,11 +1181,15 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   return w.head_dim == 128 ? launch_kv<128>(p, s) : launch_kv<64>(p, s);
 }
 
-int window_decode_splits(int batch, int kv_heads, long most_seen) {
-  const long groups = (long)batch * kv_heads;
+// Shares of a head's keys, at most: two workgroups per compute unit; but a share costs the joining workgroup as much as most of a tile of keys (its sums
+// of 32 heads, in proportion less of fewer), so no more than make the reading of a share and the joining of all of them about equal.
+int window_decode_splits(int batch, int heads, int kv_heads, long most_seen) {
+  const int group = heads / kv_heads, nh = group < 32 ? group : 32;
+  const long groups = (long)batch * kv_heads * ((group + 31) / 32), tiles = (most_seen + 31) / 32;
   long splits = (512 + groups - 1) / groups;
-  const long tiles = (most_seen + 31) / 32;
-  if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;      // two tiles per wave at least
+  const long most = (tiles + kShareTiles - 1) / kShareTiles, level = (long)sqrt(40.0 * tiles / nh);
+  if (splits > most) splits = most;
+  if (splits > level) splits = level;
   return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
 }
 

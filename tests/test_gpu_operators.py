@@ -168,6 +168,23 @@ def test_window_decode_matches_oracle(case):
     assert np.all(np.abs(l - l_ref)[fine] < 1e-5 * (1 + np.abs(l_ref[fine])))
 
 
+def test_window_decode_calls_share_a_workspace():
+    """Calls of one size after each other with one workspace, lengths from none to the whole window, so that the shares that a head's keys are cut
+    into are many, few and one: each as with a workspace of its own."""
+    nb, H, KV, dh, window, sinks = 3, 8, 2, 64, 4000, 4
+    _say("decode calls with one workspace")
+    ck, cv = (to_dev(_rnd(68, c, (nb * 4004, KV * dh), "bf16"), "bf16").view(nb, 4004, -1) for c in ("k", "v"))
+    ws = tbp.tbp_window_decode_workspace(nb, H, KV, dh, window, sinks)
+    assert ws is not None
+    for i, lengths in enumerate(([4000, 1, 300], [0, 0, 0], [257, 256, 255], [9999, 5000, 4004], [700, 0, 31], [4004, 2000, 1000]) * 2):
+        q = to_dev(_rnd(69 + i, "q", (nb, H * dh), "bf16"), "bf16")
+        out, lse = tbp.tbp_window_decode(q, ck, cv, _ints(lengths), H, KV, dh, window, sinks, workspace=ws)
+        o2, l2 = tbp.tbp_window_decode(q, ck, cv, _ints(lengths), H, KV, dh, window, sinks)
+        assert torch.equal(out, o2) and torch.equal(lse, l2) and not bool(ws[:256].any())
+        for b, n in enumerate(lengths):
+            assert bool(torch.isfinite(lse[b]).all()) == (n > 0)
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_tokens_one_by_one_are_the_sequence_at_once(interleaved):
     """Appending and decoding token by token, over a ring that wraps, gives the rows of the rotation and forward of the whole sequence."""
