@@ -91,7 +91,7 @@ tbp_status tbp_window_attention_p1(int dtype, int batch, int n_heads, int n_kv_h
 struct DecodeSpace { int splits; size_t part_o, part_ml, bytes; };
 static DecodeSpace decode_space(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks) {
   DecodeSpace d{};
-  d.splits = tbp::window_decode_splits(batch, n_heads, n_kv_heads, (long)window + sinks);
+  d.splits = tbp::window_decode_splits(batch, n_heads, n_kv_heads, head_dim, (long)window + sinks);
   const size_t parts = (size_t)batch * n_heads * d.splits, groups = (n_heads / n_kv_heads + 31) / 32;
   d.part_o = align_up((size_t)batch * n_kv_heads * groups * sizeof(unsigned), 256);
   d.part_ml = d.part_o + align_up(parts * head_dim * sizeof(float), 256);

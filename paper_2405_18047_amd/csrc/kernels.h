@@ -242,7 +242,7 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
 hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, const void* out,
                                const void* d_out, long ld_out, const float* lse, void* dqkv, long ld_dqkv, float* delta,
                                float* partial, hipStream_t s);
-int window_decode_splits(int batch, int heads, int kv_heads, long most_seen);
+int window_decode_splits(int batch, int heads, int kv_heads, int head_dim, long most_seen);
 hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths, const void* q, long ld_q, const void* cache_k,
                          const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, unsigned* arrived,
                          float* part_o, float2* part_ml, hipStream_t s);

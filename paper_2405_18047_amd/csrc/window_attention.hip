@@ -884,7 +884,8 @@ struct WinDecodeParams {
   float scale_log2e;
 };
 
-constexpr int kShareTiles = 8;         // two per wave
+// Tiles of a share, at least: two per wave, at head_dim 64 four (us, 8 / 16 tiles: 300 keys at 64 8.3 / 7.0, 500 12.1 / 10.7; 700 at 128 9.0 / 11.5).
+constexpr int share_tiles(int head_dim) { return 1024 / head_dim; }
 
 // Numbers that another workgroup, perhaps on another XCD, reads behind a counter: written through to memory that all of them see, and read from
 // there.  (A fence that writes the whole L2 back instead cost 40 to 80 us a call where many workgroups have one.)
@@ -898,11 +899,14 @@ __device__ __forceinline__ float2 load_shared(const float* p) {
 }
 
 // Asynchronous global -> LDS copy of 16 bytes per lane from a 64-bit address (a cache may be longer than a buffer descriptor's range).
+// PAST: not kept in the caches, for more keys than they hold (64 sequences of 4096 keys of 8 heads of 128 201 -> 183 us; 16.4 MB 11.5 -> 12.0).
+template <bool PAST>
 __device__ __forceinline__ void dma16_far(uint32_t lds_base, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(src) : "memory");
+  if constexpr (PAST) asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(lds_base), "v"(src) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(src) : "memory");
 }
 
-template <int DH>
+template <int DH, bool PAST>
 __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, IMG = 32 * HT::RB, SLOT = 2 * IMG, NCH = IMG / 1024, RING = 2;
@@ -920,8 +924,8 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
   const int first = len - reach > p.sinks ? len - reach : p.sinks;
   const int seen = n_sink + (len > first ? len - first : 0);
   const int r0 = (first - p.sinks) % ring;                     // ring place of the window's first key
-  // shares of the tiles that there are: at most `splits`, none below kShareTiles; the workgroups behind them have nothing to do
-  const int tiles = (seen + 31) / 32, even = (tiles + p.splits - 1) / p.splits, per = even > kShareTiles ? even : kShareTiles;
+  // shares of the tiles that there are: at most `splits`, none below share_tiles; the workgroups behind them have nothing to do
+  const int tiles = (seen + 31) / 32, even = (tiles + p.splits - 1) / p.splits, per = even > share_tiles(DH) ? even : share_tiles(DH);
   const int shares = tiles > per ? (tiles + per - 1) / per : 1;
   if (sp >= shares) return;
   const int t0 = sp * per, t1 = t0 + per < tiles ? t0 + per : tiles;
@@ -946,8 +950,8 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
       int x = r0 + v - n_sink;
       x = x >= ring ? x - ring : x;
       const long off = (long)(v < n_sink ? v : p.sinks + x) * p.ld_c + 8 * G16;
-      dma16_far(base + c * 1024, kbase + off);
-      dma16_far(base + IMG + c * 1024, vbase + off);
+      dma16_far<PAST>(base + c * 1024, kbase + off);
+      dma16_far<PAST>(base + IMG + c * 1024, vbase + off);
     }
   };
   f32x16 ot[DT];
@@ -1070,19 +1074,19 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
     const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
     const long at = ((long)b * p.H + hk * p.G + gq0 + r) * p.splits;
     float M = -INFINITY, L = 0.f;
-#pragma unroll 8
-    for (int k = 0; k < shares; k++) M = fmaxf(M, load_shared(reinterpret_cast<const float*>(p.part_ml + at + k)).x);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int k = 0; k < shares; k++) {
+    for (int k = 0; k < shares; k++) {                         // (one pass: the loads of eight shares wait for memory together)
       const float2 ml = load_shared(reinterpret_cast<const float*>(p.part_ml + at + k));
       const float2 x = load_shared(p.part_o + (at + k) * DH + c), z = load_shared(p.part_o + (at + k) * DH + c + 2);
-      const float f = __builtin_amdgcn_exp2f(ml.x - (M == -INFINITY ? 0.f : M));
-      L += f * ml.y;
-      o[0] += f * x.x;
-      o[1] += f * x.y;
-      o[2] += f * z.x;
-      o[3] += f * z.y;
+      const float m2 = fmaxf(M, ml.x), ref2 = m2 == -INFINITY ? 0.f : m2;
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref2), keep = __builtin_amdgcn_exp2f(M - ref2);
+      M = m2;
+      L = L * keep + f * ml.y;
+      o[0] = o[0] * keep + f * x.x;
+      o[1] = o[1] * keep + f * x.y;
+      o[2] = o[2] * keep + f * z.x;
+      o[3] = o[3] * keep + f * z.y;
     }
     finish(r, c, o, M, L);
   }
@@ -1181,22 +1185,23 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   return w.head_dim == 128 ? launch_kv<128>(p, s) : launch_kv<64>(p, s);
 }
 
-// Shares of a head's keys, at most: two workgroups per compute unit; but a share costs the joining workgroup as much as most of a tile of keys (its sums
+// Shares of a head's keys, at most: a workgroup per compute unit (us, one / two of them: batch 8, 4096 keys of 8 heads of 128 35.3 / 41.9, batch 32 106 /
+// 109); but a share costs the joining workgroup as much as most of a tile of keys (its sums
 // of 32 heads, in proportion less of fewer), so no more than make the reading of a share and the joining of all of them about equal.
-int window_decode_splits(int batch, int heads, int kv_heads, long most_seen) {
+int window_decode_splits(int batch, int heads, int kv_heads, int head_dim, long most_seen) {
   const int group = heads / kv_heads, nh = group < 32 ? group : 32;
   const long groups = (long)batch * kv_heads * ((group + 31) / 32), tiles = (most_seen + 31) / 32;
-  long splits = (512 + groups - 1) / groups;
-  const long most = (tiles + kShareTiles - 1) / kShareTiles, level = (long)sqrt(40.0 * tiles / nh);
+  long splits = (256 + groups - 1) / groups;
+  const long most = (tiles + share_tiles(head_dim) - 1) / share_tiles(head_dim), level = (long)sqrt(40.0 * tiles / nh);
   if (splits > most) splits = most;
   if (splits > level) splits = level;
   return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
 }
 
-template <int DH>
+template <int DH, bool PAST>
 static hipError_t launch_decode(const WinDecodeParams& p, hipStream_t s) {
   constexpr size_t smem = 4 * 2 * 2 * 32 * DH * 2;
-  auto kern = window_decode_kernel<DH>;
+  auto kern = window_decode_kernel<DH, PAST>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.B * p.KV), (unsigned)p.splits, (unsigned)((p.G + 31) / 32)), dim3(256), smem, s, p);
@@ -1213,7 +1218,10 @@ hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths,
   p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.capacity = capacity; p.window = w.window;
   p.sinks = w.sinks; p.splits = splits;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
-  return w.head_dim == 128 ? launch_decode<128>(p, s) : launch_decode<64>(p, s);
+  // keys and values that the calls of these sizes may read, at most: more than the second-level caches hold?
+  const long most = w.window + (long)w.sinks, rows = most < capacity ? most : capacity;
+  if (4L * w.batch * w.kv_heads * rows * w.head_dim > (64L << 20)) return w.head_dim == 128 ? launch_decode<128, true>(p, s) : launch_decode<64, true>(p, s);
+  return w.head_dim == 128 ? launch_decode<128, false>(p, s) : launch_decode<64, false>(p, s);
 }
 
 }  // namespace tbp
