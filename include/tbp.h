@@ -299,7 +299,8 @@ tbp_status tbp_attention_p1(int dtype, int batch, int n_heads, int seq, int head
  * lengths: device [batch] int32 or NULL: tokens of each sequence (taken as 0 .. seq); rows behind them are padding, never
  * read, and come out as zeros (lse: -infinity).  A token's row has to be finite: in a tile of 32 keys with one that a query
  * sees, an infinite or NaN value row reaches that query.
- * Limits: 0 <= seq <= 2^20, window >= 1, sinks >= 0; leading dimensions multiples of 8 below 2^22, tensors 16-byte aligned. */
+ * Limits: 0 <= seq <= 2^20, window >= 1, sinks >= 0, batch * n_heads below 2^23; leading dimensions multiples of 8 below 2^22,
+ * tensors 16-byte aligned. */
 tbp_status tbp_window_attention_fwd(int dtype, int batch, int n_heads, int n_kv_heads, int seq, int head_dim, int window,
                                     int sinks, const int32_t* lengths, const void* qkv, int ld_qkv, void* out, int ld_out,
                                     float* lse, void* stream);
@@ -371,7 +372,9 @@ tbp_status tbp_rotary_append(int dtype, int batch, int n_new, int n_heads, int n
 tbp_status tbp_logprobs(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets, float* logp,
                         float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* stream);
 /* The derivative of the logits, d_logits [rows, ld_d] in the storage type, from lse and entropy of the forward and the derivatives of
- * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits. */
+ * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits.
+ * (p comes from x - lse: of a row whose logits are so large that lse does not show log sum, such as one of nothing but the type's lowest value,
+ * tbp_logprobs_step gives the derivative, this call does not.) */
 tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
                            const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
                            int64_t ld_d, void* stream);

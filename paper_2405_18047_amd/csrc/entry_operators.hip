@@ -27,7 +27,7 @@ tbp_status check_window(int dtype, int batch, int n_heads, int n_kv_heads, int s
   if (batch < 0 || seq < 0) return fail(TBP_EINVAL, "negative size");
   if (seq > (1 << 20)) return fail(TBP_EINVAL, "seq %d above the limit %d", seq, 1 << 20);
   if (window < 1 || sinks < 0) return fail(TBP_EINVAL, "window must be at least 1 and sinks at least 0");
-  if ((long)batch * n_heads > 0x7fffffffL) return fail(TBP_EINVAL, "batch * n_heads too large");
+  if ((long)batch * n_heads >= (1L << 23)) return fail(TBP_EINVAL, "batch * n_heads must be below 2^23");
   return TBP_OK;
 }
 

@@ -260,7 +260,7 @@ struct RotaryParams {
   // append only: x's heads are q_heads of q, kv_heads of k, kv_heads of v
   const int* lengths; int tokens_new, q_heads, kv_heads;
   void* cache_k; void* cache_v; long ld_c; int capacity, sinks;
-  int units, groups; long items;                     // set by the launch
+  int units, groups, row0; long items;               // set by the launch
 };
 hipError_t rotary(int dtype, const RotaryParams& p, hipStream_t s);
 hipError_t rotary_append(int dtype, const RotaryParams& p, hipStream_t s);

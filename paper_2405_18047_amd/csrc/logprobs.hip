@@ -1,8 +1,9 @@
 // Log probabilities of given tokens over rows of logits, with the entropy of every row and its most likely tokens, and the
-// derivative of the logits.  In units of log 2, with a reference point r near the maximum:
-//   s = sum 2^d, t = sum d 2^d, d = x log2 e - r:   lse = (r + log2 s) ln 2,  logp = x_target - lse,  H = (log2 s - t / s) ln 2,
-//   dx = dlogp (1[target] - p) - dH p (log p + H),  p = 2^(x log2 e - lse / ln 2).
-// The products x log2 e go into d unrounded (fused multiply-add), so r may be any number: s, t and lse refer to the same one.
+// derivative of the logits.  With the maximum m of a row and d = (x - m) log2 e,
+//   s = sum 2^d, t = sum d 2^d:   lse = m + ln s,  logp = (x_target - m) - ln s,  H = (log2 s - t / s) ln 2,
+//   dx = dlogp (1[target] - p) - dH p (log p + H),  p = 2^(d - log2 s).
+// The difference comes first: it is as exact as the logits for those that count, and a row of nothing but the type's lowest value (a mask
+// that leaves nothing) is the uniform distribution that it says.
 //
 // A workgroup owns a row and holds it in registers (16 or 4 pieces of 16 bytes per thread) from the statistics to the ranking or to the
 // derivative: a row is read once.  Rows longer than that are walked in blocks and read a second time for the derivative (for the ranking
@@ -45,13 +46,14 @@ template <typename T> struct Logits {
   static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;      // -infinity
 };
 
-// Statistics of a part of a row; r = -infinity: no finite logit so far (s, t: zeros, or NaN that is passed on).
-struct Stats { float r, s, t; };
+// Statistics of a part of a row; m = -infinity: nothing above it so far (s, t: zeros, or NaN that is passed on).
+struct Stats { float m, s, t; };
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
-  const float r = fmaxf(a.r, b.r);
-  const float da = a.r == -INFINITY ? 0.f : a.r - r, db = b.r == -INFINITY ? 0.f : b.r - r;
-  const float fa = a.r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(da), fb = b.r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(db);
-  return Stats{r, a.s * fa + b.s * fb, (a.t + da * a.s) * fa + (b.t + db * b.s) * fb};
+  const float m = fmaxf(a.m, b.m);
+  // (of the two one is m; the other's difference may be infinite: then its factor is zero and only has to stay clear of 0 * infinity)
+  const float da = a.m == -INFINITY ? 0.f : fmaxf((a.m - m) * kLog2e, kFar), db = b.m == -INFINITY ? 0.f : fmaxf((b.m - m) * kLog2e, kFar);
+  const float fa = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(da), fb = b.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(db);
+  return Stats{m, a.s * fa + b.s * fb, (a.t + da * a.s) * fa + (b.t + db * b.s) * fb};
 }
 
 // a is ranked before b: larger value, or the same and a lower index
@@ -130,7 +132,7 @@ struct Row {
 // met, 24 for 20 and 44 for 32 (of 128 boxes 89 for 64).  Those are collected and ranked among each other.  Rows with more of them than there is
 // room for (a great many ties) are ranked one place at a time over the whole row.
 template <typename T, int NT, int CH>
-__device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const T* x, Row<T, NT, CH>& data, const float (&piece_max)[CH], int nblk, float my_max, float lse,
+__device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const T* x, Row<T, NT, CH>& data, const float (&piece_max)[CH], int nblk, float my_max, float lse, float m, float ln_s,
                                          RankShared<NT>& sh) {
   using R = Row<T, NT, CH>;
   constexpr int NW = NT / 64;
@@ -196,7 +198,7 @@ __device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const
       const uint64_t mine = sh.key[i];
       int rank = 0;
       for (int j0 = 0; j0 < n; j0 += 64) rank += __popcll(__ballot(j0 + lane < n && sh.key[j0 + lane] > mine));
-      if (lane == 0 && rank < p.top) { out_v[rank] = key_value(mine) - lse; out_i[rank] = (int)~(uint32_t)mine; }
+      if (lane == 0 && rank < p.top) { out_v[rank] = (key_value(mine) - m) - ln_s; out_i[rank] = (int)~(uint32_t)mine; }
     }
     // fewer finite logits than places: the others in order of their index, which are among the first n + top
     if (n < p.top && wave == 0) {
@@ -231,25 +233,25 @@ __device__ __forceinline__ void rank_top(const LogprobParams& p, long row, const
     v = sh.bv[0]; best = sh.bi[0];
     for (int w = 1; w < NT / 64; w++)
       if (before(sh.bv[w], sh.bi[w], v, best)) { v = sh.bv[w]; best = sh.bi[w]; }
-    if (tid == 0) { out_v[k] = lse == -INFINITY ? -INFINITY : v - lse; out_i[k] = best; }
+    if (tid == 0) { out_v[k] = lse == -INFINITY ? -INFINITY : (v - m) - ln_s; out_i[k] = best; }
     pv = v; pi = best;
   }
 }
 
 // The derivative of one piece of a row.
-struct RowWeights { float lse2, dl, inner, dh2; int target; };      // inner = dl + dH H, dh2 = dH ln 2
-__device__ __forceinline__ RowWeights row_weights(const LogprobParams& p, long row, float lse, float entropy) {
+struct RowWeights { float m, ls, dl, inner, dh2; int target; };     // p = 2^((x - m) log2 e - ls); inner = dl + dH H, dh2 = dH ln 2
+__device__ __forceinline__ RowWeights row_weights(const LogprobParams& p, long row, float m, float ls, float entropy) {
   const int t = p.targets[row];
-  const bool given = t >= 0 && t < p.vocab, none = lse == -INFINITY;
+  const bool given = t >= 0 && t < p.vocab, none = m == -INFINITY;
   const float dl = given && !none ? p.d_logp[row] : 0.f, dh = p.d_entropy && !none ? p.d_entropy[row] : 0.f;
-  return RowWeights{none ? 0.f : lse * kLog2e, dl, dl + dh * entropy, dh * kLn2, given ? t : -1};
+  return RowWeights{none ? 0.f : m, none ? 0.f : ls, dl, dl + dh * entropy, dh * kLn2, given ? t : -1};
 }
 template <typename T>
 __device__ __forceinline__ void derive(const u32x4& x, int i, const RowWeights& w, float* v) {
   using L = Logits<T>;
 #pragma unroll
   for (int e = 0; e < L::N; e++) {
-    const float d = __builtin_fmaf(L::get(x, e), kLog2e, -w.lse2);
+    const float d = __builtin_fmaf(L::get(x, e) - w.m, kLog2e, -w.ls);
     v[e] = -__builtin_amdgcn_exp2f(d) * __builtin_fmaf(w.dh2, fmaxf(d, kFar), w.inner);
   }
   if ((unsigned)(w.target - i) < (unsigned)L::N) {
@@ -287,48 +289,48 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void lo
       mx = fmaxf(mx, piece_max[c]);
     }
     if (mx > my_max) {                               // the reference point moves to the maximum
-      const float r = mx * kLog2e, d = a.r == -INFINITY ? 0.f : a.r - r, f = __builtin_amdgcn_exp2f(d);
+      const float d = a.m == -INFINITY ? 0.f : fmaxf((a.m - mx) * kLog2e, kFar), f = __builtin_amdgcn_exp2f(d);
       a.t = (a.t + d * a.s) * f;
       a.s *= f;
-      a.r = r;
+      a.m = mx;
       my_max = mx;
     }
     data.forget();
-    const float ref = a.r == -INFINITY ? 0.f : a.r;
-    float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+    const float ref = a.m == -INFINITY ? 0.f : a.m;
+    float s[2] = {0.f, 0.f}, t = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++)
 #pragma unroll
       for (int e = 0; e < R::N; e++) {
-        const float d = __builtin_fmaf(Logits<T>::get(data.x[c], e), kLog2e, -ref), v = __builtin_amdgcn_exp2f(d);
+        const float d = (Logits<T>::get(data.x[c], e) - ref) * kLog2e, v = __builtin_amdgcn_exp2f(d);
         s[e & 1] += v;
-        t[e & 1] = __builtin_fmaf(v, fmaxf(d, kFar), t[e & 1]);
+        t = __builtin_fmaf(v, fmaxf(d, kFar), t);
       }
     a.s += s[0] + s[1];
-    a.t += t[0] + t[1];
+    a.t += t;
   }
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  for (int d = 1; d < 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
   if ((tid & 63) == 0) sh.red[tid >> 6] = a;
   __syncthreads();
   a = sh.red[tid & (NT / 64 - 1)];
 #pragma unroll
-  for (int d = 1; d < NT / 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  for (int d = 1; d < NT / 64; d <<= 1) a = join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
   // (lane 0's sums for all: lanes may differ in the last bit)
   auto first = [](float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); };
-  a = Stats{first(a.r), first(a.s), first(a.t)};
-  const bool none = a.r == -INFINITY && a.s == a.s;                 // nothing but -infinity
+  a = Stats{first(a.m), first(a.s), first(a.t)};
+  const bool none = a.m == -INFINITY && a.s == a.s;                 // nothing but -infinity
   const float ls = __builtin_amdgcn_logf(a.s);
-  const float lse = none ? -INFINITY : a.r == -INFINITY ? a.s : (a.r + ls) * kLn2, entropy = none ? 0.f : (ls - a.t / a.s) * kLn2;
+  const float lse = none ? -INFINITY : a.m == -INFINITY ? a.s : a.m + ls * kLn2, entropy = none ? 0.f : (ls - a.t / a.s) * kLn2;
   if (tid == 0) {
     const int t = p.targets[row];
-    p.logp[row] = t >= 0 && t < p.vocab ? (none ? -INFINITY : (float)x[t] - lse) : 0.f;
+    p.logp[row] = t >= 0 && t < p.vocab ? (none ? -INFINITY : ((float)x[t] - a.m) - ls * kLn2) : 0.f;
     p.entropy[row] = entropy;
     p.lse[row] = lse;
   }
   if constexpr (STEP) {
     __syncthreads();                                                // (in place: the target's logit has been read)
-    const RowWeights w = row_weights(p, row, lse, entropy);
+    const RowWeights w = row_weights(p, row, lse == lse ? a.m : lse, ls, entropy);
     T* const o = (T*)p.d_logits + row * p.ld_d;
     for (int b = 0; b < nblk; b++) {
       if (nblk > 1) data.load(x, p.vocab, b);
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void lo
     }
   } else {
     __shared__ RankShared<NT> rank;
-    if (p.top) rank_top<T, NT, CH>(p, row, x, data, piece_max, nblk, my_max, lse, rank);
+    if (p.top) rank_top<T, NT, CH>(p, row, x, data, piece_max, nblk, my_max, lse, a.m, ls * kLn2, rank);
   }
 }
 
@@ -355,7 +357,7 @@ __global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
   const long row = blockIdx.x;
   R data;
   data.load((const T*)p.logits + row * p.ld, p.vocab, blockIdx.y);
-  const RowWeights w = row_weights(p, row, p.lse[row], p.entropy[row]);
+  const RowWeights w = row_weights(p, row, p.lse[row], 0.f, p.entropy[row]);
   T* const o = (T*)p.d_logits + row * p.ld_d;
 #pragma unroll
   for (int c = 0; c < 4; c++) {
@@ -367,10 +369,28 @@ __global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
   }
 }
 
+// The rows from r0 on (a launch takes at most kLaunchRows of them: its threads are counted in 32 bits).
+constexpr int kLaunchRows = 1 << 21;
+static LogprobParams rows_from(LogprobParams p, int r0, int element) {
+  p.rows = p.rows - r0 < kLaunchRows ? p.rows - r0 : kLaunchRows;
+  p.logits = (const char*)p.logits + r0 * p.ld * element;
+  p.targets += r0; p.entropy += r0; p.lse += r0;
+  if (p.logp) p.logp += r0;
+  if (p.top) { p.top_logp += (long)r0 * p.top; p.top_ids += (long)r0 * p.top; }
+  if (p.d_logp) p.d_logp += r0;
+  if (p.d_entropy) p.d_entropy += r0;
+  if (p.d_logits) p.d_logits = (char*)p.d_logits + r0 * p.ld_d * element;
+  return p;
+}
+
 template <typename T, int NT, int CH, bool STEP>
 static hipError_t launch(const LogprobParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((logprobs_kernel<T, NT, CH, STEP>), dim3((unsigned)p.rows), dim3(NT), 0, s, p);
-  return hipGetLastError();
+  for (int r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
+    const LogprobParams q = rows_from(p, r0, sizeof(T));
+    hipLaunchKernelGGL((logprobs_kernel<T, NT, CH, STEP>), dim3((unsigned)q.rows), dim3(NT), 0, s, q);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, bool STEP>
@@ -391,10 +411,14 @@ hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s) { ret
 
 hipError_t logprobs_p1(int dtype, const LogprobParams& p, hipStream_t s) {
   const int per = 256 * 4 * (dtype ? 8 : 4);
-  const dim3 grid((unsigned)p.rows, (unsigned)((p.vocab + per - 1) / per));
-  if (dtype) hipLaunchKernelGGL((logprobs_p1_kernel<bf16_t>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((logprobs_p1_kernel<float>), grid, dim3(256), 0, s, p);
-  return hipGetLastError();
+  for (int r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
+    const LogprobParams q = rows_from(p, r0, dtype ? 2 : 4);
+    const dim3 grid((unsigned)q.rows, (unsigned)((p.vocab + per - 1) / per));
+    if (dtype) hipLaunchKernelGGL((logprobs_p1_kernel<bf16_t>), grid, dim3(256), 0, s, q);
+    else hipLaunchKernelGGL((logprobs_p1_kernel<float>), grid, dim3(256), 0, s, q);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace tbp

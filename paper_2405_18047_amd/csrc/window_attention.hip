@@ -1144,16 +1144,17 @@ WindowParts window_parts(const WindowShape& w) {
   const int sinks = w.sinks < w.seq ? w.sinks : w.seq, G = w.heads / w.kv_heads;
   r.sink_blocks = (sinks + 127) / 128;
   const long all = (w.seq + 63) / 64, seen = ((long)w.window + 126 + 64) / 64 + 1;
-  const long sink_pairs = G * all, other_pairs = G * (seen < all ? seen : all);      // pairs of the longest lists
-  // parts: about 256 workgroups at least, where the lists are long enough for them (4 pairs a part)
-  const long groups = (long)w.batch * w.kv_heads * r.blocks;
-  long parts = groups < 256 ? (256 + groups - 1) / groups : 1;
-  if (parts > (other_pairs + 3) / 4) parts = (other_pairs + 3) / 4;
-  if (parts > 32) parts = 32;
-  r.other_parts = (int)parts;
-  const long share = (other_pairs + parts - 1) / parts;
-  long sp = (sink_pairs + share - 1) / share;
-  r.sink_parts = (int)(sp > 256 ? 256 : sp < 1 ? 1 : sp);
+  const long sink_pairs = G * all, other_pairs = G * (seen < all ? seen : all);      // pairs of the longest lists, of each kind
+  // a part: enough of them for 256 workgroups, where the lists are long enough for that (4 pairs each), at most a whole list of the other blocks;
+  // of the sinks' lists, so that they make no more than 1024 parts in all (sinks may be as many as tokens, and the window short)
+  const long heads = (long)w.batch * w.kv_heads, others = r.blocks - r.sink_blocks;
+  const long pairs = heads * (r.sink_blocks * sink_pairs + others * other_pairs);
+  long share = other_pairs * (heads * r.blocks < 256 ? heads * r.blocks : 256) / 256;
+  share = share < 4 ? 4 : share;
+  share = share > other_pairs ? other_pairs : share;
+  r.other_parts = (int)((other_pairs + share - 1) / share);
+  const long sink_share = share > (pairs + 1023) / 1024 ? share : (pairs + 1023) / 1024;
+  r.sink_parts = (int)((sink_pairs + sink_share - 1) / sink_share);
   return r;
 }
 

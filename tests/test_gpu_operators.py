@@ -42,7 +42,7 @@ WINDOW_CASES = [  # seq, batch, H, KV, dh, window, sinks, lengths
     (129, 2, 2, 1, 128, 32, 3, [129, 64]), (131, 3, 6, 2, 64, 7, 0, [131, 0, 5]), (257, 1, 8, 2, 128, 100, 64, None),
     (300, 2, 4, 4, 64, 300, 0, [299, 1]), (333, 1, 5, 1, 128, 65, 129, None), (513, 1, 4, 2, 128, 1, 1, None),
     (700, 1, 3, 3, 64, 128, 200, [641]), (1001, 2, 4, 2, 128, 250, 4, [1001, 777]), (1100, 1, 8, 8, 64, 5000, 9, None),
-    (1500, 1, 2, 1, 128, 200, 1500, None), (2500, 1, 3, 1, 64, 333, 130, None),
+    (1500, 1, 2, 1, 128, 200, 1500, None), (2500, 1, 3, 1, 64, 333, 130, None), (3000, 1, 4, 2, 64, 3, 3000, None), (2049, 1, 1, 1, 128, 10, 700, [2048]),
     (90, 65, 8, 2, 64, 20, 2, None), (140, 40, 4, 4, 128, 50, 1, [140 - 3 * i for i in range(40)]), (600, 5, 16, 4, 128, 90, 5, None),
 ]
 
@@ -396,6 +396,37 @@ def test_logprobs_gradient_in_place_and_without_entropy(rows, vocab, dtype):
     tbp.tbp_logprobs_step(b, tt, w, out=b)
     assert torch.equal(a, want) and torch.equal(b, tbp.tbp_logprobs_step(dev, tt, w)[3])
     assert torch.all(a._base[:, 0] == 100.0) and torch.all(a._base[:, -2:] == 100.0) and torch.all(b._base[:, 0] == 100.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [50, 9000, 140000])
+def test_logprobs_of_rows_masked_with_the_lowest_value(vocab, dtype):
+    """Masked logits that are the type's lowest finite value: some of a row (probability zero), and all of it (the uniform distribution: entropy log
+    vocab, to the fp32 sum of that many ones; lse, which has no room for log vocab beside it, is the lowest value)."""
+    _say(f"logprobs, lowest values, vocab={vocab} {dtype}")
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    low = torch.finfo(t).min
+    x = to_dev(_rnd(84, "x", (3, vocab), dtype), dtype)
+    x[0, vocab // 2:] = low
+    x[1] = low
+    x[2, 1:] = low
+    w, targets = torch.ones(3, device=DEV), _ints([0, 3, 0])
+    logp, entropy, lse, top_logp, top_ids = tbp.tbp_logprobs(x, targets, top=5)
+    s = tbp.tbp_logprobs_step(x, targets, w)
+    half = ref.logprobs(to_np(x)[:1, :vocab // 2], [0])
+    ln = float(np.log(vocab))
+    for got in ((logp, entropy, lse), s[:3]):
+        got = [to_np(g) for g in got]
+        assert np.all(np.abs(np.array([g[0] for g in got]) - [h[0] for h in half]) <= 2e-5 * (1 + np.abs([h[0] for h in half])))
+        assert abs(got[0][1] + ln) < 2e-5 * ln and abs(got[1][1] - ln) < 2e-5 * ln and got[2][1] == float(low)
+        assert got[0][2] == 0.0 and got[1][2] == 0.0 and got[2][2] == float(x[2, 0])
+    assert top_ids[1].tolist() == [0, 1, 2, 3, 4] and top_ids[2].tolist() == [0, 1, 2, 3, 4]
+    assert np.all(np.abs(to_np(top_logp)[1] + ln) < 2e-5 * ln)
+    d = to_np(s[3])
+    want = np.full(vocab, -1.0 / vocab)
+    want[3] += 1.0
+    assert np.all(np.abs(d[1] - want) <= (2.0 ** -8 if dtype == "bf16" else 2e-5) * np.abs(want)) and not np.any(d[2])
+    assert not np.any(d[0, vocab // 2:])
 
 
 @pytest.mark.parametrize("bad", [NAN, float("inf")])

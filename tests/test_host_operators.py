@@ -36,7 +36,7 @@ LOGPROBS_STEP = dict(dtype=BF16, rows=3, vocab=50, logits=P, ld_logits=50, targe
 
 CASES = [("tbp_window_attention_fwd", WINDOW, change) for change in (
     {"dtype": F32}, {"dtype": 9}, {"head_dim": 96}, {"n_kv_heads": 3}, {"n_kv_heads": 0}, {"n_heads": 0}, {"batch": -1}, {"seq": -1},
-    {"seq": (1 << 20) + 1}, {"window": 0}, {"sinks": -1}, {"qkv": None}, {"out": None}, {"lse": None}, {"ld_qkv": 504}, {"ld_qkv": 516},
+    {"batch": 1 << 21}, {"seq": (1 << 20) + 1}, {"window": 0}, {"sinks": -1}, {"qkv": None}, {"out": None}, {"lse": None}, {"ld_qkv": 504}, {"ld_qkv": 516},
     {"ld_out": 248}, {"ld_out": 1 << 22}, {"qkv": ODD}, {"out": ODD})]
 CASES += [("tbp_window_attention_p1", WINDOW_P1, change) for change in (
     {"dtype": F32}, {"head_dim": 32}, {"window": 0}, {"d_out": None}, {"dqkv": None}, {"scratch": None}, {"scratch": C.c_void_p((1 << 20) + 16)},
@@ -100,7 +100,8 @@ def test_bad_gradient_lists_are_refused():
 def test_sizes_that_callers_are_asked_for():
     L = tbp.lib()
     # the row sums at least, and room for a bounded number of parts of key blocks; nothing of the size of the scores
-    for b, h, kv, s, dh, w, k in ((1, 32, 8, 8192, 128, 2048, 4), (4, 12, 4, 1001, 64, 300, 3), (1, 1, 1, 1, 64, 1, 0), (2, 8, 1, 100000, 128, 512, 1000)):
+    for b, h, kv, s, dh, w, k in ((1, 32, 8, 8192, 128, 2048, 4), (4, 12, 4, 1001, 64, 300, 3), (1, 1, 1, 1, 64, 1, 0), (2, 8, 1, 100000, 128, 512, 1000),
+                              (1, 64, 8, 1 << 20, 128, 1, 1 << 20), (1, 1, 1, 1 << 20, 64, 4096, 1 << 19)):
         got = L.tbp_window_attention_p1_scratch_bytes(b, h, kv, s, dh, w, k)
         assert b * h * s * 4 <= got < b * h * s * 4 + (1 << 30)
     assert L.tbp_window_attention_p1_scratch_bytes(0, 32, 8, 8192, 128, 2048, 4) == 0 == L.tbp_window_attention_p1_scratch_bytes(1, 3, 2, 8, 128, 1, 4)
