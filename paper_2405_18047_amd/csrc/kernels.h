@@ -223,10 +223,10 @@ inline int run_end(const int* mbs, int n, int i, int tokens) {
 
 // ---- sliding-window attention with sinks (bf16 storage, head_dim 64 or 128), see include/tbp.h ----------------------------------
 struct WindowShape { int batch, heads, kv_heads, seq, head_dim, window, sinks; };      // window, sinks at most seq (decode: at most capacity)
-// How the pass over the queries cuts the lists of (query head, query step) pairs of its key blocks of 128: those of the sinks into
+// How the pass over the queries cuts the lists of (query head, query step) pairs of its key blocks (of 128 or 64 keys): those of the sinks into
 // sink_parts each, the others into other_parts; a block of more than one part leaves partial sums.
 struct WindowParts {
-  int blocks, sink_blocks, sink_parts, other_parts;
+  int keys, blocks, sink_blocks, sink_parts, other_parts;
   __host__ __device__ int workgroups() const { return sink_blocks * sink_parts + (blocks - sink_blocks) * other_parts; }
   __host__ __device__ int cut_blocks() const { return (sink_parts > 1 ? sink_blocks : 0) + (other_parts > 1 ? blocks - sink_blocks : 0); }
   __host__ __device__ int partials() const { return (sink_parts > 1 ? sink_blocks * sink_parts : 0) + (other_parts > 1 ? (blocks - sink_blocks) * other_parts : 0); }

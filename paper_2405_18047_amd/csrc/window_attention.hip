@@ -546,16 +546,17 @@ struct WinKvParams {
   const float* delta;
   const int* lengths;
   bf16_t* dqkv; long ld_dqkv;
-  float* partial;                      // [B KV][sum of parts over the key blocks that are cut][2][128][DH]
+  float* partial;                      // [B KV][sum of parts over the key blocks that are cut][2][KEYS][DH]
   int B, H, KV, G, S, window, sinks;
   WindowParts parts;
   float scale, scale_log2e;
 };
 
-template <int DH>
+template <int DH, int KEYS>
 __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
   using HT = HeadTile<DH>;
-  constexpr int KEYS = 128, KS = DH / 16, DT = DH / 32, BQ = 64, KB = KEYS / 32;
+  constexpr int KS = DH / 16, DT = DH / 32, BQ = 64;
+  constexpr int KB = KEYS / 32, TPI = 4 / KB;                 // 32-key blocks of the workgroup; 32-query tiles per iteration
   constexpr int IMG = BQ * HT::RB, SLOT = 2 * IMG + 1024;     // Q image, dO image, 64 x (lse, delta); three slots
   constexpr int NCH = IMG / 1024 / 4;                         // copies per right wave and image
   constexpr int OPS = 2 * NCH + 1;                            // vector-memory operations of one issue(), per right wave
@@ -569,14 +570,15 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
 
   const int tid = threadIdx.x, lane = tid & 63, kl = lane & 31, g = lane >> 5;
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int right = wave8 >> 2, wave = wave8 & 3;             // role, and which 32 keys of the block
+  const int right = wave8 >> 2, wave = wave8 & 3;             // role
+  const int kblk = KB == 4 ? wave : wave % KB, tq_left = KB == 4 ? 0 : wave / KB;      // a left wave's 32 keys of the block, and its tile of an iteration
   const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
   const int y = (int)blockIdx.y;
   const bool sink_block = y < p.parts.sink_blocks * p.parts.sink_parts;
   const int np = sink_block ? p.parts.sink_parts : p.parts.other_parts;
   const int yy = sink_block ? y : y - p.parts.sink_blocks * p.parts.sink_parts;
   const int kb = yy / np + (sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
-  const int kv0 = kb * KEYS, kw0 = kv0 + 32 * wave, key = kw0 + kl;
+  const int kv0 = kb * KEYS, kw0 = kv0 + 32 * kblk, key = kw0 + kl;
   const long tok0 = (long)b * p.S;
   const int n = seq_end(p.lengths, b, p.S);
   const typename HT::Offsets fo = HT::offsets(lane);
@@ -587,7 +589,7 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
   const int nst = step1 > step0 ? step1 - step0 : 0;
   const int total = p.G * nst, share = (total + np - 1) / np;
   const int i0 = part * share < total ? part * share : total, i1 = i0 + share < total ? i0 + share : total;
-  const int nt = 2 * (i1 - i0);                               // 32-query tiles
+  const int nt = 2 * (i1 - i0) / TPI;                         // iterations
   const int hq0 = nst ? i0 / nst : 0, sq0 = nst ? step0 + i0 - hq0 * nst : 0;      // the first pair
   typedef LDS_AS float lds_f32;
   lds_u8* const my_hand = hand + wave * 4096 + lane * 16;     // + buffer * HAND + 1024 * {p0, p1, s0, s1}
@@ -604,23 +606,23 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
     __syncthreads();                                          // the first two steps and the K / V rows have landed
 #pragma unroll
     for (int s = 0; s < KS; s++) {
-      kfb[s] = HT::rows_frag(kvimg, fo, 32 * wave, s);
-      vfb[s] = HT::rows_frag(kvimg + KVIMG, fo, 32 * wave, s);
+      kfb[s] = HT::rows_frag(kvimg, fo, 32 * kblk, s);
+      vfb[s] = HT::rows_frag(kvimg + KVIMG, fo, 32 * kblk, s);
     }
     __syncthreads();                                          // every left wave has its rows: the area is free again
     int st_at = sq0;                                          // the step that tile `it` lies in
     const int past = key >= p.sinks ? key + p.window : 0x7fffffff;      // the first query past the lane's key's window
     for (int it = 0; it <= nt; it++) {
-      const int qt0 = st_at * BQ + 32 * (it & 1);
+      const int tile = TPI * it + tq_left, qt0 = st_at * BQ + 32 * (tile & 1);
       lds_u8* const out = my_hand + (it & 1) * HAND;
       if (it < nt && unseen(qt0, kw0)) {
 #pragma unroll
         for (int i = 0; i < 4; i++) *reinterpret_cast<LDS_AS u32x4*>(out + 1024 * i) = u32x4{0, 0, 0, 0};
       } else if (it < nt) {
-        lds_u8* const slot = lds + ((it >> 1) % 3) * SLOT;
-        lds_u8* const qimg = slot + (it & 1) * HALF;
+        lds_u8* const slot = lds + ((tile >> 1) % 3) * SLOT;
+        lds_u8* const qimg = slot + (tile & 1) * HALF;
         lds_u8* const dimg = qimg + IMG;
-        const lds_f32* const stat = reinterpret_cast<const lds_f32*>(slot + 2 * IMG) + 32 * (it & 1);
+        const lds_f32* const stat = reinterpret_cast<const lds_f32*>(slot + 2 * IMG) + 32 * (tile & 1);
         f32x16 sa, da;
 #pragma unroll
         for (int e = 0; e < 16; e++) { sa[e] = 0.f; da[e] = 0.f; }
@@ -666,7 +668,7 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
         *reinterpret_cast<LDS_AS bf16x8*>(out + 2048) = ks[0];
         *reinterpret_cast<LDS_AS bf16x8*>(out + 3072) = ks[1];
       }
-      if (it & 1) st_at = st_at + 1 == step1 ? step0 : st_at + 1;
+      if (TPI == 2 || (it & 1)) st_at = st_at + 1 == step1 ? step0 : st_at + 1;
       __syncthreads();
     }
     __syncthreads();                                          // every right wave's copies have landed: the ring is free
@@ -731,7 +733,7 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
     const uint32_t bytes = (uint32_t)((left > 0 ? left : 0) * p.ld_qkv * 2);
     const u32x4 dk = make_desc(kb0, bytes), dv = make_desc(kb0 + (long)p.KV * DH, bytes);
 #pragma unroll
-    for (int i = 0; i < 2 * NCH; i++) {
+    for (int i = 0; i < NCH * KEYS / 64; i++) {
       int row; unsigned go;
       HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
       const unsigned off = row < left ? go : kOob;
@@ -745,15 +747,16 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
   __syncthreads();
   __syncthreads();                                            // the left waves have read their K and V rows
   for (int it = 0; it <= nt; it++) {
-    if (it > 0) {
-      const int tile = it - 1;
-      if (has_cols) {
+    if (it > 0 && has_cols) {
+#pragma unroll
+      for (int tq = 0; tq < TPI; tq++) {
+        const int tile = TPI * (it - 1) + tq;
         lds_u8* const qimg = lds + ((tile >> 1) % 3) * SLOT + (tile & 1) * HALF;
         lds_u8* const dimg = qimg + IMG;
         // this wave's 32 head-dim columns of dO^T and Q^T (two k-steps of 16 queries), then every key block's P and dS, each
         // fetched one key block ahead of its MFMAs (pinned, as on the left)
         bf16x8 fo_d[2], fo_q[2], kp[2][2], ks[2][2];
-        const lds_u8* const in = hand + (tile & 1) * HAND + lane * 16;
+        const lds_u8* const in = hand + ((it - 1) & 1) * HAND + tq * (KB * 4096) + lane * 16;
         auto fetch = [&](int kbk) {
 #pragma unroll
           for (int u = 0; u < 2; u++) {
@@ -777,18 +780,26 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
         }
       }
     }
-    // Pair (it + 1) / 2 is what the left waves start at the next iteration, when `it` is odd: it was issued three barriers ago and only
-    // the issue after it may still be in flight
-    if (it & 1) wait_vmem<OPS>();
-    __syncthreads();
-    // after this barrier nobody reads the pair before it / 2 any more (it even): its slot takes pair it / 2 + 2
-    if (!(it & 1)) issue();
+    if constexpr (TPI == 1) {
+      // Pair (it + 1) / 2 is what the left waves start at the next iteration, when `it` is odd: it was issued three barriers ago and only
+      // the issue after it may still be in flight
+      if (it & 1) wait_vmem<OPS>();
+      __syncthreads();
+      // after this barrier nobody reads the pair before it / 2 any more (it even): its slot takes pair it / 2 + 2
+      if (!(it & 1)) issue();
+    } else {
+      // a whole pair per iteration: the one after the left waves' was issued behind the barrier before, and the one before it, which the
+      // right waves have just finished, leaves its slot to the pair after next
+      wait_vmem<0>();
+      __syncthreads();
+      issue();
+    }
   }
   wait_vmem<0>();                                             // (copies past the end: zeros, no traffic)
   __syncthreads();                                            // ... of every wave, before the ring is reused below
 
   if (np > 1) {
-    // a part of the sums, dK unscaled: [2][128 keys][DH] fp32, 16 bytes per lane
+    // a part of the sums, dK unscaled: [2][KEYS][DH] fp32, 16 bytes per lane
     const long idx = (long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, part);
     float* const base = p.partial + idx * 2 * KEYS * DH;
     if (has_cols) {
@@ -841,9 +852,9 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
 
 // dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 16 key rows of one of them; a thread has 8
 // columns of one row of dK or dV.
-template <int DH>
+template <int DH, int KEYS>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
-  constexpr int KEYS = 128, LPR = DH / 8, ROWS = 256 / (2 * LPR);
+  constexpr int LPR = DH / 8, ROWS = 256 / (2 * LPR);
   const int per = KEYS / ROWS, cut = (int)blockIdx.y / per;
   const int kb = p.parts.sink_parts > 1 ? cut : cut + p.parts.sink_blocks;       // (blocks that are cut: the sinks', the others', or all)
   const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
@@ -1125,29 +1136,34 @@ static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int DH>
+template <int DH, int KEYS>
 static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
   constexpr size_t smem = 3 * (2 * 64 * DH * 2 + 1024) + 2 * 4 * 4096;       // three slots, two hand-over buffers
-  auto kern = window_bwd_kv_kernel<DH>;
+  auto kern = window_bwd_kv_kernel<DH, KEYS>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.KV * p.B), (unsigned)p.parts.workgroups()), dim3(512), smem, s, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.parts.cut_blocks()) return e;
-  constexpr int per = 128 / (256 / (2 * (DH / 8)));
-  hipLaunchKernelGGL((window_bwd_join_kernel<DH>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
+  constexpr int per = KEYS / (256 / (2 * (DH / 8)));
+  hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
 WindowParts window_parts(const WindowShape& w) {
   WindowParts r{};
-  r.blocks = (w.seq + 127) / 128;
+  const long heads = (long)w.batch * w.kv_heads;
+#ifndef WK
+#define WK 128
+#endif
+  r.keys = heads * ((w.seq + 127) / 128) <= WK ? 64 : 128;
+  r.blocks = (w.seq + r.keys - 1) / r.keys;
   const int sinks = w.sinks < w.seq ? w.sinks : w.seq, G = w.heads / w.kv_heads;
-  r.sink_blocks = (sinks + 127) / 128;
-  const long all = (w.seq + 63) / 64, seen = ((long)w.window + 126 + 64) / 64 + 1;
+  r.sink_blocks = (sinks + r.keys - 1) / r.keys;
+  const long all = (w.seq + 63) / 64, seen = ((long)w.window + r.keys - 2 + 64) / 64 + 1;
   const long sink_pairs = G * all, other_pairs = G * (seen < all ? seen : all);      // pairs of the longest lists, of each kind
   // a part: enough of them for 256 workgroups, where the lists are long enough for that (4 pairs each), at most a whole list of the other blocks;
   // of the sinks' lists, so that they make no more than 1024 parts in all (sinks may be as many as tokens, and the window short)
-  const long heads = (long)w.batch * w.kv_heads, others = r.blocks - r.sink_blocks;
+  const long others = r.blocks - r.sink_blocks;
   const long pairs = heads * (r.sink_blocks * sink_pairs + others * other_pairs);
   long share = other_pairs * (heads * r.blocks < 256 ? heads * r.blocks : 256) / 256;
   share = share < 4 ? 4 : share;
@@ -1160,7 +1176,7 @@ WindowParts window_parts(const WindowShape& w) {
 
 size_t window_attention_p1_partial_bytes(const WindowShape& w) {
   const WindowParts r = window_parts(w);
-  return (size_t)w.batch * w.kv_heads * r.partials() * 2 * 128 * w.head_dim * sizeof(float);
+  return (size_t)w.batch * w.kv_heads * r.partials() * 2 * r.keys * w.head_dim * sizeof(float);
 }
 
 hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const void* qkv, long ld_qkv, const void* out,
@@ -1183,7 +1199,8 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   p.B = q.B; p.H = q.H; p.KV = q.KV; p.G = q.G; p.S = q.S; p.window = q.window; p.sinks = q.sinks;
   p.parts = window_parts(w);
   p.scale = q.scale; p.scale_log2e = q.scale_log2e;
-  return w.head_dim == 128 ? launch_kv<128>(p, s) : launch_kv<64>(p, s);
+  if (p.parts.keys == 64) return w.head_dim == 128 ? launch_kv<128, 64>(p, s) : launch_kv<64, 64>(p, s);
+  return w.head_dim == 128 ? launch_kv<128, 128>(p, s) : launch_kv<64, 128>(p, s);
 }
 
 // Shares of a head's keys, at most: a workgroup per compute unit (us, one / two of them: batch 8, 4096 keys of 8 heads of 128 35.3 / 41.9, batch 32 106 /
