@@ -57,7 +57,12 @@ struct HeadOf {
 
 // ------------------------------------------------------------------------------------------ forward
 // One workgroup = 4 waves x 32 queries of one (sequence, head); keys and values stream through LDS in blocks of 64, double-buffered,
-// K one block ahead of V, the scores of the next block computed beside the exponentials of this one in a pinned order.
+// K one block ahead of V, the scores of the next block computed beside the exponentials of this one in a pinned order (AHEAD).
+// SPLIT = 2, for grids that leave compute units idle: 64 queries per workgroup, and two waves per 32 queries, each on one 32-key tile of
+// every block, whose sums meet at the end.
+// Bound by the power of the matrix pipes: [2, 4096] tokens, 32 heads on 8 of 128, window 1024, 4 sinks 150 us, 0.80 PFLOP/s of the pairs that are seen,
+// 1.05 of the tiles that are computed, at a clock of 1.8 GHz.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
+// of the block's code, 165 us).
 template <int DH, bool AHEAD, int SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
@@ -1121,8 +1126,12 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
   p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.seq; p.window = w.window; p.sinks = w.sinks;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
   const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
+  // us, 128 / 64 queries per workgroup: 8 heads of 128, 700 tokens, window 300 16.2 / 10.3; 32, 1024, 256 17.3 / 13.8; 40, 512, all 16.1 / 13.3; lost: 32 heads,
+  // 2048, 512 28.5 / 31.0, 12 heads of 64, 4 ragged sequences of 1001, 300 16.6 / 17.5
   if (w.seq > 64 && groups <= 256) return w.head_dim == 128 ? launch_fwd<128, false, 2>(p, s) : launch_fwd<64, false, 2>(p, s);
-  if (w.seq <= 256) return w.head_dim == 128 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<64, false, 1>(p, s);
+  // the scores of the next block ahead of its turn (AHEAD) / not: 32 heads of 128, 2 sequences of 4096, window 64 54.6 / 52.5, 128 68.5 / 65.3, 256 71.8 /
+  // 71.3, one of 8192, 512 107.7 / 104.4, 2048 247.9 / 250.4, 2 of 8192, all 963 / 970; 4 of 64, 4096, all 315 / 319
+  if (w.seq <= 256 || w.window <= 512) return w.head_dim == 128 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<64, false, 1>(p, s);
   return w.head_dim == 128 ? launch_fwd<128, true, 1>(p, s) : launch_fwd<64, true, 1>(p, s);
 }
 
@@ -1152,10 +1161,11 @@ static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
 WindowParts window_parts(const WindowShape& w) {
   WindowParts r{};
   const long heads = (long)w.batch * w.kv_heads;
-#ifndef WK
-#define WK 128
-#endif
-  r.keys = heads * ((w.seq + 127) / 128) <= WK ? 64 : 128;
+  // 64 keys to a block on few blocks, which are cut into parts of half the partial sums then or into none, and for short windows, of which a block of
+  // 128 sees more than it is seen by.  us of the backward, 128 / 64: 8 key heads of 128, 1024 tokens, window 256 61.3 / 48.0, 2048, 512 105.9 / 88.3,
+  // 8192, 512 369 / 334, 2 sequences of 4096, 128 207 / 182, but 1024 472 / 477, and 8192, 2048 846 / 871; 4 heads of 64, 4 ragged sequences of 1001, 300
+  // 46.7 / 41.1, 8192, 256 96.4 / 82.7; 16 heads of 64, 2048, 512 33.1 / 35.3.
+  r.keys = heads * ((w.seq + 127) / 128) <= 256 || w.window <= 768 ? 64 : 128;
   r.blocks = (w.seq + r.keys - 1) / r.keys;
   const int sinks = w.sinks < w.seq ? w.sinks : w.seq, G = w.heads / w.kv_heads;
   r.sink_blocks = (sinks + r.keys - 1) / r.keys;
