@@ -5,6 +5,8 @@
 #include "kernels.h"
 #include "rows.h"
 
+#include <type_traits>
+
 namespace tbp {
 
 // Elements that a workgroup takes at a time: 8192, of lists of up to 16 M elements 4096 (clipping 0.8 M 9.3 / 8.3 us, 0.4 M 9.2 / 8.3; 25 M 63.4 /
@@ -15,6 +17,16 @@ constexpr int64_t kSmallList = 16 << 20;
 // the norm, and with clipping into bf16: 1.6 GB 265 / 238 and 709 / 682, 810 MB 143 / 127 and 362 / 347, 405 MB 76.4 / 69.4 and 224 / 218; of
 // 202 MB, which the memory-side cache keeps, 43.8 / 39.6, but 91 / 98 with clipping.
 constexpr int64_t kStreamedBytes = (int64_t)384 << 20;
+
+// A list's tensors, or some of them, cut into pieces; of CAP tensors at most.  The table is copied with every launch: up to 16 tensors take one for 16
+// (1, 6, 12 tensors of 4096 elements, us a call one after another: tables for 96 8.6, 8.7, 8.8, for 16 8.1, 8.3, 8.3).
+template <int CAP> struct GradTable {
+  static constexpr int kCap = CAP;
+  int n, pieces, piece;                              // tensors, their pieces, elements of a piece
+  const void* src[CAP]; void* dst[CAP];
+  int64_t count[CAP];
+  int first[CAP];                                    // the tensor's first piece
+};
 
 // Accesses of 16 bytes that are not to be kept in the caches.
 template <typename T> __device__ __forceinline__ void load_past(const T* p, float* v) {
@@ -41,7 +53,8 @@ __device__ __forceinline__ double block_sum(double v) {        // of 256 threads
 }
 
 // The tensor that piece i of the list lies in.
-__device__ __forceinline__ int tensor_of(const GradTable& t, int i) {
+template <int CAP>
+__device__ __forceinline__ int tensor_of(const GradTable<CAP>& t, int i) {
   int lo = 0, hi = t.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -50,8 +63,8 @@ __device__ __forceinline__ int tensor_of(const GradTable& t, int i) {
   return lo;
 }
 
-template <typename T, bool PAST>
-__global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable t, double* __restrict__ sums) {
+template <typename T, bool PAST, int CAP>
+__global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable<CAP> t, double* __restrict__ sums) {
   constexpr int N = Vec<T>::N;
   double acc = 0.0;
   for (int i = blockIdx.x; i < t.pieces; i += gridDim.x) {
@@ -83,8 +96,8 @@ __global__ __launch_bounds__(256) void grad_sum_kernel(const double* __restrict_
   if (threadIdx.x == 0) *out = acc;
 }
 
-template <typename T, typename O>
-__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const double* __restrict__ sums, int n_sums, float max_norm, float* __restrict__ norm_out) {
+template <typename T, typename O, int CAP>
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable<CAP> t, const double* __restrict__ sums, int n_sums, float max_norm, float* __restrict__ norm_out) {
   constexpr int N = Vec<T>::N;
   double acc = 0.0;
   for (int i = threadIdx.x; i < n_sums; i += 256) acc += sums[i];
@@ -117,19 +130,17 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const doubl
   }
 }
 
-static int grid_of(const GradTable& t) { return t.pieces < kGradSums ? t.pieces : kGradSums; }
-
-// Walks the list in tables of kGradTable tensors: body(table, workgroups, sums before it).
+// Walks the list in tables: body(table, workgroups, sums before it).
 template <typename F>
 static hipError_t tables(int n, const void* const* src, void* const* dst, const int64_t* counts, F body) {
-  int sums = 0;
+  int sums = 0, i = 0;
   int64_t all = 0;
-  for (int i = 0; i < n; i++) all += counts[i];
+  for (int k = 0; k < n; k++) all += counts[k];
   const int piece = all <= kSmallList ? kSmallPiece : kPiece;
-  for (int i = 0; i < n;) {
-    GradTable t{};
+  auto fill = [&](auto& t) {
+    t.n = t.pieces = 0;
     t.piece = piece;
-    for (; i < n && t.n < kGradTable; i++) {
+    for (; i < n && t.n < t.kCap; i++) {
       if (counts[i] == 0) continue;
       const int64_t pieces = (counts[i] + piece - 1) / piece;
       if (t.pieces + pieces > (1 << 30)) break;
@@ -137,9 +148,16 @@ static hipError_t tables(int n, const void* const* src, void* const* dst, const 
       t.pieces += (int)pieces;
       t.n++;
     }
-    if (t.n == 0) continue;
-    if (hipError_t e = body(t, grid_of(t), sums); e != hipSuccess) return e;
-    sums += grid_of(t);
+    if (t.n == 0) return hipSuccess;
+    const int grid = t.pieces < kGradSums ? t.pieces : kGradSums, before = sums;
+    sums += grid;
+    return body(t, grid, before);
+  };
+  while (i < n) {
+    hipError_t e;
+    if (n - i <= 16) { GradTable<16> t; e = fill(t); }
+    else { GradTable<kGradTable> t; e = fill(t); }
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -149,9 +167,10 @@ hipError_t grad_sumsq(int dtype, int n, const void* const* grads, const int64_t*
   int64_t bytes = 0;
   for (int i = 0; i < n; i++) bytes += counts[i] * (dtype ? 2 : 4);
   const bool past = bytes > kStreamedBytes;
-  return tables(n, grads, nullptr, counts, [&](const GradTable& t, int grid, int before) {
-    auto kern = dtype ? (past ? grad_sumsq_kernel<bf16_t, true> : grad_sumsq_kernel<bf16_t, false>)
-                      : (past ? grad_sumsq_kernel<float, true> : grad_sumsq_kernel<float, false>);
+  return tables(n, grads, nullptr, counts, [&](const auto& t, int grid, int before) {
+    constexpr int CAP = std::decay_t<decltype(t)>::kCap;
+    auto kern = dtype ? (past ? grad_sumsq_kernel<bf16_t, true, CAP> : grad_sumsq_kernel<bf16_t, false, CAP>)
+                      : (past ? grad_sumsq_kernel<float, true, CAP> : grad_sumsq_kernel<float, false, CAP>);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, t, sums + before);
     *n_sums = before + grid;
     return hipGetLastError();
@@ -166,19 +185,18 @@ hipError_t grad_sum(const double* sums, int n, double* out, hipStream_t s) {
 hipError_t grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,
                      const double* sums, int n_sums, float max_norm, float* norm, hipStream_t s) {
   bool first = true;
-  const hipError_t e = tables(n, grads, outs, counts, [&](const GradTable& t, int grid, int) {
-    float* const out = first ? norm : nullptr;
+  const hipError_t e = tables(n, grads, outs, counts, [&](const auto& t, int grid, int) {
+    constexpr int CAP = std::decay_t<decltype(t)>::kCap;
+    auto kern = dtype ? (out_dtype ? grad_clip_kernel<bf16_t, bf16_t, CAP> : grad_clip_kernel<bf16_t, float, CAP>)
+                      : (out_dtype ? grad_clip_kernel<float, bf16_t, CAP> : grad_clip_kernel<float, float, CAP>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, t, sums, n_sums, max_norm, first ? norm : nullptr);
     first = false;
-    const dim3 g((unsigned)grid), b(256);
-    if (dtype && out_dtype) hipLaunchKernelGGL((grad_clip_kernel<bf16_t, bf16_t>), g, b, 0, s, t, sums, n_sums, max_norm, out);
-    else if (dtype) hipLaunchKernelGGL((grad_clip_kernel<bf16_t, float>), g, b, 0, s, t, sums, n_sums, max_norm, out);
-    else if (out_dtype) hipLaunchKernelGGL((grad_clip_kernel<float, bf16_t>), g, b, 0, s, t, sums, n_sums, max_norm, out);
-    else hipLaunchKernelGGL((grad_clip_kernel<float, float>), g, b, 0, s, t, sums, n_sums, max_norm, out);
     return hipGetLastError();
   });
   if (e != hipSuccess || !first) return e;
-  GradTable none{};                                             // nothing to clip: the norm alone
-  hipLaunchKernelGGL((grad_clip_kernel<float, float>), dim3(1), dim3(256), 0, s, none, sums, n_sums, max_norm, norm);
+  GradTable<16> none;                                           // nothing to clip: the norm alone
+  none.n = none.pieces = 0;
+  hipLaunchKernelGGL((grad_clip_kernel<float, float, 16>), dim3(1), dim3(256), 0, s, none, sums, n_sums, max_norm, norm);
   return hipGetLastError();
 }
 

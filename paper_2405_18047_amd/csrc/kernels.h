@@ -280,14 +280,8 @@ hipError_t logprobs_p1(int dtype, const LogprobParams& p, hipStream_t s);
 hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s);
 
 // ---- the norm over gradient tensors and clipping, see include/tbp.h --------------------------------------------------------------
-constexpr int kGradTable = 96;                       // tensors per launch (the table travels as a kernel argument)
+constexpr int kGradTable = 96;                       // tensors per launch, at most (the table travels as a kernel argument)
 constexpr int kGradSums = 2048;                      // sums (workgroups) per launch
-struct GradTable {
-  int n, pieces, piece;                              // tensors, their pieces, elements of a piece
-  const void* src[kGradTable]; void* dst[kGradTable];
-  int64_t count[kGradTable];
-  int first[kGradTable];                             // the tensor's first piece
-};
 hipError_t grad_sumsq(int dtype, int n, const void* const* grads, const int64_t* counts, double* sums, int* n_sums, hipStream_t s);
 hipError_t grad_sum(const double* sums, int n, double* out, hipStream_t s);
 hipError_t grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,

@@ -50,13 +50,13 @@ def _vector(t, n, dtype, what):
 
 def _matrix(t, dtype, what):
     """The leading dimension of a matrix whose rows are contiguous."""
-    shape = t.shape
-    if t.dtype is not dtype or len(shape) != 2:
+    if t.dtype is not dtype or t.dim() != 2:
         raise TypeError(f"{what} must be a matrix of type {dtype}")
+    rows, columns = t.shape
     ld, step = t.stride()
-    if step != 1 and shape[1] > 1:
+    if step != 1 and columns > 1:
         raise TypeError(f"{what} must have contiguous rows")
-    return ld if shape[0] > 1 or ld > shape[1] else shape[1]
+    return ld if rows > 1 or ld > columns else columns
 
 
 def _caches(k, v, dtype, batch, width):
@@ -82,7 +82,7 @@ def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, si
     if out is None:
         out = qkv.new_empty((qkv.shape[0], n_heads * head_dim))
     if lse is None:
-        lse = torch.empty((batch, n_heads, seq), dtype=_F32, device=qkv.device)
+        lse = qkv.new_empty((batch, n_heads, seq), dtype=_F32)
     _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
                                           qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), _matrix(out, dt, "out"),
                                           _vector(lse, batch * n_heads * seq, _F32, "lse"), _stream()))
@@ -122,7 +122,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     if out is None:
         out = q.new_empty((batch, n_heads * head_dim))
     if lse is None:
-        lse = torch.empty((batch, n_heads), dtype=_F32, device=q.device)
+        lse = q.new_empty((batch, n_heads), dtype=_F32)
     if workspace is None:
         workspace = tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks, q.device)
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
@@ -184,12 +184,12 @@ def tbp_logprobs(logits, targets, top=0):
     """logits [rows, vocab], targets [rows] (int32; outside the vocabulary: left out) -> (logp, entropy, lse), each [rows] fp32, and with top > 0
     (top_logp [rows, top] fp32, top_ids [rows, top] int32) behind them."""
     rows, vocab = logits.shape
-    stats = torch.empty((3, rows), dtype=_F32, device=logits.device)
+    stats = logits.new_empty((3, rows), dtype=_F32)
     at = stats.data_ptr()
     top_logp = top_ids = None
     if top > 0:
-        top_logp = torch.empty((rows, top), dtype=_F32, device=logits.device)
-        top_ids = torch.empty((rows, top), dtype=_I32, device=logits.device)
+        top_logp = logits.new_empty((rows, top), dtype=_F32)
+        top_ids = logits.new_empty((rows, top), dtype=_I32)
     _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits"), _vector(targets, rows, _I32, "targets"),
                               at, at + 4 * rows, at + 8 * rows, top, None if top_logp is None else top_logp.data_ptr(),
                               None if top_ids is None else top_ids.data_ptr(), _stream()))
@@ -200,7 +200,7 @@ def tbp_logprobs(logits, targets, top=0):
 def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=None):
     """-> the derivative of the logits [rows, vocab] (out: the tensor to write to, logits itself allowed)."""
     (rows, vocab), dt = logits.shape, logits.dtype
-    out = torch.empty((rows, vocab), dtype=dt, device=logits.device) if out is None else out
+    out = logits.new_empty((rows, vocab)) if out is None else out
     _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
                                  _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
                                  _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), _matrix(out, dt, "out"), _stream()))
@@ -210,9 +210,9 @@ def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=N
 def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
     """Forward and derivative in one pass -> (logp, entropy, lse, d_logits)."""
     (rows, vocab), dt = logits.shape, logits.dtype
-    stats = torch.empty((3, rows), dtype=_F32, device=logits.device)
+    stats = logits.new_empty((3, rows), dtype=_F32)
     at = stats.data_ptr()
-    out = torch.empty((rows, vocab), dtype=dt, device=logits.device) if out is None else out
+    out = logits.new_empty((rows, vocab)) if out is None else out
     _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
                                    _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
                                    out.data_ptr(), _matrix(out, dt, "out"), _stream()))
@@ -223,6 +223,7 @@ def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
 class GradList:
     """The gradient tensors of a stage (or of anything else), of one type, and where they go when they are clipped: into themselves, or
     into tensors of the same sizes and of one type.  Keeps the tensors, their addresses and a workspace; calls of one list must not overlap.
+    A call raises where a tensor has been given other memory since (by an assignment to its .data, say).
 
     A Stage's: GradList([g for v in stage.grads.values() for g in v])."""
 
@@ -238,20 +239,27 @@ class GradList:
         n, self.grads, self.outs = len(grads), grads, outs
         self._n, self._dt, self._odt = n, _dt(grads[0]) if n else 0, _dt(outs[0]) if n else 0
         self.device = grads[0].device if n else torch.device("cuda:0")
-        self._src = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in grads])
-        self._dst = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in outs])
+        self._at = [t.data_ptr() for t in grads + outs]
+        self._src = (C.c_void_p * max(n, 1))(*self._at[:n])
+        self._dst = (C.c_void_p * max(n, 1))(*self._at[n:])
         self._counts = (C.c_int64 * max(n, 1))(*[t.numel() for t in grads])
         self._ws = torch.empty(lib().tbp_grad_workspace_bytes(n), dtype=torch.uint8, device=self.device)
 
+    def _in_place(self):
+        if list(map(torch.Tensor.data_ptr, self.grads + self.outs)) != self._at:
+            raise RuntimeError("a tensor of the list has been given other memory: make a new list")
+
     def sumsq(self, out=None):
         """The sum of squares [1] float64 (stages of a pipeline add theirs up before they clip)."""
+        self._in_place()
         out = torch.empty(1, dtype=torch.float64, device=self.device) if out is None else out
         _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream()))
         return out
 
     def clip(self, max_norm, sumsq=None, norm=None):
         """Writes the outputs; -> the norm [1] float32.  sumsq: [1] float64, computed here where none is given."""
-        norm = torch.empty(1, dtype=_F32, device=self.device) if norm is None else norm
+        self._in_place()
+        norm = self._ws.new_empty(1, dtype=_F32) if norm is None else norm
         _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _vector(sumsq, 1, torch.float64, "sumsq"), max_norm,
                                    _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream()))
         return norm

@@ -126,3 +126,12 @@ def test_the_binding_refuses_other_types_and_shapes():
         tbp.GradList([x], [x[:2]])
     with pytest.raises(TypeError):
         tbp.tbp_window_decode(x, x, x, torch.zeros(4, dtype=torch.int32), 1, 1, 64, 2)
+
+
+def test_a_gradient_list_refuses_tensors_that_moved():
+    g, o = torch.zeros(8), torch.zeros(8)
+    moved = tbp.GradList([g], [o])
+    o.data = torch.zeros(8)
+    for call in (moved.sumsq, lambda: moved.clip(1.0)):
+        with pytest.raises(RuntimeError, match="other memory"):
+            call()
