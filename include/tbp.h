@@ -321,8 +321,8 @@ tbp_status tbp_window_attention_p1(int dtype, int batch, int n_heads, int n_kv_h
  * among them (its key and value are in the cache already); of a window longer than capacity - sinks, what the cache keeps.
  * out [batch, ld_out], lse [batch, n_heads] fp32.  lengths[b] <= 0: zeros, lse -infinity.  capacity > sinks.
  * workspace: device, 256-byte aligned, >= tbp_window_decode_workspace_bytes of the same sizes (may be 0: NULL), all zeros before the
- * first call with it; every call leaves it fit for the next one of the same sizes.  Calls that share one must not overlap.  Types, head
- * rules and alignment as above. */
+ * first call with it (which the zeroing has to be ordered before, where it runs on another stream); every call leaves it fit for the next
+ * one of the same sizes.  Calls that share one must not overlap.  Types, head rules and alignment as above. */
 size_t tbp_window_decode_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks);
 tbp_status tbp_window_decode(int dtype, int batch, int n_heads, int n_kv_heads, int head_dim, int window, int sinks,
                              int capacity, const int32_t* lengths, const void* q, int ld_q, const void* cache_k,

@@ -60,8 +60,9 @@ struct HeadOf {
 // K one block ahead of V, the scores of the next block computed beside the exponentials of this one in a pinned order (AHEAD).
 // SPLIT = 2, for grids that leave compute units idle: 64 queries per workgroup, and two waves per 32 queries, each on one 32-key tile of
 // every block, whose sums meet at the end.
-// Bound by the power of the matrix pipes: [2, 4096] tokens, 32 heads on 8 of 128, window 1024, 4 sinks 150 us, 0.80 PFLOP/s of the pairs that are seen,
-// 1.05 of the tiles that are computed, at a clock of 1.8 GHz.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
+// Bound by the matrix pipes, busy 54 % of the cycles that a workgroup is resident, at the clock that the card's power leaves (1.8 GHz): [2, 4096] tokens,
+// 32 heads on 8 of 128, window 1024, 4 sinks 150 to 165 us over cards, 0.73 to 0.80 PFLOP/s of the pairs that are seen, 1.05 at 150 us of the tiles that are
+// computed.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
 // of the block's code, 165 us).
 template <int DH, bool AHEAD, int SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_fwd_kernel(WinParams p) {
@@ -321,6 +322,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // ------------------------------------------------------------------------------------------ backward-p1: dQ and delta
 // dQ = scale * dS K: oriented like the forward, per 32-key tile S^T and dP^T = V dO^T are rebuilt, dS^T = P^T (dP^T - delta) is fed into
 // dQ^T += K^T dS^T.  delta = rowsum(dout * out) of its queries is computed first and left for the pass over the queries.
+// One workgroup = 4 waves x 32 queries, key blocks through LDS in two slots, as in the forward, so that the sum over the keys stays in registers and
+// no atomics are needed.  Bound by the matrix pipes at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 375 us,
+// 0.96 PFLOP/s of the three products over the seen pairs, the pipes busy 55 %.
 struct WinDqParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; const bf16_t* out; long ld_do;
@@ -537,13 +541,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ------------------------------------------------------------------------------------------ backward-p1: dK and dV
-// One workgroup = 128 keys of one (sequence, key head) and a part of the (query head of the group, 64-query step) pairs that see them,
+// One workgroup = 128 keys (64: see window_parts) of one (sequence, key head) and a part of the (query head of the group, 64-query step) pairs that see them,
 // walked as one list, so that dK and dV of shared heads add up in the accumulators.  The key blocks of the sinks are seen by every
 // later query, not just by a window of them: their lists are longer, and cut into parts of about the length of the
 // others'.  Lists are also cut where the key blocks alone are too few to fill the chip.  A key block of one part is written as it is;
 // the parts of others leave fp32 partial sums that a second launch adds up in order.
 // Roles of the waves as in the fused attention's pass: 4 "left" waves compute P and dS of their 32 keys and hand them over through
 // LDS, 4 "right" waves issue all copies and accumulate dV^T += dO^T P, dK^T += Q^T dS of one 32-query tile later.
+// Bound by the matrix pipes and the LDS beside them, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 570 us,
+// 0.84 PFLOP/s of the four products over the seen pairs, the pipes busy 49 %, the LDS 44 %.
 struct WinKvParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; long ld_do;
@@ -885,7 +891,8 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
 // tiles of 32 keys in turn, each through a ring of its own in LDS: no barrier before the waves join.  S^T = K Q^T with the query heads
 // as columns (unused ones: zeros), then O^T += V^T P^T, as in the forward.  The share that is done last joins them all (a launch for it took
 // 3.8 us, and its host side as much again).  Bound by the reading of K and V: a tile is 16 KiB at
-// head_dim 128 and 16 MFMAs, a fifteenth of the time that it takes to arrive.
+// head_dim 128 and 16 MFMAs, a fifteenth of the time that it takes to arrive.  64 ragged sequences of up to 4100 seen keys, 8 heads of 128,
+// 974 MB: 170 us, 5.7 TB/s; one sequence of 700 keys (2.9 MB) 8.9 us, of which a launch that reads nothing is 3.
 // Seen keys are numbered v = 0 .. seen - 1: the sinks, then the window in order; number v lies in slot v (sinks) or
 // sinks + (first + v - n_sink) mod ring.
 struct WinDecodeParams {
