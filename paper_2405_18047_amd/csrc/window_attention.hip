@@ -65,7 +65,7 @@ struct HeadOf {
 // computed.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
 // of the block's code, 165 us).
 template <int DH, bool AHEAD, int SPLIT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_fwd_kernel(WinParams p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT, NT = 2 / SPLIT;
   constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
@@ -337,7 +337,7 @@ struct WinDqParams {
 };
 
 template <int DH, int SPLIT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_bwd_dq_kernel(WinDqParams p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_bwd_dq_kernel(WinDqParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT;
   constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
@@ -861,8 +861,8 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
   }
 }
 
-// dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 16 key rows of one of them; a thread has 8
-// columns of one row of dK or dV.
+// dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 8 or 16 key rows of one of them; a thread has 8
+// columns of one row of dK or dV.  Bound by the latency of the parts: 38 of them 13.4 us one at a time, 7.6 eight at a time.
 template <int DH, int KEYS>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   constexpr int LPR = DH / 8, ROWS = 256 / (2 * LPR);
@@ -873,12 +873,24 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   const int row = ((int)blockIdx.y % per) * ROWS + t / LPR, col = 8 * (t % LPR);
   const int np = kb < p.parts.sink_blocks ? p.parts.sink_parts : p.parts.other_parts;
   const float* src = p.partial + ((long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, 0)) * 2 * KEYS * DH + (long)which * KEYS * DH + (long)row * DH + col;
+  constexpr long PART = 2L * KEYS * DH;
+  constexpr int AT_ONCE = 8;                         // parts on their way together
   float v[8] = {};
-  for (int i = 0; i < np; i++) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(src + (long)i * 2 * KEYS * DH), c = *reinterpret_cast<const f32x4*>(src + (long)i * 2 * KEYS * DH + 4);
+  int i = 0;
+  for (; i + AT_ONCE <= np; i += AT_ONCE) {
+    f32x4 a[AT_ONCE][2];
 #pragma unroll
-    for (int k = 0; k < 4; k++) { v[k] += a[k]; v[4 + k] += c[k]; }
+    for (int j = 0; j < AT_ONCE; j++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) a[j][h] = *reinterpret_cast<const f32x4*>(src + (i + j) * PART + 4 * h);
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++)
+#pragma unroll
+      for (int k = 0; k < 8; k++) v[k] += a[j][k >> 2][k & 3];
   }
+  for (; i < np; i++)
+#pragma unroll
+    for (int k = 0; k < 8; k++) v[k] += src[i * PART + k];
   const int krow = kb * KEYS + row;
   if (krow >= p.S) return;
 #pragma unroll
@@ -1133,13 +1145,15 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
   p.B = w.batch; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.seq; p.window = w.window; p.sinks = w.sinks;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
   const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
-  // us, 128 / 64 queries per workgroup: 8 heads of 128, 700 tokens, window 300 16.2 / 10.3; 32, 1024, 256 17.3 / 13.8; 40, 512, all 16.1 / 13.3; lost: 32 heads,
-  // 2048, 512 28.5 / 31.0, 12 heads of 64, 4 ragged sequences of 1001, 300 16.6 / 17.5
-  if (w.seq > 64 && groups <= 256) return w.head_dim == 128 ? launch_fwd<128, false, 2>(p, s) : launch_fwd<64, false, 2>(p, s);
+  // 64 queries per workgroup where those of 128 leave compute units short of work; a unit has room for 2 workgroups at head_dim 128, 4 at 64.  us, 128 / 64
+  // queries: 8 heads of 128, 700 tokens, window 300 16.2 / 10.3; 32, 1024, 256 17.3 / 13.8; 40, 512, all 16.1 / 13.3, but 32, 2048, 512 28.5 / 31.0; of 64:
+  // 12 heads, 4 ragged sequences of 1001, 300 15.7 / 11.8; 16, 4096, all 61.8 / 55.6, but 32, 4 of 2048, 256 38.4 / 39.9
+  if (w.seq > 64 && groups <= (w.head_dim == 64 ? 512 : 256)) return w.head_dim == 128 ? launch_fwd<128, false, 2>(p, s) : launch_fwd<64, false, 2>(p, s);
   // the scores of the next block ahead of its turn (AHEAD) / not: 32 heads of 128, 2 sequences of 4096, window 64 54.6 / 52.5, 128 68.5 / 65.3, 256 71.8 /
-  // 71.3, one of 8192, 512 107.7 / 104.4, 2048 247.9 / 250.4, 2 of 8192, all 963 / 970; 4 of 64, 4096, all 315 / 319
-  if (w.seq <= 256 || w.window <= 512) return w.head_dim == 128 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<64, false, 1>(p, s);
-  return w.head_dim == 128 ? launch_fwd<128, true, 1>(p, s) : launch_fwd<64, true, 1>(p, s);
+  // 71.3, one of 8192, 512 107.7 / 104.4, 2048 247.9 / 250.4, 2 of 8192, all 963 / 970.  At head_dim 64 its registers leave a unit 3 workgroups of 4: 16 heads, 2
+  // of 4096, 1024 53.2 / 47.2, 32 heads, 4 of 4096, all 302 / 293, but 16 heads, 2 of 4096, all 82.6 / 87.9
+  if (w.head_dim == 64) return launch_fwd<64, false, 1>(p, s);
+  return w.seq <= 256 || w.window <= 512 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<128, true, 1>(p, s);
 }
 
 template <int DH, int SPLIT>
@@ -1207,7 +1221,7 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   q.scale_log2e = 1.4426950408889634f * q.scale;
   const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
   hipError_t e;
-  if (groups <= 256) e = w.head_dim == 128 ? launch_dq<128, 2>(q, s) : launch_dq<64, 2>(q, s);
+  if (groups <= (w.head_dim == 64 ? 512 : 256)) e = w.head_dim == 128 ? launch_dq<128, 2>(q, s) : launch_dq<64, 2>(q, s);
   else e = w.head_dim == 128 ? launch_dq<128, 1>(q, s) : launch_dq<64, 1>(q, s);
   if (e != hipSuccess) return e;
   WinKvParams p{};

@@ -239,14 +239,15 @@ class GradList:
         n, self.grads, self.outs = len(grads), grads, outs
         self._n, self._dt, self._odt = n, _dt(grads[0]) if n else 0, _dt(outs[0]) if n else 0
         self.device = grads[0].device if n else torch.device("cuda:0")
-        self._at = [t.data_ptr() for t in grads + outs]
+        self._tensors = grads if outs is grads else grads + outs
+        self._at = [t.data_ptr() for t in self._tensors]
         self._src = (C.c_void_p * max(n, 1))(*self._at[:n])
-        self._dst = (C.c_void_p * max(n, 1))(*self._at[n:])
+        self._dst = (C.c_void_p * max(n, 1))(*self._at[-n:])
         self._counts = (C.c_int64 * max(n, 1))(*[t.numel() for t in grads])
         self._ws = torch.empty(lib().tbp_grad_workspace_bytes(n), dtype=torch.uint8, device=self.device)
 
     def _in_place(self):
-        if list(map(torch.Tensor.data_ptr, self.grads + self.outs)) != self._at:
+        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:
             raise RuntimeError("a tensor of the list has been given other memory: make a new list")
 
     def sumsq(self, out=None):
