@@ -11,6 +11,8 @@
 #include "head_tile.h"
 #include "rows.h"
 
+#include <utility>
+
 namespace tbp {
 
 // Rows at which sequence b ends.
@@ -329,7 +331,7 @@ struct WinDqParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; const bf16_t* out; long ld_do;
   const float* lse;                    // [B, H, S]
-  float* delta;                        // [B*S, H]: written here for the tokens that are there
+  float* delta;                        // [B, H, S]: written here for the tokens that are there
   const int* lengths;
   bf16_t* dqkv; long ld_dqkv;
   int B, H, KV, G, S, window, sinks;
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     for (int i = 0; i < 8; i++) dl_q += (float)o[i] * (float)dof[s][i];
   }
   dl_q += xor32(dl_q);
-  if (qlive && g == 0 && wk == 0) p.delta[(tok0 + query) * p.H + h] = dl_q;
+  if (qlive && g == 0 && wk == 0) p.delta[((long)b * p.H + h) * p.S + query] = dl_q;
   __syncthreads();                   // the second slot is free again
   for (int j = 0; j < nblk; j++) {
     wait_vmem<0>();
@@ -563,14 +565,23 @@ struct WinKvParams {
   float scale, scale_log2e;
 };
 
+// Lane I of every 16 lanes' own row, to all of the row.
+template <int I> __device__ __forceinline__ float row_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + I, 0xf, 0xf, true));
+}
+template <typename F, int... I> __device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
 template <int DH, int KEYS>
-__global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 4 : 2))) void window_bwd_kv_kernel(WinKvParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BQ = 64;
   constexpr int KB = KEYS / 32, TPI = 4 / KB;                 // 32-key blocks of the workgroup; 32-query tiles per iteration
-  constexpr int IMG = BQ * HT::RB, SLOT = 2 * IMG + 1024;     // Q image, dO image, 64 x (lse, delta); three slots
+  constexpr bool OWN = DH == 64;                              // the left waves fetch lse and delta themselves
+  constexpr int IMG = BQ * HT::RB, SLOT = 2 * IMG + (OWN ? 0 : 1024);      // Q image, dO image, 64 x (lse, delta) unless OWN; three slots
   constexpr int NCH = IMG / 1024 / 4;                         // copies per right wave and image
-  constexpr int OPS = 2 * NCH + 1;                            // vector-memory operations of one issue(), per right wave
+  constexpr int OPS = 2 * NCH + !OWN;                           // vector-memory operations of one issue(), per right wave
   constexpr int HAND = 4 * 4096;                              // one hand-over buffer: 4 wave pairs x 64 lanes x 64 bytes
   constexpr int HALF = 32 * HT::RB;                           // the second tile's rows inside an image
 
@@ -622,10 +633,27 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
     }
     __syncthreads();                                          // every left wave has its rows: the area is free again
     int st_at = sq0;                                          // the step that tile `it` lies in
+    // (OWN) lse and delta of the tile's queries, fetched an iteration ahead: lane i of 16 keeps those of register i of its half (below).
+    // Without room for them in the LDS two workgroups fit a compute unit.
+    static_assert(!OWN || TPI == 2, "a step per iteration");
+    const int sq = 8 * ((lane & 15) >> 2) + 4 * g + (lane & 3) + 32 * tq_left;
+    float next_ls = 0.f, next_dl = 0.f;
+    int sl_i = i0, sl_h = hq0, sl_st = sq0;
+    auto fetch_stats = [&] {
+      const int q = sl_st * BQ + sq;
+      const long at = ((long)b * p.H + hk * p.G + sl_h) * p.S + q;
+      next_ls = next_dl = 0.f;                                // (rows past the end: zeros, which with zero rows of Q and dO add nothing)
+      if (sl_i < i1 && q < n) { next_ls = p.lse[at]; next_dl = p.delta[at]; }
+      sl_i++;
+      if (++sl_st == step1) { sl_st = step0; sl_h++; }
+    };
+    if constexpr (OWN) fetch_stats();
     const int past = key >= p.sinks ? key + p.window : 0x7fffffff;      // the first query past the lane's key's window
     for (int it = 0; it <= nt; it++) {
       const int tile = TPI * it + tq_left, qt0 = st_at * BQ + 32 * (tile & 1);
       lds_u8* const out = my_hand + (it & 1) * HAND;
+      const float my_ls = next_ls, my_dl = next_dl;
+      if constexpr (OWN) fetch_stats();
       if (it < nt && unseen(qt0, kw0)) {
 #pragma unroll
         for (int i = 0; i < 4; i++) *reinterpret_cast<LDS_AS u32x4*>(out + 1024 * i) = u32x4{0, 0, 0, 0};
@@ -646,7 +674,7 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
 #pragma unroll
         for (int s = 0; s < KS; s++) {
           if (s + PF < KS) { fq[s + PF] = HT::rows_frag(qimg, fo, 0, s + PF); fd[s + PF] = HT::rows_frag(dimg, fo, 0, s + PF); }
-          if (s >= KS - 4) {
+          if (!OWN && s >= KS - 4) {
             const int e4 = s - (KS - 4);
             ls[e4] = *reinterpret_cast<const LDS_AS f32x4*>(stat + 8 * e4 + 4 * g);
             dl[e4] = *reinterpret_cast<const LDS_AS f32x4*>(stat + BQ + 8 * e4 + 4 * g);
@@ -657,6 +685,8 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
         }
         // register e of the tile is query qt0 + 8 (e / 4) + 4 g + e % 4
         float pv[16], sv[16];
+        if constexpr (OWN)
+          each([&](auto i) { ls[i >> 2][i & 3] = row_lane<i>(my_ls); dl[i >> 2][i & 3] = row_lane<i>(my_dl); }, std::make_integer_sequence<int, 16>());
 #pragma unroll
         for (int e = 0; e < 16; e++) pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[e], p.scale_log2e, -ls[e >> 2][e & 3]));
         if (!whole(qt0, kw0)) {
@@ -711,12 +741,12 @@ __global__ __launch_bounds__(512) void window_bwd_kv_kernel(WinKvParams p) {
       dma16(slot + wave * 1024 + c * 4096, dq, ok ? cq_off[c] : kOob);
       dma16(slot + IMG + wave * 1024 + c * 4096, dd, ok ? cd_off[c] : kOob);
     }
-    // row statistics: wave 0 fetches lse[0..63], wave 1 delta[0..63]; waves 2 and 3 issue the same instruction out of range (nothing
-    // moves) to keep the count uniform.  (Rows past the end: zeros, which with zero rows of Q and dO add nothing.)
-    const u32x4 ds = (wave & 1) == 0 ? make_desc(p.lse + ((long)b * p.H + h) * p.S + q0, (uint32_t)(left * 4))
-                                     : make_desc(p.delta + (tok0 + q0) * p.H + h, (uint32_t)(left * p.H * 4));
-    const unsigned off = (wave < 2 && lane < left) ? (unsigned)((wave & 1) == 0 ? lane * 4 : lane * p.H * 4) : kOob;
-    dma4(slot + 2 * IMG + wave * 256, ds, off);
+    if constexpr (!OWN) {
+      // row statistics: wave 0 fetches lse[0..63], wave 1 delta[0..63]; waves 2 and 3 issue the same instruction out of range (nothing
+      // moves) to keep the count uniform.  (Rows past the end: zeros, as above.)
+      const u32x4 ds = make_desc(((wave & 1) == 0 ? p.lse : p.delta) + ((long)b * p.H + h) * p.S + q0, (uint32_t)(left * 4));
+      dma4(slot + 2 * IMG + wave * 256, ds, wave < 2 && lane < left ? (unsigned)(lane * 4) : kOob);
+    }
     is_i++;
     if (++is_st == step1) { is_st = step0; is_h++; }
   };
@@ -1168,7 +1198,7 @@ static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
 
 template <int DH, int KEYS>
 static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
-  constexpr size_t smem = 3 * (2 * 64 * DH * 2 + 1024) + 2 * 4 * 4096;       // three slots, two hand-over buffers
+  constexpr size_t smem = 3 * (2 * 64 * DH * 2 + (DH == 64 ? 0 : 1024)) + 2 * 4 * 4096;       // three slots, two hand-over buffers
   auto kern = window_bwd_kv_kernel<DH, KEYS>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
@@ -1182,11 +1212,11 @@ static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
 WindowParts window_parts(const WindowShape& w) {
   WindowParts r{};
   const long heads = (long)w.batch * w.kv_heads;
-  // 64 keys to a block on few blocks, which are cut into parts of half the partial sums then or into none, and for short windows, of which a block of
-  // 128 sees more than it is seen by.  us of the backward, 128 / 64: 8 key heads of 128, 1024 tokens, window 256 61.3 / 48.0, 2048, 512 105.9 / 88.3,
-  // 8192, 512 369 / 334, 2 sequences of 4096, 128 207 / 182, but 1024 472 / 477, and 8192, 2048 846 / 871; 4 heads of 64, 4 ragged sequences of 1001, 300
-  // 46.7 / 41.1, 8192, 256 96.4 / 82.7; 16 heads of 64, 2048, 512 33.1 / 35.3.
-  r.keys = heads * ((w.seq + 127) / 128) <= 256 || w.window <= 768 ? 64 : 128;
+  // 64 keys to a block at head_dim 64, where two such workgroups fit a compute unit; at 128 on few blocks, which are cut into parts of half the partial
+  // sums then or into none, and for short windows, of which a block of 128 sees more than it is seen by.  us of the backward, 128 / 64: 8 key heads of 128,
+  // 1024 tokens, window 256 61.3 / 48.0, 2048, 512 105.9 / 88.3, 8192, 512 369 / 334, 2 sequences of 4096, 128 207 / 182, but 1024 472 / 477, and 8192,
+  // 2048 846 / 871; 16 heads of 64, 2 sequences of 4096, all 315 / 288, window 1024 171 / 156; 4 ragged ones of 1001, 4 heads, 300 42.4 / 35.3.
+  r.keys = w.head_dim == 64 || heads * ((w.seq + 127) / 128) <= 256 || w.window <= 768 ? 64 : 128;
   r.blocks = (w.seq + r.keys - 1) / r.keys;
   const int sinks = w.sinks < w.seq ? w.sinks : w.seq, G = w.heads / w.kv_heads;
   r.sink_blocks = (sinks + r.keys - 1) / r.keys;
@@ -1230,8 +1260,8 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   p.B = q.B; p.H = q.H; p.KV = q.KV; p.G = q.G; p.S = q.S; p.window = q.window; p.sinks = q.sinks;
   p.parts = window_parts(w);
   p.scale = q.scale; p.scale_log2e = q.scale_log2e;
-  if (p.parts.keys == 64) return w.head_dim == 128 ? launch_kv<128, 64>(p, s) : launch_kv<64, 64>(p, s);
-  return w.head_dim == 128 ? launch_kv<128, 128>(p, s) : launch_kv<64, 128>(p, s);
+  if (w.head_dim == 64) return launch_kv<64, 64>(p, s);
+  return p.parts.keys == 64 ? launch_kv<128, 64>(p, s) : launch_kv<128, 128>(p, s);
 }
 
 // Shares of a head's keys, at most: a workgroup per compute unit (us, one / two of them: batch 8, 4096 keys of 8 heads of 128 35.3 / 41.9, batch 32 106 /
