@@ -79,13 +79,17 @@ def _sequences(rows, seq):
 def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, sinks=0, lengths=None, out=None, lse=None):
     """qkv [batch*seq, (n_heads + 2 n_kv_heads) head_dim] (q | k | v, rotated) -> (out [batch*seq, n_heads*head_dim], lse2 [batch, heads, seq])."""
     batch, dt = _sequences(qkv.shape[0], seq), qkv.dtype
+    ld_out = n_heads * head_dim
     if out is None:
-        out = qkv.new_empty((qkv.shape[0], n_heads * head_dim))
+        out = qkv.new_empty((qkv.shape[0], ld_out))
+    else:
+        ld_out = _matrix(out, dt, "out")
     if lse is None:
         lse = qkv.new_empty((batch, n_heads, seq), dtype=_F32)
+    else:
+        _vector(lse, batch * n_heads * seq, _F32, "lse")
     _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
-                                          qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), _matrix(out, dt, "out"),
-                                          _vector(lse, batch * n_heads * seq, _F32, "lse"), _stream()))
+                                          qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), ld_out, lse.data_ptr(), _stream()))
     return out, lse
 
 
@@ -95,15 +99,17 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     ld_out = _matrix(out, dt, "out")
     if _matrix(d_out, dt, "d_out") != ld_out or d_out.shape != out.shape:
         raise TypeError("d_out must have out's shape and leading dimension")
+    ld_dqkv = (n_heads + 2 * n_kv_heads) * head_dim
     if dqkv is None:
-        dqkv = qkv.new_empty((qkv.shape[0], (n_heads + 2 * n_kv_heads) * head_dim))
+        dqkv = qkv.new_empty((qkv.shape[0], ld_dqkv))
+    else:
+        ld_dqkv = _matrix(dqkv, dt, "dqkv")
     L = lib()
     if scratch is None:
-        scratch = torch.empty(L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks),
-                              dtype=torch.uint8, device=qkv.device)
+        scratch = qkv.new_empty(L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks), dtype=torch.uint8)
     _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
                                      qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), d_out.data_ptr(), ld_out,
-                                     _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), _matrix(dqkv, dt, "dqkv"),
+                                     _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), ld_dqkv,
                                      scratch.data_ptr(), _stream()))
     return dqkv
 
@@ -119,15 +125,20 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     (out [batch, n_heads*head_dim], lse2 [batch, heads]).  A program that decodes keeps a workspace (tbp_window_decode_workspace)."""
     batch, dt = q.shape[0], q.dtype
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
+    ld_out = n_heads * head_dim
     if out is None:
-        out = q.new_empty((batch, n_heads * head_dim))
+        out = q.new_empty((batch, ld_out))
+    else:
+        ld_out = _matrix(out, dt, "out")
     if lse is None:
         lse = q.new_empty((batch, n_heads), dtype=_F32)
+    else:
+        _vector(lse, batch * n_heads, _F32, "lse")
     if workspace is None:
         workspace = tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks, q.device)
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
                                    q.data_ptr(), _matrix(q, dt, "q"), cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
-                                   _matrix(out, dt, "out"), _vector(lse, batch * n_heads, _F32, "lse"),
+                                   ld_out, lse.data_ptr(),
                                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()))
     return out, lse
 
@@ -154,11 +165,14 @@ def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP
     are given.  out: new [rows, n_heads*head_dim], or the tensor to write to (x itself: in place)."""
     n_pos, rot_dim = _table(table)
     rows, dt = x.shape[0], x.dtype
+    ld_out = n_heads * head_dim
     if out is None:
-        out = x.new_empty((rows, n_heads * head_dim))
+        out = x.new_empty((rows, ld_out))
+    else:
+        ld_out = _matrix(out, dt, "out")
     _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
                             (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), _matrix(x, dt, "x"), out.data_ptr(),
-                            _matrix(out, dt, "out"), _stream()))
+                            ld_out, _stream()))
     return out
 
 
@@ -171,11 +185,14 @@ def tbp_rotary_append(qkv, n_heads, n_kv_heads, head_dim, table, lengths, cache_
     if n_new * batch != rows:
         raise ValueError(f"{rows} rows are no whole number of tokens for {batch} sequences")
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
+    ld_q = n_heads * head_dim
     if q_out is None:
-        q_out = qkv.new_empty((rows, n_heads * head_dim))
+        q_out = qkv.new_empty((rows, ld_q))
+    else:
+        ld_q = _matrix(q_out, dt, "q_out")
     _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos,
                                    _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), _matrix(qkv, dt, "qkv"), q_out.data_ptr(),
-                                   _matrix(q_out, dt, "q_out"), cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream()))
+                                   ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream()))
     return q_out
 
 
@@ -200,10 +217,14 @@ def tbp_logprobs(logits, targets, top=0):
 def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=None):
     """-> the derivative of the logits [rows, vocab] (out: the tensor to write to, logits itself allowed)."""
     (rows, vocab), dt = logits.shape, logits.dtype
-    out = logits.new_empty((rows, vocab)) if out is None else out
+    ld_out = vocab
+    if out is None:
+        out = logits.new_empty((rows, vocab))
+    else:
+        ld_out = _matrix(out, dt, "out")
     _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
                                  _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
-                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), _matrix(out, dt, "out"), _stream()))
+                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream()))
     return out
 
 
@@ -212,10 +233,14 @@ def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
     (rows, vocab), dt = logits.shape, logits.dtype
     stats = logits.new_empty((3, rows), dtype=_F32)
     at = stats.data_ptr()
-    out = logits.new_empty((rows, vocab)) if out is None else out
+    ld_out = vocab
+    if out is None:
+        out = logits.new_empty((rows, vocab))
+    else:
+        ld_out = _matrix(out, dt, "out")
     _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
                                    _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
-                                   out.data_ptr(), _matrix(out, dt, "out"), _stream()))
+                                   out.data_ptr(), ld_out, _stream()))
     return (*stats.unbind(), out)
 
 
