@@ -65,7 +65,8 @@ struct HeadOf {
 // Bound by the matrix pipes, busy 54 % of the cycles that a workgroup is resident, at the clock that the card's power leaves (1.8 GHz): [2, 4096] tokens,
 // 32 heads on 8 of 128, window 1024, 4 sinks 150 to 165 us over cards, 0.73 to 0.80 PFLOP/s of the pairs that are seen, 1.05 at 150 us of the tiles that are
 // computed.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
-// of the block's code, 165 us).
+// of the block's code, 165 us).  No more than the registers bounds the workgroups of a compute unit: head_dim 64, window 256, 4 sequences of 2048, 32 heads
+// 49.1 us with two, 38.4 with four.
 template <int DH, bool AHEAD, int SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
@@ -325,8 +326,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // dQ = scale * dS K: oriented like the forward, per 32-key tile S^T and dP^T = V dO^T are rebuilt, dS^T = P^T (dP^T - delta) is fed into
 // dQ^T += K^T dS^T.  delta = rowsum(dout * out) of its queries is computed first and left for the pass over the queries.
 // One workgroup = 4 waves x 32 queries, key blocks through LDS in two slots, as in the forward, so that the sum over the keys stays in registers and
-// no atomics are needed.  Bound by the matrix pipes at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 375 us,
-// 0.96 PFLOP/s of the three products over the seen pairs, the pipes busy 55 %.
+// no atomics are needed.  Bound by the matrix pipes at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 360 us,
+// 1.0 PFLOP/s of the three products over the seen pairs, the pipes busy 56 %.
 struct WinDqParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; const bf16_t* out; long ld_do;
@@ -550,8 +551,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // the parts of others leave fp32 partial sums that a second launch adds up in order.
 // Roles of the waves as in the fused attention's pass: 4 "left" waves compute P and dS of their 32 keys and hand them over through
 // LDS, 4 "right" waves issue all copies and accumulate dV^T += dO^T P, dK^T += Q^T dS of one 32-query tile later.
-// Bound by the matrix pipes and the LDS beside them, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 570 us,
-// 0.84 PFLOP/s of the four products over the seen pairs, the pipes busy 49 %, the LDS 44 %.
+// Bound by the matrix pipes and the LDS beside them, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 545 us,
+// 0.88 PFLOP/s of the four products over the seen pairs, the pipes busy 50 %, the LDS 44 %.  Short windows are bound by the latency of the copies, issued a
+// step ahead: 12 heads on 4 of 64, 4 ragged sequences of 1001, window 300 19 us.  (lse and delta fetched by the left waves at head_dim 128 too: 20 us more.)
 struct WinKvParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; long ld_do;
