@@ -44,6 +44,7 @@ WINDOW_CASES = [  # seq, batch, H, KV, dh, window, sinks, lengths
     (700, 1, 3, 3, 64, 128, 200, [641]), (1001, 2, 4, 2, 128, 250, 4, [1001, 777]), (1100, 1, 8, 8, 64, 5000, 9, None),
     (1500, 1, 2, 1, 128, 200, 1500, None), (2500, 1, 3, 1, 64, 333, 130, None), (3000, 1, 4, 2, 64, 3, 3000, None), (2049, 1, 1, 1, 128, 10, 700, [2048]),
     (90, 65, 8, 2, 64, 20, 2, None), (140, 40, 4, 4, 128, 50, 1, [140 - 3 * i for i in range(40)]), (600, 5, 16, 4, 128, 90, 5, None),
+    (1100, 4, 16, 8, 128, 800, 5, [1100, 1037, 3, 900]), (1090, 2, 16, 16, 128, 900, 140, None), (1030, 4, 16, 4, 64, 800, 70, [1030, 1029, 0, 600]),
 ]
 
 
