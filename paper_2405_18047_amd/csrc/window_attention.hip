@@ -1266,17 +1266,30 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   return p.parts.keys == 64 ? launch_kv<128, 64>(p, s) : launch_kv<128, 128>(p, s);
 }
 
-// Shares of a head's keys, at most: a workgroup per compute unit (us, one / two of them: batch 8, 4096 keys of 8 heads of 128 35.3 / 41.9, batch 32 106 /
-// 109); but a share costs the joining workgroup as much as most of a tile of keys (its sums
-// of 32 heads, in proportion less of fewer), so no more than make the reading of a share and the joining of all of them about equal.
+// Shares of a head's keys, at most: as many as make the rounds of workgroups (one per compute unit at head_dim 128, two at 64) short by this model, whose
+// times, in us, are those of a tile in a workgroup when the chip is full, of one that has it to itself (the latency of its copies), and of a share's
+// start and end.  us, as many as leave no compute unit without one / by the model, 8 heads of 128: 12 sequences of 4096 keys 62.9 / 49.9, 20 87.9 / 71.7,
+// 33 151 / 126, 48 168 / 147, 5 of 16384 96.0 / 68.3, 64 of 4096 181.6 / 181.9; but 20 ragged ones 48.2 / 54.1 (lengths are not known here).
+// A share costs the joining workgroup as much as most of a tile of keys (its sums of 32 heads, in proportion less of fewer), so no more than make the
+// reading of a share and the joining of all of them about equal.
 int window_decode_splits(int batch, int heads, int kv_heads, int head_dim, long most_seen) {
+  constexpr float kFull = 0.74f, kAlone = 0.44f, kStart = 4.f;
   const int group = heads / kv_heads, nh = group < 32 ? group : 32;
-  const long groups = (long)batch * kv_heads * ((group + 31) / 32), tiles = (most_seen + 31) / 32;
-  long splits = (256 + groups - 1) / groups;
-  const long most = (tiles + share_tiles(head_dim) - 1) / share_tiles(head_dim), level = (long)sqrt(40.0 * tiles / nh);
-  if (splits > most) splits = most;
-  if (splits > level) splits = level;
-  return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+  const long groups = (long)batch * kv_heads * ((group + 31) / 32), tiles = (most_seen + 31) / 32, slots = head_dim == 64 ? 512 : 256;
+  long most = (tiles + share_tiles(head_dim) - 1) / share_tiles(head_dim);
+  const long level = (long)sqrt(40.0 * tiles / nh), some = 8 * slots / groups;
+  most = most < level ? most : level;
+  most = most < some ? most : some;
+  most = most < 64 ? most : 64;
+  int splits = 1;
+  float best = 0.f;
+  for (int n = 1; n == 1 || n <= most; n++) {
+    const long rounds = groups * n / slots, rest = groups * n % slots, share = (tiles + n - 1) / n;
+    const float last = kAlone + (kFull - kAlone) * (float)rest / (float)slots;
+    const float us = rounds * (share * kFull + kStart) + (rest ? share * last + kStart : 0.f);
+    if (n == 1 || us < 0.99f * best) { best = us; splits = n; }
+  }
+  return splits;
 }
 
 template <int DH, bool PAST>

@@ -142,6 +142,7 @@ def test_window_attention_gradient_against_differences():
 DECODE_CASES = [  # lengths, H, KV, dh, window, sinks, capacity
     ([1], 1, 1, 64, 1, 0, 1), ([0, 1, 2], 4, 2, 128, 3, 1, 8), ([5, 33, 64, 65], 8, 2, 128, 16, 4, 20), ([500], 32, 8, 128, 1024, 4, 1028),
     ([700, 31, 0, 1300], 12, 4, 64, 300, 3, 303), ([1000, 37], 40, 1, 128, 2000, 0, 1024), ([90] * 70, 6, 6, 64, 33, 2, 120),
+    ([700 - 9 * i for i in range(50)], 16, 8, 128, 600, 4, 640), ([333, 0, 340] * 30, 8, 8, 64, 400, 0, 400), ([900] * 33, 8, 8, 128, 1000, 0, 901),
     ([3000, 2999], 8, 4, 128, 5000, 7, 1500), ([129, 128, 127], 35, 1, 64, 128, 0, 128), ([4, 3], 2, 1, 128, 10, 100, 101),
 ]
 
