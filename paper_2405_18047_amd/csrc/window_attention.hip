@@ -552,8 +552,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // Roles of the waves as in the fused attention's pass: 4 "left" waves compute P and dS of their 32 keys and hand them over through
 // LDS, 4 "right" waves issue all copies and accumulate dV^T += dO^T P, dK^T += Q^T dS of one 32-query tile later.
 // Bound by the matrix pipes and the LDS beside them, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 545 us,
-// 0.88 PFLOP/s of the four products over the seen pairs, the pipes busy 50 %, the LDS 44 %.  Short windows are bound by the latency of the copies, issued a
-// step ahead: 12 heads on 4 of 64, 4 ragged sequences of 1001, window 300 19 us.  (lse and delta fetched by the left waves at head_dim 128 too: 20 us more.)
+// 0.88 PFLOP/s of the four products over the seen pairs, the pipes busy 50 %, the LDS 44 %.  Short windows are bound by the chain of a step (scores,
+// exponentials, hand-over, barrier) in few workgroups: 12 heads on 4 of 64, 4 ragged sequences of 1001, window 300 19 us.  Tried at head_dim 128: lse and delta
+// fetched by the left waves, 20 us more; with 64 keys, and the LDS so freed a fourth slot, copies a step earlier: 177 -> 184 us at 2 of 4096, window 128.
 struct WinKvParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; long ld_do;
