@@ -48,15 +48,17 @@ def _vector(t, n, dtype, what):
     return t.data_ptr()
 
 
-def _matrix(t, dtype, what):
-    """The leading dimension of a matrix whose rows are contiguous."""
+def _matrix(t, dtype, what, rows, columns):
+    """The leading dimension of a matrix of contiguous rows, of which a call reads or writes the first `rows` and of these the first `columns`."""
     if t.dtype is not dtype or t.dim() != 2:
         raise TypeError(f"{what} must be a matrix of type {dtype}")
-    rows, columns = t.shape
+    have, wide = t.shape
+    if have < rows or wide < columns:
+        raise TypeError(f"{what} must have {rows} rows of {columns} columns, not {have} of {wide}")
     ld, step = t.stride()
-    if step != 1 and columns > 1:
+    if step != 1 and wide > 1:
         raise TypeError(f"{what} must have contiguous rows")
-    return ld if rows > 1 or ld > columns else columns
+    return ld if have > 1 or ld > wide else wide
 
 
 def _caches(k, v, dtype, batch, width):
@@ -78,37 +80,38 @@ def _sequences(rows, seq):
 # ---- sliding-window attention ------------------------------------------------------------------------------------------
 def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, sinks=0, lengths=None, out=None, lse=None):
     """qkv [batch*seq, (n_heads + 2 n_kv_heads) head_dim] (q | k | v, rotated) -> (out [batch*seq, n_heads*head_dim], lse2 [batch, heads, seq])."""
-    batch, dt = _sequences(qkv.shape[0], seq), qkv.dtype
-    ld_out = n_heads * head_dim
+    rows, dt = qkv.shape[0], qkv.dtype
+    batch, ld_out = _sequences(rows, seq), n_heads * head_dim
+    ld_qkv = _matrix(qkv, dt, "qkv", rows, (n_heads + 2 * n_kv_heads) * head_dim)
     if out is None:
-        out = qkv.new_empty((qkv.shape[0], ld_out))
+        out = qkv.new_empty((rows, ld_out))
     else:
-        ld_out = _matrix(out, dt, "out")
+        ld_out = _matrix(out, dt, "out", rows, ld_out)
     if lse is None:
         lse = qkv.new_empty((batch, n_heads, seq), dtype=_F32)
     else:
         _vector(lse, batch * n_heads * seq, _F32, "lse")
     _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
-                                          qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), ld_out, lse.data_ptr(), _stream()))
+                                          qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(), _stream()))
     return out, lse
 
 
 def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head_dim, window, sinks=0, lengths=None, dqkv=None, scratch=None):
     """-> dqkv [batch*seq, (n_heads + 2 n_kv_heads) head_dim] (dq | dk | dv, not rotated back)."""
-    batch, dt = _sequences(qkv.shape[0], seq), qkv.dtype
-    ld_out = _matrix(out, dt, "out")
-    if _matrix(d_out, dt, "d_out") != ld_out or d_out.shape != out.shape:
+    rows, dt = qkv.shape[0], qkv.dtype
+    batch, ld_dqkv = _sequences(rows, seq), (n_heads + 2 * n_kv_heads) * head_dim
+    ld_qkv, ld_out = _matrix(qkv, dt, "qkv", rows, ld_dqkv), _matrix(out, dt, "out", rows, n_heads * head_dim)
+    if d_out.shape != out.shape or _matrix(d_out, dt, "d_out", rows, n_heads * head_dim) != ld_out:
         raise TypeError("d_out must have out's shape and leading dimension")
-    ld_dqkv = (n_heads + 2 * n_kv_heads) * head_dim
     if dqkv is None:
-        dqkv = qkv.new_empty((qkv.shape[0], ld_dqkv))
+        dqkv = qkv.new_empty((rows, ld_dqkv))
     else:
-        ld_dqkv = _matrix(dqkv, dt, "dqkv")
+        ld_dqkv = _matrix(dqkv, dt, "dqkv", rows, ld_dqkv)
     L = lib()
     if scratch is None:
         scratch = qkv.new_empty(L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks), dtype=torch.uint8)
     _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
-                                     qkv.data_ptr(), _matrix(qkv, dt, "qkv"), out.data_ptr(), d_out.data_ptr(), ld_out,
+                                     qkv.data_ptr(), ld_qkv, out.data_ptr(), d_out.data_ptr(), ld_out,
                                      _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), ld_dqkv,
                                      scratch.data_ptr(), _stream()))
     return dqkv
@@ -126,10 +129,11 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     batch, dt = q.shape[0], q.dtype
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
     ld_out = n_heads * head_dim
+    ld_q = _matrix(q, dt, "q", batch, ld_out)
     if out is None:
         out = q.new_empty((batch, ld_out))
     else:
-        ld_out = _matrix(out, dt, "out")
+        ld_out = _matrix(out, dt, "out", batch, ld_out)
     if lse is None:
         lse = q.new_empty((batch, n_heads), dtype=_F32)
     else:
@@ -137,7 +141,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     if workspace is None:
         workspace = tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks, q.device)
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
-                                   q.data_ptr(), _matrix(q, dt, "q"), cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
+                                   q.data_ptr(), ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
                                    ld_out, lse.data_ptr(),
                                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()))
     return out, lse
@@ -166,12 +170,13 @@ def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP
     n_pos, rot_dim = _table(table)
     rows, dt = x.shape[0], x.dtype
     ld_out = n_heads * head_dim
+    ld_x = _matrix(x, dt, "x", rows, ld_out)
     if out is None:
         out = x.new_empty((rows, ld_out))
     else:
-        ld_out = _matrix(out, dt, "out")
+        ld_out = _matrix(out, dt, "out", rows, ld_out)
     _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
-                            (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), _matrix(x, dt, "x"), out.data_ptr(),
+                            (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), ld_x, out.data_ptr(),
                             ld_out, _stream()))
     return out
 
@@ -186,12 +191,13 @@ def tbp_rotary_append(qkv, n_heads, n_kv_heads, head_dim, table, lengths, cache_
         raise ValueError(f"{rows} rows are no whole number of tokens for {batch} sequences")
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
     ld_q = n_heads * head_dim
+    ld_qkv = _matrix(qkv, dt, "qkv", rows, ld_q + 2 * n_kv_heads * head_dim)
     if q_out is None:
         q_out = qkv.new_empty((rows, ld_q))
     else:
-        ld_q = _matrix(q_out, dt, "q_out")
+        ld_q = _matrix(q_out, dt, "q_out", rows, ld_q)
     _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos,
-                                   _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), _matrix(qkv, dt, "qkv"), q_out.data_ptr(),
+                                   _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), ld_qkv, q_out.data_ptr(),
                                    ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream()))
     return q_out
 
@@ -207,7 +213,7 @@ def tbp_logprobs(logits, targets, top=0):
     if top > 0:
         top_logp = logits.new_empty((rows, top), dtype=_F32)
         top_ids = logits.new_empty((rows, top), dtype=_I32)
-    _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits"), _vector(targets, rows, _I32, "targets"),
+    _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                               at, at + 4 * rows, at + 8 * rows, top, None if top_logp is None else top_logp.data_ptr(),
                               None if top_ids is None else top_ids.data_ptr(), _stream()))
     logp, entropy, lse = stats.unbind()
@@ -221,8 +227,8 @@ def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=N
     if out is None:
         out = logits.new_empty((rows, vocab))
     else:
-        ld_out = _matrix(out, dt, "out")
-    _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
+        ld_out = _matrix(out, dt, "out", rows, vocab)
+    _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                  _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
                                  _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream()))
     return out
@@ -237,8 +243,8 @@ def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
     if out is None:
         out = logits.new_empty((rows, vocab))
     else:
-        ld_out = _matrix(out, dt, "out")
-    _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits"), _vector(targets, rows, _I32, "targets"),
+        ld_out = _matrix(out, dt, "out", rows, vocab)
+    _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                    _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
                                    out.data_ptr(), ld_out, _stream()))
     return (*stats.unbind(), out)

@@ -135,3 +135,53 @@ def test_a_gradient_list_refuses_tensors_that_moved():
     for call in (moved.sumsq, lambda: moved.clip(1.0)):
         with pytest.raises(RuntimeError, match="other memory"):
             call()
+
+
+def _bf(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def _i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def _good_calls():
+    """One call of every operator that takes tensors of the caller's, with arguments that fit: 6 tokens, 4 query heads on 2 key heads of 64."""
+    table = torch.zeros((16, 32, 2))
+    return {
+        "window_fwd": (tbp.tbp_window_attention_fwd, dict(qkv=_bf(6, 512), seq=3, n_heads=4, n_kv_heads=2, head_dim=64, window=2, lengths=_i32(2), out=_bf(6, 256),
+                                                          lse=torch.zeros((2, 4, 3)))),
+        "window_p1": (tbp.tbp_window_attention_p1, dict(qkv=_bf(6, 512), out=_bf(6, 256), d_out=_bf(6, 256), lse=torch.zeros((2, 4, 3)), seq=3, n_heads=4,
+                                                        n_kv_heads=2, head_dim=64, window=2, lengths=_i32(2), dqkv=_bf(6, 512),
+                                                        scratch=torch.zeros(1 << 20, dtype=torch.uint8))),
+        "decode": (tbp.tbp_window_decode, dict(q=_bf(2, 256), cache_k=_bf(2, 8, 128), cache_v=_bf(2, 8, 128), lengths=_i32(2), n_heads=4, n_kv_heads=2, head_dim=64,
+                                               window=9000, out=_bf(2, 256), lse=torch.zeros((2, 4)), workspace=torch.zeros(1 << 22, dtype=torch.uint8))),
+        "rotary": (tbp.tbp_rotary, dict(x=_bf(6, 384), n_heads=6, head_dim=64, table=table, positions=_i32(6), out=_bf(6, 384))),
+        "append": (tbp.tbp_rotary_append, dict(qkv=_bf(6, 512), n_heads=4, n_kv_heads=2, head_dim=64, table=table, lengths=_i32(2), cache_k=_bf(2, 8, 128),
+                                               cache_v=_bf(2, 8, 128), q_out=_bf(6, 256))),
+        "logprobs": (tbp.tbp_logprobs, dict(logits=_bf(6, 50), targets=_i32(6))),
+        "logprobs_p1": (tbp.tbp_logprobs_p1, dict(logits=_bf(6, 50), targets=_i32(6), lse=torch.zeros(6), entropy=torch.zeros(6), d_logp=torch.zeros(6),
+                                                  d_entropy=torch.zeros(6), out=_bf(6, 50))),
+        "logprobs_step": (tbp.tbp_logprobs_step, dict(logits=_bf(6, 50), targets=_i32(6), d_logp=torch.zeros(6), d_entropy=torch.zeros(6), out=_bf(6, 50))),
+    }
+
+
+def _beside(rows, columns, ld):
+    """A view of `columns` columns of an array of `ld`: its leading dimension would cover more."""
+    return _bf(rows, ld)[:, :columns]
+
+
+@pytest.mark.parametrize("name,what,given", [
+    ("window_fwd", "qkv", _beside(6, 504, 1024)), ("window_fwd", "out", _bf(5, 256)), ("window_fwd", "out", _beside(6, 248, 512)),
+    ("window_p1", "qkv", _beside(6, 448, 512)), ("window_p1", "out", _bf(5, 256)), ("window_p1", "out", _beside(6, 128, 256)), ("window_p1", "d_out", _bf(5, 256)),
+    ("window_p1", "dqkv", _bf(5, 512)), ("window_p1", "dqkv", _beside(6, 384, 512)), ("decode", "q", _beside(2, 128, 256)), ("decode", "out", _bf(1, 256)),
+    ("decode", "out", _beside(2, 64, 256)), ("rotary", "x", _beside(6, 256, 512)), ("rotary", "out", _bf(5, 384)), ("rotary", "out", _beside(6, 256, 384)),
+    ("append", "qkv", _beside(6, 384, 512)), ("append", "q_out", _bf(2, 256)), ("append", "q_out", _beside(6, 192, 256)), ("logprobs_p1", "out", _bf(5, 50)),
+    ("logprobs_p1", "out", _beside(6, 49, 64)), ("logprobs_step", "out", _bf(5, 50)), ("logprobs_step", "out", _beside(6, 49, 64))],
+    ids=lambda v: v if isinstance(v, str) else "x".join(map(str, v.shape)))
+def test_matrices_that_a_call_would_pass_the_end_of_are_refused(name, what, given):
+    call, good = _good_calls()[name]
+    if (name, what) == ("window_p1", "out"):
+        good["d_out"] = given
+    with pytest.raises(TypeError, match=what):
+        call(**{**good, what: given})
