@@ -48,6 +48,15 @@ def _vector(t, n, dtype, what):
     return t.data_ptr()
 
 
+def _memory(t, what):
+    """(address, bytes) of a contiguous tensor that serves as plain memory (None: null)."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise TypeError(f"{what} must be contiguous")
+    return t.data_ptr(), t.nbytes
+
+
 def _matrix(t, dtype, what, rows, columns):
     """The leading dimension of a matrix of contiguous rows, of which a call reads or writes the first `rows` and of these the first `columns`."""
     if t.dtype is not dtype or t.dim() != 2:
@@ -108,12 +117,16 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     else:
         ld_dqkv = _matrix(dqkv, dt, "dqkv", rows, ld_dqkv)
     L = lib()
+    need = L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks)
     if scratch is None:
-        scratch = qkv.new_empty(L.tbp_window_attention_p1_scratch_bytes(batch, n_heads, n_kv_heads, seq, head_dim, window, sinks), dtype=torch.uint8)
+        scratch = qkv.new_empty(need, dtype=torch.uint8)
+    at, nbytes = _memory(scratch, "scratch")
+    if nbytes < need:
+        raise ValueError(f"scratch must have {need} bytes, not {nbytes}")
     _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
                                      qkv.data_ptr(), ld_qkv, out.data_ptr(), d_out.data_ptr(), ld_out,
                                      _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), ld_dqkv,
-                                     scratch.data_ptr(), _stream()))
+                                     at, _stream()))
     return dqkv
 
 
@@ -140,10 +153,10 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
         _vector(lse, batch * n_heads, _F32, "lse")
     if workspace is None:
         workspace = tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks, q.device)
+    at, nbytes = _memory(workspace, "workspace")
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
                                    q.data_ptr(), ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
-                                   ld_out, lse.data_ptr(),
-                                   None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()))
+                                   ld_out, lse.data_ptr(), at, nbytes, _stream()))
     return out, lse
 
 

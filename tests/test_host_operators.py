@@ -185,3 +185,18 @@ def test_matrices_that_a_call_would_pass_the_end_of_are_refused(name, what, give
         good["d_out"] = given
     with pytest.raises(TypeError, match=what):
         call(**{**good, what: given})
+
+
+def test_scratch_and_workspace_that_are_too_small_are_refused():
+    """The backward's scratch (whose size the C entry point is not told) and the decode's workspace, also where a tensor stands for more entries than it has memory."""
+    call, good = _good_calls()["window_p1"]
+    need = tbp.lib().tbp_window_attention_p1_scratch_bytes(2, 4, 2, 3, 64, 2, 0)
+    assert need > 1
+    for scratch in (torch.zeros(need - 1, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(need // 4, dtype=torch.uint8)):
+        with pytest.raises((TypeError, ValueError), match="scratch"):
+            call(**{**good, "scratch": scratch})
+    call, good = _good_calls()["decode"]
+    need = tbp.lib().tbp_window_decode_workspace_bytes(2, 4, 2, 64, 9000, 0)
+    assert need > 1
+    with pytest.raises(TypeError, match="workspace"):
+        call(**{**good, "workspace": torch.zeros(1, dtype=torch.uint8).expand(need)})
