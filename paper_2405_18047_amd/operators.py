@@ -2,9 +2,9 @@
 positions, log probabilities of tokens, the norm of all gradients with clipping.
 
 As in binding.py: argument marshalling only, on torch's current stream; outputs and workspaces are allocated where the caller
-passes none.  Index tensors (lengths, positions, targets) are int32 on the device.  The checks here are those that the C entry
-points cannot make (types, shapes and strides of tensors); the single-token calls are bound by the host, which is why they
-are written out rather than shared by many small functions.
+passes none.  Index tensors (lengths, positions, targets) are int32.  The checks here are those that the C entry points cannot
+make (types, shapes and strides of tensors, the sizes of memory, and that all of it is on the current device); the single-token
+calls are bound by the host, which is why they are written out rather than shared by many small functions.
 """
 from __future__ import annotations
 
@@ -12,7 +12,7 @@ import ctypes as C
 
 import torch
 
-from .binding import TBP_BF16, TBP_F32, _check, _stream, lib
+from .binding import TBP_BF16, TBP_F32, _check, lib
 
 __all__ = [
     "TBP_ROTARY_HALF", "TBP_ROTARY_INTERLEAVED", "TBP_ROTARY_PLAIN", "TBP_ROTARY_LINEAR", "TBP_ROTARY_BASE", "TBP_ROTARY_RAMP",
@@ -37,6 +37,19 @@ def _dt(t):
         return _CODE[t.dtype]
     except KeyError:
         raise TypeError(f"unsupported tensor dtype {t.dtype}") from None
+
+
+def _stream_of(first, *others):
+    """torch's current stream, which is the current device's: where the tensors of a call (None: left out) have to be."""
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise TypeError(f"tensors of one call must be on one GPU, not on {first.device} and {t.device}")
+    if device < 0:
+        raise TypeError(f"tensors must be on the GPU, not on {first.device}")
+    if device != torch._C._cuda_getDevice():
+        raise TypeError(f"tensors are on {first.device}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _vector(t, n, dtype, what):
@@ -101,7 +114,7 @@ def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, si
     else:
         _vector(lse, batch * n_heads * seq, _F32, "lse")
     _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
-                                          qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(), _stream()))
+                                          qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(), _stream_of(qkv, lengths, out, lse)))
     return out, lse
 
 
@@ -126,7 +139,7 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
                                      qkv.data_ptr(), ld_qkv, out.data_ptr(), d_out.data_ptr(), ld_out,
                                      _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), ld_dqkv,
-                                     at, _stream()))
+                                     at, _stream_of(qkv, lengths, out, d_out, lse, dqkv, scratch)))
     return dqkv
 
 
@@ -156,7 +169,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     at, nbytes = _memory(workspace, "workspace")
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
                                    q.data_ptr(), ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
-                                   ld_out, lse.data_ptr(), at, nbytes, _stream()))
+                                   ld_out, lse.data_ptr(), at, nbytes, _stream_of(q, cache_k, cache_v, lengths, out, lse, workspace)))
     return out, lse
 
 
@@ -166,7 +179,8 @@ def tbp_rotary_table(n_pos, rot_dim, base, scaling=TBP_ROTARY_PLAIN, factor=1.0,
     """-> table [n_pos, rot_dim/2, 2] of cosines and sines."""
     t = torch.empty((n_pos, rot_dim // 2, 2), dtype=_F32, device=device)
     sc = tbp_rotary_scale(scaling, factor, low, high, original, magnitude)
-    _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), t.data_ptr(), _stream()))
+    with torch.cuda.device(t.device):
+        _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), t.data_ptr(), _stream_of(t)))
     return t
 
 
@@ -190,7 +204,7 @@ def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP
         ld_out = _matrix(out, dt, "out", rows, ld_out)
     _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
                             (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), ld_x, out.data_ptr(),
-                            ld_out, _stream()))
+                            ld_out, _stream_of(x, table, positions, out)))
     return out
 
 
@@ -211,7 +225,7 @@ def tbp_rotary_append(qkv, n_heads, n_kv_heads, head_dim, table, lengths, cache_
         ld_q = _matrix(q_out, dt, "q_out", rows, ld_q)
     _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos,
                                    _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), ld_qkv, q_out.data_ptr(),
-                                   ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream()))
+                                   ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream_of(qkv, table, lengths, cache_k, cache_v, q_out)))
     return q_out
 
 
@@ -228,7 +242,7 @@ def tbp_logprobs(logits, targets, top=0):
         top_ids = logits.new_empty((rows, top), dtype=_I32)
     _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                               at, at + 4 * rows, at + 8 * rows, top, None if top_logp is None else top_logp.data_ptr(),
-                              None if top_ids is None else top_ids.data_ptr(), _stream()))
+                              None if top_ids is None else top_ids.data_ptr(), _stream_of(logits, targets)))
     logp, entropy, lse = stats.unbind()
     return (logp, entropy, lse, top_logp, top_ids) if top > 0 else (logp, entropy, lse)
 
@@ -243,7 +257,7 @@ def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=N
         ld_out = _matrix(out, dt, "out", rows, vocab)
     _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                  _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
-                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream()))
+                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream_of(logits, targets, lse, entropy, d_logp, d_entropy, out)))
     return out
 
 
@@ -259,7 +273,7 @@ def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
         ld_out = _matrix(out, dt, "out", rows, vocab)
     _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                    _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
-                                   out.data_ptr(), ld_out, _stream()))
+                                   out.data_ptr(), ld_out, _stream_of(logits, targets, d_logp, d_entropy, out)))
     return (*stats.unbind(), out)
 
 
@@ -298,7 +312,7 @@ class GradList:
         """The sum of squares [1] float64 (stages of a pipeline add theirs up before they clip)."""
         self._in_place()
         out = torch.empty(1, dtype=torch.float64, device=self.device) if out is None else out
-        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream()))
+        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream_of(self._ws, out)))
         return out
 
     def clip(self, max_norm, sumsq=None, norm=None):
@@ -306,5 +320,5 @@ class GradList:
         self._in_place()
         norm = self._ws.new_empty(1, dtype=_F32) if norm is None else norm
         _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _vector(sumsq, 1, torch.float64, "sumsq"), max_norm,
-                                   _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream()))
+                                   _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream_of(self._ws, sumsq, norm)))
         return norm

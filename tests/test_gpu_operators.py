@@ -501,6 +501,39 @@ def test_grad_clip_in_place_of_unaligned_views_and_of_norms_that_are_not_finite(
     assert np.all(np.abs(to_np(big) - 1 / np.sqrt(3)) < 1e-6)
 
 
+# ------------------------------------------------------------------------------------------- refusals
+def test_one_tensor_of_the_host_among_a_call_s_is_refused():
+    """The host refuses it; nothing is launched."""
+    _say("tensors of the host")
+    dev = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype, device=DEV)
+    f, i = torch.float32, torch.int32
+    table = dev(16, 32, 2, dtype=f)
+    heads = dict(n_heads=4, n_kv_heads=2, head_dim=64)
+    calls = [
+        (tbp.tbp_window_attention_fwd, dict(qkv=dev(6, 512), seq=3, **heads, window=2, lengths=dev(2, dtype=i), out=dev(6, 256), lse=dev(2, 4, 3, dtype=f))),
+        (tbp.tbp_window_attention_p1, dict(qkv=dev(6, 512), out=dev(6, 256), d_out=dev(6, 256), lse=dev(2, 4, 3, dtype=f), seq=3, **heads, window=2,
+                                           lengths=dev(2, dtype=i), dqkv=dev(6, 512), scratch=dev(1 << 20, dtype=torch.uint8))),
+        (tbp.tbp_window_decode, dict(q=dev(2, 256), cache_k=dev(2, 8, 128), cache_v=dev(2, 8, 128), lengths=dev(2, dtype=i), **heads, window=9000,
+                                     out=dev(2, 256), lse=dev(2, 4, dtype=f), workspace=dev(1 << 22, dtype=torch.uint8))),
+        (tbp.tbp_rotary, dict(x=dev(6, 384), n_heads=6, head_dim=64, table=table, positions=dev(6, dtype=i), out=dev(6, 384))),
+        (tbp.tbp_rotary_append, dict(qkv=dev(6, 512), **heads, table=table, lengths=dev(2, dtype=i), cache_k=dev(2, 8, 128), cache_v=dev(2, 8, 128),
+                                     q_out=dev(6, 256))),
+        (tbp.tbp_logprobs, dict(logits=dev(6, 50), targets=dev(6, dtype=i))),
+        (tbp.tbp_logprobs_p1, dict(logits=dev(6, 50), targets=dev(6, dtype=i), lse=dev(6, dtype=f), entropy=dev(6, dtype=f), d_logp=dev(6, dtype=f),
+                                   d_entropy=dev(6, dtype=f), out=dev(6, 50))),
+        (tbp.tbp_logprobs_step, dict(logits=dev(6, 50), targets=dev(6, dtype=i), d_logp=dev(6, dtype=f), d_entropy=dev(6, dtype=f), out=dev(6, 50))),
+        (tbp.GradList([dev(8, dtype=f)]).clip, dict(max_norm=1.0, sumsq=dev(1, dtype=torch.float64), norm=dev(1, dtype=f))),
+        (tbp.GradList([dev(8, dtype=f)]).sumsq, dict(out=dev(1, dtype=torch.float64))),
+    ]
+    for call, good in calls:
+        call(**good)
+        for k, v in good.items():
+            if isinstance(v, torch.Tensor):
+                with pytest.raises(TypeError, match="GPU"):
+                    call(**{**good, k: v.cpu()})
+    torch.cuda.synchronize()
+
+
 # ------------------------------------------------------------------------------------------- streams, graphs
 def _everything(s):
     """One call of each operator into fixed outputs."""

@@ -200,3 +200,18 @@ def test_scratch_and_workspace_that_are_too_small_are_refused():
     assert need > 1
     with pytest.raises(TypeError, match="workspace"):
         call(**{**good, "workspace": torch.zeros(1, dtype=torch.uint8).expand(need)})
+
+
+@pytest.mark.parametrize("name", list(_good_calls()))
+def test_tensors_of_the_host_are_refused(name):
+    """Their addresses mean nothing to a kernel."""
+    call, good = _good_calls()[name]
+    with pytest.raises(TypeError, match="GPU"):
+        call(**good)
+
+
+def test_gradients_of_the_host_are_refused():
+    some = tbp.GradList([torch.zeros(8)])
+    for call in (some.sumsq, lambda: some.clip(1.0)):
+        with pytest.raises(TypeError, match="GPU"):
+            call()
