@@ -193,9 +193,17 @@ def _table(table):
 
 def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP_ROTARY_HALF, backward=False, out=None):
     """The first n_heads*head_dim columns of x [rows, ld], turned (backward: the derivative).  seq: tokens per sequence, where no positions
-    are given.  out: new [rows, n_heads*head_dim], or the tensor to write to (x itself: in place)."""
+    are given (None: all rows are one sequence).  out: new [rows, n_heads*head_dim], or the tensor to write to (x itself: in place)."""
     n_pos, rot_dim = _table(table)
     rows, dt = x.shape[0], x.dtype
+    if positions is not None:
+        seq = 1
+    elif seq is None:
+        seq = max(rows, 1)
+        if rows > n_pos:
+            raise ValueError(f"{rows} rows and a table of {n_pos} positions: positions or seq must be given")
+    elif seq < 1:
+        raise ValueError(f"seq must be at least 1, not {seq}")
     ld_out = n_heads * head_dim
     ld_x = _matrix(x, dt, "x", rows, ld_out)
     if out is None:
@@ -203,7 +211,7 @@ def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP
     else:
         ld_out = _matrix(out, dt, "out", rows, ld_out)
     _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
-                            (seq or n_pos) if positions is None else 1, 1 if backward else 0, x.data_ptr(), ld_x, out.data_ptr(),
+                            seq, 1 if backward else 0, x.data_ptr(), ld_x, out.data_ptr(),
                             ld_out, _stream_of(x, table, positions, out)))
     return out
 

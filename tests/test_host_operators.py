@@ -215,3 +215,14 @@ def test_gradients_of_the_host_are_refused():
     for call in (some.sumsq, lambda: some.clip(1.0)):
         with pytest.raises(TypeError, match="GPU"):
             call()
+
+
+def test_rotary_rows_of_no_position_are_refused():
+    """Neither positions nor a length of the sequences: one sequence, which the table has to cover; it does not start again behind the table's end."""
+    table = torch.zeros((5, 32, 2))
+    with pytest.raises(ValueError, match="seq"):
+        tbp.tbp_rotary(_bf(6, 384), 6, 64, table)
+    with pytest.raises(ValueError, match="seq"):
+        tbp.tbp_rotary(_bf(6, 384), 6, 64, table, seq=0)
+    with pytest.raises(TypeError, match="GPU"):                  # (as many rows as positions: nothing but the place of the tensors is wrong)
+        tbp.tbp_rotary(_bf(5, 384), 6, 64, table)
