@@ -143,7 +143,7 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     return dqkv
 
 
-def tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks=0, device="cuda:0"):
+def tbp_window_decode_workspace(batch, n_heads, n_kv_heads, head_dim, window, sinks=0, device="cuda"):
     """The workspace of tbp_window_decode calls of these sizes (which must not overlap), or None where they need none."""
     nbytes = lib().tbp_window_decode_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, window, sinks)
     return torch.zeros(nbytes, dtype=torch.uint8, device=device) if nbytes else None
@@ -175,7 +175,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
 
 # ---- rotary positions ----------------------------------------------------------------------------------------------------
 def tbp_rotary_table(n_pos, rot_dim, base, scaling=TBP_ROTARY_PLAIN, factor=1.0, low=1.0, high=32.0, original=4096.0, magnitude=1.0,
-                     device="cuda:0"):
+                     device="cuda"):
     """-> table [n_pos, rot_dim/2, 2] of cosines and sines."""
     t = torch.empty((n_pos, rot_dim // 2, 2), dtype=_F32, device=device)
     sc = tbp_rotary_scale(scaling, factor, low, high, original, magnitude)
@@ -304,7 +304,7 @@ class GradList:
             raise TypeError("gradients must have one type, outputs one type, and all one device")
         n, self.grads, self.outs = len(grads), grads, outs
         self._n, self._dt, self._odt = n, _dt(grads[0]) if n else 0, _dt(outs[0]) if n else 0
-        self.device = grads[0].device if n else torch.device("cuda:0")
+        self.device = grads[0].device if n else torch.device("cuda")
         self._tensors = grads if outs is grads else grads + outs
         self._at = [t.data_ptr() for t in self._tensors]
         self._src = (C.c_void_p * max(n, 1))(*self._at[:n])

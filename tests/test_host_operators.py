@@ -226,3 +226,19 @@ def test_rotary_rows_of_no_position_are_refused():
         tbp.tbp_rotary(_bf(6, 384), 6, 64, table, seq=0)
     with pytest.raises(TypeError, match="GPU"):                  # (as many rows as positions: nothing but the place of the tensors is wrong)
         tbp.tbp_rotary(_bf(5, 384), 6, 64, table)
+
+
+def test_new_memory_is_the_current_device_s(monkeypatch):
+    """A process that has chosen its GPU gets workspaces and tables there: a device without an index is torch's current one."""
+    asked = []
+
+    def note(*shape, **kw):
+        asked.append(torch.device(kw["device"]))
+        raise InterruptedError
+
+    monkeypatch.setattr(torch, "zeros", note)
+    monkeypatch.setattr(torch, "empty", note)
+    for call in (lambda: tbp.tbp_window_decode_workspace(2, 4, 2, 64, 9000), lambda: tbp.tbp_rotary_table(8, 64, 1e4), lambda: tbp.GradList([])):
+        with pytest.raises(InterruptedError):
+            call()
+    assert asked == [torch.device("cuda")] * 3
