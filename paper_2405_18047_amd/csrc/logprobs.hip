@@ -372,14 +372,14 @@ __global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
   }
 }
 
-// The rows from r0 on (a launch takes at most kLaunchRows of them: its threads are counted in 32 bits).
+// The rows from r0 on (a launch takes at most kLaunchRows of them: its threads are counted in 32 bits).  r0 runs past the largest row count.
 constexpr int kLaunchRows = 1 << 21;
-static LogprobParams rows_from(LogprobParams p, int r0, int element) {
-  p.rows = p.rows - r0 < kLaunchRows ? p.rows - r0 : kLaunchRows;
+static LogprobParams rows_from(LogprobParams p, long r0, int element) {
+  p.rows = p.rows - r0 < kLaunchRows ? (int)(p.rows - r0) : kLaunchRows;
   p.logits = (const char*)p.logits + r0 * p.ld * element;
   p.targets += r0; p.entropy += r0; p.lse += r0;
   if (p.logp) p.logp += r0;
-  if (p.top) { p.top_logp += (long)r0 * p.top; p.top_ids += (long)r0 * p.top; }
+  if (p.top) { p.top_logp += r0 * p.top; p.top_ids += r0 * p.top; }
   if (p.d_logp) p.d_logp += r0;
   if (p.d_entropy) p.d_entropy += r0;
   if (p.d_logits) p.d_logits = (char*)p.d_logits + r0 * p.ld_d * element;
@@ -388,7 +388,7 @@ static LogprobParams rows_from(LogprobParams p, int r0, int element) {
 
 template <typename T, int NT, int CH, bool STEP>
 static hipError_t launch(const LogprobParams& p, hipStream_t s) {
-  for (int r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
+  for (long r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
     const LogprobParams q = rows_from(p, r0, sizeof(T));
     hipLaunchKernelGGL((logprobs_kernel<T, NT, CH, STEP>), dim3((unsigned)q.rows), dim3(NT), 0, s, q);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -414,7 +414,7 @@ hipError_t logprobs_step(int dtype, const LogprobParams& p, hipStream_t s) { ret
 
 hipError_t logprobs_p1(int dtype, const LogprobParams& p, hipStream_t s) {
   const int per = 256 * 4 * (dtype ? 8 : 4);
-  for (int r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
+  for (long r0 = 0; r0 < p.rows; r0 += kLaunchRows) {
     const LogprobParams q = rows_from(p, r0, dtype ? 2 : 4);
     const dim3 grid((unsigned)q.rows, (unsigned)((p.vocab + per - 1) / per));
     if (dtype) hipLaunchKernelGGL((logprobs_p1_kernel<bf16_t>), grid, dim3(256), 0, s, q);

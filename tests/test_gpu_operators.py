@@ -446,6 +446,21 @@ def test_logprobs_of_rows_that_are_not_finite(bad, vocab):
     assert got[4][1].tolist() == [-1] * 4
 
 
+def test_logprobs_of_as_many_rows_as_there_may_be():
+    """2^31 - 1 rows of one logit each: the launches of a part of the rows each end behind the last one."""
+    rows = 2 ** 31 - 1
+    _say("logprobs of 2^31 - 1 rows")
+    x = torch.empty((rows, 1), dtype=torch.bfloat16, device=DEV).normal_()
+    targets, w = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.ones(rows, device=DEV)
+    logp, entropy, lse = tbp.tbp_logprobs(x, targets)
+    out = torch.full_like(x, NAN)
+    tbp.tbp_logprobs_p1(x, targets, lse, entropy, w, out=out)
+    for a, b, c, d, e in zip(*(t.view(-1).split(1 << 28) for t in (x, logp, entropy, lse, out))):
+        assert torch.equal(d, a.float()) and not bool(b.any()) and not bool(c.any()) and not bool(e.any())
+    del x, targets, w, logp, entropy, lse, out, a, b, c, d, e
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------------------------------- gradient norm and clipping
 def _grads(sizes, dtype, scale=1.0):
     host = [_rnd(91, f"g{i}", (s,), dtype, scale) for i, s in enumerate(sizes)]
