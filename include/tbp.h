@@ -372,9 +372,7 @@ tbp_status tbp_rotary_append(int dtype, int batch, int n_new, int n_heads, int n
 tbp_status tbp_logprobs(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets, float* logp,
                         float* entropy, float* lse, int top, float* top_logp, int32_t* top_ids, void* stream);
 /* The derivative of the logits, d_logits [rows, ld_d] in the storage type, from lse and entropy of the forward and the derivatives of
- * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits.
- * (p comes from x - lse: of a row whose logits are so large that lse does not show log sum, such as one of nothing but the type's lowest value,
- * tbp_logprobs_step gives the derivative, this call does not.) */
+ * logp and entropy (d_entropy may be NULL): dx = d_logp (1[target] - p) - d_entropy p (log p + entropy).  d_logits may be logits. */
 tbp_status tbp_logprobs_p1(int dtype, int rows, int vocab, const void* logits, int64_t ld_logits, const int32_t* targets,
                            const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
                            int64_t ld_d, void* stream);

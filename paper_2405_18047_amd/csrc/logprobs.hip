@@ -354,21 +354,50 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void lo
 
 // The derivative by itself: a workgroup takes 4 pieces per thread of one row, for rows and parts of rows are all alike here.  Bound by memory:
 // [1023, 131072] bf16, 536 MB read and written, 100 us, 5.4 TB/s.
+// p comes from x - lse, as exact as lse is: below kCoarse half of its last place is 2^-15 at most.  A row beyond (nothing but the type's lowest
+// value, say, where lse does not show ln s at all) is one workgroup's alone, which sums it up again first; alone, for d_logits may be the logits.
+constexpr float kCoarse = 1024.f;
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_p1_kernel(LogprobParams p) {
   using R = Row<T, 256, 4>;
   const long row = blockIdx.x;
-  R data;
-  data.load((const T*)p.logits + row * p.ld, p.vocab, blockIdx.y);
-  const RowWeights w = row_weights(p, row, p.lse[row], 0.f, p.entropy[row]);
+  const T* const x = (const T*)p.logits + row * p.ld;
   T* const o = (T*)p.d_logits + row * p.ld_d;
+  R data;
+  auto derivative = [&](int blk, const RowWeights& w) {
 #pragma unroll
-  for (int c = 0; c < 4; c++) {
-    const int i = R::at(blockIdx.y, c);
-    if (i >= p.vocab) break;
-    float v[R::N];
-    derive<T>(data.x[c], i, w, v);
-    store_piece<T>(o, i, p.vocab, v);
+    for (int c = 0; c < 4; c++) {
+      const int i = R::at(blk, c);
+      if (i >= p.vocab) break;
+      float v[R::N];
+      derive<T>(data.x[c], i, w, v);
+      store_piece<T>(o, i, p.vocab, v);
+    }
+  };
+  data.load(x, p.vocab, blockIdx.y);
+  const float lse = p.lse[row], entropy = p.entropy[row];
+  if (!(__builtin_fabsf(lse) >= kCoarse && __builtin_fabsf(lse) < INFINITY)) {
+    derivative(blockIdx.y, row_weights(p, row, lse, 0.f, entropy));
+    return;
+  }
+  if (blockIdx.y) return;
+  __shared__ float red[2][4];
+  const int tid = threadIdx.x;
+  float m = -INFINITY, s = 0.f;
+  for (int i = tid; i < p.vocab; i += 256) m = fmaxf(m, (float)x[i]);
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if ((tid & 63) == 0) red[0][tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  for (int i = tid; i < p.vocab; i += 256) s += __builtin_amdgcn_exp2f(((float)x[i] - m) * kLog2e);
+  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
+  if ((tid & 63) == 0) red[1][tid >> 6] = s;
+  __syncthreads();                                                  // (in place: the whole row has been read)
+  s = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  const RowWeights w = row_weights(p, row, m, __builtin_amdgcn_logf(s), entropy);
+  for (int b = 0; b < (int)gridDim.y; b++) {
+    data.load(x, p.vocab, b);
+    derivative(b, w);
   }
 }
 

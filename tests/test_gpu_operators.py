@@ -431,6 +431,35 @@ def test_logprobs_of_rows_masked_with_the_lowest_value(vocab, dtype):
     assert not np.any(d[0, vocab // 2:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [50, 9000, 140001])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_logprobs_gradient_of_rows_whose_lse_does_not_show_the_sum(vocab, dtype, in_place):
+    """The derivative by itself, from lse and entropy: rows of nothing but the type's lowest value (the uniform distribution), and rows of logits so large
+    that a unit of lse's last place is 2^-9 and more; between them ordinary rows."""
+    _say(f"logprobs gradient, large logits, vocab={vocab} {dtype} in place={in_place}")
+    low = float(torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min)
+    x = _rnd(85, "x", (6, vocab), dtype, 3.0)
+    x[1], x[2, 7:], x[2, :7] = low, low, low / 2
+    x[3:5] = si.store_round(x[3:5] + np.array([[20000.0], [-300000.0]]), dtype)
+    t, wl, wh = [0, 3, 2, vocab - 1, 1, -1], np.linspace(1, -1, 6).astype(np.float32), np.linspace(-0.5, 0.5, 6).astype(np.float32)
+    g_ref = np.zeros((6, vocab))
+    for r, row in enumerate(x.astype(np.float64)):               # (differences from the maximum first: 64 bits do not hold the sum beside the lowest value either)
+        d = row - row.max()
+        s = np.exp(d).sum()
+        lp, p = d - np.log(s), np.exp(d) / s
+        entropy = -(p * np.maximum(lp, -1e4)).sum()
+        g_ref[r] = -p * (wl[r] if t[r] >= 0 else 0.0) - wh[r] * p * (np.maximum(lp, -1e4) + entropy)
+        if t[r] >= 0:
+            g_ref[r, t[r]] += wl[r]
+    dev, tt, fl, fh = _logits_dev(x, dtype, 3, 1), _ints(t), torch.from_numpy(wl).to(DEV), torch.from_numpy(wh).to(DEV)
+    _, entropy, lse = tbp.tbp_logprobs(dev, tt)
+    got = to_np(tbp.tbp_logprobs_p1(dev, tt, lse, entropy, fl, fh, out=dev if in_place else None))
+    # as in test_logprobs_match_oracle; ordinary rows have p from lse
+    assert np.all(np.abs(got - g_ref) <= (2.0 ** -8 if dtype == "bf16" else 2e-5) * np.abs(g_ref) + 2e-5)
+    assert torch.all(dev._base[:, 0] == 100.0) and torch.all(dev._base[:, -2:] == 100.0)
+
+
 @pytest.mark.parametrize("bad", [NAN, float("inf")])
 @pytest.mark.parametrize("vocab", [100, 70001])
 def test_logprobs_of_rows_that_are_not_finite(bad, vocab):
