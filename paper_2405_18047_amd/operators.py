@@ -39,16 +39,16 @@ def _dt(t):
         raise TypeError(f"unsupported tensor dtype {t.dtype}") from None
 
 
-def _stream_of(first, *others):
-    """torch's current stream, which is the current device's: where the tensors of a call (None: left out) have to be."""
-    device = first.get_device()
+def _stream_of(device, *others):
+    """torch's current stream, which is that of the current device: `device`, a tensor's get_device().  The others that the caller has brought (None: none)
+    have to be there too."""
     for t in others:
         if t is not None and t.get_device() != device:
-            raise TypeError(f"tensors of one call must be on one GPU, not on {first.device} and {t.device}")
+            raise TypeError(f"tensors of one call must be on one GPU, not on {t.device} and {f'cuda:{device}' if device >= 0 else 'the host'}")
     if device < 0:
-        raise TypeError(f"tensors must be on the GPU, not on {first.device}")
+        raise TypeError("tensors must be on the GPU")
     if device != torch._C._cuda_getDevice():
-        raise TypeError(f"tensors are on {first.device}, which is not the current device")
+        raise TypeError(f"tensors are on the GPU cuda:{device}, which is not the current one")
     return torch._C._cuda_getCurrentRawStream(device)
 
 
@@ -105,6 +105,7 @@ def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, si
     rows, dt = qkv.shape[0], qkv.dtype
     batch, ld_out = _sequences(rows, seq), n_heads * head_dim
     ld_qkv = _matrix(qkv, dt, "qkv", rows, (n_heads + 2 * n_kv_heads) * head_dim)
+    given = out, lse
     if out is None:
         out = qkv.new_empty((rows, ld_out))
     else:
@@ -114,7 +115,7 @@ def tbp_window_attention_fwd(qkv, seq, n_heads, n_kv_heads, head_dim, window, si
     else:
         _vector(lse, batch * n_heads * seq, _F32, "lse")
     _check(lib().tbp_window_attention_fwd(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
-                                          qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(), _stream_of(qkv, lengths, out, lse)))
+                                          qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(), _stream_of(qkv.get_device(), lengths, *given)))
     return out, lse
 
 
@@ -125,6 +126,7 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     ld_qkv, ld_out = _matrix(qkv, dt, "qkv", rows, ld_dqkv), _matrix(out, dt, "out", rows, n_heads * head_dim)
     if d_out.shape != out.shape or _matrix(d_out, dt, "d_out", rows, n_heads * head_dim) != ld_out:
         raise TypeError("d_out must have out's shape and leading dimension")
+    given = dqkv, scratch
     if dqkv is None:
         dqkv = qkv.new_empty((rows, ld_dqkv))
     else:
@@ -139,7 +141,7 @@ def tbp_window_attention_p1(qkv, out, d_out, lse, seq, n_heads, n_kv_heads, head
     _check(L.tbp_window_attention_p1(_dt(qkv), batch, n_heads, n_kv_heads, seq, head_dim, window, sinks, _vector(lengths, batch, _I32, "lengths"),
                                      qkv.data_ptr(), ld_qkv, out.data_ptr(), d_out.data_ptr(), ld_out,
                                      _vector(lse, batch * n_heads * seq, _F32, "lse"), dqkv.data_ptr(), ld_dqkv,
-                                     at, _stream_of(qkv, lengths, out, d_out, lse, dqkv, scratch)))
+                                     at, _stream_of(qkv.get_device(), lengths, out, d_out, lse, *given)))
     return dqkv
 
 
@@ -156,6 +158,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
     ld_out = n_heads * head_dim
     ld_q = _matrix(q, dt, "q", batch, ld_out)
+    given = out, lse, workspace
     if out is None:
         out = q.new_empty((batch, ld_out))
     else:
@@ -169,7 +172,7 @@ def tbp_window_decode(q, cache_k, cache_v, lengths, n_heads, n_kv_heads, head_di
     at, nbytes = _memory(workspace, "workspace")
     _check(lib().tbp_window_decode(_dt(q), batch, n_heads, n_kv_heads, head_dim, window, sinks, capacity, _vector(lengths, batch, _I32, "lengths"),
                                    q.data_ptr(), ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, out.data_ptr(),
-                                   ld_out, lse.data_ptr(), at, nbytes, _stream_of(q, cache_k, cache_v, lengths, out, lse, workspace)))
+                                   ld_out, lse.data_ptr(), at, nbytes, _stream_of(q.get_device(), cache_k, cache_v, lengths, *given)))
     return out, lse
 
 
@@ -180,7 +183,7 @@ def tbp_rotary_table(n_pos, rot_dim, base, scaling=TBP_ROTARY_PLAIN, factor=1.0,
     t = torch.empty((n_pos, rot_dim // 2, 2), dtype=_F32, device=device)
     sc = tbp_rotary_scale(scaling, factor, low, high, original, magnitude)
     with torch.cuda.device(t.device):
-        _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), t.data_ptr(), _stream_of(t)))
+        _check(lib().tbp_rotary_table(n_pos, rot_dim, base, C.byref(sc), t.data_ptr(), _stream_of(t.get_device())))
     return t
 
 
@@ -206,13 +209,14 @@ def tbp_rotary(x, n_heads, head_dim, table, positions=None, seq=None, layout=TBP
         raise ValueError(f"seq must be at least 1, not {seq}")
     ld_out = n_heads * head_dim
     ld_x = _matrix(x, dt, "x", rows, ld_out)
+    given = out
     if out is None:
         out = x.new_empty((rows, ld_out))
     else:
         ld_out = _matrix(out, dt, "out", rows, ld_out)
     _check(lib().tbp_rotary(_dt(x), rows, n_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos, _vector(positions, rows, _I32, "positions"),
                             seq, 1 if backward else 0, x.data_ptr(), ld_x, out.data_ptr(),
-                            ld_out, _stream_of(x, table, positions, out)))
+                            ld_out, _stream_of(x.get_device(), table, positions, given)))
     return out
 
 
@@ -227,13 +231,14 @@ def tbp_rotary_append(qkv, n_heads, n_kv_heads, head_dim, table, lengths, cache_
     capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
     ld_q = n_heads * head_dim
     ld_qkv = _matrix(qkv, dt, "qkv", rows, ld_q + 2 * n_kv_heads * head_dim)
+    given = q_out
     if q_out is None:
         q_out = qkv.new_empty((rows, ld_q))
     else:
         ld_q = _matrix(q_out, dt, "q_out", rows, ld_q)
     _check(lib().tbp_rotary_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, rot_dim, layout, table.data_ptr(), n_pos,
                                    _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(), ld_qkv, q_out.data_ptr(),
-                                   ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream_of(qkv, table, lengths, cache_k, cache_v, q_out)))
+                                   ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks, _stream_of(qkv.get_device(), table, lengths, cache_k, cache_v, given)))
     return q_out
 
 
@@ -250,7 +255,7 @@ def tbp_logprobs(logits, targets, top=0):
         top_ids = logits.new_empty((rows, top), dtype=_I32)
     _check(lib().tbp_logprobs(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, logits.dtype, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                               at, at + 4 * rows, at + 8 * rows, top, None if top_logp is None else top_logp.data_ptr(),
-                              None if top_ids is None else top_ids.data_ptr(), _stream_of(logits, targets)))
+                              None if top_ids is None else top_ids.data_ptr(), _stream_of(logits.get_device(), targets)))
     logp, entropy, lse = stats.unbind()
     return (logp, entropy, lse, top_logp, top_ids) if top > 0 else (logp, entropy, lse)
 
@@ -259,13 +264,14 @@ def tbp_logprobs_p1(logits, targets, lse, entropy, d_logp, d_entropy=None, out=N
     """-> the derivative of the logits [rows, vocab] (out: the tensor to write to, logits itself allowed)."""
     (rows, vocab), dt = logits.shape, logits.dtype
     ld_out = vocab
+    given = out
     if out is None:
         out = logits.new_empty((rows, vocab))
     else:
         ld_out = _matrix(out, dt, "out", rows, vocab)
     _check(lib().tbp_logprobs_p1(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                  _vector(lse, rows, _F32, "lse"), _vector(entropy, rows, _F32, "entropy"), _vector(d_logp, rows, _F32, "d_logp"),
-                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream_of(logits, targets, lse, entropy, d_logp, d_entropy, out)))
+                                 _vector(d_entropy, rows, _F32, "d_entropy"), out.data_ptr(), ld_out, _stream_of(logits.get_device(), targets, lse, entropy, d_logp, d_entropy, given)))
     return out
 
 
@@ -275,13 +281,14 @@ def tbp_logprobs_step(logits, targets, d_logp, d_entropy=None, out=None):
     stats = logits.new_empty((3, rows), dtype=_F32)
     at = stats.data_ptr()
     ld_out = vocab
+    given = out
     if out is None:
         out = logits.new_empty((rows, vocab))
     else:
         ld_out = _matrix(out, dt, "out", rows, vocab)
     _check(lib().tbp_logprobs_step(_dt(logits), rows, vocab, logits.data_ptr(), _matrix(logits, dt, "logits", rows, vocab), _vector(targets, rows, _I32, "targets"),
                                    _vector(d_logp, rows, _F32, "d_logp"), _vector(d_entropy, rows, _F32, "d_entropy"), at, at + 4 * rows, at + 8 * rows,
-                                   out.data_ptr(), ld_out, _stream_of(logits, targets, d_logp, d_entropy, out)))
+                                   out.data_ptr(), ld_out, _stream_of(logits.get_device(), targets, d_logp, d_entropy, given)))
     return (*stats.unbind(), out)
 
 
@@ -311,6 +318,7 @@ class GradList:
         self._dst = (C.c_void_p * max(n, 1))(*self._at[-n:])
         self._counts = (C.c_int64 * max(n, 1))(*[t.numel() for t in grads])
         self._ws = torch.empty(lib().tbp_grad_workspace_bytes(n), dtype=torch.uint8, device=self.device)
+        self._at_device = self._ws.get_device()
 
     def _in_place(self):
         if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:
@@ -319,14 +327,16 @@ class GradList:
     def sumsq(self, out=None):
         """The sum of squares [1] float64 (stages of a pipeline add theirs up before they clip)."""
         self._in_place()
+        given = out
         out = torch.empty(1, dtype=torch.float64, device=self.device) if out is None else out
-        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream_of(self._ws, out)))
+        _check(lib().tbp_grad_sumsq(self._dt, self._n, self._src, self._counts, _vector(out, 1, torch.float64, "out"), self._ws.data_ptr(), _stream_of(self._at_device, given)))
         return out
 
     def clip(self, max_norm, sumsq=None, norm=None):
         """Writes the outputs; -> the norm [1] float32.  sumsq: [1] float64, computed here where none is given."""
         self._in_place()
+        given = norm
         norm = self._ws.new_empty(1, dtype=_F32) if norm is None else norm
         _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _vector(sumsq, 1, torch.float64, "sumsq"), max_norm,
-                                   _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream_of(self._ws, sumsq, norm)))
+                                   _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream_of(self._at_device, sumsq, given)))
         return norm
