@@ -297,8 +297,9 @@ tbp_status tbp_attention_p1(int dtype, int batch, int n_heads, int seq, int head
  * qkv: device [batch*seq, ld_qkv], column blocks q [n_heads*head_dim] | k | v [n_kv_heads*head_dim each], q and k already
  * rotated; out: device [batch*seq, ld_out]; lse: device [batch, n_heads, seq] fp32, as for tbp_attention_fwd.
  * lengths: device [batch] int32 or NULL: tokens of each sequence (taken as 0 .. seq); rows behind them are padding, never
- * read, and come out as zeros (lse: -infinity).  A token's row has to be finite: in a tile of 32 keys with one that a query
- * sees, an infinite or NaN value row reaches that query.
+ * read, and come out as zeros (lse: -infinity).  The rows of the tokens that are there have to be
+ * finite: products with what a query does not see are formed too, with a weight of zero, so an infinite or NaN row may reach every
+ * result of its sequence and key head, earlier tokens' among them, and no others.
  * Limits: 0 <= seq <= 2^20, window >= 1, sinks >= 0, batch * n_heads below 2^23; leading dimensions multiples of 8 below 2^22,
  * tensors 16-byte aligned. */
 tbp_status tbp_window_attention_fwd(int dtype, int batch, int n_heads, int n_kv_heads, int seq, int head_dim, int window,

@@ -107,6 +107,29 @@ def test_window_attention_with_wide_rows_keeps_what_is_beside_them():
     assert torch.all(out[:, wo:] == 7.0) and torch.all(dwide[:, :8] == 7.0) and torch.all(dwide[:, 8 + w:] == 7.0)
 
 
+@pytest.mark.parametrize("seq,dh,window,sinks", [(300, 64, 40, 3), (1500, 128, 700, 0), (1500, 128, 100, 5)])
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+def test_window_attention_keeps_what_is_not_finite_within_its_sequence_and_key_head(seq, dh, window, sinks, bad):
+    nb, H, KV = 6, 16, 8
+    _say(f"window attention with {bad} seq={seq} dh={dh} window={window}")
+    _, _, a, ddo = _window_inputs((seq, nb, H, KV, dh, window, sinks, None), 71)
+    lengths = _ints([seq, seq, seq - 70, seq, seq, seq])
+    run = lambda a: (lambda o, l: (o, l, tbp.tbp_window_attention_p1(a, o, ddo, l, seq, H, KV, dh, window, sinks, lengths)))(
+        *tbp.tbp_window_attention_fwd(a, seq, H, KV, dh, window, sinks, lengths))
+    clean = run(a)
+    for column in (H + 3, H + KV + 3):                           # a key, then a value, of key head 3 of sequence 1
+        dirty = a.clone()
+        dirty[seq + 45, column * dh + 7] = bad
+        got = run(dirty)
+        ours = torch.zeros((nb, seq, H + 2 * KV), dtype=torch.bool, device=DEV)
+        ours[1][:, [6, 7, H + 3, H + KV + 3]] = True             # its two query heads, the key head's derivatives
+        same = lambda x, y, heads: bool((x == y).view(nb, seq, heads, dh).all(dim=3)[~ours[:, :, :heads]].all())
+        assert same(got[0], clean[0], H) and same(got[2], clean[2], H + 2 * KV)
+        assert bool((got[1] == clean[1]).transpose(1, 2)[~ours[:, :, :H]].all())
+        if bad != bad or column == H + KV + 3:                   # (an infinite key may have a score of -infinity, which is a probability of zero)
+            assert not bool(torch.isfinite(got[0].view(nb, seq, H, dh)[1, 45, 6:8]).all())
+
+
 @pytest.mark.parametrize("gain", [8.0, 0.02])
 @pytest.mark.parametrize("dh", [64, 128])
 def test_window_attention_score_range(gain, dh):
