@@ -87,6 +87,62 @@ def test_window_attention_matches_oracle(case):
         assert not np.any(got[b * seq + m:(b + 1) * seq]) and not np.any(to_np(out)[b * seq + m:(b + 1) * seq])
 
 
+def _row_errors(qkv, do, seq, H, KV, dh, window, sinks, lengths=None):
+    """The oracle's out | dq | dk | dv with, for every row of every head of each, the error (a norm over the head's columns) that the arithmetic allows.
+
+    A probability or score gradient rounded to bf16 is off by sigma = 2^-8 / sqrt 3 of itself at most, as a root mean square, in random directions: a row that
+    adds n of them up with weights w and vectors x is off by sigma sqrt(sum w^2 |x|^2).  The output's error (P rounded, then the result: sigma sqrt 2 of
+    it) reaches delta = do . o, and by dS = P (dP - delta) dq and dk.  Six times that, one rounding of the result, and 1e-3 for fp32 (dP - delta of
+    a row that sees one key, lse)."""
+    sigma, nb, G = 2.0 ** -8 / 3 ** 0.5, len(qkv) // seq, H // KV
+    want = [ref.window_attention_fwd(qkv, seq, H, KV, dh, window, sinks, lengths)[0]]
+    g = ref.window_attention_p1(qkv, do, seq, H, KV, dh, window, sinks, lengths)
+    want += [g[:, :H * dh], g[:, H * dh:(H + KV) * dh], g[:, (H + KV) * dh:]]
+    off = [np.zeros((len(qkv), n)) for n in (H, H, KV, KV)]       # squares
+    sq = lambda z: (z * z).sum(axis=1)
+    for b in range(nb):
+        n = ref._length(lengths, b, seq)
+        rows = slice(b * seq, b * seq + n)
+        for h in range(H if n else 0):
+            q, k, v = ref._heads(qkv, rows, h, H, KV, dh)
+            o, d = want[0][rows, h * dh:(h + 1) * dh], do[rows, h * dh:(h + 1) * dh]
+            p, _ = ref._softmax(q, k, window, sinks)
+            dp = d @ v.T
+            ds, p2 = (p * (dp - (dp * p).sum(axis=1, keepdims=True))) ** 2, p * p
+            o_err = p2 @ sq(v)                                   # (of the sum; the result's own rounding is beside it)
+            delta = (d * d * (o * o + o_err[:, None] / dh)).sum(axis=1) * 2
+            off[0][rows, h] += o_err
+            off[1][rows, h] += (ds @ sq(k) + delta * sq(p @ k)) / dh
+            off[2][rows, h // G] += (ds.T @ sq(q) + p2.T @ (delta * sq(q))) / dh
+            off[3][rows, h // G] += p2.T @ sq(d)
+    size = [np.sqrt((w.reshape(len(qkv), -1, dh) ** 2).sum(axis=2)) for w in want]
+    return want, [6 * sigma * np.sqrt(e) + 2.0 ** -8 * s + 1e-3 for e, s in zip(off, size)]
+
+
+def _rows_fit(got, want, bounds, dh):
+    """-> largest (error / bound) of the rows of out, dq, dk, dv."""
+    return [float((np.sqrt(((a - w).reshape(len(w), -1, dh) ** 2).sum(axis=2)) / e).max()) for a, w, e in zip(got, want, bounds)]
+
+
+@pytest.mark.parametrize("case", WINDOW_CASES, ids=str)
+def test_window_attention_rows_are_right_to_their_own_size(case):
+    """Late rows, whose sums of many small terms are small, are held to that, not to the largest element of all."""
+    seq, nb, H, KV, dh, window, sinks, lengths = case
+    _say(f"window attention row by row {case}")
+    qkv, do, a, ddo = _window_inputs(case, 61)
+    want, bounds = _row_errors(qkv, do, seq, H, KV, dh, window, sinks, lengths)
+    n = None if lengths is None else _ints(lengths)
+    out, lse = tbp.tbp_window_attention_fwd(a, seq, H, KV, dh, window, sinks, n)
+    g = tbp.tbp_window_attention_p1(a, out, ddo, lse, seq, H, KV, dh, window, sinks, n)
+    again = tbp.tbp_window_attention_fwd(a, seq, H, KV, dh, window, sinks, n)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])           # and the same every time
+    assert torch.equal(g, tbp.tbp_window_attention_p1(a, out, ddo, lse, seq, H, KV, dh, window, sinks, n))
+    g = to_np(g)
+    fit = _rows_fit([to_np(out), g[:, :H * dh], g[:, H * dh:(H + KV) * dh], g[:, (H + KV) * dh:]], want, bounds, dh)
+    _say("   largest error over its bound: " + ", ".join(f"{n} {f:.2f}" for n, f in zip(("out", "dq", "dk", "dv"), fit)))
+    assert max(fit) < 1
+
+
 def test_window_attention_with_wide_rows_keeps_what_is_beside_them():
     seq, nb, H, KV, dh, window, sinks = 203, 2, 4, 2, 64, 40, 3
     _say("window attention, wide rows")
