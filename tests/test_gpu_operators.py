@@ -554,6 +554,56 @@ def test_logprobs_of_rows_that_are_not_finite(bad, vocab):
     assert got[4][1].tolist() == [-1] * 4
 
 
+# more rows than compute units: 256 threads of 16 pieces up to 256 * 16 * N logits (N = 8 bf16, 4 fp32), 512 threads up to twice that, beyond it blocks of 256 * 16
+# pieces (with the derivative 1024 threads); one wave of 16 pieces up to 64 * 16 * N
+MANY_ROWS = [("bf16", 9001), ("bf16", 32000), ("bf16", 50257), ("bf16", 70001), ("f32", 3999), ("f32", 5003), ("f32", 16384), ("f32", 20011), ("f32", 40009),
+             ("bf16", 8191), ("bf16", 2048)]
+
+
+@pytest.mark.parametrize("dtype,vocab", MANY_ROWS)
+def test_logprobs_of_many_rows_match_oracle(dtype, vocab):
+    """As in test_logprobs_match_oracle, over more rows than compute units: every width of a row's threads; rows of padded and of even length."""
+    rows = 259
+    _say(f"logprobs of many rows vocab={vocab} {dtype}")
+    x, t = _logits(rows, vocab, dtype, 86)
+    some = [0, 1, 2, 3, 4, 100, 256, 257, 258]                   # (the oracle's rows; the others are compared between the calls)
+    x64 = x[some].astype(np.float64)
+    lp_ref, h_ref, lse_ref = ref.logprobs(x64, t[some])
+    wl, wh = np.linspace(-1, 1, rows).astype(np.float32), np.linspace(0.5, -0.5, rows).astype(np.float32)
+    g_ref = ref.logprobs_p1(x64, t[some], wl[some].astype(np.float64), wh[some].astype(np.float64))
+    fl, fh = torch.from_numpy(wl).to(DEV), torch.from_numpy(wh).to(DEV)
+    bound = (2.0 ** -8 if dtype == "bf16" else 2e-5) * np.abs(g_ref) + 2e-5
+    for pad, off in ((0, 0), (9, 5)):
+        dev, tt = _logits_dev(x, dtype, pad, off), _ints(t.tolist())
+        got = {k: tbp.tbp_logprobs(dev, tt, top=k) for k in (0, 20, 64)}
+        s = tbp.tbp_logprobs_step(dev, tt, fl, fh)
+        for k, g in list(got.items()) + [(0, s)]:
+            for a, r in zip(g[:3], (lp_ref, h_ref, lse_ref)):
+                a = to_np(a)[some]
+                fine = _same_infinities(a, r)
+                assert np.all(np.abs(a[fine] - r[fine]) <= 2e-5 * (1 + np.abs(r[fine])))
+            for a, b in zip(g[:3], got[0][:3]):                  # every row, whichever kernel it went through: to the order of the sums
+                a, b = to_np(a), to_np(b)
+                fine = _same_infinities(a, b)
+                assert np.all(np.abs(a[fine] - b[fine]) <= 2e-5 * (1 + np.abs(b[fine])))
+            if not k:
+                continue
+            ids, v = g[4].cpu().numpy(), to_np(g[3])
+            for i, r in enumerate(some):
+                want = np.lexsort((np.arange(vocab), -x64[i]))[:k]
+                assert ids[r].tolist() == want.tolist(), (k, r)
+                vr = x64[i, want] - lse_ref[i] if np.isfinite(lse_ref[i]) else np.full(k, -np.inf)
+                fine = _same_infinities(v[r], vr)
+                assert np.all(np.abs(v[r][fine] - vr[fine]) <= 2e-5 * (1 + np.abs(vr[fine])))
+            order = torch.topk(dev.float(), k, dim=1).values     # (of every row: the values, which ties do not change)
+            assert torch.equal(torch.gather(dev.float(), 1, g[4].long()), order)
+        for d in (tbp.tbp_logprobs_p1(dev, tt, got[0][2], got[0][1], fl, fh), s[3]):
+            assert np.all(np.abs(to_np(d[some]) - g_ref) <= bound) and bool(torch.isfinite(d).all())
+        again = dev.clone()
+        tbp.tbp_logprobs_step(again, tt, fl, fh, out=again)
+        assert torch.equal(again, s[3])
+
+
 def test_logprobs_of_as_many_rows_as_there_may_be():
     """2^31 - 1 rows of one logit each: the launches of a part of the rows each end behind the last one."""
     rows = 2 ** 31 - 1
