@@ -674,6 +674,42 @@ def test_grad_clip_in_place_of_unaligned_views_and_of_norms_that_are_not_finite(
     assert np.all(np.abs(to_np(big) - 1 / np.sqrt(3)) < 1e-6)
 
 
+def _big_reference(tensors, max_norm):
+    total = sum(float((t.double() ** 2).sum()) for t in tensors)
+    return total, min(1.0, max_norm / total ** 0.5)
+
+
+@pytest.mark.parametrize("sizes,dtype,out", [
+    ([9_000_001, 3, 7_777_777, 1_000_003], "f32", "f32"),        # just above 16 M elements: pieces of 8192
+    ([9_000_001, 3, 7_777_777, 1_000_003], "bf16", "bf16"),
+    ([60_000_011, 45_000_017, 5], "f32", "bf16"),                # 420 MB: the norm reads past the caches; 6 pieces and more to a workgroup
+    ([210_000_013, 100_003], "bf16", "f32"),
+    ([10_000_019], "f32", "f32"),                                # pieces of 4096, several to a workgroup
+], ids=lambda v: v if isinstance(v, str) else str(sum(v)))
+def test_grad_clip_of_large_lists(sizes, dtype, out):
+    """Sums of squares and clipped tensors against torch in 64 bits on the device, with a view that no piece of 16 bytes is aligned in among them."""
+    _say(f"grad clip of {sum(sizes)} elements {dtype} -> {out}")
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(93)
+    t, o = torch.bfloat16 if dtype == "bf16" else torch.float32, torch.bfloat16 if out == "bf16" else torch.float32
+    grads = [torch.randn(s + 1, generator=gen, device=DEV, dtype=t)[1 if i % 2 else 0:][:s] for i, s in enumerate(sizes)]
+    outs = [torch.full((s,), 7.0, dtype=o, device=DEV) for s in sizes]
+    total, c = _big_reference(grads, 1.0)
+    lst = tbp.GradList(grads, outs)
+    norm, sq = lst.clip(1.0), lst.sumsq()
+    # fp64 sums of this many squares: 1e-12 of the sum; the norm rounded to fp32; factor and product in fp32, one rounding of the result
+    assert abs(float(sq) - total) <= 1e-12 * total and abs(float(norm) - total ** 0.5) <= 2.0 ** -23 * total ** 0.5
+    for g, r in zip(grads, outs):
+        want = g.double() * c
+        assert bool(((r.double() - want).abs() <= (2.0 ** -8 if out == "bf16" else 2.0 ** -22) * want.abs()).all())
+    if t is o:
+        inplace = [g.clone() for g in grads]
+        tbp.GradList(inplace).clip(1.0, sumsq=sq)
+        assert all(torch.equal(a, b) for a, b in zip(inplace, outs))
+    tbp.GradList(grads, outs).clip(2.0 * total ** 0.5)           # nothing to clip: passed on
+    assert all(torch.equal(r, g.to(o)) for g, r in zip(grads, outs))
+
+
 # ------------------------------------------------------------------------------------------- refusals
 def test_one_tensor_of_the_host_among_a_call_s_is_refused():
     """The host refuses it; nothing is launched."""
