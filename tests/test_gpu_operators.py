@@ -396,6 +396,42 @@ def test_rotary_append_matches_oracle(dtype, n_new, lengths, capacity, sinks):
     assert np.array_equal(to_np(cv), v_ref)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,dh,rot,H,KV", [("bf16", 128, 128, 18, 3), ("bf16", 128, 64, 9, 3), ("f32", 64, 64, 13, 1), ("bf16", 20, 12, 25, 5)])
+def test_rotary_append_of_many_tokens(dtype, dh, rot, H, KV, interleaved):
+    """Enough of them that a thread has four heads, of which q, k and v may be some: as rotating all of the rows by themselves (products of
+    fp32 that may be contracted otherwise, one rounding of either)."""
+    nb, n_new, capacity, sinks = 64, 200 if dh > 64 else 700, 150, 4
+    assert nb * n_new * ((H + 2 * KV + 3) // 4) * (dh // 8) >= 4 * 256 * 256
+    _say(f"rotary append of many tokens {dtype} dh={dh} rot={rot} H={H} KV={KV} interleaved={interleaved}")
+    layout = tbp.TBP_ROTARY_INTERLEAVED if interleaved else tbp.TBP_ROTARY_HALF
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(74)
+    qkv = torch.randn((nb * n_new, (H + 2 * KV) * dh), generator=gen, device=DEV).to(t)
+    lengths = [n_new + 37 * b if b % 5 else n_new - 3 * b for b in range(nb)]
+    table = tbp.tbp_rotary_table(4000, rot, 10000.0)
+    ck, cv = (torch.full((nb, capacity, KV * dh), 7.0, device=DEV, dtype=t) for _ in range(2))
+    q = tbp.tbp_rotary_append(qkv, H, KV, dh, table, _ints(lengths), ck, cv, sinks, layout=layout)
+    pos = torch.tensor([[n - n_new + i for i in range(n_new)] for n in lengths], device=DEV)
+    turned = tbp.tbp_rotary(qkv, H + KV, dh, table, pos.clamp(min=0).to(torch.int32).view(-1), layout=layout).view(nb, n_new, -1)
+    want_q = torch.where(pos[..., None] >= 0, turned[..., :H * dh], torch.zeros((), device=DEV, dtype=t))
+    near = lambda a, b: bool(((a.float() - b.float()).abs() <= (2.0 ** -7 if dtype == "bf16" else 2.0 ** -22) * b.float().abs() + 1e-5).all())
+    assert near(q.view(nb, n_new, -1), want_q) and not bool(q.view(nb, n_new, -1)[pos < 0].any())
+    v = qkv.view(nb, n_new, -1)[..., (H + KV) * dh:]
+    want_k, want_v = torch.full_like(ck, 7.0), torch.full_like(cv, 7.0)
+    for b, n in enumerate(lengths):
+        new = [p for p in range(max(n - n_new, 0), n) if p < sinks or p >= n - (capacity - sinks)]
+        rows, at = torch.tensor([ref.cache_row(p, capacity, sinks) for p in new], device=DEV), torch.tensor([p - (n - n_new) for p in new], device=DEV)
+        want_k[b, rows], want_v[b, rows] = turned[b, at, H * dh:], v[b, at]
+    assert near(ck, want_k) and torch.equal(ck == 7.0, want_k == 7.0) and torch.equal(cv, want_v)
+    # and the rotation itself against the oracle, on some rows
+    some = [0, 1, n_new * nb // 2, n_new * nb - 1]
+    x, at = to_np(qkv[some]), pos.view(-1)[some].clamp(min=0).cpu().numpy()
+    y = ref.rotary(x, H + KV, dh, ref.rotary_theta(rot, 10000.0), at, interleaved)
+    assert np.all(np.abs(to_np(turned.reshape(nb * n_new, -1)[some]) - y) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22) * np.abs(y) + 1e-6 * np.max(np.abs(x)))
+
+
 # ------------------------------------------------------------------------------------------- log probabilities
 LOGIT_CASES = [(1, 1), (1, 2), (3, 7), (5, 63), (4, 64), (9, 1000), (2, 4097), (6, 50257), (1, 131072), (2, 200003), (300, 517), (700, 3001)]
 
