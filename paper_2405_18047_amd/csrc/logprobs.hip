@@ -425,17 +425,35 @@ static hipError_t launch(const LogprobParams& p, hipStream_t s) {
   return hipSuccess;
 }
 
+// Threads and pieces per thread of a row (256 x 4: 1024 N logits at a time, longer rows in blocks), chosen by length, by whether there are more rows than
+// compute units, and by what follows the statistics: the derivative reads a row that is not held a second time, the ranking costs a narrow workgroup
+// more than a wide one, and statistics alone gain nothing by holding the row, while pieces behind its end cost as much as others.  us, bf16 (N = 8), rows x
+// logits / N, the chosen form and the other that is nearest; fp32 and rows of odd length (unaligned) put the same ones ahead:
+//   statistics   7 x 256 64x4 3.9, 256x4 4.2; 4096 x 256 7.6, 17.0; 7 x 1024 256x4 4.2, 64x16 5.8; 4096 x 512 64x16 14.7, 256x4 17.2, x 1024 18.3, 18.2;
+//                7 x 2000 256x4 5.4, 1024x4 6.3; 300 x 2000 7.1, 256x16 9.4; 7 x 4096 1024x4 6.3, 256x4 7.1; 300 x 4096 256x16 10.6, 256x4 10.3, 4096 x 4096
+//                54.0, 56.5; 7 x 6000 512x16 8.1, 1024x16 12.1; 300 x 6000 256x4 12.9, 512x16 15.3; 7 x 16600 1024x4 15.9, 1024x16 21.8; 300 x 16600 32.6, 256x16 31.4
+//   20 ranked    7 x 256 256x4 8.4, 64x4 13.3; 4096 x 256 64x4 22.2, 256x4 28.2; 300 x 1024 256x4 11.1, 64x16 20.7; 7 x 2000 1024x4 9.6, 256x4 12.0; 300 x 2000
+//                256x4 14.7, 256x16 16.5; 7 x 4096 1024x4 9.9, 256x16 13.4; 300 x 4096 256x16 18.0, 1024x4 15.8, 4096 x 4096 73.6, 90.5; 300 x 6000 512x16 22.1,
+//                256x16 27.3; 7 x 16032 1024x16 17.8, 1024x4 21.0; 300 x 16032 1024x4 37.4, 256x16 43.3; 7 x 16600 24.4, 1024x16 32.8
+//   derivative   300 x 256 64x4 5.3, 256x4 5.7; 300 x 1024 256x4 7.2, 64x16 10.3; 4096 x 1024 64x16 27.6, 256x4 30.0; 7 x 4096 1024x4 9.0, 256x16 10.1; 4096 x 4096
+//                256x16 106.6, 1024x4 116.5; 7 x 6000 512x16 12.1, 1024x4 12.9, 4096 x 6000 170, 184; 300 x 16032 1024x16 50.0, 1024x4 55.2; 300 x 16600 1024x4 60.6,
+//                256x16 63.2, 1024x16 77.3
 template <typename T, bool STEP>
 static hipError_t launch_t(const LogprobParams& p, hipStream_t s) {
   constexpr int N = Logits<T>::N;
-  const bool many = p.rows > 256;
-  if (p.vocab <= 64 * 4 * N && p.top <= 32) return launch<T, 64, 4, STEP>(p, s);
-  if (p.vocab <= 64 * 16 * N && many && p.top <= 32) return launch<T, 64, 16, STEP>(p, s);
-  if (p.vocab <= 256 * 4 * N) return launch<T, 256, 4, STEP>(p, s);
-  if (many && (p.vocab <= 256 * 16 * N || (!STEP && p.vocab > 512 * 16 * N))) return launch<T, 256, 16, STEP>(p, s);
-  if (many && p.vocab <= 512 * 16 * N) return launch<T, 512, 16, STEP>(p, s);
-  if (p.vocab <= 1024 * 4 * N) return launch<T, 1024, 4, STEP>(p, s);
-  return launch<T, 1024, 16, STEP>(p, s);
+  const bool many = p.rows > 256, crowd = p.rows > 2048, top = p.top > 0;
+  if (p.vocab <= 256 * N && (!top || (crowd && p.top <= 32))) return launch<T, 64, 4, STEP>(p, s);
+  if (p.vocab <= 1024 * N) return crowd && !top ? launch<T, 64, 16, STEP>(p, s) : launch<T, 256, 4, STEP>(p, s);
+  if constexpr (STEP) {
+    if (p.vocab <= 4096 * N) return many ? launch<T, 256, 16, STEP>(p, s) : launch<T, 1024, 4, STEP>(p, s);
+    if (p.vocab <= 8192 * N) return launch<T, 512, 16, STEP>(p, s);
+    return p.vocab <= 16384 * N ? launch<T, 1024, 16, STEP>(p, s) : launch<T, 1024, 4, STEP>(p, s);
+  } else {
+    if (p.vocab <= 2048 * N) return many || !top ? launch<T, 256, 4, STEP>(p, s) : launch<T, 1024, 4, STEP>(p, s);
+    if (p.vocab <= 4096 * N) return many ? launch<T, 256, 16, STEP>(p, s) : launch<T, 1024, 4, STEP>(p, s);
+    if (p.vocab <= 8192 * N) return many && !top ? launch<T, 256, 4, STEP>(p, s) : launch<T, 512, 16, STEP>(p, s);
+    return p.vocab <= 16384 * N && !many && top ? launch<T, 1024, 16, STEP>(p, s) : launch<T, 1024, 4, STEP>(p, s);
+  }
 }
 
 hipError_t logprobs(int dtype, const LogprobParams& p, hipStream_t s) { return dtype ? launch_t<bf16_t, false>(p, s) : launch_t<float, false>(p, s); }

@@ -590,8 +590,7 @@ def test_logprobs_of_rows_that_are_not_finite(bad, vocab):
     assert got[4][1].tolist() == [-1] * 4
 
 
-# more rows than compute units: 256 threads of 16 pieces up to 256 * 16 * N logits (N = 8 bf16, 4 fp32), 512 threads up to twice that, beyond it blocks of 256 * 16
-# pieces (with the derivative 1024 threads); one wave of 16 pieces up to 64 * 16 * N
+# more rows than compute units: rows of every length at which another width of a row's threads is chosen, for the statistics, the ranking and the derivative
 MANY_ROWS = [("bf16", 9001), ("bf16", 32000), ("bf16", 50257), ("bf16", 70001), ("f32", 3999), ("f32", 5003), ("f32", 16384), ("f32", 20011), ("f32", 40009),
              ("bf16", 8191), ("bf16", 2048)]
 
@@ -638,6 +637,33 @@ def test_logprobs_of_many_rows_match_oracle(dtype, vocab):
         again = dev.clone()
         tbp.tbp_logprobs_step(again, tt, fl, fh, out=again)
         assert torch.equal(again, s[3])
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 1999), ("bf16", 2048), ("bf16", 5003), ("bf16", 8192), ("f32", 77), ("f32", 1024), ("f32", 3001)])
+def test_logprobs_of_thousands_of_short_rows_match_oracle(dtype, vocab):
+    """Rows that one wave takes, with and without the ranking and the derivative."""
+    rows = 2101
+    _say(f"logprobs of thousands of rows vocab={vocab} {dtype}")
+    x, t = _logits(rows, vocab, dtype, 87)
+    some = [0, 1, 2, 3, 4, 1000, 2047, 2048, 2100]
+    x64 = x[some].astype(np.float64)
+    refs = ref.logprobs(x64, t[some])
+    wl, wh = np.linspace(-1, 1, rows).astype(np.float32), np.linspace(0.5, -0.5, rows).astype(np.float32)
+    g_ref = ref.logprobs_p1(x64, t[some], wl[some].astype(np.float64), wh[some].astype(np.float64))
+    dev, tt = _logits_dev(x, dtype, 9, 5), _ints(t.tolist())
+    s = tbp.tbp_logprobs_step(dev, tt, torch.from_numpy(wl).to(DEV), torch.from_numpy(wh).to(DEV))
+    for k in (0, 5, 32, 33):
+        got = tbp.tbp_logprobs(dev, tt, top=k)
+        for stats in (got, s):
+            for a, r in zip(stats[:3], refs):
+                a = to_np(a)[some]
+                fine = _same_infinities(a, r)
+                assert np.all(np.abs(a[fine] - r[fine]) <= 2e-5 * (1 + np.abs(r[fine])))
+        if k:
+            assert all(got[4][r].tolist() == np.lexsort((np.arange(vocab), -x64[i]))[:k].tolist() for i, r in enumerate(some))
+            assert torch.equal(torch.gather(dev.float(), 1, got[4].long()), torch.topk(dev.float(), k, dim=1).values)
+    assert np.all(np.abs(to_np(s[3][some]) - g_ref) <= (2.0 ** -8 if dtype == "bf16" else 2e-5) * np.abs(g_ref) + 2e-5)
+    assert bool(torch.isfinite(s[3]).all())
 
 
 def test_logprobs_of_as_many_rows_as_there_may_be():
