@@ -184,9 +184,10 @@ static hipError_t launch_w(RotaryParams p, hipStream_t s) {
     }
     return hipSuccess;
   };
-  // heads per thread: four read the table less and load more at a time; one, where four leave fewer than 4 workgroups per compute unit (us, one / four
-  // heads: 1024 rows of 40 heads of 128 6.7 / 6.8, 8192 rows 45.9 / 38.5)
-  if ((long)p.rows * ((p.heads + 3) / 4) * p.units >= 4 * 256 * 256) return run(std::integral_constant<int, 4>{});
+  // heads per thread: four read the table less and load more at a time; one, where four leave fewer than 3 workgroups to two compute units.  us, one /
+  // four heads, 40 heads of 128, bf16, half-split: 256 rows 3.9 / 4.1, 512 5.1 / 4.8, 1024 9.0 / 5.7, 8192 41.0 / 30.1; interleaved 3.4 / 3.7, 4.3 / 4.2, 7.5 / 5.2,
+  // 37.6 / 28.2; fp32 4.3 / 4.2, 7.4 / 5.2, 11.6 / 7.5, 70.3 / 54.0; 12 heads of 64, bf16: 2048 rows 4.1 / 4.2, 4096 5.9 / 4.9, 8192 10.4 / 5.9
+  if ((long)p.rows * ((p.heads + 3) / 4) * p.units >= 384 * 256) return run(std::integral_constant<int, 4>{});
   return run(std::integral_constant<int, 1>{});
 }
 
@@ -201,6 +202,9 @@ static hipError_t launch_t(const RotaryParams& p, hipStream_t s) {
   auto run = [&](auto width) {
     constexpr int W = decltype(width)::value;
     if constexpr (W > 1) if (p.interleaved) return launch_w<T, W, INSIDE, APPEND>(p, s);
+    // ACROSS where it can be: us, across / beside, four heads a thread each: 40 heads of 128, bf16, 1024 rows 5.7 / 6.0, 8192 30.1 / 29.7, half of the columns turned
+    // 30.6 / 33.0, fp32 54.0 / 55.4; 12 heads of 64, 8192 rows 5.9 / 7.9, 32768 19.7 / 24.4.  Interleaved pairs, pieces that hold them / column by column: 8192 rows
+    // of 40 heads 28.2 / 52.5, fp32 53.6 / 68.1
     const int pieces = p.dh / W;
     if constexpr (W * sizeof(T) >= 4) if (!p.interleaved && pieces <= 64 && (pieces & (pieces - 1)) == 0) return launch_w<T, W, ACROSS, APPEND>(p, s);
     return launch_w<T, W, BESIDE, APPEND>(p, s);
