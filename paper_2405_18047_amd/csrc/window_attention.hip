@@ -1252,6 +1252,9 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   q.B = w.batch; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.seq; q.window = w.window; q.sinks = w.sinks;
   q.scale = 1.f / sqrtf((float)w.head_dim);
   q.scale_log2e = 1.4426950408889634f * q.scale;
+  // 64 queries per workgroup as in the forward.  us of the whole backward, 128 / 64 queries of dq: 8 heads of 128, 700 tokens, window 300 33.4 / 26.9; 32, 1024, 256
+  // 49.6 / 47.2; 40, 1024, 256 54.6 / 56.9; 32, 2 of 2048, 256 125.7 / 127.9; of 64: 12 heads, 4 ragged sequences of 1001, 300 39.0 / 36.7; 16, 4096, all 188 / 176; 32, 2
+  // of 1024, all 78.2 / 76.3; 2048, 256 52.2 / 53.1; 4 of 2048, 256 120.8 / 126.5
   const long groups = (long)w.batch * w.heads * ((w.seq + 127) / 128);
   hipError_t e;
   if (groups <= (w.head_dim == 64 ? 512 : 256)) e = w.head_dim == 128 ? launch_dq<128, 2>(q, s) : launch_dq<64, 2>(q, s);
@@ -1269,10 +1272,16 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
 
 // Shares of a head's keys, at most: as many as make the rounds of workgroups (one per compute unit at head_dim 128, two at 64) short by this model, whose
 // times, in us, are those of a tile in a workgroup when the chip is full, of one that has it to itself (the latency of its copies), and of a share's
-// start and end.  us, as many as leave no compute unit without one / by the model, 8 heads of 128: 12 sequences of 4096 keys 62.9 / 49.9, 20 87.9 / 71.7,
-// 33 151 / 126, 48 168 / 147, 5 of 16384 96.0 / 68.3, 64 of 4096 181.6 / 181.9; but 20 ragged ones 48.2 / 54.1 (lengths are not known here).
+// start and end.  They are those of head_dim 128; only their proportions matter, which half the bytes per tile and twice the workgroups per compute unit
+// leave as they are: of 1, 2, 3, 4, 6, 8, 12, 16, 24 or 32 shares the model's are within 2 % of the fastest at both from 1000 keys on, us, one share / the model's / the fastest,
+// 8 key heads of 128, 4 query heads each: 1 sequence of 4096 keys 56.3 / 10.7 / 10.6, 8 76.3 / 30.5 / 30.7, 12 78.2 / 47.7 / 47.5, 20 81.6 / 69.7 / 69.7, 33
+// 147.6 / 122.0 / 121.6, 64 174.2 / 174.6 / 174.2, 5 of 16384 keys 96 / 68 (as many as leave no compute unit without one / the model's); of 64: 1 38.3 / 9.6 / 9.5,
+// 8 47.3 / 16.9 / 16.8, 12 56.4 / 24.6 / 25.6, 20 59.3 / 34.8 / 34.7, 33 71.2 / 60.8 / 61.0, 64 89.6 / 89.6 / 89.6.  Lengths are not known here: all are taken for the
+// longest (20 ragged ones 54.1, where as many as leave no compute unit without one take 48.2), and a cache that keeps less than the window for the window.
 // A share costs the joining workgroup as much as most of a tile of keys (its sums of 32 heads, in proportion less of fewer), so no more than make the
-// reading of a share and the joining of all of them about equal.
+// reading of a share and the joining of all of them about equal.  That is coarse where it binds: 32 query heads on one key head of 128, 300 keys in two shares 11.5, in
+// one 8.7; 4096 in twelve 19.5, in sixteen 15.8 (whose tiles are two for every wave); 4 query heads, 300 keys 8.2, 7.7.  Nor more than eight rounds of workgroups (64
+// sequences of 4096 keys in eight shares 235, in one 174) or 64 shares, which bounds the workspace.
 int window_decode_splits(int batch, int heads, int kv_heads, int head_dim, long most_seen) {
   constexpr float kFull = 0.74f, kAlone = 0.44f, kStart = 4.f;
   const int group = heads / kv_heads, nh = group < 32 ? group : 32;
