@@ -33,7 +33,7 @@ class Shape:
 
 
 class WindowAttention:
-    """x + Wo Attention(RoPE(RMSNorm(x) Wqkv)): forward, backward-p1 and backward-p2, and the form for new tokens."""
+    """x + Wo Attention(RoPE(RMSNorm(x) Wqkv)): forward, backward-p1 and backward-p2, and the form for a new token."""
 
     def __init__(self, c: Shape, table, params):
         self.c, self.table = c, table
@@ -68,8 +68,8 @@ class WindowAttention:
         self.kept = None
         return [tbp.tbp_gemm(tbp.TN, h, dqkv, out_f32=True), tbp.tbp_gemm(tbp.TN, out, dy, out_f32=True), self.dg]
 
-    def new_tokens(self, x, cache, workspace, lengths):
-        """x [batch * n_new, d], the sequences `lengths` long with them; -> the same for the last of them [batch, d]."""
+    def new_token(self, x, cache, workspace, lengths):
+        """x [batch, d]: one new token of every sequence, `lengths` long with it (the decode answers for one at a time) -> [batch, d]."""
         c = self.c
         qkv = tbp.tbp_gemm(tbp.NN, tbp.tbp_rmsnorm_fwd(x, self.g, EPS), self.w_qkv)
         q = tbp.tbp_rotary_append(qkv, c.n_heads, c.n_kv_heads, c.head_dim, self.table, lengths, *cache, c.sinks)
@@ -163,7 +163,7 @@ class Model:
         x = self.embedding[tokens]
         n = 3 * self.c.layers
         for i, (a, (cache, workspace)) in enumerate(zip(self.attention, caches)):
-            x = a.new_tokens(x, cache, workspace, lengths)
+            x = a.new_token(x, cache, workspace, lengths)
             w_gu, w_d, g2 = self.params[n + 3 * i:n + 3 * i + 3]
             m = tbp.tbp_swiglu_fwd(tbp.tbp_gemm(tbp.NN, tbp.tbp_rmsnorm_fwd(x, g2, EPS), w_gu))
             x = tbp.tbp_gemm(tbp.NN, m, w_d, R=x)
