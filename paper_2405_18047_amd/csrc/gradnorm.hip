@@ -4,6 +4,8 @@
 // The sums of the workgroups lie side by side in a workspace; every workgroup of the clipping launch adds them up for itself, in order.
 // Bound by memory, which gradients cross twice: the factor depends on all of them, and they are more than the caches hold.  405 M of them in fp32
 // (1.62 GB) 240 us for the norm, 6.8 TB/s, and 445 us clipped into bf16, 5.5 TB/s; 0.8 M of them, in the caches, 3.8 + 4.5 us, two launches.
+// Long lists pay for a launch of each pass per 96 tensors, and every clipping workgroup for all of the sums: 400 M elements in 12 tensors 670 us, in 96 687, in 291 742,
+// in 1000 1043; 10 M in 12 22.2, in 291 50.9, in 1000 122.
 #include "kernels.h"
 #include "rows.h"
 

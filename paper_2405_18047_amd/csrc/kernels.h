@@ -222,7 +222,7 @@ inline int run_end(const int* mbs, int n, int i, int tokens) {
 }
 
 // ---- sliding-window attention with sinks (bf16 storage, head_dim 64 or 128), see include/tbp.h ----------------------------------
-struct WindowShape { int batch, heads, kv_heads, seq, head_dim, window, sinks; };      // window, sinks at most seq (decode: at most capacity)
+struct WindowShape { int batch, heads, kv_heads, seq, head_dim, window, sinks; };      // window, sinks at most seq (decode: as the caller gives them)
 // How the pass over the queries cuts the lists of (query head, query step) pairs of its key blocks (of 128 or 64 keys): those of the sinks into
 // sink_parts each, the others into other_parts; a block of more than one part leaves partial sums.
 struct WindowParts {

@@ -6,6 +6,10 @@
 // The orientation of the products, the row order that feeds the accumulators of one product into the next, and the LDS images are
 // those of the fused attention (attention.hip); what differs is which key blocks a query block meets (the blocks of the
 // sinks, then those of the window) and, in the pass over the queries, which (query head, query block) pairs a key block meets.
+//
+// Rounded to bf16 on the way are P before P V and P^T dO, and dS before dS K and dS^T Q: a matrix instruction takes both operands of one type, that of v, dO, k
+// and q, and fp32 ones run at a sixteenth of the rate.  Scores, maxima, sums, statistics and accumulators are fp32.  Off the definition in 64 bits by, over the values' root
+// mean square: outputs 0.0021, with the derivatives 0.0024; the last rounding of results that are exact before it gives 0.0017.
 #include "kernels.h"
 #include "gfx950.h"
 #include "head_tile.h"
@@ -62,10 +66,11 @@ struct HeadOf {
 // K one block ahead of V, the scores of the next block computed beside the exponentials of this one in a pinned order (AHEAD).
 // SPLIT = 2, for grids that leave compute units idle: 64 queries per workgroup, and two waves per 32 queries, each on one 32-key tile of
 // every block, whose sums meet at the end.
-// Bound by the matrix pipes, busy 54 % of the cycles that a workgroup is resident, at the clock that the card's power leaves (1.8 GHz): [2, 4096] tokens,
-// 32 heads on 8 of 128, window 1024, 4 sinks 150 to 165 us over cards, 0.73 to 0.80 PFLOP/s of the pairs that are seen, 1.05 at 150 us of the tiles that are
-// computed.  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies
-// of the block's code, 165 us).  No more than the registers bounds the workgroups of a compute unit: head_dim 64, window 256, 4 sequences of 2048, 32 heads
+// No unit is full: matrix pipes are busy 54 % of the cycles that a workgroup is resident, vector instructions are issued in 56 %, and the two waves of a SIMD
+// overlap them only in part, at the clock that the card's power leaves (1.8 GHz).  [2, 4096] tokens, 32 heads on 8 of 128, window 1024, 4 sinks 150 to 167 us
+// over cards, 0.72 to 0.80 PFLOP/s of the pairs that are seen, 0.82 to 0.92 of those that are computed (1.14 times as many, for the tiles at the window's two
+// edges).  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies of the block's code, 165 us for 152).  No more than
+// the registers bounds the workgroups of a compute unit: head_dim 64, window 256, 4 sequences of 2048, 32 heads
 // 49.1 us with two, 38.4 with four.
 template <int DH, bool AHEAD, int SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
@@ -326,8 +331,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // dQ = scale * dS K: oriented like the forward, per 32-key tile S^T and dP^T = V dO^T are rebuilt, dS^T = P^T (dP^T - delta) is fed into
 // dQ^T += K^T dS^T.  delta = rowsum(dout * out) of its queries is computed first and left for the pass over the queries.
 // One workgroup = 4 waves x 32 queries, key blocks through LDS in two slots, as in the forward, so that the sum over the keys stays in registers and
-// no atomics are needed.  Bound by the matrix pipes at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 360 us,
-// 1.0 PFLOP/s of the three products over the seen pairs, the pipes busy 56 %.
+// no atomics are needed.  As in the forward no unit is full, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 355 to 378
+// us, 0.96 to 1.02 PFLOP/s of the three products over the seen pairs, matrix pipes busy 56 %, vector instructions 45 %.
 struct WinDqParams {
   const bf16_t* qkv; long ld_qkv;
   const bf16_t* dout; const bf16_t* out; long ld_do;
@@ -551,8 +556,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // the parts of others leave fp32 partial sums that a second launch adds up in order.
 // Roles of the waves as in the fused attention's pass: 4 "left" waves compute P and dS of their 32 keys and hand them over through
 // LDS, 4 "right" waves issue all copies and accumulate dV^T += dO^T P, dK^T += Q^T dS of one 32-query tile later.
-// Bound by the matrix pipes and the LDS beside them, at the clock that the power leaves: 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 545 us,
-// 0.88 PFLOP/s of the four products over the seen pairs, the pipes busy 50 %, the LDS 44 %.  Short windows are bound by the chain of a step (scores,
+// 8192 tokens, 32 heads on 8 of 128, window 2048, 4 sinks 535 to 570 us, 0.85 to 0.90 PFLOP/s of the four products over the seen pairs, at the clock that the power
+// leaves: matrix pipes busy 50 %, the LDS 44 %, vector instructions 29 %; a step of the left waves and one of the right waves meet at every barrier.  Of the tiles
+// that the right waves multiply 4 % are zeros because no pair of them is seen (window 2048; 128 with 64 keys 17 %).  Short windows are bound by the chain of a step (scores,
 // exponentials, hand-over, barrier) in few workgroups: 12 heads on 4 of 64, 4 ragged sequences of 1001, window 300 19 us.  Tried at head_dim 128: lse and delta
 // fetched by the left waves, 20 us more; with 64 keys, and the LDS so freed a fourth slot, copies a step earlier: 177 -> 184 us at 2 of 4096, window 128.
 struct WinKvParams {
@@ -1225,7 +1231,8 @@ WindowParts window_parts(const WindowShape& w) {
   r.sink_blocks = (sinks + r.keys - 1) / r.keys;
   const long all = (w.seq + 63) / 64, seen = ((long)w.window + r.keys - 2 + 64) / 64 + 1;
   const long sink_pairs = G * all, other_pairs = G * (seen < all ? seen : all);      // pairs of the longest lists, of each kind
-  // a part: enough of them for 256 workgroups, where the lists are long enough for that (4 pairs each), at most a whole list of the other blocks;
+  // a part: enough of them for 256 workgroups (for 512, 4 ragged sequences of 1001, 4 key heads of 64 42 us for 35), where the lists are long enough for that (4 pairs
+  // each; 6, 8 and 12 took the same time), at most a whole list of the other blocks;
   // of the sinks' lists, so that they make no more than 1024 parts in all (sinks may be as many as tokens, and the window short)
   const long others = r.blocks - r.sink_blocks;
   const long pairs = heads * (r.sink_blocks * sink_pairs + others * other_pairs);
