@@ -349,7 +349,7 @@ typedef struct {
   float magnitude;
 } tbp_rotary_scale;
 size_t tbp_rotary_table_bytes(int n_pos, int rot_dim);
-/* scale: host, NULL for PLAIN. */
+/* scale: host, NULL for PLAIN.  n_pos * rot_dim/2 below 2^32 - 256. */
 tbp_status tbp_rotary_table(int n_pos, int rot_dim, float base, const tbp_rotary_scale* scale, void* table, void* stream);
 /* y = the rotation of x, or its derivative (backward != 0: dx from dy, the transposed rotation).  x [rows, ld_x], y [rows, ld_y],
  * the first n_heads*head_dim columns; y may be x itself (other overlaps not).  positions: device [rows] int32, or NULL: row % seq.

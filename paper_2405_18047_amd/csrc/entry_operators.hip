@@ -137,6 +137,7 @@ size_t tbp_rotary_table_bytes(int n_pos, int rot_dim) {
 tbp_status tbp_rotary_table(int n_pos, int rot_dim, float base, const tbp_rotary_scale* scale, void* table, void* stream) {
   if (n_pos < 1 || rot_dim < 2 || rot_dim % 2 || !(base > 0.f) || !table) return fail(TBP_EINVAL, "bad rotary table arguments");
   if (rot_dim > 4096) return fail(TBP_EINVAL, "rot_dim above the limit 4096");
+  if ((long)n_pos * (rot_dim / 2) >= (1L << 32) - 256) return fail(TBP_EINVAL, "a table of 2^32 - 256 entries or more");      // (a launch's threads)
   if (misaligned(table, 8)) return fail(TBP_EINVAL, "table must be 8-byte aligned");
   tbp::RotaryScale sc{tbp::ROTARY_PLAIN, 1.f, 0.f, 1.f, 1.f, 1.f};
   if (scale) {

@@ -242,3 +242,8 @@ def test_new_memory_is_the_current_device_s(monkeypatch):
         with pytest.raises(InterruptedError):
             call()
     assert asked == [torch.device("cuda")] * 3
+
+
+@pytest.mark.parametrize("n_pos,rot_dim", [(1 << 26, 128), ((1 << 31) - 1, 4), ((1 << 31) - 1, 4096)])
+def test_rotary_tables_of_more_entries_than_a_launch_has_threads_are_refused(n_pos, rot_dim):
+    _refused(tbp.lib().tbp_rotary_table(n_pos, rot_dim, 1e4, None, P, None), "entries")
