@@ -6,7 +6,7 @@ Kinds of case:
             gradient), "append" (new tokens: q normed and rotated, k into the cache, v into the cache)
   packed    causal attention over sequences of different lengths that lie one behind the other: "fwd", "step" (forward and
             backward-p1)
-  stash     tensors kept in 8 bits with a scale for 32 tokens of a column: "keep" (stored, and taken out again), "dw" (the
+  stash     tensors kept in 8 bits with a scale for up to 1024 tokens of a column: "keep" (stored, and taken out again), "dw" (the
             inputs and output derivatives of a linear layer stored per micro-batch, and the weight gradient from them)
 
 With own = False the operators are computed in plain torch operations in 32 bits; with own = True by this library.
@@ -21,8 +21,7 @@ own = False
 
 DEV = "cuda:0"
 EPS = 1e-5
-#: bits of the mantissa, exponent of the largest value, exponent of the smallest normal one
-FORMATS = {"e4m3": (3, 8, -6), "e5m2": (2, 15, -14)}
+BLOCK = 1024                    # tokens of a column that share a scale
 
 
 # ----------------------------------------------------------------------------------------------------------- cases
@@ -42,10 +41,9 @@ def _packed(name, op, rows, seqs, spread, heads, kv_heads, head_dim, behind=0):
             "kv_heads": kv_heads, "head_dim": head_dim, "behind": behind}
 
 
-def _stash(name, op, micro_batches, tokens, cols, other, dtype, format="e4m3", d_format="e4m3"):
-    """cols, format: of the tensor (dw: the layer's inputs); other, d_format: of its output derivatives (dw)."""
-    return {"name": name, "kind": "stash", "op": op, "micro_batches": micro_batches, "tokens": tokens, "cols": cols, "other": other,
-            "dtype": dtype, "format": format, "d_format": d_format}
+def _stash(name, op, micro_batches, tokens, cols, other, dtype):
+    """cols: of the tensor (dw: the layer's inputs); other: of its output derivatives (dw)."""
+    return {"name": name, "kind": "stash", "op": op, "micro_batches": micro_batches, "tokens": tokens, "cols": cols, "other": other, "dtype": dtype}
 
 
 def listed():
@@ -71,7 +69,7 @@ def listed():
         # the 7B stage's down projection over a whole step
         _stash("stash_dw_7b", "dw", 8, 4096, 11008, 4096, "bf16"),
         # its output projection at the shorter context, one micro-batch after the other
-        _stash("stash_dw_s1024", "dw", 4, 1024, 4096, 4096, "bf16", "e4m3", "e5m2"),
+        _stash("stash_dw_s1024", "dw", 4, 1024, 4096, 4096, "bf16"),
         # odd sizes: tokens and columns that end inside a tile
         _stash("stash_dw_odd", "dw", 3, 333, 520, 1001, "f32"),
     ]
@@ -104,9 +102,9 @@ def _draw_one(rng):
         seqs = min(_log_int(rng, 1, 100), rows - behind)
         return _packed("", rng.choice(["fwd", "step"]), rows, seqs, rng.choice([1, 4, 30]), heads, kv, rng.choice([64, 128]), behind)
     if rng.random() < 0.4:
-        return _stash("", "keep", 1, _log_int(rng, 1, 8192), _log_int(rng, 16, 12288), 0, rng.choice(["bf16", "bf16", "f32"]), rng.choice(["e4m3", "e5m2"]))
+        return _stash("", "keep", 1, _log_int(rng, 1, 8192), _log_int(rng, 16, 12288), 0, rng.choice(["bf16", "bf16", "f32"]))
     return _stash("", "dw", rng.choice([1, 2, 3, 4, 8]), _log_int(rng, 32, 4096), _log_int(rng, 64, 11008), _log_int(rng, 64, 11008),
-                  rng.choice(["bf16", "bf16", "f32"]), "e4m3", rng.choice(["e4m3", "e4m3", "e5m2"]))
+                  rng.choice(["bf16", "bf16", "f32"]))
 
 
 def draw(rng):
@@ -220,10 +218,9 @@ def prepare(case, seed):
         state["tbp"] = tbp
         if case["kind"] == "stash":
             # the stash of a stage, which lives from step to step
-            format = {"e4m3": tbp.TBP_E4M3, "e5m2": tbp.TBP_E5M2}
-            state["kept"] = tbp.Stash8(case["tokens"], case["cols"], case["micro_batches"], state["x"].dtype, format[case["format"]], device=DEV)
+            state["kept"] = tbp.Stash8(case["tokens"], case["cols"], case["micro_batches"], state["x"].dtype, device=DEV)
             if case["op"] == "dw":
-                state["d_kept"] = tbp.Stash8(case["tokens"], case["other"], case["micro_batches"], state["x"].dtype, format[case["d_format"]], device=DEV)
+                state["d_kept"] = tbp.Stash8(case["tokens"], case["other"], case["micro_batches"], state["x"].dtype, device=DEV)
     return state
 
 
@@ -343,27 +340,23 @@ def _power(e):
     return ((e + 127) << 23).to(torch.int32).view(torch.float32)
 
 
-def _held(x, format):
-    """The values that x [micro-batches, tokens, columns] is held as, in 32 bits: of every 32 tokens of a column (from the first token of the
-    micro-batch on) the smallest power of two is taken as scale with which the largest one is in the format's range."""
-    bits, top, low = FORMATS[format]
+def _held(x):
+    """The values that x [micro-batches, tokens, columns] is held as, in 32 bits: of every 1024 tokens of a column (from the first token of the
+    micro-batch on) whole multiples, -127 .. 127, of the smallest power of two with which the largest one is in that range."""
     M, n, c = x.shape
-    pad = -n % 32
-    b = torch.cat([x.float(), torch.zeros((M, pad, c), device=DEV)], dim=1).view(M, (n + pad) // 32, 32, c)
+    tall = min(n, BLOCK)
+    b = torch.cat([x.float(), torch.zeros((M, -n % tall, c), device=DEV)], dim=1).view(M, -1, tall, c)
     part, exponent = torch.frexp(b.abs().amax(dim=2, keepdim=True))           # part in 1/2 .. 1
-    e = (exponent - 1 - top + (part > 0.875).int()).clamp(min=-126)
-    v = b * _power(-e)
-    fine = bits - (torch.frexp(v)[1] - 1).clamp(min=low)                      # 2^-fine: the distance of the format's values there
-    return (torch.round(v * _power(fine)) * _power(-fine) * _power(e)).view(M, n + pad, c)[:, :n]
+    e = (exponent - 7 + (part > 127 / 128).int()).clamp(min=-126)
+    return (torch.round(b * _power(-e)) * _power(e)).view(M, -1, c)[:, :n]
 
 
 def _plain_stash(state):
     case, x = state["case"], state["x"]
-    held = _held(x, case["format"])
+    held = _held(x)
     if case["op"] == "keep":
         return held[0].to(x.dtype)
-    d = _held(state["dy"], case["d_format"])
-    return torch.matmul(held.reshape(-1, case["cols"]).t(), d.reshape(-1, case["other"]))
+    return torch.matmul(held.reshape(-1, case["cols"]).t(), _held(state["dy"]).reshape(-1, case["other"]))
 
 
 def run(state):
@@ -469,35 +462,29 @@ def _exact_packed(case, seed):
     return (out, lse, dqkv) if step else (out, lse)
 
 
-def _nearest(x, format):
-    """The definition, by a table of all values of the format: each value goes to the nearest one, ties to the even code."""
-    bits, top, low = FORMATS[format]
-    codes = torch.arange((top - low + 2) << bits, device=DEV)
-    field, frac = codes >> bits, (codes & ((1 << bits) - 1)).double() / (1 << bits)
-    two = torch.full((), 2.0, dtype=torch.float64, device=DEV)
-    values = torch.where(field == 0, frac * 2.0 ** low, (1 + frac) * torch.cumprod(two.expand(top - low + 1), 0)[(field - 1).clamp(min=0)] * 2.0 ** (low - 1))
-    values = values[values <= 1.75 * 2.0 ** top]
-    middles = (values[1:] + values[:-1]) / 2
+def _nearest(x):
+    """The definition: the nearest multiple of the scale, halves to the even one."""
     M, n, c = x.shape
     held = torch.empty((M, n, c), dtype=torch.float64, device=DEV)
-    for t in range(0, n, 32):
-        b = x[:, t:t + 32].double()
-        part, e = torch.frexp(b.abs().amax(dim=1, keepdim=True) / values[-1])
+    for t in range(0, n, BLOCK):
+        b = x[:, t:t + BLOCK].double()
+        part, e = torch.frexp(b.abs().amax(dim=1, keepdim=True) / 127)
         e = torch.where(part == 0.5, e - 1, e).clamp(min=-126)                # the power of two at or above the quotient
         scale = ((e.long() + 1023) << 52).view(torch.float64)
         a = b.abs() / scale
-        lo, hi = torch.bucketize(a, middles), torch.bucketize(a, middles, right=True)
-        held[:, t:t + 32] = values[torch.where(lo % 2 == 0, lo, hi)] * scale * torch.sign(b)
+        whole = torch.floor(a)
+        up = (a - whole > 0.5) | ((a - whole == 0.5) & (torch.remainder(whole, 2) == 1))
+        held[:, t:t + BLOCK] = (whole + up) * scale * torch.sign(b)
     return held
 
 
 def _exact_stash(case, seed):
     s = _stash_inputs(case, seed)
     if case["op"] == "keep":
-        return _nearest(s["x"], case["format"])[0]
+        return _nearest(s["x"])[0]
     dw = torch.zeros((case["cols"], case["other"]), dtype=torch.float64, device=DEV)
     for mb in range(case["micro_batches"]):
-        dw += _nearest(s["x"][mb:mb + 1], case["format"])[0].t() @ _nearest(s["dy"][mb:mb + 1], case["d_format"])[0]
+        dw += _nearest(s["x"][mb:mb + 1])[0].t() @ _nearest(s["dy"][mb:mb + 1])[0]
     return dw
 
 
