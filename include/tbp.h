@@ -394,6 +394,64 @@ tbp_status tbp_grad_sumsq(int dtype, int n, const void* const* grads, const int6
 tbp_status tbp_grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,
                          const double* sumsq, float max_norm, float* norm, void* workspace, void* stream);
 
+/* ---- operators of a stage that is trained on packed documents, and of a stash in 8 bits ----------------------------------
+ * Norms of query and key heads with the rotary positions, causal attention over packed sequences, and linear layers' inputs and
+ * output derivatives kept in 8 bits for backward-p2.  They follow the rules at the top of this file. */
+
+/* Norms of the query and key heads, and the rotary positions in the same pass: of every head y = R (x / sqrt(mean(x^2) + eps) * g),
+ * g the gains gq (query heads) or gk (key heads), device [head_dim] in the storage type, R the rotation of the first rot_dim columns as
+ * for tbp_rotary (rot_dim 0: none, table not read).  x [rows, ld_x]: column blocks q [n_heads*head_dim] | k [n_kv_heads*head_dim];
+ * y [rows, ld_y] likewise; y may be x itself (other overlaps not; backward-p1 needs x).  head_dim even, at most 512.  positions, seq,
+ * table, layout and positions outside the table as for tbp_rotary.  Any alignment of the element type; 16-byte alignment of rows,
+ * pieces and gains is faster. */
+tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
+                       int rot_dim, int layout, const void* table, int n_pos, const int32_t* positions, int seq, const void* x,
+                       int ld_x, void* y, int ld_y, void* stream);
+/* Its backward-p1 (Section 3.1): dx [rows, ld_dx] from dy [rows, ld_dy] and the forward's x; dx may be dy itself.  The gains' gradient
+ * is backward-p2 work and is left, as by tbp_rmsnorm_p1_partials, as tbp_qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim) partial
+ * rows (at most 512, 0 without rows) in partials_out [partial rows][2*head_dim] fp32, of gq and of gk: tbp_gain_partials_sum with d = 2*head_dim adds them
+ * up, those of several micro-batches in one call.  Results do not depend on timing. */
+int tbp_qk_norm_partial_rows(int rows, int n_heads, int n_kv_heads, int head_dim);
+tbp_status tbp_qk_norm_p1(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
+                          int rot_dim, int layout, const void* table, int n_pos, const int32_t* positions, int seq, const void* dy,
+                          int ld_dy, const void* x, int ld_x, void* dx, int ld_dx, float* partials_out, void* stream);
+/* New tokens into the caches as by tbp_rotary_append, with q and k normed first. */
+tbp_status tbp_qk_norm_append(int dtype, int batch, int n_new, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq,
+                              const void* gk, int rot_dim, int layout, const void* table, int n_pos, const int32_t* lengths,
+                              const void* qkv, int ld_qkv, void* q_out, int ld_q, void* cache_k, void* cache_v, int ld_cache,
+                              int capacity, int sinks, void* stream);
+
+/* Causal attention over n_seqs sequences of any lengths that lie one behind the other: sequence b is the rows starts[b] .. starts[b+1]-1 of
+ * qkv [rows, ld_qkv] (starts: device [n_seqs+1] int32, ascending, starts[0] = 0; a sequence may be empty), and its query i sees its keys
+ * j <= i.  Rows behind the last sequence (from starts[n_seqs] on) are padding: never read, zeros in every result, lse -infinity.  Entries
+ * outside 0 .. rows are taken as the nearest of these and starts[0] as 0; where they do not ascend, results are undefined (nothing outside the
+ * tensors is touched).  lse: device [n_heads, rows] fp32.  Types, head rules, layouts, alignment and finite rows as for tbp_window_attention_fwd.
+ * Limits: 0 <= rows <= 2^22, 0 <= n_seqs <= 2^20, n_heads * (rows / 64 + n_seqs + 1) below 2^27. */
+tbp_status tbp_packed_attention_fwd(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, const int32_t* starts,
+                                    const void* qkv, int ld_qkv, void* out, int ld_out, float* lse, void* stream);
+/* Its backward-p1, as tbp_window_attention_p1.  scratch: device, 256-byte aligned, >= tbp_packed_attention_p1_scratch_bytes of the same sizes. */
+size_t tbp_packed_attention_p1_scratch_bytes(int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim);
+tbp_status tbp_packed_attention_p1(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, const int32_t* starts,
+                                   const void* qkv, int ld_qkv, const void* out, const void* d_out, int ld_out, const float* lse,
+                                   void* dqkv, int ld_dqkv, void* scratch, void* stream);
+
+/* A stash in 8 bits of one tensor (a linear layer's input or output derivative, kept from backward-p1 to backward-p2): `slots` micro-batches of
+ * [tokens, cols] each.  Of every 1024 tokens of a column, counted from a slot's first, the values are held as q 2^e: q = -127 .. 127 an
+ * 8-bit integer, rounded to the nearest, halves to even; e the smallest exponent, -126 .. 121, with which the largest of them is in that range (values above 127 2^121 are held as that).
+ * A block that holds an infinity or a NaN stands for NaN throughout.  Caller's memory, 16-byte aligned, of tbp_stash8_bytes (about cols * tokens bytes a
+ * slot; 0 for sizes outside the limits), which has to be all zeros or put into before it is read; slots that are all zeros hold zeros.
+ * tbp_stash8_put stores x [tokens, ld_x] into a slot, tbp_stash8_get takes y [tokens, ld_y] out of it, rounded to the storage type. */
+size_t tbp_stash8_bytes(int slots, int tokens, int cols);
+tbp_status tbp_stash8_put(int dtype, int slots, int tokens, int cols, int slot, const void* x, int ld_x, void* stash, void* stream);
+tbp_status tbp_stash8_get(int dtype, int slots, int tokens, int cols, int slot, const void* stash, void* y, int ld_y, void* stream);
+/* backward-p2 of a linear layer from two such stashes (Section 3.1; Section 3.2: the slots are one contraction length, without a copy): dw [m, ld_dw]
+ * fp32 (= or +=) X^T dY, X [n * tokens, m] and dY [n * tokens, cols n_out] the n slots from `first` on.  The sums over a block of 1024 tokens are
+ * exact integers, those over the blocks fp32 (of a block less than fp32's smallest normal number may be lost), in an order that does not depend on timing.  n == 0 writes zeros (or leaves an accumulated dw alone).
+ * workspace: device, 256-byte aligned, >= tbp_stash8_dw_workspace_bytes of the same sizes (may be 0: NULL); calls that share one must not overlap. */
+size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n);
+tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,
+                         int ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid (no paper passage: it prices the hardware, not the method): a register-resident loop of
  * 32x32x16 bf16 MFMAs, blocks x 4 wavefronts x iters x 16 instructions = blocks*iters*2^21 FLOP, touching no memory
  * inside the loop.  What it sustains is the practical ceiling of the matrix pipes under the chip's power management,

@@ -127,6 +127,18 @@ def lib() -> C.CDLL:
         L.tbp_grad_workspace_bytes.argtypes, L.tbp_grad_workspace_bytes.restype = [i32], size
         L.tbp_grad_sumsq.argtypes = [i32, i32] + [ptr] * 5
         L.tbp_grad_clip.argtypes = [i32] * 3 + [ptr] * 4 + [f32, ptr, ptr, ptr]
+        L.tbp_qk_norm.argtypes = [i32] * 5 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr]
+        L.tbp_qk_norm_partial_rows.argtypes = [i32] * 4
+        L.tbp_qk_norm_p1.argtypes = [i32] * 5 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, ptr]
+        L.tbp_qk_norm_append.argtypes = [i32] * 6 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]
+        L.tbp_packed_attention_fwd.argtypes = [i32] * 6 + [ptr, ptr, i32, ptr, i32, ptr, ptr]
+        L.tbp_packed_attention_p1_scratch_bytes.argtypes, L.tbp_packed_attention_p1_scratch_bytes.restype = [i32] * 5, size
+        L.tbp_packed_attention_p1.argtypes = [i32] * 6 + [ptr, ptr, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, ptr]
+        L.tbp_stash8_bytes.argtypes, L.tbp_stash8_bytes.restype = [i32] * 3, size
+        L.tbp_stash8_put.argtypes = [i32] * 5 + [ptr, i32, ptr, ptr]
+        L.tbp_stash8_get.argtypes = [i32] * 5 + [ptr, ptr, i32, ptr]
+        L.tbp_stash8_dw_workspace_bytes.argtypes, L.tbp_stash8_dw_workspace_bytes.restype = [i32] * 4, size
+        L.tbp_stash8_dw.argtypes = [i32] * 6 + [ptr, ptr, ptr, i32, i32, ptr, size, ptr]
         _lib = L
     return _lib
 

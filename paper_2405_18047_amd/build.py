@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtbp.so")
 SOURCES = ["gemm.hip", "elementwise.hip", "attention.hip", "stage.hip", "window_attention.hip", "rotary.hip", "logprobs.hip",
-           "gradnorm.hip", "entry_operators.hip"]
+           "gradnorm.hip", "qk_norm.hip", "stash8.hip", "entry_operators.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

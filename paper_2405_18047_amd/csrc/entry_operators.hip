@@ -1,4 +1,5 @@
-// C entry points of the operators for long contexts, the last stage and serving: argument checks, then the launches.
+// C entry points of the operators around a stage (long contexts, the last stage and serving; packed documents and a stash in 8 bits): argument
+// checks, then the launches.
 #include "entry.h"
 #include "kernels.h"
 
@@ -307,6 +308,205 @@ tbp_status tbp_grad_clip(int dtype, int out_dtype, int n, const void* const* gra
   double* const sums = static_cast<double*>(workspace);
   if (!sumsq) TBP_HIP(tbp::grad_sumsq(dtype, n, grads, counts, sums, &n_sums, stream_of(stream)));
   TBP_HIP(tbp::grad_clip(dtype, out_dtype, n, grads, outs, counts, sumsq ? sumsq : sums, n_sums, max_norm, norm, stream_of(stream)));
+  return TBP_OK;
+}
+
+// ---- norms of query and key heads with rotary positions ------------------------------------------------------------------------
+static tbp_status check_qk_norm(int dtype, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk, int rot_dim,
+                                int layout, const void* table, int n_pos) {
+  if (check_storage(dtype) != TBP_OK) return TBP_EINVAL;
+  if (n_heads < 0 || n_kv_heads < 0) return fail(TBP_EINVAL, "negative size");
+  if (head_dim < 2 || head_dim % 2 || head_dim > tbp::kQkNormMaxHead) return fail(TBP_EINVAL, "head_dim must be even and 2 .. %d", tbp::kQkNormMaxHead);
+  if (((long)n_heads + 2L * n_kv_heads) * head_dim >= (1L << 30)) return fail(TBP_EINVAL, "heads too many");
+  if (!(eps >= 0.f)) return fail(TBP_EINVAL, "eps must be at least 0");
+  if (rot_dim && check_rotary(dtype, head_dim, rot_dim, layout, table, n_pos) != TBP_OK) return TBP_EINVAL;
+  const size_t e = dtype == TBP_BF16 ? 2 : 4;
+  if ((n_heads && (!gq || misaligned(gq, e))) || (n_kv_heads && (!gk || misaligned(gk, e))))
+    return fail(TBP_EINVAL, "gains must be non-null and aligned to their elements");
+  return TBP_OK;
+}
+
+static tbp::QkNormParams qk_norm_params(int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk, int rot_dim,
+                                        int layout, const void* table, int n_pos, const int32_t* positions, int seq) {
+  tbp::QkNormParams p{};
+  p.rows = rows; p.q_heads = n_heads; p.kv_heads = n_kv_heads; p.dh = head_dim; p.eps = eps; p.gq = gq; p.gk = gk;
+  p.half = rot_dim / 2; p.interleaved = rot_dim ? layout : 0; p.table = static_cast<const float2*>(table); p.n_pos = n_pos;
+  p.positions = positions; p.seq = seq < 1 ? 1 : seq;
+  return p;
+}
+
+tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
+                       int rot_dim, int layout, const void* table, int n_pos, const int32_t* positions, int seq, const void* x,
+                       int ld_x, void* y, int ld_y, void* stream) {
+  if (rows < 0) return fail(TBP_EINVAL, "negative size");
+  if (check_qk_norm(dtype, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos) != TBP_OK) return TBP_EINVAL;
+  if (rot_dim && !positions && seq < 1) return fail(TBP_EINVAL, "without positions seq must be at least 1");
+  const long columns = ((long)n_heads + n_kv_heads) * head_dim;
+  if (ld_x < columns || ld_y < columns) return fail(TBP_EINVAL, "leading dimensions must cover the %ld head columns", columns);
+  if (rows == 0 || columns == 0) return TBP_OK;
+  if (!x || !y) return fail(TBP_EINVAL, "null pointer");
+  const size_t e = dtype == TBP_BF16 ? 2 : 4;
+  if (misaligned(x, e) || misaligned(y, e)) return fail(TBP_EINVAL, "tensors must be aligned to their elements");
+  if (x == y && ld_x != ld_y) return fail(TBP_EINVAL, "in place both leading dimensions must be the same");
+  tbp::QkNormParams p = qk_norm_params(rows, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos, positions, seq);
+  p.x = x; p.ld_x = ld_x; p.y = y; p.ld_y = ld_y;
+  TBP_HIP(tbp::qk_norm(dtype, p, stream_of(stream)));
+  return TBP_OK;
+}
+
+int tbp_qk_norm_partial_rows(int rows, int n_heads, int n_kv_heads, int head_dim) {
+  if (rows < 1 || n_heads < 0 || n_kv_heads < 0 || n_heads + (long)n_kv_heads < 1 || head_dim < 2) return 0;
+  return tbp::qk_norm_partial_rows(rows, (long)n_heads + n_kv_heads, head_dim);
+}
+
+tbp_status tbp_qk_norm_p1(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
+                          int rot_dim, int layout, const void* table, int n_pos, const int32_t* positions, int seq, const void* dy,
+                          int ld_dy, const void* x, int ld_x, void* dx, int ld_dx, float* partials_out, void* stream) {
+  if (rows < 0) return fail(TBP_EINVAL, "negative size");
+  if (check_qk_norm(dtype, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos) != TBP_OK) return TBP_EINVAL;
+  if (rot_dim && !positions && seq < 1) return fail(TBP_EINVAL, "without positions seq must be at least 1");
+  const long columns = ((long)n_heads + n_kv_heads) * head_dim;
+  if (ld_x < columns || ld_dy < columns || ld_dx < columns) return fail(TBP_EINVAL, "leading dimensions must cover the %ld head columns", columns);
+  if (rows == 0 || columns == 0) return TBP_OK;
+  if (!dy || !x || !dx || !partials_out) return fail(TBP_EINVAL, "null pointer");
+  const size_t e = dtype == TBP_BF16 ? 2 : 4;
+  if (misaligned(dy, e) || misaligned(x, e) || misaligned(dx, e) || misaligned(partials_out, 4)) return fail(TBP_EINVAL, "tensors must be aligned to their elements");
+  if (dx == dy && ld_dx != ld_dy) return fail(TBP_EINVAL, "in place both leading dimensions must be the same");
+  if (dx == x) return fail(TBP_EINVAL, "dx may be dy, not x");
+  tbp::QkNormParams p = qk_norm_params(rows, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos, positions, seq);
+  p.x = x; p.ld_x = ld_x; p.dy = dy; p.ld_dy = ld_dy; p.y = dx; p.ld_y = ld_dx; p.partials = partials_out;
+  p.n_partials = tbp_qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim);
+  TBP_HIP(tbp::qk_norm_p1(dtype, p, stream_of(stream)));
+  return TBP_OK;
+}
+
+tbp_status tbp_qk_norm_append(int dtype, int batch, int n_new, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq,
+                              const void* gk, int rot_dim, int layout, const void* table, int n_pos, const int32_t* lengths,
+                              const void* qkv, int ld_qkv, void* q_out, int ld_q, void* cache_k, void* cache_v, int ld_cache,
+                              int capacity, int sinks, void* stream) {
+  if (check_heads(n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
+  if (check_qk_norm(dtype, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos) != TBP_OK) return TBP_EINVAL;
+  if (batch < 0 || n_new < 0) return fail(TBP_EINVAL, "negative size");
+  if ((long)batch * n_new > 0x7fffffffL) return fail(TBP_EINVAL, "batch * n_new too large");
+  if (sinks < 0 || capacity <= sinks) return fail(TBP_EINVAL, "capacity must be above sinks, sinks at least 0");
+  const long wq = (long)n_heads * head_dim, wkv = (long)n_kv_heads * head_dim;
+  if (ld_qkv < wq + 2 * wkv || ld_q < wq || ld_cache < wkv) return fail(TBP_EINVAL, "leading dimensions must cover the head columns");
+  if (batch == 0 || n_new == 0) return TBP_OK;
+  if (!lengths || !qkv || !q_out || !cache_k || !cache_v) return fail(TBP_EINVAL, "null pointer");
+  const size_t e = dtype == TBP_BF16 ? 2 : 4;
+  if (misaligned(qkv, e) || misaligned(q_out, e) || misaligned(cache_k, e) || misaligned(cache_v, e))
+    return fail(TBP_EINVAL, "tensors must be aligned to their elements");
+  tbp::QkNormParams p = qk_norm_params(batch * n_new, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos, nullptr, 1);
+  p.x = qkv; p.ld_x = ld_qkv; p.y = q_out; p.ld_y = ld_q; p.lengths = lengths; p.tokens_new = n_new;
+  p.cache_k = cache_k; p.cache_v = cache_v; p.ld_c = ld_cache; p.capacity = capacity; p.sinks = sinks;
+  TBP_HIP(tbp::qk_norm_append(dtype, p, stream_of(stream)));
+  return TBP_OK;
+}
+
+// ---- causal attention over packed sequences ------------------------------------------------------------------------------------
+static tbp_status check_packed(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim) {
+  if (dtype != TBP_BF16) return fail(TBP_EINVAL, "packed attention is built for bf16 storage only");
+  if (head_dim != 64 && head_dim != 128) return fail(TBP_EINVAL, "packed attention needs head_dim 64 or 128");
+  if (check_heads(n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
+  if (n_seqs < 0 || rows < 0) return fail(TBP_EINVAL, "negative size");
+  if (rows > (1 << 22) || n_seqs > (1 << 20)) return fail(TBP_EINVAL, "rows above 2^22 or n_seqs above 2^20");
+  if ((long)n_heads * (rows / 64 + n_seqs + 1) >= (1L << 27)) return fail(TBP_EINVAL, "n_heads * (rows / 64 + n_seqs + 1) must be below 2^27");
+  return TBP_OK;
+}
+
+tbp_status tbp_packed_attention_fwd(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, const int32_t* starts,
+                                    const void* qkv, int ld_qkv, void* out, int ld_out, float* lse, void* stream) {
+  if (check_packed(dtype, n_seqs, rows, n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
+  if (rows == 0) return TBP_OK;
+  if (!starts || !qkv || !out || !lse) return fail(TBP_EINVAL, "null pointer");
+  if (check_ld("ld_qkv", ld_qkv, ((long)n_heads + 2L * n_kv_heads) * head_dim) != TBP_OK) return TBP_EINVAL;
+  if (check_ld("ld_out", ld_out, (long)n_heads * head_dim) != TBP_OK) return TBP_EINVAL;
+  if (misaligned(qkv, 16) || misaligned(out, 16)) return fail(TBP_EINVAL, "qkv and out must be 16-byte aligned");
+  TBP_HIP(tbp::packed_attention_fwd(tbp::PackedShape{starts, n_seqs, rows, n_heads, n_kv_heads, head_dim}, qkv, ld_qkv, out, ld_out, lse, stream_of(stream)));
+  return TBP_OK;
+}
+
+size_t tbp_packed_attention_p1_scratch_bytes(int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim) {
+  if (rows < 1 || check_packed(TBP_BF16, n_seqs, rows, n_heads, n_kv_heads, head_dim) != TBP_OK) return 0;
+  return delta_bytes(1, n_heads, rows) + tbp::packed_attention_p1_partial_bytes(tbp::PackedShape{nullptr, n_seqs, rows, n_heads, n_kv_heads, head_dim});
+}
+
+tbp_status tbp_packed_attention_p1(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, const int32_t* starts,
+                                   const void* qkv, int ld_qkv, const void* out, const void* d_out, int ld_out, const float* lse,
+                                   void* dqkv, int ld_dqkv, void* scratch, void* stream) {
+  if (check_packed(dtype, n_seqs, rows, n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
+  if (rows == 0) return TBP_OK;
+  if (!starts || !qkv || !out || !d_out || !lse || !dqkv || !scratch) return fail(TBP_EINVAL, "null pointer");
+  const long columns = ((long)n_heads + 2L * n_kv_heads) * head_dim;
+  if (check_ld("ld_qkv", ld_qkv, columns) != TBP_OK || check_ld("ld_dqkv", ld_dqkv, columns) != TBP_OK) return TBP_EINVAL;
+  if (check_ld("ld_out", ld_out, (long)n_heads * head_dim) != TBP_OK) return TBP_EINVAL;
+  if (misaligned(qkv, 16) || misaligned(out, 16) || misaligned(d_out, 16) || misaligned(dqkv, 16) || misaligned(scratch, 256))
+    return fail(TBP_EINVAL, "tensors must be 16-byte aligned, scratch 256-byte aligned");
+  TBP_HIP(tbp::packed_attention_p1(tbp::PackedShape{starts, n_seqs, rows, n_heads, n_kv_heads, head_dim}, qkv, ld_qkv, out, d_out, ld_out, lse, dqkv, ld_dqkv,
+                                   static_cast<float*>(scratch), reinterpret_cast<float*>(static_cast<char*>(scratch) + delta_bytes(1, n_heads, rows)),
+                                   stream_of(stream)));
+  return TBP_OK;
+}
+
+// ---- a stash in 8 bits -----------------------------------------------------------------------------------------------------------
+static tbp_status check_stash8(int slots, int tokens, int cols) {
+  if (slots < 0 || tokens < 1 || cols < 1) return fail(TBP_EINVAL, "slots must be at least 0, tokens and cols at least 1");
+  if (tokens > (1 << 22) || cols >= (1 << 22)) return fail(TBP_EINVAL, "tokens above 2^22, or cols not below it");
+  if ((long)slots * ((tokens + 63) / 64) >= (1L << 30)) return fail(TBP_EINVAL, "slots * tokens too large");
+  return TBP_OK;
+}
+
+static size_t stash8_data_bytes(int slots, int tokens, int cols) { return (size_t)slots * ((tokens + 63) / 64) * ((cols + 31) / 32) * 2048; }
+
+static tbp::Stash8Slot stash8_slot(int slots, int tokens, int cols, int slot, const void* stash) {
+  tbp::Stash8Slot p{};
+  p.data = static_cast<unsigned char*>(const_cast<void*>(stash));
+  p.scales = reinterpret_cast<float*>(p.data + stash8_data_bytes(slots, tokens, cols));
+  p.tokens = tokens; p.cols = cols; p.slot = slot;
+  p.steps = (tokens + 63) / 64; p.blocks = (tokens + tbp::kStash8Block - 1) / tbp::kStash8Block; p.col_blocks = (cols + 31) / 32;
+  return p;
+}
+
+size_t tbp_stash8_bytes(int slots, int tokens, int cols) {
+  if (slots < 1 || check_stash8(slots, tokens, cols) != TBP_OK) return 0;
+  return stash8_data_bytes(slots, tokens, cols) + (size_t)slots * ((tokens + tbp::kStash8Block - 1) / tbp::kStash8Block) * ((cols + 31) / 32) * 32 * sizeof(float);
+}
+
+static tbp_status check_stash8_slot(int dtype, int slots, int tokens, int cols, int slot, const void* x, int ld, const void* stash) {
+  if (check_storage(dtype) != TBP_OK || check_stash8(slots, tokens, cols) != TBP_OK) return TBP_EINVAL;
+  if (slot < 0 || slot >= slots) return fail(TBP_EINVAL, "slot %d of %d", slot, slots);
+  if (ld < cols) return fail(TBP_EINVAL, "leading dimension smaller than cols");
+  if (!x || !stash) return fail(TBP_EINVAL, "null pointer");
+  if (misaligned(x, dtype == TBP_BF16 ? 2 : 4) || misaligned(stash, 16)) return fail(TBP_EINVAL, "the tensor must be aligned to its elements, the stash to 16 bytes");
+  return TBP_OK;
+}
+
+tbp_status tbp_stash8_put(int dtype, int slots, int tokens, int cols, int slot, const void* x, int ld_x, void* stash, void* stream) {
+  if (check_stash8_slot(dtype, slots, tokens, cols, slot, x, ld_x, stash) != TBP_OK) return TBP_EINVAL;
+  TBP_HIP(tbp::stash8_put(dtype, stash8_slot(slots, tokens, cols, slot, stash), x, ld_x, stream_of(stream)));
+  return TBP_OK;
+}
+
+tbp_status tbp_stash8_get(int dtype, int slots, int tokens, int cols, int slot, const void* stash, void* y, int ld_y, void* stream) {
+  if (check_stash8_slot(dtype, slots, tokens, cols, slot, y, ld_y, stash) != TBP_OK) return TBP_EINVAL;
+  TBP_HIP(tbp::stash8_get(dtype, stash8_slot(slots, tokens, cols, slot, stash), y, ld_y, stream_of(stream)));
+  return TBP_OK;
+}
+
+size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n) {
+  return 0;
+}
+
+tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,
+                         int ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  if (check_stash8(slots, tokens, m) != TBP_OK || check_stash8(slots, tokens, n_out) != TBP_OK) return TBP_EINVAL;
+  if (first < 0 || n < 0 || first > slots - n) return fail(TBP_EINVAL, "slots %d .. %ld of %d", first, (long)first + n - 1, slots);
+  if (ld_dw < n_out) return fail(TBP_EINVAL, "leading dimension smaller than n_out");
+  if (n == 0 && accumulate) return TBP_OK;
+  if (!x_stash || !dy_stash || !dw) return fail(TBP_EINVAL, "null pointer");
+  if (misaligned(x_stash, 16) || misaligned(dy_stash, 16) || misaligned(dw, 4)) return fail(TBP_EINVAL, "stashes must be 16-byte aligned, dw 4-byte");
+  TBP_HIP(tbp::stash8_dw(stash8_slot(slots, tokens, m, first, x_stash), stash8_slot(slots, tokens, n_out, first, dy_stash), n, dw, ld_dw, accumulate,
+                         stream_of(stream)));
   return TBP_OK;
 }
 

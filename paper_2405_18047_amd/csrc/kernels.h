@@ -247,6 +247,13 @@ hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths,
                          const void* cache_v, long ld_cache, void* out, long ld_out, float* lse, int splits, unsigned* arrived,
                          float* part_o, float2* part_ml, hipStream_t s);
 
+// ---- causal attention over packed sequences (the same kernels), see include/tbp.h ------------------------------------------------
+struct PackedShape { const int* starts; int seqs, rows, heads, kv_heads, head_dim; };
+size_t packed_attention_p1_partial_bytes(const PackedShape& w);
+hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s);
+hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qkv, const void* out, const void* d_out, long ld_out, const float* lse,
+                               void* dqkv, long ld_dqkv, float* delta, float* partial, hipStream_t s);
+
 // ---- rotary positions, see include/tbp.h ---------------------------------------------------------------------------------------
 enum { ROTARY_PLAIN = 0, ROTARY_LINEAR = 1, ROTARY_BASE = 2, ROTARY_RAMP = 3 };      // tbp_rotary_scaling
 struct RotaryScale { int kind; float factor, low, high, original, magnitude; };
@@ -286,6 +293,38 @@ hipError_t grad_sumsq(int dtype, int n, const void* const* grads, const int64_t*
 hipError_t grad_sum(const double* sums, int n, double* out, hipStream_t s);
 hipError_t grad_clip(int dtype, int out_dtype, int n, const void* const* grads, void* const* outs, const int64_t* counts,
                      const double* sums, int n_sums, float max_norm, float* norm, hipStream_t s);
+
+// ---- norms of query and key heads with rotary positions, see include/tbp.h ----------------------------------------------------------
+struct QkNormParams {
+  const void* x; long ld_x; void* y; long ld_y;      // rows of q_heads + kv_heads heads of dh columns; y (p1: dx) may be x (p1: dy)
+  const void* dy; long ld_dy;                        // p1 only
+  const void* gq; const void* gk; float eps;
+  const float2* table; int n_pos;                    // half 0: none
+  const int* positions; int seq;                     // position of row r: positions[r], or r % seq
+  int rows, q_heads, kv_heads, dh, half, interleaved;
+  float* partials; int n_partials;                   // p1: [n_partials][2][dh]
+  // append only: x's heads are q_heads of q, kv_heads of k, kv_heads of v
+  const int* lengths; int tokens_new;
+  void* cache_k; void* cache_v; long ld_c; int capacity, sinks;
+  int units, lanes, q_groups, kv_groups, row0; long items;      // set by the launch
+};
+constexpr int kQkNormMaxHead = 512, kQkNormPartials = 512;
+int qk_norm_partial_rows(int rows, int heads, int head_dim);
+hipError_t qk_norm(int dtype, const QkNormParams& p, hipStream_t s);
+hipError_t qk_norm_p1(int dtype, const QkNormParams& p, hipStream_t s);
+hipError_t qk_norm_append(int dtype, const QkNormParams& p, hipStream_t s);
+
+// ---- a stash in 8 bits, see include/tbp.h and stash8.hip ---------------------------------------------------------------------------
+constexpr int kStash8Block = 1024;                   // tokens of a column that share a scale
+struct Stash8Slot {
+  unsigned char* data; float* scales;                // of the whole stash
+  int tokens, cols, slot;
+  int steps, blocks, col_blocks;                     // 64 tokens, kStash8Block tokens, 32 columns: each rounded up
+};
+hipError_t stash8_put(int dtype, const Stash8Slot& p, const void* x, long ld, hipStream_t s);
+hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStream_t s);
+// over n slots from x.slot on (dy: the same slots, tokens and steps)
+hipError_t stash8_dw(const Stash8Slot& x, const Stash8Slot& dy, int n, float* dw, long ld, int accumulate, hipStream_t s);
 
 // Limits enforced by the host before any launch.
 inline int max_d_model(int dtype) { return dtype == 1 ? 8192 : 4096; }

@@ -30,20 +30,6 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(long n, int half, dou
   table[idx] = make_float2((float)(magnitude * c), (float)(magnitude * s));
 }
 
-// W elements as they lie in memory.  Each is touched once: 16-byte pieces go past the caches' retention (nontemporal), which takes the
-// [8192, 5120] case from 38.5 us to 32.6, fp32 from 61.0 to 54.6.
-template <typename T, int W> struct Piece {
-  struct alignas(sizeof(T) * W) Raw { T v[W]; };
-  static __device__ __forceinline__ Raw load(const T* p) {
-    if constexpr (sizeof(Raw) == 16) return __builtin_bit_cast(Raw, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
-    else return *reinterpret_cast<const Raw*>(p);
-  }
-  static __device__ __forceinline__ void store(T* p, const Raw& r) {
-    if constexpr (sizeof(Raw) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p));
-    else *reinterpret_cast<Raw*>(p) = r;
-  }
-};
-
 // A thread owns one unit of a row's heads and applies the cosines and sines that it holds to HPT consecutive heads.  A unit is
 //   INSIDE  W columns that hold whole pairs (interleaved);
 //   ACROSS  W columns whose partners are another lane's (half-split heads of 1, 2, 4 .. 64 pieces): a head is then read and written in one piece;

@@ -40,11 +40,46 @@ struct KeyBlocks {
   __device__ __forceinline__ int key0(int j) const { return (j < n_sink ? j : win0 + j - n_sink) << 6; }
 };
 
+// Sequences that lie one behind the other (PACKED): sequence b has the rows starts[b] .. starts[b + 1] - 1 of `rows`, all causal; lse and delta are [H][rows].
+// Blocks of BQ queries (or keys) are numbered without a look at all lengths: sequence b's are those from starts[b] / BQ + b on, whose places do not
+// overlap since a sequence of n tokens has at most (starts[b + 1] / BQ - starts[b] / BQ) + 1 blocks.  Numbers that no block has end at once; the rows behind
+// the last sequence are a sequence without tokens, whose results are zeros.  Starts are taken as 0 .. rows and the first as 0.
+struct Packed { const int* starts; int seqs, rows; };
+inline __host__ __device__ long packed_blocks(const Packed& p, int block) { return (long)p.rows / block + p.seqs + 1; }
+
+__device__ __forceinline__ int packed_start(const Packed& p, int b) {
+  const int s = b > 0 ? p.starts[b] : 0;
+  return s < 0 ? 0 : s < p.rows ? s : p.rows;
+}
+
+// The sequence of a workgroup and its block in it.  n: tokens; S: rows to be written.
+struct SeqOf {
+  long tok0; int n, S, block;
+  template <int BLOCK> __device__ __forceinline__ static SeqOf packed(const Packed& p, int number) {
+    // the last of the sequences 0 .. seqs (the rows behind them) whose numbers begin at or before this one, 64 at a time
+    const int lane = threadIdx.x & 63;
+    int lo = 0, size = p.seqs + 1;
+    while (size > 1) {
+      const int step = (size + 63) / 64, b = lo + lane * step;
+      const bool before = lane * step < size && packed_start(p, b) / BLOCK + b <= number;
+      const unsigned long long all = __ballot(before);               // (the first one is among them)
+      const int last = all ? 63 - __builtin_clzll(all) : 0;
+      lo += last * step;
+      size = size - last * step < step ? size - last * step : step;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int first = packed_start(p, lo), end = lo < p.seqs ? packed_start(p, lo + 1) : p.rows;
+    const int S = end > first ? end - first : 0;
+    return SeqOf{first, lo < p.seqs ? S : 0, S, number - first / BLOCK - lo};
+  }
+};
+
 struct WinParams {
   const bf16_t* qkv; long ld_qkv;      // [B*S, >= (H + 2 KV) DH]: q | k | v column blocks
   bf16_t* out; long ld_out;            // [B*S, >= H*DH]
   float* lse;                          // [B, H, S]: log2 of the row's sum of exp2(score * scale * log2 e)
   const int* lengths;                  // [B] or nullptr
+  Packed packed;                       // PACKED: the sequences (B 1, S rows, no window, no sinks)
   int B, H, KV, G, S, window, sinks;
   float scale_log2e;
 };
@@ -72,7 +107,7 @@ struct HeadOf {
 // edges).  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies of the block's code, 165 us for 152).  No more than
 // the registers bounds the workgroups of a compute unit: head_dim 64, window 256, 4 sequences of 2048, 32 heads
 // 49.1 us with two, 38.4 with four.
-template <int DH, bool AHEAD, int SPLIT>
+template <int DH, bool AHEAD, int SPLIT, bool PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT, NT = 2 / SPLIT;
@@ -85,26 +120,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 
   const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qb = (int)gridDim.y - 1 - (int)blockIdx.y;             // last query blocks first: the first ones may have short windows
-  const HeadOf at((int)blockIdx.x, p.B, p.KV, p.G);
+  const int x = PACKED ? (int)blockIdx.x % p.H : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / p.H : (int)blockIdx.y;
+  int qb = (PACKED ? (int)gridDim.x / p.H : (int)gridDim.y) - 1 - y;             // last query blocks first: the first ones may have short windows
+  const HeadOf at(x, p.B, p.KV, p.G);
   const int b = at.b, h = at.h;
+  SeqOf seq{(long)b * p.S, 0, p.S, qb};
+  if constexpr (PACKED) { seq = SeqOf::packed<BQ>(p.packed, qb); qb = seq.block; }
+  const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
   const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
-  const long tok0 = (long)b * p.S;
-  const int n = seq_end(p.lengths, b, p.S);
+  const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
+  const int n = PACKED ? seq.n : seq_end(p.lengths, b, p.S);
   constexpr int LPR = DH / 8, RPI = 64 / LPR;                       // lanes per row and rows per wave-wide store
   const int rl = lane / LPR, piece = lane % LPR;
 
   if (q0 >= n) {                                                    // (uniform) nothing but padding
     if (wk == 0) {
       for (int r0 = 0; r0 < 32; r0 += RPI)
-        if (qw0 + r0 + rl < p.S) *reinterpret_cast<u32x4*>(p.out + (tok0 + qw0 + r0 + rl) * p.ld_out + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
-      if (g == 0 && query < p.S) p.lse[((long)b * p.H + h) * p.S + query] = -INFINITY;
+        if (qw0 + r0 + rl < S) *reinterpret_cast<u32x4*>(p.out + (tok0 + qw0 + r0 + rl) * p.ld_out + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
+      if (g == 0 && query < S) p.lse[stat0 + query] = -INFINITY;
     }
     return;
   }
   const int q_last = (q0 + BQ < n ? q0 + BQ : n) - 1;
-  const KeyBlocks kbs(q0, q_last, p.window, p.sinks);
+  const KeyBlocks kbs(q0, q_last, window, sinks);
 
   const typename HT::Offsets fo = HT::offsets(lane);
   // rows r0 .. of the sequence, at most `rows` of them and none from n on, as seen from column `col`
@@ -179,8 +218,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     if (kv0 > qw0 + 31) return;        // every key of the block is after every query of this wave
     lds_u8* const kimg = lds + ((j + 1) & 1) * SLOT + wk_rows;   // (after the last block: an older one, whose scores nobody uses)
     lds_u8* const vimg = lds + (j & 1) * SLOT + IMG + wk_rows;
-    const bool low = kv0 < qw0 + 32 - p.window && kv0 + 32 * NT > p.sinks;         // some query of this wave is past the window of some key
-    if (!AHEAD && low && kv0 >= p.sinks && kv0 + 32 * NT <= qw0 + 1 - p.window) return;      // ... and every query past that of every key
+    const bool low = kv0 < qw0 + 32 - window && kv0 + 32 * NT > sinks;         // some query of this wave is past the window of some key
+    if (!AHEAD && low && kv0 >= sinks && kv0 + 32 * NT <= qw0 + 1 - window) return;      // ... and every query past that of every key
     bf16x8 kf[2][NT];
     if constexpr (AHEAD) {
 #pragma unroll
@@ -191,7 +230,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
       scores(st, lds + (j & 1) * SLOT + wk_rows);
     }
     if (low || kv0 + 32 * NT - 1 > qw0) {
-      const int hi = query - kv0 - 4 * g, lo = hi - p.window, sk = p.sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
+      const int hi = query - kv0 - 4 * g, lo = hi - window, sk = sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
 #pragma unroll
       for (int kt = 0; kt < NT; kt++)
 #pragma unroll
@@ -315,13 +354,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
         for (int r = 0; r < 4; r++) v[r] = (bf16_t)(live ? ot[t][4 * e4 + r] * inv : 0.f);
         *reinterpret_cast<LDS_AS bf16x4*>(erow + ql * EROW + (32 * t + 8 * e4 + 4 * g) * 2) = v;
       }
-    if (g == 0 && query < p.S) p.lse[((long)b * p.H + h) * p.S + query] = live ? m + __builtin_amdgcn_logf(lq) : -INFINITY;
+    if (g == 0 && query < S) p.lse[stat0 + query] = live ? m + __builtin_amdgcn_logf(lq) : -INFINITY;
   }
   // (LDS operations of a wave execute in order: the reads below see this wave's own writes above)
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += RPI) {
     const int qrow = qw0 + r0 + rl;
-    if (qrow < p.S)
+    if (qrow < S)
       *reinterpret_cast<u32x4*>(p.out + (tok0 + qrow) * p.ld_out + h * DH + 8 * piece) =
           *reinterpret_cast<const LDS_AS u32x4*>(erow + (r0 + rl) * EROW + 16 * piece);
   }
@@ -339,12 +378,13 @@ struct WinDqParams {
   const float* lse;                    // [B, H, S]
   float* delta;                        // [B, H, S]: written here for the tokens that are there
   const int* lengths;
+  Packed packed;
   bf16_t* dqkv; long ld_dqkv;
   int B, H, KV, G, S, window, sinks;
   float scale, scale_log2e;
 };
 
-template <int DH, int SPLIT>
+template <int DH, int SPLIT, bool PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_bwd_dq_kernel(WinDqParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT;
@@ -357,24 +397,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 
   const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qb = (int)gridDim.y - 1 - (int)blockIdx.y;
-  const HeadOf at((int)blockIdx.x, p.B, p.KV, p.G);
+  const int x = PACKED ? (int)blockIdx.x % p.H : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / p.H : (int)blockIdx.y;
+  int qb = (PACKED ? (int)gridDim.x / p.H : (int)gridDim.y) - 1 - y;
+  const HeadOf at(x, p.B, p.KV, p.G);
   const int b = at.b, h = at.h;
+  SeqOf seq{(long)b * p.S, 0, p.S, qb};
+  if constexpr (PACKED) { seq = SeqOf::packed<BQ>(p.packed, qb); qb = seq.block; }
+  const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;
   const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
-  const long tok0 = (long)b * p.S;
-  const int n = seq_end(p.lengths, b, p.S);
+  const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
+  const int n = PACKED ? seq.n : seq_end(p.lengths, b, p.S);
   constexpr int LPR = DH / 8, RPI = 64 / LPR;
   const int rl = lane / LPR, piece = lane % LPR;
 
   if (q0 >= n) {
     if (wk == 0)
       for (int r0 = 0; r0 < 32; r0 += RPI)
-        if (qw0 + r0 + rl < p.S) *reinterpret_cast<u32x4*>(p.dqkv + (tok0 + qw0 + r0 + rl) * p.ld_dqkv + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
+        if (qw0 + r0 + rl < S) *reinterpret_cast<u32x4*>(p.dqkv + (tok0 + qw0 + r0 + rl) * p.ld_dqkv + h * DH + 8 * piece) = u32x4{0, 0, 0, 0};
     return;
   }
   const int q_last = (q0 + BQ < n ? q0 + BQ : n) - 1;
-  const KeyBlocks kbs(q0, q_last, p.window, p.sinks);
+  const KeyBlocks kbs(q0, q_last, window, sinks);
 
   const typename HT::Offsets fo = HT::offsets(lane);
   auto rows_desc = [&](const bf16_t* base, long ld, int r0, int rows, long col) {
@@ -412,7 +456,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     }
   };
   const bool qlive = query < n;
-  const float lse_q = qlive ? p.lse[((long)b * p.H + h) * p.S + query] : 0.f;
+  const float lse_q = qlive ? p.lse[stat0 + query] : 0.f;
 
   f32x16 dqt[DT];
 #pragma unroll
@@ -450,7 +494,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     for (int i = 0; i < 8; i++) dl_q += (float)o[i] * (float)dof[s][i];
   }
   dl_q += xor32(dl_q);
-  if (qlive && g == 0 && wk == 0) p.delta[((long)b * p.H + h) * p.S + query] = dl_q;
+  if (qlive && g == 0 && wk == 0) p.delta[stat0 + query] = dl_q;
   __syncthreads();                   // the second slot is free again
   for (int j = 0; j < nblk; j++) {
     wait_vmem<0>();
@@ -459,12 +503,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     const int kv0 = kbs.key0(j);
     lds_u8* const kimg = lds + (j & 1) * SLOT;
     lds_u8* const vimg = kimg + IMG;
-    const int hi = query - kv0 - 4 * g, lo = hi - p.window, sk = p.sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
+    const int hi = query - kv0 - 4 * g, lo = hi - window, sk = sinks - kv0 - 4 * g;      // seen: <= hi, and > lo or < sk
 #pragma unroll 1
     for (int kt = SPLIT == 2 ? wk : 0; kt < (SPLIT == 2 ? wk + 1 : 2); kt++) {
       const int t0 = kv0 + 32 * kt;  // (uniform over the wave) tiles that none of its queries sees a key of
-      if (t0 > qw0 + 31 || (t0 >= p.sinks && t0 + 32 <= qw0 + 1 - p.window)) continue;
-      const bool edge = t0 + 31 > qw0 || (t0 < qw0 + 32 - p.window && t0 + 32 > p.sinks);
+      if (t0 > qw0 + 31 || (t0 >= sinks && t0 + 32 <= qw0 + 1 - window)) continue;
+      const bool edge = t0 + 31 > qw0 || (t0 < qw0 + 32 - window && t0 + 32 > sinks);
       f32x16 st, dp;
 #pragma unroll
       for (int e = 0; e < 16; e++) { st[e] = 0.f; dp[e] = 0.f; }
@@ -542,7 +586,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += RPI) {
     const int qrow = qw0 + r0 + rl;
-    if (qrow < p.S)
+    if (qrow < S)
       *reinterpret_cast<u32x4*>(p.dqkv + (tok0 + qrow) * p.ld_dqkv + h * DH + 8 * piece) =
           *reinterpret_cast<const LDS_AS u32x4*>(erow + (r0 + rl) * EROW + 16 * piece);
   }
@@ -567,6 +611,7 @@ struct WinKvParams {
   const float* lse;
   const float* delta;
   const int* lengths;
+  Packed packed;
   bf16_t* dqkv; long ld_dqkv;
   float* partial;                      // [B KV][sum of parts over the key blocks that are cut][2][KEYS][DH]
   int B, H, KV, G, S, window, sinks;
@@ -582,7 +627,7 @@ template <typename F, int... I> __device__ __forceinline__ void each(F f, std::i
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-template <int DH, int KEYS>
+template <int DH, int KEYS, bool PACKED>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 4 : 2))) void window_bwd_kv_kernel(WinKvParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BQ = 64;
@@ -603,20 +648,26 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int right = wave8 >> 2, wave = wave8 & 3;             // role
   const int kblk = KB == 4 ? wave : wave % KB, tq_left = KB == 4 ? 0 : wave / KB;      // a left wave's 32 keys of the block, and its tile of an iteration
-  const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
-  const int y = (int)blockIdx.y;
-  const bool sink_block = y < p.parts.sink_blocks * p.parts.sink_parts;
+  const int b = PACKED ? 0 : (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
+  const int y = PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y;
+  const bool sink_block = !PACKED && y < p.parts.sink_blocks * p.parts.sink_parts;
   const int np = sink_block ? p.parts.sink_parts : p.parts.other_parts;
-  const int yy = sink_block ? y : y - p.parts.sink_blocks * p.parts.sink_parts;
-  const int kb = yy / np + (sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
+  const int yy = sink_block ? y : y - (PACKED ? 0 : p.parts.sink_blocks * p.parts.sink_parts);
+  const int number = yy / np + (PACKED || sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
+  SeqOf seq{(long)b * p.S, 0, p.S, number};
+  if constexpr (PACKED) seq = SeqOf::packed<KEYS>(p.packed, number);
+  const int kb = seq.block, S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int kv0 = kb * KEYS, kw0 = kv0 + 32 * kblk, key = kw0 + kl;
-  const long tok0 = (long)b * p.S;
-  const int n = seq_end(p.lengths, b, p.S);
+  const long tok0 = seq.tok0;
+  const int n = PACKED ? seq.n : seq_end(p.lengths, b, p.S);
+  if (PACKED && kv0 >= S) return;                             // (uniform) a number that no block has
+  // lse and delta of query head h's rows of the sequence
+  auto stat0 = [&](int h) { return PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S; };
   const typename HT::Offsets fo = HT::offsets(lane);
   // steps of 64 queries that see the block, for each of the G query heads; this part's share of the G * nst pairs
   const int step0 = kv0 / BQ, nq = (n + BQ - 1) / BQ;
   int step1 = nq;
-  if (kv0 >= p.sinks && (long)kv0 + KEYS + p.window - 2 < n) step1 = (kv0 + KEYS + p.window - 2) / BQ + 1;
+  if (kv0 >= sinks && (long)kv0 + KEYS + window - 2 < n) step1 = (kv0 + KEYS + window - 2) / BQ + 1;
   const int nst = step1 > step0 ? step1 - step0 : 0;
   const int total = p.G * nst, share = (total + np - 1) / np;
   const int i0 = part * share < total ? part * share : total, i1 = i0 + share < total ? i0 + share : total;
@@ -628,8 +679,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
   lds_u8* const kvimg = lds + 2 * SLOT;
   static_assert(2 * KVIMG <= SLOT + 2 * HAND, "K and V images must fit in the third slot plus the hand-over area");
   // 32 x 32 tiles of queries from q and keys from k of which no pair is seen; and of which every pair is
-  auto unseen = [&](int q, int k) { return q + 31 < k || (q - (k + 31) >= p.window && k >= p.sinks); };
-  auto whole = [&](int q, int k) { return q >= k + 31 && (q + 31 - k < p.window || k + 32 <= p.sinks); };
+  auto unseen = [&](int q, int k) { return q + 31 < k || (q - (k + 31) >= window && k >= sinks); };
+  auto whole = [&](int q, int k) { return q >= k + 31 && (q + 31 - k < window || k + 32 <= sinks); };
 
   if (!right) {
     // ------------------------------------------------------------------ left: S, dP, P, dS
@@ -650,14 +701,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
     int sl_i = i0, sl_h = hq0, sl_st = sq0;
     auto fetch_stats = [&] {
       const int q = sl_st * BQ + sq;
-      const long at = ((long)b * p.H + hk * p.G + sl_h) * p.S + q;
+      const long at = stat0(hk * p.G + sl_h) + q;
       next_ls = next_dl = 0.f;                                // (rows past the end: zeros, which with zero rows of Q and dO add nothing)
       if (sl_i < i1 && q < n) { next_ls = p.lse[at]; next_dl = p.delta[at]; }
       sl_i++;
       if (++sl_st == step1) { sl_st = step0; sl_h++; }
     };
     if constexpr (OWN) fetch_stats();
-    const int past = key >= p.sinks ? key + p.window : 0x7fffffff;      // the first query past the lane's key's window
+    const int past = key >= sinks ? key + window : 0x7fffffff;      // the first query past the lane's key's window
     for (int it = 0; it <= nt; it++) {
       const int tile = TPI * it + tq_left, qt0 = st_at * BQ + 32 * (tile & 1);
       lds_u8* const out = my_hand + (it & 1) * HAND;
@@ -753,7 +804,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
     if constexpr (!OWN) {
       // row statistics: wave 0 fetches lse[0..63], wave 1 delta[0..63]; waves 2 and 3 issue the same instruction out of range (nothing
       // moves) to keep the count uniform.  (Rows past the end: zeros, as above.)
-      const u32x4 ds = make_desc(((wave & 1) == 0 ? p.lse : p.delta) + ((long)b * p.H + h) * p.S + q0, (uint32_t)(left * 4));
+      const u32x4 ds = make_desc(((wave & 1) == 0 ? p.lse : p.delta) + stat0(h) + q0, (uint32_t)(left * 4));
       dma4(slot + 2 * IMG + wave * 256, ds, wave < 2 && lane < left ? (unsigned)(lane * 4) : kOob);
     }
     is_i++;
@@ -850,7 +901,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
 
   if (np > 1) {
     // a part of the sums, dK unscaled: [2][KEYS][DH] fp32, 16 bytes per lane
-    const long idx = (long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, part);
+    const long idx = PACKED ? ((long)hk * packed_blocks(p.packed, KEYS) + number) * np + part : (long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, part);
     float* const base = p.partial + idx * 2 * KEYS * DH;
     if (has_cols) {
 #pragma unroll
@@ -891,7 +942,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
     for (int r0 = 0; r0 < KEYS / 4; r0 += RPI) {
       const int row = KEYS / 4 * wave + r0 + rl;              // this wave's quarter of the key rows
       const int krow = kv0 + row;
-      if (krow < p.S) {
+      if (krow < S) {
         bf16_t* const out = p.dqkv + (tok0 + krow) * p.ld_dqkv + (long)(p.H + hk) * DH + 8 * piece;
         *reinterpret_cast<u32x4*>(out) = *reinterpret_cast<const LDS_AS u32x4*>(edk + row * EROW + 16 * piece);
         *reinterpret_cast<u32x4*>(out + (long)p.KV * DH) = *reinterpret_cast<const LDS_AS u32x4*>(edv + row * EROW + 16 * piece);
@@ -902,16 +953,22 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
 
 // dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 8 or 16 key rows of one of them; a thread has 8
 // columns of one row of dK or dV.  Bound by the latency of the parts: 38 of them 13.4 us one at a time, 7.6 eight at a time.
-template <int DH, int KEYS>
+template <int DH, int KEYS, bool PACKED>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   constexpr int LPR = DH / 8, ROWS = 256 / (2 * LPR);
-  const int per = KEYS / ROWS, cut = (int)blockIdx.y / per;
-  const int kb = p.parts.sink_parts > 1 ? cut : cut + p.parts.sink_blocks;       // (blocks that are cut: the sinks', the others', or all)
-  const int b = (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
+  const int per = KEYS / ROWS, cut = (PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) / per;
+  const int number = !PACKED && p.parts.sink_parts == 1 ? cut + p.parts.sink_blocks : cut;       // (blocks that are cut: the sinks', the others', or all)
+  const int b = PACKED ? 0 : (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
+  SeqOf seq{(long)b * p.S, 0, p.S, number};
+  if constexpr (PACKED) seq = SeqOf::packed<KEYS>(p.packed, number);
+  const int kb = seq.block;
   const int which = (int)threadIdx.x / (ROWS * LPR), t = (int)threadIdx.x % (ROWS * LPR);
-  const int row = ((int)blockIdx.y % per) * ROWS + t / LPR, col = 8 * (t % LPR);
-  const int np = kb < p.parts.sink_blocks ? p.parts.sink_parts : p.parts.other_parts;
-  const float* src = p.partial + ((long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, 0)) * 2 * KEYS * DH + (long)which * KEYS * DH + (long)row * DH + col;
+  const int row = ((PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) % per) * ROWS + t / LPR, col = 8 * (t % LPR);
+  const int np = !PACKED && kb < p.parts.sink_blocks ? p.parts.sink_parts : p.parts.other_parts;
+  const long first = PACKED ? ((long)hk * packed_blocks(p.packed, KEYS) + number) * np : (long)blockIdx.x * p.parts.partials() + p.parts.partial_of(kb, 0);
+  const int krow = kb * KEYS + row;
+  if (krow >= seq.S) return;
+  const float* src = p.partial + first * 2 * KEYS * DH + (long)which * KEYS * DH + (long)row * DH + col;
   constexpr long PART = 2L * KEYS * DH;
   constexpr int AT_ONCE = 8;                         // parts on their way together
   float v[8] = {};
@@ -930,11 +987,9 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   for (; i < np; i++)
 #pragma unroll
     for (int k = 0; k < 8; k++) v[k] += src[i * PART + k];
-  const int krow = kb * KEYS + row;
-  if (krow >= p.S) return;
 #pragma unroll
   for (int k = 0; k < 8; k++) v[k] *= which ? 1.f : p.scale;
-  Vec<bf16_t>::store(p.dqkv + ((long)b * p.S + krow) * p.ld_dqkv + (long)(p.H + which * p.KV + hk) * DH + col, v);
+  Vec<bf16_t>::store(p.dqkv + (seq.tok0 + krow) * p.ld_dqkv + (long)(p.H + which * p.KV + hk) * DH + col, v);
 }
 
 // ------------------------------------------------------------------------------------------ one new token per sequence
@@ -1167,13 +1222,14 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <int DH, bool AHEAD, int SPLIT>
+template <int DH, bool AHEAD, int SPLIT, bool PACKED = false>
 static hipError_t launch_fwd(const WinParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
-  auto kern = window_fwd_kernel<DH, AHEAD, SPLIT>;
+  auto kern = window_fwd_kernel<DH, AHEAD, SPLIT, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128)), dim3(256), smem, s, p);
+  const dim3 grid = PACKED ? dim3((unsigned)(p.H * packed_blocks(p.packed, 128 / SPLIT))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
 
@@ -1195,26 +1251,34 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
   return w.seq <= 256 || w.window <= 512 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<128, true, 1>(p, s);
 }
 
-template <int DH, int SPLIT>
+template <int DH, int SPLIT, bool PACKED = false>
 static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
-  auto kern = window_bwd_dq_kernel<DH, SPLIT>;
+  auto kern = window_bwd_dq_kernel<DH, SPLIT, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128)), dim3(256), smem, s, p);
+  const dim3 grid = PACKED ? dim3((unsigned)(p.H * packed_blocks(p.packed, 128 / SPLIT))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
 
-template <int DH, int KEYS>
+template <int DH, int KEYS, bool PACKED = false>
 static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
   constexpr size_t smem = 3 * (2 * 64 * DH * 2 + (DH == 64 ? 0 : 1024)) + 2 * 4 * 4096;       // three slots, two hand-over buffers
-  auto kern = window_bwd_kv_kernel<DH, KEYS>;
+  auto kern = window_bwd_kv_kernel<DH, KEYS, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  constexpr int per = KEYS / (256 / (2 * (DH / 8)));
+  if constexpr (PACKED) {
+    const long blocks = p.KV * packed_blocks(p.packed, KEYS);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.parts.other_parts)), dim3(512), smem, s, p);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || p.parts.other_parts == 1) return e;
+    hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, true>), dim3((unsigned)(blocks * per)), dim3(256), 0, s, p);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.KV * p.B), (unsigned)p.parts.workgroups()), dim3(512), smem, s, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.parts.cut_blocks()) return e;
-  constexpr int per = KEYS / (256 / (2 * (DH / 8)));
-  hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, false>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -1275,6 +1339,61 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
   p.scale = q.scale; p.scale_log2e = q.scale_log2e;
   if (w.head_dim == 64) return launch_kv<64, 64>(p, s);
   return p.parts.keys == 64 ? launch_kv<128, 64>(p, s) : launch_kv<128, 128>(p, s);
+}
+
+// ---- packed sequences: the same kernels, by rules on the mean length, since the lengths are on the device
+static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, w.rows}; }
+
+hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s) {
+  WinParams p{};
+  p.qkv = (const bf16_t*)qkv; p.ld_qkv = ld_qkv; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.packed = packed_of(w);
+  p.B = 1; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.rows;
+  p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
+  const long blocks = w.rows / 128 + w.seqs, groups = w.heads * blocks;
+  const bool few = groups <= (w.head_dim == 64 ? 512 : 256);
+  if (few) return w.head_dim == 128 ? launch_fwd<128, false, 2, true>(p, s) : launch_fwd<64, false, 2, true>(p, s);
+  if (w.head_dim == 64) return launch_fwd<64, false, 1, true>(p, s);
+  return w.rows / (w.seqs > 0 ? w.seqs : 1) <= 256 ? launch_fwd<128, false, 1, true>(p, s) : launch_fwd<128, true, 1, true>(p, s);
+}
+
+// Keys to a block and parts of a block's list of (query head, query step) pairs.
+static WindowParts packed_parts(const PackedShape& w) {
+  WindowParts r{};
+  const int seqs = w.seqs > 0 ? w.seqs : 1, G = w.heads / w.kv_heads, mean = (w.rows + seqs - 1) / seqs;
+  r.keys = w.head_dim == 64 || (long)w.kv_heads * (w.rows / 128 + seqs) <= 256 || mean <= 768 ? 64 : 128;
+  const long blocks = (long)w.kv_heads * (w.rows / r.keys + seqs), pairs = (long)G * ((mean + 63) / 64);
+  long parts = (256 + blocks - 1) / blocks;
+  parts = parts < (pairs + 3) / 4 ? parts : (pairs + 3) / 4;
+  r.other_parts = (int)parts;
+  return r;
+}
+
+size_t packed_attention_p1_partial_bytes(const PackedShape& w) {
+  const WindowParts r = packed_parts(w);
+  return r.other_parts == 1 ? 0 : (size_t)w.kv_heads * packed_blocks(packed_of(w), r.keys) * r.other_parts * 2 * r.keys * w.head_dim * sizeof(float);
+}
+
+hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qkv, const void* out, const void* d_out, long ld_out, const float* lse,
+                               void* dqkv, long ld_dqkv, float* delta, float* partial, hipStream_t s) {
+  WinDqParams q{};
+  q.qkv = (const bf16_t*)qkv; q.ld_qkv = ld_qkv; q.dout = (const bf16_t*)d_out; q.out = (const bf16_t*)out; q.ld_do = ld_out;
+  q.lse = lse; q.delta = delta; q.packed = packed_of(w); q.dqkv = (bf16_t*)dqkv; q.ld_dqkv = ld_dqkv;
+  q.B = 1; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.rows;
+  q.scale = 1.f / sqrtf((float)w.head_dim);
+  q.scale_log2e = 1.4426950408889634f * q.scale;
+  const long groups = (long)w.heads * (w.rows / 128 + w.seqs);
+  hipError_t e;
+  if (groups <= (w.head_dim == 64 ? 512 : 256)) e = w.head_dim == 128 ? launch_dq<128, 2, true>(q, s) : launch_dq<64, 2, true>(q, s);
+  else e = w.head_dim == 128 ? launch_dq<128, 1, true>(q, s) : launch_dq<64, 1, true>(q, s);
+  if (e != hipSuccess) return e;
+  WinKvParams p{};
+  p.qkv = q.qkv; p.ld_qkv = ld_qkv; p.dout = q.dout; p.ld_do = ld_out; p.lse = lse; p.delta = delta; p.packed = q.packed;
+  p.dqkv = q.dqkv; p.ld_dqkv = ld_dqkv; p.partial = partial;
+  p.B = 1; p.H = q.H; p.KV = q.KV; p.G = q.G; p.S = q.S;
+  p.parts = packed_parts(w);
+  p.scale = q.scale; p.scale_log2e = q.scale_log2e;
+  if (w.head_dim == 64) return launch_kv<64, 64, true>(p, s);
+  return p.parts.keys == 64 ? launch_kv<128, 64, true>(p, s) : launch_kv<128, 128, true>(p, s);
 }
 
 // Shares of a head's keys, at most: as many as make the rounds of workgroups (one per compute unit at head_dim 128, two at 64) short by this model, whose

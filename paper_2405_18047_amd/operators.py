@@ -1,5 +1,6 @@
 """Binding of the operators for long contexts, the last stage and serving: sliding-window attention with sinks, rotary
-positions, log probabilities of tokens, the norm of all gradients with clipping.
+positions, log probabilities of tokens, the norm of all gradients with clipping; and of those of a stage that is trained on packed
+documents: norms of query and key heads, attention over packed sequences, a stash in 8 bits.
 
 As in binding.py: argument marshalling only, on torch's current stream; outputs and workspaces are allocated where the caller
 passes none.  Index tensors (lengths, positions, targets) are int32.  The checks here are those that the C entry points cannot
@@ -18,6 +19,7 @@ __all__ = [
     "TBP_ROTARY_HALF", "TBP_ROTARY_INTERLEAVED", "TBP_ROTARY_PLAIN", "TBP_ROTARY_LINEAR", "TBP_ROTARY_BASE", "TBP_ROTARY_RAMP",
     "tbp_rotary_scale", "tbp_rotary_table", "tbp_rotary", "tbp_rotary_append", "tbp_window_attention_fwd", "tbp_window_attention_p1",
     "tbp_window_decode_workspace", "tbp_window_decode", "tbp_logprobs", "tbp_logprobs_p1", "tbp_logprobs_step", "GradList",
+    "tbp_qk_norm", "tbp_qk_norm_p1", "tbp_qk_norm_append", "tbp_packed_attention_fwd", "tbp_packed_attention_p1", "Stash8", "tbp_stash8_dw",
 ]
 
 TBP_ROTARY_HALF, TBP_ROTARY_INTERLEAVED = 0, 1
@@ -340,3 +342,195 @@ class GradList:
         _check(lib().tbp_grad_clip(self._dt, self._odt, self._n, self._src, self._dst, self._counts, _vector(sumsq, 1, torch.float64, "sumsq"), max_norm,
                                    _vector(norm, 1, _F32, "norm"), self._ws.data_ptr(), _stream_of(self._at_device, sumsq, given)))
         return norm
+
+
+# ---- norms of query and key heads with rotary positions ------------------------------------------------------------------------
+def _norm_place(x, rows, table, positions, seq):
+    """(n_pos, rot_dim, the table's address, seq) of a call on `rows` rows; no table: no rotation."""
+    if table is None:
+        if positions is not None:
+            raise ValueError("positions without a table")
+        return 0, 0, None, 1
+    n_pos, rot_dim = _table(table)
+    if positions is not None:
+        seq = 1
+    elif seq is None:
+        seq = max(rows, 1)
+        if rows > n_pos:
+            raise ValueError(f"{rows} rows and a table of {n_pos} positions: positions or seq must be given")
+    elif seq < 1:
+        raise ValueError(f"seq must be at least 1, not {seq}")
+    return n_pos, rot_dim, table.data_ptr(), seq
+
+
+def tbp_qk_norm(qk, gq, gk, n_heads, n_kv_heads, head_dim, eps, table=None, positions=None, seq=None, layout=TBP_ROTARY_HALF, out=None):
+    """The first (n_heads + n_kv_heads) head_dim columns of qk [rows, ld] (q | k), every head normed, times gq or gk [head_dim], and rotated (no table: not
+    rotated).  positions, seq as for tbp_rotary.  out: new [rows, (n_heads + n_kv_heads) head_dim], or the tensor to write to (qk itself: in place)."""
+    rows, dt = qk.shape[0], qk.dtype
+    n_pos, rot_dim, at, seq = _norm_place(qk, rows, table, positions, seq)
+    ld_out = (n_heads + n_kv_heads) * head_dim
+    ld_x = _matrix(qk, dt, "qk", rows, ld_out)
+    given = out
+    if out is None:
+        out = qk.new_empty((rows, ld_out))
+    else:
+        ld_out = _matrix(out, dt, "out", rows, ld_out)
+    _check(lib().tbp_qk_norm(_dt(qk), rows, n_heads, n_kv_heads, head_dim, eps, _vector(gq, head_dim, dt, "gq"), _vector(gk, head_dim, dt, "gk"), rot_dim, layout,
+                             at, n_pos, _vector(positions, rows, _I32, "positions"), seq, qk.data_ptr(), ld_x, out.data_ptr(), ld_out,
+                             _stream_of(qk.get_device(), gq, gk, table, positions, given)))
+    return out
+
+
+def tbp_qk_norm_p1(d_out, qk, gq, gk, n_heads, n_kv_heads, head_dim, eps, table=None, positions=None, seq=None, layout=TBP_ROTARY_HALF, out=None, partials=None):
+    """-> (dqk [rows, (n_heads + n_kv_heads) head_dim], partial rows [tbp_qk_norm_partial_rows, 2 head_dim] fp32 of the gains' gradient, for
+    tbp_gain_partials_sum).  qk: the forward's input; out: the tensor to write to (d_out itself: in place); partials: rows to write them to."""
+    rows, dt = qk.shape[0], qk.dtype
+    n_pos, rot_dim, at, seq = _norm_place(qk, rows, table, positions, seq)
+    ld_dx = (n_heads + n_kv_heads) * head_dim
+    ld_x, ld_dy = _matrix(qk, dt, "qk", rows, ld_dx), _matrix(d_out, dt, "d_out", rows, ld_dx)
+    given = out, partials
+    if out is None:
+        out = qk.new_empty((rows, ld_dx))
+    else:
+        ld_dx = _matrix(out, dt, "out", rows, ld_dx)
+    L = lib()
+    n = L.tbp_qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim)
+    if partials is None:
+        partials = qk.new_empty((n, 2 * head_dim), dtype=_F32)
+    else:
+        _vector(partials, n * 2 * head_dim, _F32, "partials")
+    _check(L.tbp_qk_norm_p1(_dt(qk), rows, n_heads, n_kv_heads, head_dim, eps, _vector(gq, head_dim, dt, "gq"), _vector(gk, head_dim, dt, "gk"), rot_dim, layout,
+                            at, n_pos, _vector(positions, rows, _I32, "positions"), seq, d_out.data_ptr(), ld_dy, qk.data_ptr(), ld_x, out.data_ptr(), ld_dx,
+                            partials.data_ptr(), _stream_of(qk.get_device(), d_out, gq, gk, table, positions, *given)))
+    return out, partials
+
+
+def tbp_qk_norm_append(qkv, gq, gk, n_heads, n_kv_heads, head_dim, eps, table, lengths, cache_k, cache_v, sinks=0, layout=TBP_ROTARY_HALF, q_out=None):
+    """tbp_rotary_append with q and k normed first (table None: not rotated); -> q [batch*n_new, n_heads*head_dim]."""
+    n_pos, rot_dim = (0, 0) if table is None else _table(table)
+    batch, rows, dt = lengths.shape[0], qkv.shape[0], qkv.dtype
+    n_new = 0 if batch == 0 else rows // batch
+    if n_new * batch != rows:
+        raise ValueError(f"{rows} rows are no whole number of tokens for {batch} sequences")
+    capacity, ld_cache = _caches(cache_k, cache_v, dt, batch, n_kv_heads * head_dim)
+    ld_q = n_heads * head_dim
+    ld_qkv = _matrix(qkv, dt, "qkv", rows, ld_q + 2 * n_kv_heads * head_dim)
+    given = q_out
+    if q_out is None:
+        q_out = qkv.new_empty((rows, ld_q))
+    else:
+        ld_q = _matrix(q_out, dt, "q_out", rows, ld_q)
+    _check(lib().tbp_qk_norm_append(_dt(qkv), batch, n_new, n_heads, n_kv_heads, head_dim, eps, _vector(gq, head_dim, dt, "gq"), _vector(gk, head_dim, dt, "gk"),
+                                    rot_dim, layout, None if table is None else table.data_ptr(), n_pos, _vector(lengths, batch, _I32, "lengths"), qkv.data_ptr(),
+                                    ld_qkv, q_out.data_ptr(), ld_q, cache_k.data_ptr(), cache_v.data_ptr(), ld_cache, capacity, sinks,
+                                    _stream_of(qkv.get_device(), gq, gk, table, lengths, cache_k, cache_v, given)))
+    return q_out
+
+
+# ---- causal attention over packed sequences ------------------------------------------------------------------------------------
+def _starts(starts):
+    if starts.dim() != 1 or starts.shape[0] < 1:
+        raise TypeError("starts must be a vector of n_seqs + 1 entries")
+    return _vector(starts, starts.shape[0], _I32, "starts"), starts.shape[0] - 1
+
+
+def tbp_packed_attention_fwd(qkv, starts, n_heads, n_kv_heads, head_dim, out=None, lse=None):
+    """qkv [rows, (n_heads + 2 n_kv_heads) head_dim] (q | k | v, rotated), sequence b in rows starts[b] .. starts[b + 1] - 1 -> (out [rows, n_heads*head_dim],
+    lse2 [heads, rows]); rows behind the last sequence: zeros and -infinity."""
+    rows, dt, ld_out = qkv.shape[0], qkv.dtype, n_heads * head_dim
+    at, n = _starts(starts)
+    ld_qkv = _matrix(qkv, dt, "qkv", rows, (n_heads + 2 * n_kv_heads) * head_dim)
+    given = out, lse
+    if out is None:
+        out = qkv.new_empty((rows, ld_out))
+    else:
+        ld_out = _matrix(out, dt, "out", rows, ld_out)
+    if lse is None:
+        lse = qkv.new_empty((n_heads, rows), dtype=_F32)
+    else:
+        _vector(lse, n_heads * rows, _F32, "lse")
+    _check(lib().tbp_packed_attention_fwd(_dt(qkv), n, rows, n_heads, n_kv_heads, head_dim, at, qkv.data_ptr(), ld_qkv, out.data_ptr(), ld_out, lse.data_ptr(),
+                                          _stream_of(qkv.get_device(), starts, *given)))
+    return out, lse
+
+
+def tbp_packed_attention_p1(qkv, out, d_out, lse, starts, n_heads, n_kv_heads, head_dim, dqkv=None, scratch=None):
+    """-> dqkv [rows, (n_heads + 2 n_kv_heads) head_dim] (dq | dk | dv, not rotated back)."""
+    rows, dt, ld_dqkv = qkv.shape[0], qkv.dtype, (n_heads + 2 * n_kv_heads) * head_dim
+    at_starts, n = _starts(starts)
+    ld_qkv, ld_out = _matrix(qkv, dt, "qkv", rows, ld_dqkv), _matrix(out, dt, "out", rows, n_heads * head_dim)
+    if d_out.shape != out.shape or _matrix(d_out, dt, "d_out", rows, n_heads * head_dim) != ld_out:
+        raise TypeError("d_out must have out's shape and leading dimension")
+    given = dqkv, scratch
+    if dqkv is None:
+        dqkv = qkv.new_empty((rows, ld_dqkv))
+    else:
+        ld_dqkv = _matrix(dqkv, dt, "dqkv", rows, ld_dqkv)
+    L = lib()
+    need = L.tbp_packed_attention_p1_scratch_bytes(n, rows, n_heads, n_kv_heads, head_dim)
+    if scratch is None:
+        scratch = qkv.new_empty(need, dtype=torch.uint8)
+    at, nbytes = _memory(scratch, "scratch")
+    if nbytes < need:
+        raise ValueError(f"scratch must have {need} bytes, not {nbytes}")
+    _check(L.tbp_packed_attention_p1(_dt(qkv), n, rows, n_heads, n_kv_heads, head_dim, at_starts, qkv.data_ptr(), ld_qkv, out.data_ptr(), d_out.data_ptr(), ld_out,
+                                     _vector(lse, n_heads * rows, _F32, "lse"), dqkv.data_ptr(), ld_dqkv, at,
+                                     _stream_of(qkv.get_device(), starts, out, d_out, lse, *given)))
+    return dqkv
+
+
+# ---- a stash in 8 bits -----------------------------------------------------------------------------------------------------------
+class Stash8:
+    """`slots` micro-batches [tokens, cols] of one tensor, held in 8 bits with a power of two as scale for every 1024 tokens of a column: a linear layer's inputs or
+    output derivatives between backward-p1 and backward-p2 (tbp_stash8_dw), or what a functional operation needs again (get).  A slot that nothing
+    was put into holds zeros.  dtype: of the tensors that get returns."""
+
+    def __init__(self, tokens, cols, slots=1, dtype=torch.bfloat16, device="cuda"):
+        nbytes = lib().tbp_stash8_bytes(slots, tokens, cols)
+        if nbytes == 0:
+            raise ValueError(f"no stash of {slots} slots of {tokens} tokens of {cols} columns: " + lib().tbp_last_error().decode())
+        self.tokens, self.cols, self.slots, self.dtype = tokens, cols, slots, dtype
+        self.memory = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+
+    def put(self, slot, x):
+        """x [tokens, cols], in the storage type or fp32, into a slot."""
+        if x.shape != (self.tokens, self.cols):
+            raise TypeError(f"x must be [{self.tokens}, {self.cols}], not {list(x.shape)}")
+        _check(lib().tbp_stash8_put(_dt(x), self.slots, self.tokens, self.cols, slot, x.data_ptr(), _matrix(x, x.dtype, "x", self.tokens, self.cols),
+                                    self.memory.data_ptr(), _stream_of(x.get_device(), self.memory)))
+
+    def get(self, slot, out=None):
+        """-> what the slot holds, [tokens, cols] (out: the tensor to write to)."""
+        ld = self.cols
+        given = out
+        if out is None:
+            out = self.memory.new_empty((self.tokens, self.cols), dtype=self.dtype)
+        else:
+            ld = _matrix(out, out.dtype, "out", self.tokens, self.cols)
+        _check(lib().tbp_stash8_get(_dt(out), self.slots, self.tokens, self.cols, slot, self.memory.data_ptr(), out.data_ptr(), ld,
+                                    _stream_of(self.memory.get_device(), given)))
+        return out
+
+
+def tbp_stash8_dw(x, dy, first=0, n=None, dw=None, accumulate=False, workspace=None):
+    """X^T dY over the slots first .. first + n - 1 (None: to the last one) of two stashes of the same slots and tokens -> dw [x.cols, dy.cols] fp32
+    (accumulate: added to the given dw)."""
+    if (x.slots, x.tokens) != (dy.slots, dy.tokens):
+        raise ValueError(f"stashes of {x.slots} slots of {x.tokens} tokens and of {dy.slots} of {dy.tokens}")
+    n = x.slots - first if n is None else n
+    ld = dy.cols
+    given = dw, workspace
+    if dw is None:
+        if accumulate:
+            raise ValueError("accumulate needs a dw to add to")
+        dw = x.memory.new_empty((x.cols, dy.cols), dtype=_F32)
+    else:
+        ld = _matrix(dw, _F32, "dw", x.cols, dy.cols)
+    L = lib()
+    need = L.tbp_stash8_dw_workspace_bytes(x.tokens, x.cols, dy.cols, n)
+    if workspace is None and need:
+        workspace = x.memory.new_empty(need)
+    at, nbytes = _memory(workspace, "workspace")
+    _check(L.tbp_stash8_dw(x.slots, x.tokens, x.cols, dy.cols, first, n, x.memory.data_ptr(), dy.memory.data_ptr(), dw.data_ptr(), ld, 1 if accumulate else 0,
+                           at, nbytes, _stream_of(x.memory.get_device(), dy.memory, *given)))
+    return dw

@@ -1,0 +1,583 @@
+"""GPU parity of the operators around packed documents against the oracle in 64 bits.
+
+Tolerances, from the arithmetic:
+  norms   a value rounded once is off by half a step (bf16 2^-8, fp32 2^-24 of it); what fp32 loses before is below 2^-20 of the head's largest term: 512 squares
+          in a tree of at most 8 + 6 levels and a serial part of 16, two roundings of the reciprocal root, the table's, and five products and sums.
+          Derivatives 2^-18 of their largest term (the same sums over three factors).  The gains' gradient: N terms of that accuracy added in chains of
+          at most 64 a lane, then in trees: 2^-16 of the terms' magnitudes.
+  packed  as for sliding-window attention: per row of a head (tests/test_gpu_operators.py, _row_errors), lse 1e-5 relative to its size + 1.
+  stash   what is held, exactly; the weight gradient's blocks are exact, and b of them added in fp32 lose at most b 2^-24 of their magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2405_18047_amd as tbp
+import seeded_inputs as si
+from gpu_util import DEV, to_dev, to_np
+from oracle import operators as ops
+from oracle import packed as ref
+from test_gpu_operators import _row_errors
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def _rnd(seed, name, shape, dtype, scale=1.0):
+    return si.store_round(scale * si.standard_normal(seed, name, shape), dtype)
+
+
+def _say(msg):
+    print(msg, flush=True)
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+# --------------------------------------------------------------------------------------- norms of query and key heads
+NORM_CASES = [  # rows, H, KV, dh, rot, layout, dtype, positions
+    (1, 1, 1, 64, 64, 0, "bf16", False), (1, 1, 0, 2, 2, 1, "f32", False), (3, 0, 2, 64, 32, 0, "bf16", True), (5, 4, 2, 128, 128, 1, "bf16", True),
+    (33, 3, 1, 96, 96, 0, "bf16", False), (33, 3, 1, 96, 32, 1, "f32", True), (7, 2, 1, 6, 4, 0, "bf16", True), (17, 5, 5, 62, 30, 1, "bf16", True),
+    (9, 2, 2, 512, 512, 0, "f32", True), (9, 2, 2, 512, 100, 0, "bf16", False), (11, 3, 1, 510, 510, 1, "f32", True), (64, 6, 2, 80, 0, 0, "bf16", False),
+    (129, 8, 8, 256, 64, 0, "f32", False), (1001, 12, 4, 64, 64, 0, "bf16", True), (2050, 10, 2, 128, 64, 1, "bf16", True), (1500, 7, 3, 128, 128, 0, "f32", True),
+    (700, 32, 8, 128, 128, 0, "bf16", False),
+]
+
+
+def _norm_inputs(case, seed=5):
+    rows, H, KV, dh, rot, layout, dtype, given = case
+    w = (H + KV) * dh
+    x = _rnd(seed, "x", (rows, w), dtype) * si.store_round(np.exp(si.standard_normal(seed, "scale", (1, w))), dtype)
+    x = si.store_round(x, dtype)
+    x[rows // 2] = 0                                            # a row of zeros: only eps under the root
+    dy = _rnd(seed, "dy", (rows, w), dtype)
+    gq, gk = si.store_round(1 + 0.2 * si.standard_normal(seed, "gq", (dh,)), dtype), si.store_round(1 + 0.2 * si.standard_normal(seed, "gk", (dh,)), dtype)
+    n_pos = 50
+    pos = (np.arange(rows) * 37 + 11) % n_pos if given else np.arange(rows) % n_pos
+    table = tbp.tbp_rotary_table(n_pos, rot, 1e4, device=DEV) if rot else None
+    ang = pos[:, None] * 1e4 ** (-np.arange(rot // 2) * 2.0 / max(rot, 1))[None, :]
+    where = dict(table=table, layout=layout) | ({} if not rot else {"positions": _ints(pos)} if given else {"seq": n_pos})
+    return x, dy, gq, gk, ang, where
+
+
+def _heads_top(t, heads):
+    """The largest magnitude of every row's head, spread over the head."""
+    t = np.abs(t).reshape(len(t), heads, -1)
+    return np.broadcast_to(t.max(axis=2, keepdims=True), t.shape).reshape(len(t), -1)
+
+
+@pytest.mark.parametrize("ld", [0, 8, 3])
+@pytest.mark.parametrize("case", NORM_CASES, ids=str)
+def test_norms_match_oracle(case, ld):
+    rows, H, KV, dh, rot, layout, dtype, given = case
+    eps, w = 1e-3, (H + KV) * dh
+    _say(f"norm {case} ld +{ld}")
+    x, dy, gq, gk, ang, where = _norm_inputs(case)
+    y_ref = ref.qk_norm(x, gq, gk, H, KV, eps, ang, layout)
+    dx_ref, dg_ref = ref.qk_norm_p1(dy, x, gq, gk, H, KV, eps, ang, layout)
+
+    def dev(t):                                                  # in rows of w + ld columns; what lies beside must not matter, nor be touched
+        big = torch.full((rows, w + ld), 77.0, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device=DEV)
+        big[:, :w] = to_dev(t, dtype)
+        return big
+    xd, dd, gqd, gkd = dev(x), dev(dy), to_dev(gq, dtype), to_dev(gk, dtype)
+    heads = (gqd, gkd, H, KV, dh, eps)
+    out = torch.full_like(xd, 77.0)
+    tbp.tbp_qk_norm(xd, *heads, **where, out=out)
+    fresh = tbp.tbp_qk_norm(xd, *heads, **where)
+    dx = torch.full_like(xd, 77.0)
+    _, parts = tbp.tbp_qk_norm_p1(dd, xd, *heads, **where, out=dx)
+    dg = tbp.tbp_gain_partials_sum(parts)
+    # in place: the same bits
+    xi, di = xd.clone(), dd.clone()
+    tbp.tbp_qk_norm(xi, *heads, **where, out=xi)
+    _, parts2 = tbp.tbp_qk_norm_p1(di, xd, *heads, **where, out=di)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :w], fresh) and torch.equal(xi, out) and torch.equal(di, dx) and torch.equal(parts, parts2)
+    for t in (out, dx):
+        assert torch.all(t[:, w:] == 77.0)
+    got = to_np(out[:, :w])
+    assert np.all(np.abs(got - y_ref) <= HALF_STEP[dtype] * np.abs(y_ref) + 2.0 ** -20 * _heads_top(y_ref, H + KV))
+    h3 = lambda t: t.reshape(rows, H + KV, dh)
+    r = 1 / np.sqrt((h3(x.astype(np.float64)) ** 2).mean(axis=2, keepdims=True) + eps)
+    dn = ref._turn(h3(dy.astype(np.float64)), ang, layout, True) * ref._gains(gq, gk, H, KV)
+    n = h3(x) * r
+    term = r * (np.abs(dn).max(axis=2, keepdims=True) + np.abs(n).max(axis=2, keepdims=True) * np.abs(dn * n).mean(axis=2, keepdims=True))
+    got = h3(to_np(dx[:, :w]))
+    assert np.all(np.abs(got - h3(dx_ref)) <= HALF_STEP[dtype] * np.abs(h3(dx_ref)) + 2.0 ** -18 * term)
+    each = np.abs(dn / ref._gains(gq, gk, H, KV) * n).sum(axis=0)
+    size = np.stack([each[:H].sum(axis=0), each[H:].sum(axis=0)])
+    assert parts.shape == (tbp.lib().tbp_qk_norm_partial_rows(rows, H, KV, dh), 2 * dh)
+    assert np.all(np.abs(to_np(dg).reshape(2, dh) - dg_ref) <= 2.0 ** -16 * size + 1e-30)
+
+
+def test_norms_of_misaligned_rows():
+    rows, H, KV, dh = 21, 3, 1, 64
+    x, dy, gq, gk, ang, where = _norm_inputs((rows, H, KV, dh, 64, 0, "bf16", True))
+    w = 4 * dh
+    xa, da = (torch.zeros(rows * w + 1, dtype=torch.bfloat16, device=DEV)[1:].view(rows, w) for _ in range(2))
+    g = torch.zeros(dh + 1, dtype=torch.bfloat16, device=DEV)
+    xa.copy_(to_dev(x, "bf16")), da.copy_(to_dev(dy, "bf16"))
+    g[1:] = to_dev(gq, "bf16")
+    heads = (g[1:], to_dev(gk, "bf16"), H, KV, dh, 1e-3)
+    good = (to_dev(gq, "bf16"), to_dev(gk, "bf16"), H, KV, dh, 1e-3)
+    want, got = tbp.tbp_qk_norm(to_dev(x, "bf16"), *good, **where), tbp.tbp_qk_norm(xa, *heads, **where)
+    wdx, _ = tbp.tbp_qk_norm_p1(to_dev(dy, "bf16"), to_dev(x, "bf16"), *good, **where)
+    gdx, _ = tbp.tbp_qk_norm_p1(da, xa, *heads, **where)
+    # (the sums are taken in another order: a step of bf16 where a value lies at the border)
+    for u, v in ((want, got), (wdx, gdx)):
+        u, v = to_np(u), to_np(v)
+        assert np.all(np.abs(u - v) <= 2.0 ** -7 * np.abs(u) + 2.0 ** -18 * _heads_top(u, H + KV))
+
+
+def test_norms_of_positions_outside_the_table():
+    H, KV, dh, rot = 2, 1, 64, 32
+    x = to_dev(_rnd(9, "x", (5, 192), "f32"), "f32")
+    g = torch.ones(dh, device=DEV)
+    table = tbp.tbp_rotary_table(8, rot, 1e4, device=DEV)
+    y = tbp.tbp_qk_norm(x, g, g, H, KV, dh, 1e-5, table, positions=_ints([0, 8, -1, 7, 2 ** 31 - 1])).view(5, 3, dh)
+    bad = torch.tensor([False, True, True, False, True], device=DEV)
+    assert torch.all(torch.isnan(y[bad][..., :rot])) and torch.all(torch.isfinite(y[bad][..., rot:])) and torch.all(torch.isfinite(y[~bad]))
+
+
+def test_a_norm_of_values_that_are_not_finite_stays_in_its_head():
+    H, KV, dh = 3, 1, 64
+    x = to_dev(_rnd(9, "x", (4, 256), "bf16"), "bf16")
+    dy = to_dev(_rnd(9, "dy", (4, 256), "bf16"), "bf16")
+    g = torch.ones(dh, dtype=torch.bfloat16, device=DEV)
+    clean, dclean = tbp.tbp_qk_norm(x, g, g, H, KV, dh, 1e-5), tbp.tbp_qk_norm_p1(dy, x, g, g, H, KV, dh, 1e-5)[0]
+    x[1, 70], x[2, 3] = NAN, INF
+    y, dx = tbp.tbp_qk_norm(x, g, g, H, KV, dh, 1e-5), tbp.tbp_qk_norm_p1(dy, x, g, g, H, KV, dh, 1e-5)[0]
+    hurt = torch.zeros((4, 4, dh), dtype=torch.bool, device=DEV)
+    hurt[1, 1], hurt[2, 0] = True, True
+    hurt = hurt.view(4, 256)
+    assert torch.equal(y[~hurt], clean[~hurt]) and torch.equal(dx[~hurt], dclean[~hurt])
+    assert torch.all(torch.isnan(y[1, 64:128])) and torch.all(torch.isnan(dx[1, 64:128]))
+
+
+APPEND_CASES = [  # batch, n_new, H, KV, dh, rot, layout, dtype, capacity, sinks, lengths
+    (1, 1, 1, 1, 64, 64, 0, "bf16", 3, 0, [1]), (3, 1, 4, 2, 128, 128, 0, "bf16", 9, 2, [1, 40, 0]), (2, 5, 2, 1, 96, 32, 1, "f32", 4, 1, [3, 17]),
+    (4, 3, 3, 3, 62, 30, 1, "bf16", 7, 0, [3, 2, 30, -5]), (2, 40, 8, 2, 64, 0, 0, "bf16", 16, 4, [40, 60]), (16, 1, 32, 8, 128, 128, 0, "bf16", 30, 4, list(range(20, 36))),
+    (3, 400, 8, 4, 128, 64, 0, "bf16", 500, 3, [400, 399, 450]),
+]
+
+
+@pytest.mark.parametrize("case", APPEND_CASES, ids=str)
+def test_norm_append_is_the_norm_and_the_cache_s_rule(case):
+    nb, n, H, KV, dh, rot, layout, dtype, capacity, sinks, lengths = case
+    _say(f"append {case}")
+    wq, wkv, eps = H * dh, KV * dh, 1e-5
+    qkv = to_dev(_rnd(3, "qkv", (nb * n, wq + 2 * wkv), dtype), dtype)
+    gq, gk = (to_dev(si.store_round(1 + 0.2 * si.standard_normal(3, k, (dh,)), dtype), dtype) for k in ("gq", "gk"))
+    table = tbp.tbp_rotary_table(512, rot, 1e4, device=DEV) if rot else None
+    ck, cv = (torch.full((nb, capacity, wkv), 77.0, dtype=qkv.dtype, device=DEV) for _ in range(2))
+    q = tbp.tbp_qk_norm_append(qkv, gq, gk, H, KV, dh, eps, table, _ints(lengths), ck, cv, sinks=sinks, layout=layout)
+    pos = np.concatenate([np.arange(m - n, m) for m in lengths])
+    there = torch.tensor(pos >= 0, device=DEV)
+    place = {"positions": _ints(np.maximum(pos, 0))} if rot else {}
+    y = tbp.tbp_qk_norm(qkv, gq, gk, H, KV, dh, eps, table, **place, layout=layout)
+    torch.cuda.synchronize()
+    same = dict(rtol=2.0 ** -7 if dtype == "bf16" else 2.0 ** -20, atol=2.0 ** -18)      # (four heads to a thread or one: the same sums, but which of them the compiler fuses)
+    assert torch.allclose(q[there].float(), y[there][:, :wq].float(), **same) and not q[~there].any()
+    wk, wv = (torch.full((nb, capacity, wkv), 77.0, dtype=qkv.dtype, device=DEV) for _ in range(2))
+    for r, p in enumerate(pos):
+        if p >= 0:
+            at = ops.cache_row(int(p), capacity, sinks)
+            wk[r // n, at], wv[r // n, at] = y[r, wq:], qkv[r, wq + wkv:]
+    assert torch.allclose(ck.float(), wk.float(), **same) and torch.equal(cv, wv)
+
+
+# ------------------------------------------------------------------------------------------------- packed sequences
+def _starts(lengths):
+    return [0] + list(np.cumsum(lengths))
+
+
+PACKED_CASES = [  # lengths, rows behind, H, KV, dh
+    ([1], 0, 1, 1, 64), ([], 5, 2, 1, 128), ([0, 0, 3, 0], 0, 4, 2, 128), ([1, 1, 1, 2], 1, 2, 2, 64), ([64, 63, 65], 0, 3, 1, 64), ([128, 127, 129, 1], 3, 4, 2, 128),
+    ([300], 0, 8, 2, 128), ([37, 500, 1, 0, 211], 130, 6, 2, 64), ([5] * 70 + [0] * 70 + [9] * 3, 2, 4, 4, 64), ([700, 650], 0, 16, 4, 128), ([1100], 200, 4, 1, 64),
+    ([257, 1, 400, 1, 256], 0, 40, 8, 128), ([33] * 40, 0, 32, 8, 128), ([1500, 3, 800], 5, 8, 8, 128), ([900, 40, 1200, 7, 300], 0, 24, 8, 64), ([2100, 30], 0, 16, 16, 128),
+    ([3] * 4200, 1, 2, 1, 64), ([1200, 900, 1000], 64, 32, 8, 128),
+]
+
+
+def _packed_inputs(case, seed=8):
+    lengths, behind, H, KV, dh = case
+    starts = _starts(lengths)
+    rows = starts[-1] + behind
+    qkv, do = _rnd(seed, "qkv", (rows, (H + 2 * KV) * dh), "bf16"), _rnd(seed, "do", (rows, H * dh), "bf16")
+    dev = to_dev(qkv, "bf16"), to_dev(do, "bf16")
+    for t in dev:
+        t[starts[-1]:] = NAN                                     # what lies behind the sequences must not matter
+    return starts, rows, qkv.astype(np.float64), do.astype(np.float64), *dev
+
+
+@pytest.mark.parametrize("case", PACKED_CASES, ids=lambda c: f"{len(c[0])}x{max(c[0], default=0)}+{c[1]}-{c[2]}-{c[3]}-{c[4]}")
+def test_packed_attention_matches_oracle(case):
+    lengths, behind, H, KV, dh = case
+    _say(f"packed attention {case[1:]}, {len(lengths)} sequences")
+    starts, rows, qkv, do, dqkv_in, ddo = _packed_inputs(case)
+    s = _ints(starts)
+    out = torch.full((rows, H * dh), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((H, rows), 5.0, device=DEV)
+    got = torch.full((rows, (H + 2 * KV) * dh), 5.0, dtype=torch.bfloat16, device=DEV)
+    tbp.tbp_packed_attention_fwd(dqkv_in, s, H, KV, dh, out=out, lse=lse)
+    tbp.tbp_packed_attention_p1(dqkv_in, out, ddo, lse, s, H, KV, dh, dqkv=got)
+    again, lse2 = tbp.tbp_packed_attention_fwd(dqkv_in, s, H, KV, dh)
+    g2 = tbp.tbp_packed_attention_p1(dqkv_in, again, ddo, lse2, s, H, KV, dh)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again) and torch.equal(lse, lse2) and torch.equal(got, g2)      # the same every time
+    end = starts[-1]
+    assert not out[end:].any() and not got[end:].any() and torch.all(torch.isneginf(lse[:, end:]))
+    if end == 0:
+        return
+    _, lse_ref = ref.packed_attention_fwd(qkv, starts, H, KV, dh)
+    l = to_np(lse) * np.log(2.0)
+    assert np.all(np.abs(l[:, :end] - lse_ref[:, :end]) < 1e-5 * (1 + np.abs(lse_ref[:, :end])))
+    out, got = to_np(out), to_np(got)
+    done = set()
+    for a, b in zip(starts[:-1], starts[1:]):
+        if b == a or (len(lengths) > 50 and b - a in done and a % 97 and b != end):      # (many alike: some of them)
+            continue
+        done.add(b - a)
+        want, tol = _row_errors(qkv[a:b], do[a:b], b - a, H, KV, dh, b - a, 0)
+        have = [out[a:b], got[a:b, :H * dh], got[a:b, H * dh:(H + KV) * dh], got[a:b, (H + KV) * dh:]]
+        for name, w, t, g in zip(("out", "dq", "dk", "dv"), want, tol, have):
+            err = np.sqrt(((g - w).reshape(b - a, -1, dh) ** 2).sum(axis=2))
+            assert np.all(err <= t), (name, a, b, float((err / t).max()))
+
+
+def test_packed_attention_of_one_sequence_is_window_attention():
+    n, H, KV, dh = 777, 8, 2, 128
+    _, _, _, _, qkv, do = _packed_inputs(([n], 0, H, KV, dh))
+    out, lse = tbp.tbp_packed_attention_fwd(qkv, _ints([0, n]), H, KV, dh)
+    want, wlse = tbp.tbp_window_attention_fwd(qkv, n, H, KV, dh, n)
+    g = tbp.tbp_packed_attention_p1(qkv, out, do, lse, _ints([0, n]), H, KV, dh)
+    wg = tbp.tbp_window_attention_p1(qkv, want, do, wlse, n, H, KV, dh, n)
+    for a, b in ((out, want), (lse, wlse[0]), (g, wg)):          # (the two may cut the work differently)
+        assert (a.float() - b.float()).norm() <= 4e-3 * b.float().norm()
+
+
+def test_packed_attention_in_wider_rows():
+    """Leading dimensions above the columns; what lies beside is neither read nor touched."""
+    case = ([70, 131, 3], 9, 4, 2, 64)
+    starts, rows, qkv, do, dqkv_in, ddo = _packed_inputs(case)
+    lengths, behind, H, KV, dh = case
+    w = (H + 2 * KV) * dh
+    s = _ints(starts)
+    out, lse = tbp.tbp_packed_attention_fwd(dqkv_in, s, H, KV, dh)
+    g = tbp.tbp_packed_attention_p1(dqkv_in, out, ddo, lse, s, H, KV, dh)
+    big = torch.full((rows, w + 24), NAN, dtype=torch.bfloat16, device=DEV)
+    big[:, :w] = dqkv_in
+    o2, d2, g2 = (torch.full((rows, c), 3.0, dtype=torch.bfloat16, device=DEV) for c in (H * dh + 8, H * dh + 8, w + 16))
+    d2[:, :H * dh] = ddo
+    _, lse2 = tbp.tbp_packed_attention_fwd(big[:, :w], s, H, KV, dh, out=o2[:, :H * dh])
+    tbp.tbp_packed_attention_p1(big[:, :w], o2[:, :H * dh], d2[:, :H * dh], lse2, s, H, KV, dh, dqkv=g2[:, :w])
+    assert torch.equal(o2[:, :H * dh], out) and torch.equal(g2[:, :w], g) and torch.equal(lse, lse2)
+    assert torch.all(o2[:, H * dh:] == 3.0) and torch.all(g2[:, w:] == 3.0)
+
+
+def test_packed_sequences_with_large_scores_and_one_infinite_row():
+    """Scores of hundreds, and a row that is not finite: it reaches its own sequence and key head, no others."""
+    H, KV, dh, starts = 4, 2, 64, [0, 200, 330, 700]
+    qkv = to_dev(_rnd(4, "qkv", (700, 512), "bf16"), "bf16")
+    qkv[:, :384] *= 6
+    out, lse = tbp.tbp_packed_attention_fwd(qkv, _ints(starts), H, KV, dh)
+    want, lse_ref = ref.packed_attention_fwd(to_np(qkv), starts, H, KV, dh)
+    assert np.max(np.abs(to_np(out) - want)) < 1e-2 * np.max(np.abs(want))
+    assert np.all(np.abs(to_np(lse) * np.log(2.0) - lse_ref) < 1e-5 * (1 + np.abs(lse_ref)))
+    qkv[250, 256:320] = INF                                      # the first key head's key
+    hurt, lse2 = tbp.tbp_packed_attention_fwd(qkv, _ints(starts), H, KV, dh)
+    kept = torch.ones((700, 256), dtype=torch.bool, device=DEV)
+    kept[200:330, :128] = False
+    assert torch.equal(hurt[kept], out[kept])
+
+
+@pytest.mark.parametrize("starts", [[0, 50, 20, 100], [0, 100, 0, 100], [0, -7, 300, 40], [99, 2 ** 31 - 1, -2 ** 31, 5], [0, 30, 30, 1000]], ids=str)
+def test_starts_that_do_not_ascend_touch_nothing_else(starts):
+    """Results are undefined then, but stay inside the tensors."""
+    rows, H, KV, dh = 100, 4, 2, 64
+    qkv = to_dev(_rnd(4, "qkv", (rows, 512), "bf16"), "bf16")
+    around = torch.full((rows + 512, 512), 9.0, dtype=torch.bfloat16, device=DEV)
+    out = torch.full((rows + 512, 256), 9.0, dtype=torch.bfloat16, device=DEV)
+    stat = torch.full((H * rows + 8192,), 9.0, device=DEV)
+    s = _ints(starts)
+    tbp.tbp_packed_attention_fwd(qkv, s, H, KV, dh, out=out[256:256 + rows], lse=stat[4096:4096 + H * rows].view(H, rows))
+    tbp.tbp_packed_attention_p1(qkv, out[256:256 + rows], out[256:256 + rows].clone(), stat[4096:4096 + H * rows].view(H, rows), s, H, KV, dh, dqkv=around[256:256 + rows])
+    torch.cuda.synchronize()
+    for t in (around, out):
+        assert torch.all(t[:256] == 9.0) and torch.all(t[256 + rows:] == 9.0)
+    assert torch.all(stat[:4096] == 9.0) and torch.all(stat[4096 + H * rows:] == 9.0)
+
+
+# ------------------------------------------------------------------------------------------------- a stash in 8 bits
+STASH_CASES = [  # tokens, cols, slots, dtype
+    (1, 1, 1, "bf16"), (1, 8, 2, "f32"), (63, 33, 1, "bf16"), (64, 32, 3, "f32"), (65, 31, 2, "bf16"), (129, 72, 1, "f32"), (1024, 40, 2, "bf16"), (1025, 97, 2, "bf16"),
+    (2500, 130, 1, "f32"), (333, 520, 3, "bf16"),
+]
+
+
+def _tensor(tokens, cols, dtype, seed):
+    """Columns of very different scales, exact border values, zeros."""
+    x = si.standard_normal(seed, "x", (tokens, cols)) * np.exp(4 * si.standard_normal(seed, "scale", (1, cols)))
+    x = si.store_round(x, dtype)
+    if cols > 6 and tokens > 8:
+        x[:, 1] = 0
+        x[:, 2] = np.linspace(-127, 127, tokens).round()
+        x[3, 3], x[4, 3], x[5, 3] = 130.0, 1.0, 3.0
+        x[3, 4] = 2.0 ** 127
+        x[:, 5] = np.where(x[:, 5] > 0, 2.0 ** -126, -2.0 ** -126)
+    return x
+
+
+@pytest.mark.parametrize("ld", [0, 8, 1])
+@pytest.mark.parametrize("case", STASH_CASES, ids=str)
+def test_stash_holds_what_the_oracle_says(case, ld):
+    tokens, cols, slots, dtype = case
+    _say(f"stash {case} ld +{ld}")
+    kept = tbp.Stash8(tokens, cols, slots, torch.float32, device=DEV)
+    assert not kept.get(slots - 1).any()                        # nothing put: zeros
+    xs = [_tensor(tokens, cols, dtype, 20 + i) for i in range(slots)]
+    for i in reversed(range(slots)):
+        big = torch.full((tokens, cols + ld), NAN, device=DEV, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+        big[:, :cols] = to_dev(xs[i], dtype)
+        kept.put(i, big[:, :cols])
+    for i in range(slots):
+        want = ref.held(xs[i])
+        assert np.array_equal(to_np(kept.get(i)), want)
+        out = torch.full((tokens + 2, cols + ld), 7.0, dtype=torch.bfloat16, device=DEV)
+        kept.get(i, out=out[1:-1, :cols])
+        assert np.array_equal(to_np(out[1:-1, :cols]), si.store_round(want, "bf16").astype(np.float64))
+        assert torch.all(out[0] == 7.0) and torch.all(out[-1] == 7.0) and torch.all(out[:, cols:] == 7.0)
+
+
+def test_every_bf16_value_is_held_as_the_oracle_says():
+    """All finite bf16 values, 64 of one exponent to a column: every rounding, every scale."""
+    bits = np.arange(1 << 16, dtype=np.uint32)
+    v = (bits << 16).view(np.float32)
+    v = v[np.isfinite(v)]
+    v = v[np.argsort(np.abs(v), kind="stable")]
+    x = v[:len(v) // 64 * 64].reshape(-1, 64).T.copy()
+    t = torch.from_numpy(x).to(DEV, torch.bfloat16)
+    kept = tbp.Stash8(64, x.shape[1], 1, torch.float32, device=DEV)
+    kept.put(0, t)
+    assert np.array_equal(to_np(kept.get(0)), ref.held(x))
+
+
+def test_blocks_that_are_not_finite():
+    x = to_dev(_rnd(2, "x", (1100, 40), "bf16"), "bf16")
+    kept = tbp.Stash8(1100, 40, 1, torch.float32, device=DEV)
+    x[5, 3], x[1050, 7], x[0, 9] = NAN, INF, -INF
+    kept.put(0, x)
+    y = kept.get(0)
+    bad = torch.zeros((1100, 40), dtype=torch.bool, device=DEV)
+    bad[:1024, 3], bad[1024:, 7], bad[:1024, 9] = True, True, True
+    assert torch.equal(torch.isnan(y), bad) and torch.all(torch.isfinite(y[~bad]))
+    d = tbp.Stash8(1100, 33, 1, device=DEV)
+    d.put(0, to_dev(_rnd(3, "d", (1100, 33), "bf16"), "bf16"))
+    for dw, row in ((tbp.tbp_stash8_dw(kept, d), True), (tbp.tbp_stash8_dw(d, kept).t(), False)):
+        nan = torch.isnan(dw)
+        assert torch.all(nan[[3, 7, 9]]) and int(nan.sum()) == 3 * 33
+    kept.put(0, torch.zeros_like(x))                             # the slot is whole again
+    assert not kept.get(0).any() and not tbp.tbp_stash8_dw(kept, d).any()
+
+
+DW_CASES = [  # tokens, m, n_out, slots, dtype
+    (1, 1, 1, 1, "f32"), (64, 32, 32, 1, "bf16"), (65, 33, 31, 2, "bf16"), (63, 200, 7, 3, "f32"), (128, 192, 192, 1, "bf16"), (100, 193, 260, 5, "bf16"), (1024, 256, 128, 2, "bf16"),
+    (1025, 130, 300, 2, "f32"), (1100, 64, 513, 3, "bf16"), (333, 520, 1001, 3, "f32"), (2048, 700, 40, 1, "bf16"), (40, 1500, 900, 9, "bf16"), (3200, 96, 64, 2, "bf16"),
+]
+
+
+@pytest.mark.parametrize("case", DW_CASES, ids=str)
+def test_weight_gradients_from_the_stash(case):
+    tokens, m, n_out, slots, dtype = case
+    _say(f"dw {case}")
+    xs, ds = [_tensor(tokens, m, dtype, 40 + i) for i in range(slots)], [_tensor(tokens, n_out, dtype, 60 + i) for i in range(slots)]
+    for t in xs + ds:
+        t[np.abs(t) > 2.0 ** 60] = 1.0                          # (products stay in range)
+    kx, kd = tbp.Stash8(tokens, m, slots, device=DEV), tbp.Stash8(tokens, n_out, slots, device=DEV)
+    for i in range(slots):
+        kx.put(i, to_dev(xs[i], dtype)), kd.put(i, to_dev(ds[i], dtype))
+    blocks = slots * -(-tokens // ref.BLOCK)
+
+    def close(got, want, size, adds):
+        err = np.abs(to_np(got) - want)
+        # (the product of two scales is rounded to a multiple of 2^-149, off by 2^-150 at most, and multiplies a sum of at most 2^24: 2^-126 a block)
+        assert np.all(err <= adds * (2.0 ** -24 * size + 2.0 ** -126)), float((err / (size + 1e-300)).max())
+    want, size = ref.stash8_dw(xs, ds)
+    dw = tbp.tbp_stash8_dw(kx, kd)
+    close(dw, want, size, blocks)
+    assert torch.equal(dw, tbp.tbp_stash8_dw(kx, kd))            # the same every time
+    # into a wider array, added to what is there; a part of the slots
+    first, n = slots // 2, slots - slots // 2
+    part, psize = ref.stash8_dw(xs[first:], ds[first:])
+    base = torch.full((m + 1, n_out + 3), 0.5, device=DEV)
+    tbp.tbp_stash8_dw(kx, kd, first=first, dw=base[:m, :n_out], accumulate=True)
+    close(base[:m, :n_out], part + 0.5, psize + 0.5, blocks + 1)
+    assert torch.all(base[m:] == 0.5) and torch.all(base[:, n_out:] == 0.5)
+    tbp.tbp_stash8_dw(kx, kd, first=first, n=1, dw=base[:m, :n_out])
+    one, osize = ref.stash8_dw(xs[first:first + 1], ds[first:first + 1])
+    close(base[:m, :n_out], one, osize, blocks)
+    # no slots: zeros, or nothing
+    kept = base.clone()
+    tbp.tbp_stash8_dw(kx, kd, n=0, dw=base[:m, :n_out], accumulate=True)
+    assert torch.equal(base, kept)
+    tbp.tbp_stash8_dw(kx, kd, n=0, dw=base[:m, :n_out])
+    assert not base[:m, :n_out].any() and torch.all(base[m:] == 0.5) and torch.all(base[:, n_out:] == 0.5)
+
+
+def test_integer_sums_at_their_largest():
+    """1024 products of 127 * 127 and their signs: the integers' range, and fp32's whole numbers."""
+    kx, kd = tbp.Stash8(1024, 40, 1, device=DEV), tbp.Stash8(1024, 50, 1, device=DEV)
+    x, d = torch.full((1024, 40), 127.0, device=DEV), torch.full((1024, 50), -127.0, device=DEV)
+    x[7, 3] = 126.0
+    kx.put(0, x), kd.put(0, d)
+    dw = tbp.tbp_stash8_dw(kx, kd)
+    assert torch.all(dw[4:] == -1024 * 127 * 127) and torch.all(dw[3] == -1024 * 127 * 127 + 127)
+
+
+# ------------------------------------------------------------------------------------- together, captured, on other streams
+def _layer(seed, starts, H, KV, dh, d):
+    """What a layer of packed documents has: hidden rows, weights of its projections, gains, the output's derivative, positions in the documents."""
+    rows, w = starts[-1], (H + 2 * KV) * dh
+    t = {"x": to_dev(_rnd(seed, "x", (rows, d), "bf16"), "bf16"), "w": to_dev(_rnd(seed, "w", (d, w), "bf16", d ** -0.5), "bf16"),
+         "gq": to_dev(si.store_round(1 + 0.2 * si.standard_normal(seed, "gq", (dh,)), "bf16"), "bf16"),
+         "gk": to_dev(si.store_round(1 + 0.2 * si.standard_normal(seed, "gk", (dh,)), "bf16"), "bf16"), "do": to_dev(_rnd(seed, "do", (rows, H * dh), "bf16"), "bf16")}
+    t["starts"] = _ints(starts)
+    t["positions"] = _ints(np.concatenate([np.arange(b - a) for a, b in zip(starts[:-1], starts[1:])]))
+    t["table"] = tbp.tbp_rotary_table(max(np.diff(starts)), dh, 1e4, device=DEV)
+    return t
+
+
+def _layer_step(t, kept, d_kept, slot, H, KV, dh, eps=1e-5):
+    """Forward and backward-p1 of the attention block of a layer; p2's operands into the stash.  -> out, dx, partial rows of the gains' gradient"""
+    qk = (H + KV) * dh
+    qkv = tbp.tbp_gemm(tbp.NN, t["x"], t["w"])
+    raw = qkv[:, :qk].clone()                                    # (backward-p1 needs what went into the norms)
+    place = dict(table=t["table"], positions=t["positions"])
+    tbp.tbp_qk_norm(raw, t["gq"], t["gk"], H, KV, dh, eps, **place, out=qkv[:, :qk])
+    out, lse = tbp.tbp_packed_attention_fwd(qkv, t["starts"], H, KV, dh)
+    kept.put(slot, t["x"])
+    d = tbp.tbp_packed_attention_p1(qkv, out, t["do"], lse, t["starts"], H, KV, dh)
+    _, parts = tbp.tbp_qk_norm_p1(d[:, :qk], raw, t["gq"], t["gk"], H, KV, dh, eps, **place, out=d[:, :qk])
+    d_kept.put(slot, d)
+    return out, tbp.tbp_gemm(tbp.NT, d, t["w"]), parts
+
+
+def _layer_reference(t, H, KV, dh, eps=1e-5):
+    """The same in 64 bits by autograd on the host: out, dx, dw, dg."""
+    v = {k: t[k].detach().cpu().double() for k in ("x", "w", "gq", "gk", "do", "table")}
+    x, w, gq, gk = (v[k].requires_grad_() for k in ("x", "w", "gq", "gk"))
+    qkv = x @ w
+    heads = qkv.view(len(x), H + 2 * KV, dh)
+    z = heads[:, :H + KV]
+    z = z / torch.sqrt((z * z).mean(dim=2, keepdim=True) + eps) * torch.cat([gq.expand(H, dh), gk.expand(KV, dh)])
+    cs = v["table"][t["positions"].cpu().long()][:, None]
+    a, b = z[..., :dh // 2], z[..., dh // 2:]
+    z = torch.cat([a * cs[..., 0] - b * cs[..., 1], a * cs[..., 1] + b * cs[..., 0]], dim=2)
+    starts, out = t["starts"].tolist(), []
+    for s, e in zip(starts[:-1], starts[1:]):
+        q, k, u = z[s:e, :H], z[s:e, H:].repeat_interleave(H // KV, dim=1), heads[s:e, H + KV:].repeat_interleave(H // KV, dim=1)
+        p = torch.softmax((q.transpose(0, 1) @ k.permute(1, 2, 0) / dh ** 0.5).masked_fill(torch.ones(e - s, e - s).triu(1).bool(), -INF), dim=2)
+        out.append((p @ u.transpose(0, 1)).transpose(0, 1).reshape(e - s, H * dh))
+    out = torch.cat(out)
+    out.backward(v["do"])
+    return out.detach(), x.grad, w.grad, torch.cat([gq.grad, gk.grad])
+
+
+def test_a_layer_of_packed_documents():
+    """Two micro-batches forward and through backward-p1, backward-p2 once from the stash, against 64 bits on the host.
+
+    Every tensor that is passed on is rounded to bf16, by 2^-8 / sqrt 3 at most as a root mean square; out has four such roundings behind it
+    (qkv, the norms, P, out), dx and the derivatives seven: below 1 and 1.6 %.  The stash adds, as root mean square, half a step over sqrt 3, a step at
+    most 1/63.5 of the block's largest value and values of 1/4 of it at least: 1.8 % of each operand and, in random directions, of dw."""
+    H, KV, dh, d = 4, 2, 64, 192
+    docs = [[0, 50, 51, 180, 300], [0, 128, 300]]
+    layers = [_layer(70 + i, s, H, KV, dh, d) for i, s in enumerate(docs)]
+    for t in layers[1:]:
+        t.update(w=layers[0]["w"], gq=layers[0]["gq"], gk=layers[0]["gk"])
+    kept, d_kept = tbp.Stash8(300, d, 2, device=DEV), tbp.Stash8(300, (H + 2 * KV) * dh, 2, device=DEV)
+    parts, dw_ref, dg_ref = [], 0, 0
+    rel = lambda a, b: float((a.detach().cpu().double() - b).norm() / b.norm())
+    for i, t in enumerate(layers):
+        out, dx, p = _layer_step(t, kept, d_kept, i, H, KV, dh)
+        o, x, w, g = _layer_reference(t, H, KV, dh)
+        _say(f"   out {rel(out, o):.2e} dx {rel(dx, x):.2e}")
+        assert rel(out, o) < 1e-2 and rel(dx, x) < 1.6e-2
+        parts.append(p)
+        dw_ref, dg_ref = dw_ref + w, dg_ref + g
+    dw, dg = tbp.tbp_stash8_dw(kept, d_kept), tbp.tbp_gain_partials_sum(torch.cat(parts))
+    _say(f"   dw {rel(dw, dw_ref):.2e} dg {rel(dg, dg_ref):.2e}")
+    assert rel(dw, dw_ref) < (1.8e-2 ** 2 * 2 + 1.6e-2 ** 2) ** 0.5 and rel(dg, dg_ref) < 1.6e-2
+
+
+def test_a_captured_layer_gives_the_eager_bits_on_every_replay():
+    H, KV, dh, d = 4, 2, 64, 192
+    docs = [0, 50, 51, 180, 300]
+    t = _layer(70, docs, H, KV, dh, d)
+    kept, d_kept = tbp.Stash8(300, d, 1, device=DEV), tbp.Stash8(300, (H + 2 * KV) * dh, 1, device=DEV)
+
+    def step():
+        out, dx, parts = _layer_step(t, kept, d_kept, 0, H, KV, dh)
+        return out, dx, tbp.tbp_gain_partials_sum(parts), tbp.tbp_stash8_dw(kept, d_kept), kept.get(0)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step()
+    for seed in (1, 2, 3):
+        t["x"].copy_(to_dev(_rnd(seed, "x2", (300, d), "bf16"), "bf16"))
+        t["starts"].copy_(_ints([[0, 300, 300, 300, 300], [0, 1, 2, 3, 290], [0, 77, 150, 151, 300]][seed - 1]))
+        want = [w.clone() for w in step()]
+        torch.cuda.synchronize()
+        for r in recorded:
+            r.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(recorded, want):
+            assert torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    H, KV, dh, d = 4, 2, 64, 192
+    docs = [[0, 50, 51, 180, 300], [0, 128, 300]]
+    layers = [_layer(80 + i, s, H, KV, dh, d) for i, s in enumerate(docs)]
+    stash = lambda: (tbp.Stash8(300, d, 1, device=DEV), tbp.Stash8(300, (H + 2 * KV) * dh, 1, device=DEV))
+    stashes = [stash() for _ in layers]
+
+    def step(i):
+        out, dx, parts = _layer_step(layers[i], *stashes[i], 0, H, KV, dh)
+        return out, dx, tbp.tbp_gain_partials_sum(parts), tbp.tbp_stash8_dw(*stashes[i])
+
+    want = [[w.clone() for w in step(i)] for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(3):
+        got = []
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got.append(step(i))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            for u, v in zip(a, b):
+                assert torch.equal(u, v)
+
+
+def test_answering_goes_on_from_a_packed_prompt():
+    """A prompt as a packed sequence, then token by token over the cache: the new token's output is that of the longer prompt."""
+    H, KV, dh, n, more = 8, 2, 64, 90, 4
+    g = [to_dev(si.store_round(1 + 0.2 * si.standard_normal(2, k, (dh,)), "bf16"), "bf16") for k in ("gq", "gk")]
+    raw = to_dev(_rnd(2, "qkv", (n + more, (H + 2 * KV) * dh), "bf16"), "bf16")
+    table = tbp.tbp_rotary_table(128, dh, 1e4, device=DEV)
+    qkv = raw.clone()
+    tbp.tbp_qk_norm(raw, *g, H, KV, dh, 1e-5, table, out=qkv)
+    want, _ = tbp.tbp_packed_attention_fwd(qkv, _ints([0, n + more]), H, KV, dh)
+    ck, cv = (torch.zeros((1, 128, KV * dh), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    tbp.tbp_qk_norm_append(raw[:n], *g, H, KV, dh, 1e-5, table, _ints([n]), ck, cv)
+    for i in range(n, n + more):
+        q = tbp.tbp_qk_norm_append(raw[i:i + 1], *g, H, KV, dh, 1e-5, table, _ints([i + 1]), ck, cv)
+        out, _ = tbp.tbp_window_decode(q, ck, cv, _ints([i + 1]), H, KV, dh, 1024)
+        # (two roundings of P and of the result on either side)
+        assert (out[0].float() - want[i].float()).norm() <= 1e-2 * want[i].float().norm()
