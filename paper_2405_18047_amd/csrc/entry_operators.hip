@@ -494,7 +494,8 @@ tbp_status tbp_stash8_get(int dtype, int slots, int tokens, int cols, int slot, 
 }
 
 size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n) {
-  return 0;
+  if (n < 1 || check_stash8(n, tokens, m) != TBP_OK || check_stash8(n, tokens, n_out) != TBP_OK) return 0;
+  return tbp::stash8_plan(m, n_out, n * ((tokens + 63) / 64), n * ((tokens + tbp::kStash8Block - 1) / tbp::kStash8Block)).bytes;
 }
 
 tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,
@@ -505,8 +506,10 @@ tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int
   if (n == 0 && accumulate) return TBP_OK;
   if (!x_stash || !dy_stash || !dw) return fail(TBP_EINVAL, "null pointer");
   if (misaligned(x_stash, 16) || misaligned(dy_stash, 16) || misaligned(dw, 4)) return fail(TBP_EINVAL, "stashes must be 16-byte aligned, dw 4-byte");
+  const size_t need = tbp_stash8_dw_workspace_bytes(tokens, m, n_out, n);
+  if (need && (!workspace || misaligned(workspace, 256) || workspace_bytes < need)) return fail(TBP_EINVAL, "workspace must be 256-byte aligned and have %zu bytes", need);
   TBP_HIP(tbp::stash8_dw(stash8_slot(slots, tokens, m, first, x_stash), stash8_slot(slots, tokens, n_out, first, dy_stash), n, dw, ld_dw, accumulate,
-                         stream_of(stream)));
+                         static_cast<float*>(workspace), stream_of(stream)));
   return TBP_OK;
 }
 

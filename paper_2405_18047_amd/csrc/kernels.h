@@ -323,8 +323,11 @@ struct Stash8Slot {
 };
 hipError_t stash8_put(int dtype, const Stash8Slot& p, const void* x, long ld, hipStream_t s);
 hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStream_t s);
+// How a product of m x n over so many steps of 64 tokens in so many blocks runs: tiles of a wave, shares of the contraction and blocks of each, bytes for the shares' sums (0: one share).
+struct Stash8Plan { int mb, nb, shares, share; size_t bytes; };
+Stash8Plan stash8_plan(int m, int n, int steps, int blocks);
 // over n slots from x.slot on (dy: the same slots, tokens and steps)
-hipError_t stash8_dw(const Stash8Slot& x, const Stash8Slot& dy, int n, float* dw, long ld, int accumulate, hipStream_t s);
+hipError_t stash8_dw(const Stash8Slot& x, const Stash8Slot& dy, int n, float* dw, long ld, int accumulate, float* part, hipStream_t s);
 
 // Limits enforced by the host before any launch.
 inline int max_d_model(int dtype) { return dtype == 1 ? 8192 : 4096; }

@@ -13,6 +13,8 @@
 #include "kernels.h"
 #include "rows.h"
 
+#include <type_traits>
+
 namespace tbp {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -24,46 +26,106 @@ constexpr int kTopExponent = 121;                // of a scale: 127 2^121 is the
 
 // ------------------------------------------------------------------------------------------ into the stash, and out of it
 // One workgroup = 64 columns of one block of tokens, 8 threads side by side with 8 columns each (128 bytes of a row, bf16) and 64 of them below each other
-// with 16 tokens each, which stay in registers between the two looks at them: the largest magnitude of every column, then the rounding.
-// Magnitudes are compared as bit patterns, in which NaN is above infinity.
+// with 16 tokens each, which stay in registers as they were loaded between the two looks at them: the largest magnitude of every column, then the rounding.
+// Magnitudes are compared as bit patterns, in which NaN is above infinity (bf16: two to an instruction).
+template <typename T> struct Rows8;              // 8 columns of a row as they lie in memory
+template <> struct Rows8<bf16_t> {
+  u32x4 q;
+  __device__ __forceinline__ void load(const bf16_t* p) { q = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+  __device__ __forceinline__ void set(int c, bf16_t v) {
+    const unsigned b = (unsigned)__builtin_bit_cast(unsigned short, v);
+    q[c / 2] = c % 2 ? (q[c / 2] & 0xffffu) | (b << 16) : (q[c / 2] & 0xffff0000u) | b;
+  }
+  __device__ __forceinline__ void clear() { q = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ float get(int c) const { return __uint_as_float(c % 2 ? q[c / 2] & 0xffff0000u : q[c / 2] << 16); }
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  struct Top {
+    u32x4 m = {0, 0, 0, 0};
+    static __device__ __forceinline__ unsigned more(unsigned a, unsigned b) {
+      return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    __device__ __forceinline__ void add(const Rows8& r) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) m[i] = more(m[i], r.q[i] & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ void across(int d) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) m[i] = more(m[i], (unsigned)__shfl_xor((int)m[i], d));
+    }
+    __device__ __forceinline__ unsigned get(int c) const { return c % 2 ? m[c / 2] & 0xffff0000u : m[c / 2] << 16; }
+  };
+};
+template <> struct Rows8<float> {
+  u32x4 q[2];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) q[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+  }
+  __device__ __forceinline__ void set(int c, float v) { q[c / 4][c % 4] = __float_as_uint(v); }
+  __device__ __forceinline__ void clear() { q[0] = q[1] = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ float get(int c) const { return __uint_as_float(q[c / 4][c % 4]); }
+  struct Top {
+    unsigned m[8] = {};
+    __device__ __forceinline__ void add(const Rows8& r) {
+#pragma unroll
+      for (int c = 0; c < 8; c++) {
+        const unsigned a = r.q[c / 4][c % 4] & 0x7fffffffu;
+        m[c] = a > m[c] ? a : m[c];
+      }
+    }
+    __device__ __forceinline__ void across(int d) {
+#pragma unroll
+      for (int c = 0; c < 8; c++) {
+        const unsigned a = (unsigned)__shfl_xor((int)m[c], d);
+        m[c] = a > m[c] ? a : m[c];
+      }
+    }
+    __device__ __forceinline__ unsigned get(int c) const { return m[c]; }
+  };
+};
+
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* __restrict__ x, long ld) {
-  __shared__ unsigned top[8][64];
-  __shared__ float scale_of[64];
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];      // per wave 8 KiB of units; magnitudes and scales of the columns
+  unsigned (*const top)[64] = reinterpret_cast<unsigned (*)[64]>(smem_raw + 8 * 8192);
+  float* const scale_of = reinterpret_cast<float*>(smem_raw + 8 * 8192 + 8 * 256);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid & 7, rg = tid >> 3;
   const int c0 = (int)blockIdx.x * 64 + 8 * cg, block = (int)blockIdx.y, t0 = block * kStash8Block + 16 * rg;
-  float v[16][8];
-  const int cn = p.cols - c0;                      // columns from here on
+  const int cn = p.cols - c0, tn = p.tokens - t0;  // columns and tokens from here on
+  Rows8<T> v[16];
 #pragma unroll
-  for (int r = 0; r < 16; r++) {
-    const int t = t0 + r;
-    const T* const row = x + (long)t * ld + c0;
-    if (WIDE && t < p.tokens && cn >= 8) {
-      if constexpr (sizeof(T) == 2) Vec<bf16_t>::load(row, v[r]);
-      else { Vec<float>::load(row, v[r]); Vec<float>::load(row + 4, v[r] + 4); }
+  for (int r = 0; r < 16; r++) v[r].clear();
+  if (cn > 0 && tn > 0) {
+    // (all loads before the first use of one, from the last row where there are no more: a load under a condition is waited for there)
+    const T* const at = x + (long)t0 * ld + c0;
+    if (WIDE && cn >= 8) {
+#pragma unroll
+      for (int r = 0; r < 16; r++) v[r].load(at + (long)(r < tn ? r : tn - 1) * ld);
     } else {
 #pragma unroll
-      for (int c = 0; c < 8; c++) v[r][c] = t < p.tokens && c < cn ? (float)row[c] : 0.f;
+      for (int r = 0; r < 16; r++)
+#pragma unroll
+        for (int c = 0; c < 8; c++) v[r].set(c, at[(long)(r < tn ? r : tn - 1) * ld + (c < cn ? c : cn - 1)]);
+      if (cn < 8) {
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+#pragma unroll
+          for (int c = 0; c < 8; c++) if (c >= cn) v[r].set(c, (T)0.f);
+      }
+    }
+    if (tn < 16) {
+#pragma unroll
+      for (int r = 0; r < 16; r++) if (r >= tn) v[r].clear();
     }
   }
-  unsigned m[8];
+  typename Rows8<T>::Top m;
 #pragma unroll
-  for (int c = 0; c < 8; c++) {
-    m[c] = 0;
+  for (int r = 0; r < 16; r++) m.add(v[r]);
 #pragma unroll
-    for (int r = 0; r < 16; r++) {
-      const unsigned a = __float_as_uint(v[r][c]) & 0x7fffffffu;
-      m[c] = a > m[c] ? a : m[c];
-    }
-#pragma unroll
-    for (int d = 8; d < 64; d *= 2) {
-      const unsigned a = (unsigned)__shfl_xor((int)m[c], d);
-      m[c] = a > m[c] ? a : m[c];
-    }
-  }
+  for (int d = 8; d < 64; d *= 2) m.across(d);
   if (lane < 8) {
 #pragma unroll
-    for (int c = 0; c < 8; c++) top[wave][8 * cg + c] = m[c];
+    for (int c = 0; c < 8; c++) top[wave][8 * cg + c] = m.get(c);
   }
   __syncthreads();
   if (tid < 64) {
@@ -79,18 +141,22 @@ __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* 
     if (c < 32 * p.col_blocks) p.scales[((long)p.slot * p.blocks + block) * 32 * p.col_blocks + c] = s;
   }
   __syncthreads();
-  if (c0 >= 32 * p.col_blocks || t0 >= 64 * p.steps) return;
-  unsigned char* const unit = p.data + (((long)p.slot * p.steps + t0 / 64) * p.col_blocks + c0 / 32) * kUnit + ((rg >> 1) & 1) * 1024 +
-                              (32 * (rg & 1) + c0 % 32) * 16;
+  // The wave's 64 columns x 128 tokens are 8 halves of units, put together in LDS and stored as whole KiB (16 bytes at a time, spread over the lines, took
+  // 35.4 us for 4096 x 11008, bf16).  Piece l of a half lies at l ^ (l / 8 % 8): the 8 lanes side by side write 128 bytes apart.
+  unsigned char* const mine = smem_raw + wave * 8192;
+  const int half = (cg >> 2) * 4 + ((rg & 7) >> 1), piece = 32 * (rg & 1) + 8 * (cg & 3);
 #pragma unroll
   for (int c = 0; c < 8; c++) {
     const float s = scale_of[8 * cg + c];
     const bool fine = s == s;
     const float inv = fine ? __uint_as_float((254u << 23) - __float_as_uint(s)) : 0.f;      // 2^-e
+    float x16[16];
+#pragma unroll
+    for (int r = 0; r < 16; r++) x16[r] = v[r].get(c);
     if (s == __uint_as_float((unsigned)(kTopExponent + 127) << 23)) {      // (rare: the one scale that values may pass the range of)
       const float most = 127.f * s;
 #pragma unroll
-      for (int r = 0; r < 16; r++) v[r][c] = fminf(fmaxf(v[r][c], -most), most);
+      for (int r = 0; r < 16; r++) x16[r] = fminf(fmaxf(x16[r], -most), most);
     }
     u32x4 o;
 #pragma unroll
@@ -98,11 +164,19 @@ __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* 
       // x 2^-e + 1.5 2^23, rounded once: the integer is in the low bits
       unsigned b[4];
 #pragma unroll
-      for (int i = 0; i < 4; i++) b[i] = __float_as_uint(__builtin_fmaf(v[4 * q + i][c], inv, 12582912.f));
+      for (int i = 0; i < 4; i++) b[i] = __float_as_uint(__builtin_fmaf(x16[4 * q + i], inv, 12582912.f));
       const unsigned lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u);
       o[q] = fine ? lo | (hi << 16) : 0u;
     }
-    *reinterpret_cast<u32x4*>(unit + 16 * c) = o;
+    *reinterpret_cast<u32x4*>(mine + half * 1024 + ((piece + c) ^ (piece >> 3)) * 16) = o;
+  }
+  // (LDS operations of a wave execute in order)
+#pragma unroll
+  for (int h = 0; h < 8; h++) {
+    const int cb = 2 * (int)blockIdx.x + (h >> 2), t = block * kStash8Block + wave * 128 + 32 * (h & 3);
+    if (cb < p.col_blocks && t < 64 * p.steps)
+      *reinterpret_cast<u32x4*>(p.data + (((long)p.slot * p.steps + t / 64) * p.col_blocks + cb) * kUnit + (h & 1) * 1024 + lane * 16) =
+          *reinterpret_cast<const u32x4*>(mine + h * 1024 + (lane ^ (lane >> 3)) * 16);
   }
 }
 
@@ -139,11 +213,12 @@ __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __rest
 }
 
 // ------------------------------------------------------------------------------------------ dW = X^T dY
-// One workgroup = 4 waves, 2 x 2, each 128 x 32 NB of the output; the contraction in steps of 64 tokens through a ring of four slots in LDS, filled by
-// asynchronous copies three steps ahead.  The units are copied as they are: every fragment is 64 lanes x 16 bytes in a row.
+// One workgroup = 4 waves, 2 x 2, each 128 x 32 NB of the output; the contraction in steps of 64 tokens through a ring of slots in LDS, filled by
+// asynchronous copies all but one of them ahead.  The units are copied as they are: every fragment is 64 lanes x 16 bytes in a row.
 // The integer sums of a block of tokens are exact: 1024 x 127^2 is below 2^24, so that they are exact in fp32 as well, in which the blocks are added
 // up, each with the product of the two columns' scales.  That takes three vector instructions per element and block, done tile by tile in front of the tile's first
 // product of the next block, and a second set of accumulators, which one wave per SIMD has the registers for.
+constexpr int dw_slots(int mb, int nb, int per_cu) { return (160 * 1024 / per_cu - 8 * 2048) / (2 * (mb + nb) * kUnit); }
 struct Stash8Dw {
   const unsigned char* x; const float* xs; int xb;     // units, scales, column blocks
   const unsigned char* dy; const float* ds; int db;
@@ -153,13 +228,15 @@ struct Stash8Dw {
   long first_step, first_block;                        // of the run
   int total;                                           // steps of the run
   int tiles_m, tiles_n;
+  int shares, share;                                   // of the contraction: how many, and blocks of each but the last
+  float* part;                                         // shares > 1: [share][tile][wave][tile of 32 x 32][quarter][lane][4], as the accumulators lie
 };
 
-template <int MB, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void stash8_dw_kernel(Stash8Dw p) {
+template <int MB, int NB, int PER_CU>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER_CU))) void stash8_dw_kernel(Stash8Dw p) {
   constexpr int WM = 2, WN = 2;
   constexpr int UA = MB * WM, UB = NB * WN;            // units of a step
-  constexpr int SLOT = (UA + UB) * kUnit, SLOTS = 4;
+  constexpr int SLOT = (UA + UB) * kUnit, SLOTS = dw_slots(MB, NB, PER_CU), AHEAD = SLOTS - 1;
   constexpr int OPS = 2 * (UA + UB) / 4;               // copies of a step, per wave
   static_assert(2 * UA % 4 == 0 && 2 * UB % 4 == 0 && UA <= 8 && UB <= 8, "copies are shared out evenly");
   constexpr int SCALES = 512 * 4, RING = 8;            // 256 scales of x, 256 of dy; as many blocks may be under way as steps, and one in use
@@ -174,7 +251,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   // tiles: ids go round the 8 XCDs; each gets a run of them, walked in bands of 4 rows, so that what an XCD works on at a time shares operands in its cache
   int tm, tn;
   {
-    const int tiles = p.tiles_m * p.tiles_n, id = (int)blockIdx.x, per = tiles / 8, rest = tiles % 8;
+    const int tiles = p.tiles_m * p.tiles_n, id = (int)blockIdx.x % tiles, per = tiles / 8, rest = tiles % 8;
     const int xcd = id % 8, at = id / 8;
     const int t = xcd * per + (xcd < rest ? xcd : rest) + at;
     const int band = t / (4 * p.tiles_n), in = t - band * 4 * p.tiles_n;
@@ -182,34 +259,57 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     tn = in / rows;
     tm = 4 * band + in - tn * rows;
   }
+  // the share's steps: whole blocks, so that their integer sums stay whole
+  const int share = (int)blockIdx.x / (p.tiles_m * p.tiles_n);
+  auto step_of = [&](long b) {                         // at which the run's block b begins
+    const long slot = b / p.blocks;
+    const long s = slot * p.steps + (b - slot * p.blocks) * kStepsPerBlock;
+    return (int)(s < p.total ? s : p.total);
+  };
+  const int s0 = step_of((long)share * p.share), total = step_of((long)(share + 1) * p.share) - s0;
+  // block -1, which is added before the first one
+  for (int i = (int)threadIdx.x; i < SCALES / 4; i += 256) reinterpret_cast<LDS_AS float*>(sc + (RING - 1) * SCALES)[i] = 0.f;
   const int ub_a = tm * UA, ub_b = tn * UB;            // first column blocks
   const int na = p.xb - ub_a < UA ? p.xb - ub_a : UA, nb = p.db - ub_b < UB ? p.db - ub_b : UB;
 
-  // The copies of step s into its slot: chunks of 1 KiB, x's units first; chunks past the last column block, and steps past the last one, deliver zeros.
-  int at_block = 0, in_block = 0, in_slot = 0;         // of the next step to be copied: blocks since the run's first, steps since the block's and the slot's first
-  auto issue = [&](int s) {
-    const bool live = s < p.total;
-    const long step = p.first_step + (live ? s : 0);
-    const u32x4 da = make_desc(p.x + (step * p.xb + ub_a) * kUnit, live ? na * kUnit : 0);
-    const u32x4 db = make_desc(p.dy + (step * p.db + ub_b) * kUnit, live ? nb * kUnit : 0);
-    const uint32_t slot = lds0 + (s % SLOTS) * SLOT;
-#pragma unroll
-    for (int i = 0; i < OPS; i++) {
-      const int chunk = wave + 4 * i;                  // (uniform)
-      if (4 * i < 2 * UA) dma16(slot + chunk * 1024, da, chunk * 1024 + lane * 16);
-      else dma16(slot + chunk * 1024, db, (chunk - 2 * UA) * 1024 + lane * 16);
-    }
+  // The copies of a step into its slot, in order from step 0 on: chunks of 1 KiB, x's units first; chunks past the last column block, and steps past the last one,
+  // deliver zeros.  begin() sets up the next step's, copy(i) issues the wave's i-th.
+  const long step0 = p.first_step + s0, block0 = p.first_block + (long)share * p.share;
+  const int in = s0 % p.steps;                         // steps of its slot before the share's first
+  const unsigned char* at_a = p.x + (step0 * p.xb + ub_a) * kUnit;
+  const unsigned char* at_b = p.dy + (step0 * p.db + ub_b) * kUnit;
+  const float* at_sa = p.xs + (block0 * p.xb + ub_a) * 32;
+  const float* at_sb = p.ds + (block0 * p.db + ub_b) * 32;
+  const long next_a = (long)p.xb * kUnit, next_b = (long)p.db * kUnit;
+  int to_come = total, in_slot = in;                   // steps to be copied; of the next one: steps since the slot's first, and since the block's
+  int in_block = 0;
+  uint32_t slot_w = lds0 + wave * 1024, scale_w = sc0 + wave * 256;
+  u32x4 da, db;
+  auto begin = [&] {
+    const bool live = to_come > 0;
+    da = make_desc(at_a, live ? na * kUnit : 0);
+    db = make_desc(at_b, live ? nb * kUnit : 0);
     if (in_block == 0) {                               // the scales of the block that begins
-      const long b = p.first_block + at_block;
-      const u32x4 sa = make_desc(p.xs + (b * p.xb + ub_a) * 32, live ? na * 128 : 0);
-      const u32x4 sb = make_desc(p.ds + (b * p.db + ub_b) * 32, live ? nb * 128 : 0);
-      const uint32_t to = sc0 + (at_block % RING) * SCALES + wave * 256;
-      dma4(to, sa, wave * 256 + lane * 4);
-      dma4(to + 1024, sb, wave * 256 + lane * 4);
+      const u32x4 sa = make_desc(at_sa, live ? na * 128 : 0), sb = make_desc(at_sb, live ? nb * 128 : 0);
+      dma4(scale_w, sa, wave * 256 + lane * 4);
+      dma4(scale_w + 1024, sb, wave * 256 + lane * 4);
+      at_sa += p.xb * 32;
+      at_sb += p.db * 32;
+      scale_w = scale_w + SCALES >= sc0 + RING * SCALES ? sc0 + wave * 256 : scale_w + SCALES;
     }
-    in_block++;
-    if (++in_slot == p.steps) { in_slot = 0; in_block = 0; at_block++; }
-    else if (in_block == kStepsPerBlock) { in_block = 0; at_block++; }
+  };
+  const uint32_t voff = wave * 1024 + lane * 16;
+  auto copy = [&](int i) {
+    if (4 * i < 2 * UA) dma16(slot_w + i * 4096, da, voff + i * 4096);
+    else dma16(slot_w + i * 4096, db, voff + i * 4096 - 2 * UA * 1024);
+  };
+  auto done = [&] {
+    at_a += next_a;
+    at_b += next_b;
+    to_come--;
+    slot_w = slot_w + SLOT >= lds0 + SLOTS * SLOT ? lds0 + wave * 1024 : slot_w + SLOT;
+    in_block = in_block + 1 == kStepsPerBlock ? 0 : in_block + 1;
+    if (++in_slot == p.steps) { in_slot = 0; in_block = 0; }
   };
 
   i32x16 ia[MB][NB];
@@ -221,76 +321,112 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 #pragma unroll
       for (int e = 0; e < 16; e++) { fa[i][j][e] = 0.f; ia[i][j][e] = 0; }
 
+  // Fragments of a half step: first the first tile's, then those of its row and column.
   i32x4 fra[2][MB], frb[2][NB];
-  auto fetch = [&](int to, int s, int half) {
-    lds_u8* const slot = lds + (s % SLOTS) * SLOT + half * 1024 + lane * 16;
-#pragma unroll
-    for (int i = 0; i < MB; i++) fra[to][i] = *reinterpret_cast<LDS_AS const i32x4*>(slot + (wm * MB + i) * kUnit);
-#pragma unroll
-    for (int j = 0; j < NB; j++) frb[to][j] = *reinterpret_cast<LDS_AS const i32x4*>(slot + (UA + wn * NB + j) * kUnit);
+  lds_u8* const mine = lds + lane * 16;
+  auto fetch = [&](int to, int slot, int half, int k) {
+    lds_u8* const from = mine + slot + half * 1024;
+    if (k == 0) frb[to][0] = *reinterpret_cast<LDS_AS const i32x4*>(from + (UA + wn * NB) * kUnit);
+    else if (k == 1) fra[to][0] = *reinterpret_cast<LDS_AS const i32x4*>(from + wm * MB * kUnit);
+    else if (k < NB + 1) frb[to][k - 1] = *reinterpret_cast<LDS_AS const i32x4*>(from + (UA + wn * NB + k - 1) * kUnit);
+    else fra[to][k - NB] = *reinterpret_cast<LDS_AS const i32x4*>(from + (wm * MB + k - NB) * kUnit);
   };
-  // what the block's integer sums add to the result: tile row i
-  auto add_block = [&](int i, int block) {
-    const LDS_AS float* const s = reinterpret_cast<const LDS_AS float*>(sc + (block % RING) * SCALES);
-    f32x4 sa[4];
+  // what the block's integer sums add to the result: a tile, by the scales of its rows and of the lane's column
+  f32x4 sa[4];
+  float sb[NB];
+  auto scales_of = [&](int i, int block) {
+    const LDS_AS float* const s = reinterpret_cast<const LDS_AS float*>(sc + (block & (RING - 1)) * SCALES);
 #pragma unroll
     for (int q = 0; q < 4; q++) sa[q] = *reinterpret_cast<const LDS_AS f32x4*>(s + 32 * (wm * MB + i) + 8 * q + 4 * g);
+    if (i == 0) {
 #pragma unroll
-    for (int j = 0; j < NB; j++) {
-      const float sb = s[256 + 32 * (wn * NB + j) + (lane & 31)];
-#pragma unroll
-      for (int e = 0; e < 16; e++) fa[i][j][e] = __builtin_fmaf((float)ia[i][j][e], sa[e >> 2][e & 3] * sb, fa[i][j][e]);
+      for (int j = 0; j < NB; j++) sb[j] = s[256 + 32 * (wn * NB + j) + (lane & 31)];
     }
   };
+  auto add_tile = [&](int i, int j) {
+#pragma unroll
+    for (int e = 0; e < 16; e++) fa[i][j][e] = __builtin_fmaf((float)ia[i][j][e], sa[e >> 2][e & 3] * sb[j], fa[i][j][e]);
+    asm volatile("" : "+v"(fa[i][j]));                // (here and now: the compiler would keep all the integers for later)
+  };
 
-  // first steps of blocks among the next to be waited for
-  auto begins = [&](int step_in_slot) { return step_in_slot % kStepsPerBlock == 0; };
-  issue(0);
-  issue(1);
-  issue(2);
+  // One step, in a pinned order (the compiler would put each fragment's read right before its product): the second half's fragments are fetched beside the products
+  // of the first, the next step's first half beside those of the second, and copies issued there.
+  // BEGIN: the block's first step, whose products start from zero, and in front of each of them the tile's sums of the block before.
+  int slot_r = 0;
+  auto step = [&](auto is_first, int before) {
+    constexpr bool BEGIN = decltype(is_first)::value;
+    // step s + 1 has landed (no more than the copies of the steps behind it are under way, or fewer, where scales are among them); every wave is done with step s - 1
+    wait_vmem<(AHEAD - 2) * OPS>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int next_r = slot_r + SLOT == SLOTS * SLOT ? 0 : slot_r + SLOT;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < MB * NB; k++) {
+      const int i = k / NB, j = k % NB;
+      if constexpr (BEGIN) {
+        if (j == 0) scales_of(i, before);
+        add_tile(i, j);
+#pragma unroll
+        for (int e = 0; e < 16; e++) ia[i][j][e] = 0;
+      }
+      ia[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fra[0][i], frb[0][j], ia[i][j], 0, 0, 0);
+      if (k < MB + NB) fetch(1, slot_r, 1, k);
+      if (k == MB * NB - 1) begin();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int k = 0; k < MB * NB; k++) {
+      const int i = k / NB, j = k % NB;
+      ia[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fra[1][i], frb[1][j], ia[i][j], 0, 0, 0);
+      if (k < MB + NB) fetch(0, next_r, 0, k);
+      if (k < OPS) copy(k);
+      if (k == MB * NB - 1) done();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    slot_r = next_r;
+  };
+  static_assert(OPS <= MB * NB && MB + NB <= MB * NB, "a step's copies and fragments beside its products");
+  for (int i = 0; i < AHEAD; i++) {
+    begin();
+#pragma unroll
+    for (int k = 0; k < OPS; k++) copy(k);
+    done();
+  }
   wait_vmem<0>();
   __syncthreads();
-  fetch(0, 0, 0);
-  int block = -1, here = 0, ahead = 2 % p.steps;       // the block in work; steps since the slot's first, of this step and of the one after next
-  for (int s = 0; s < p.total; s++) {
-    // step s + 1 has landed (only step s + 2 may still be under way); every wave is done with step s - 1
-    if (begins(ahead)) wait_vmem<OPS + 2>(); else wait_vmem<OPS>();
-    __syncthreads();
-    issue(s + 3);
-    fetch(1, s, 1);
-    if (begins(here)) {
 #pragma unroll
-      for (int i = 0; i < MB; i++) {
-        if (block >= 0) add_block(i, block);
-#pragma unroll
-        for (int j = 0; j < NB; j++) {
-          i32x16 z;
-#pragma unroll
-          for (int e = 0; e < 16; e++) z[e] = 0;
-          ia[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fra[0][i], frb[0][j], z, 0, 0, 0);
-        }
-      }
-      block++;
-    } else {
-#pragma unroll
-      for (int i = 0; i < MB; i++)
-#pragma unroll
-        for (int j = 0; j < NB; j++) ia[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fra[0][i], frb[0][j], ia[i][j], 0, 0, 0);
-    }
-    fetch(0, s + 1, 0);
-#pragma unroll
-    for (int i = 0; i < MB; i++)
-#pragma unroll
-      for (int j = 0; j < NB; j++) ia[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fra[1][i], frb[1][j], ia[i][j], 0, 0, 0);
-    if (++here == p.steps) here = 0;
-    if (++ahead == p.steps) ahead = 0;
+  for (int k = 0; k < MB + NB; k++) fetch(0, 0, 0, k);
+  int block = 0, left = p.steps - in;                  // blocks since the share's first; steps left of the slot
+  for (int s = 0; s < total; block++) {
+    const int n = left < kStepsPerBlock ? left : kStepsPerBlock;
+    step(std::true_type(), block - 1);                 // (before the first block: zeros, by scales that are zeros)
+    for (int i = 1; i < n; i++) step(std::false_type(), 0);
+    s += n;
+    left = left == n ? p.steps : left - n;
   }
   wait_vmem<0>();                                      // (copies past the end: zeros)
+  if (p.shares > 1) {
+    f32x4* const part = reinterpret_cast<f32x4*>(p.part) + (((long)share * p.tiles_m * p.tiles_n + (long)tm * p.tiles_n + tn) * 4 + wave) * (MB * NB * 256) + lane;
+#pragma unroll
+    for (int i = 0; i < MB; i++) {
+      scales_of(i, block - 1);
+#pragma unroll
+      for (int j = 0; j < NB; j++) {
+        add_tile(i, j);
+#pragma unroll
+        for (int q = 0; q < 4; q++) part[((i * NB + j) * 4 + q) * 64] = f32x4{fa[i][j][4 * q], fa[i][j][4 * q + 1], fa[i][j][4 * q + 2], fa[i][j][4 * q + 3]};
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < MB; i++) {
-    if (block >= 0) add_block(i, block);
+    scales_of(i, block - 1);
 #pragma unroll
     for (int j = 0; j < NB; j++) {
+      add_tile(i, j);
       const int n = 32 * (ub_b + wn * NB + j) + (lane & 31);
       if (n < p.N) {
 #pragma unroll
@@ -306,18 +442,41 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   }
 }
 
+// The shares of a tile, added up in order: a thread has 4 elements of every share.
+template <int MB, int NB>
+__global__ __launch_bounds__(256) void stash8_join_kernel(Stash8Dw p) {
+  const long tiles = (long)p.tiles_m * p.tiles_n;
+  const int tile = (int)blockIdx.x / (MB * NB * 4), in = (int)blockIdx.x % (MB * NB * 4);      // 256 of a tile's 4 x MB NB x 256 threads
+  const int wave = in / (MB * NB), t = in % (MB * NB), lane = (int)threadIdx.x & 63, q = (int)threadIdx.x >> 6;
+  const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
+  const int m = 32 * (tm * 2 * MB + (wave >> 1) * MB + t / NB) + 8 * q + 4 * (lane >> 5), n = 32 * (tn * 2 * NB + (wave & 1) * NB + t % NB) + (lane & 31);
+  if (n >= p.N || m >= p.M) return;
+  const f32x4* const part = reinterpret_cast<const f32x4*>(p.part) + (tile * 4L + wave) * (MB * NB * 256) + (t * 4 + q) * 64 + lane;
+  f32x4 v = part[0];
+  for (int s = 1; s < p.shares; s++) v += part[s * tiles * 4 * (MB * NB * 256)];
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+    if (m + e < p.M) {
+      float* const o = p.dw + (long)(m + e) * p.ld + n;
+      *o = p.accumulate ? *o + v[e] : v[e];
+    }
+}
+
 // ------------------------------------------------------------------------------------------ launches
-hipError_t stash8_put(int dtype, const Stash8Slot& p, const void* x, long ld, hipStream_t s) {
-  const dim3 grid((unsigned)((p.cols + 63) / 64), (unsigned)p.blocks), block(512);
-  const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % (dtype ? 8 : 4) == 0;
-  if (dtype) {
-    if (wide) hipLaunchKernelGGL((stash8_put_kernel<bf16_t, true>), grid, block, 0, s, p, (const bf16_t*)x, ld);
-    else hipLaunchKernelGGL((stash8_put_kernel<bf16_t, false>), grid, block, 0, s, p, (const bf16_t*)x, ld);
-  } else {
-    if (wide) hipLaunchKernelGGL((stash8_put_kernel<float, true>), grid, block, 0, s, p, (const float*)x, ld);
-    else hipLaunchKernelGGL((stash8_put_kernel<float, false>), grid, block, 0, s, p, (const float*)x, ld);
-  }
+template <typename T, bool WIDE>
+static hipError_t launch_put(const Stash8Slot& p, const void* x, long ld, hipStream_t s) {
+  constexpr size_t smem = 8 * 8192 + 8 * 256 + 256;
+  auto kern = stash8_put_kernel<T, WIDE>;
+  static AttrOnce once;
+  if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)((p.cols + 63) / 64), (unsigned)p.blocks), dim3(512), smem, s, p, (const T*)x, ld);
   return hipGetLastError();
+}
+
+hipError_t stash8_put(int dtype, const Stash8Slot& p, const void* x, long ld, hipStream_t s) {
+  const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % (dtype ? 8 : 4) == 0;
+  if (dtype) return wide ? launch_put<bf16_t, true>(p, x, ld, s) : launch_put<bf16_t, false>(p, x, ld, s);
+  return wide ? launch_put<float, true>(p, x, ld, s) : launch_put<float, false>(p, x, ld, s);
 }
 
 hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStream_t s) {
@@ -333,26 +492,50 @@ hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStrea
   return hipGetLastError();
 }
 
-template <int MB, int NB>
+// Tiles of 96 x 96 to a wave and one workgroup to a compute unit, or of 64 x 64 and two, by the time that their rounds of workgroups take.  Shares of the
+// contraction where there are few tiles, each of whole blocks.
+Stash8Plan stash8_plan(int m, int n, int steps, int blocks) {
+  const long mb = (m + 31) / 32, nb = (n + 31) / 32;
+  const long large = ((mb + 5) / 6) * ((nb + 5) / 6), small = ((mb + 3) / 4) * ((nb + 3) / 4);
+  const float of_large = (float)((large + 255) / 256) * (0.603f * steps + 9.f), rest = (float)(small % 512);
+  const float of_small = (float)(small / 512) * (0.524f * steps + 8.f) + (rest ? (rest <= 256 ? 0.4f : 0.524f) * steps + 8.f : 0.f);
+  if (large >= 256 && of_large < of_small) return Stash8Plan{3, 3, 1, blocks, 0};
+  Stash8Plan r{2, 2, 1, blocks, 0};
+  long shares = 512 / small;
+  shares = shares < steps / 4 ? shares : steps / 4;
+  shares = shares < blocks ? shares : blocks;
+  if (shares >= 3) {
+    r.share = (int)((blocks + shares - 1) / shares);
+    r.shares = (blocks + r.share - 1) / r.share;
+    r.bytes = (size_t)r.shares * small * 128 * 128 * sizeof(float);
+  }
+  return r;
+}
+
+template <int MB, int NB, int PER_CU>
 static hipError_t launch_dw(Stash8Dw p, hipStream_t s) {
-  constexpr size_t smem = 4 * (2 * MB + 2 * NB) * kUnit + 8 * 2048;
-  auto kern = stash8_dw_kernel<MB, NB>;
+  constexpr size_t smem = dw_slots(MB, NB, PER_CU) * (2 * MB + 2 * NB) * kUnit + 8 * 2048;
+  auto kern = stash8_dw_kernel<MB, NB, PER_CU>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   p.tiles_m = (p.xb + 2 * MB - 1) / (2 * MB);
   p.tiles_n = (p.db + 2 * NB - 1) / (2 * NB);
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(256), smem, s, p);
+  const long tiles = (long)p.tiles_m * p.tiles_n;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * p.shares)), dim3(256), smem, s, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.shares == 1) return e;
+  hipLaunchKernelGGL((stash8_join_kernel<MB, NB>), dim3((unsigned)(tiles * MB * NB * 4)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t stash8_dw(const Stash8Slot& x, const Stash8Slot& dy, int n, float* dw, long ld, int accumulate, hipStream_t s) {
+hipError_t stash8_dw(const Stash8Slot& x, const Stash8Slot& dy, int n, float* dw, long ld, int accumulate, float* part, hipStream_t s) {
   Stash8Dw p{};
   p.x = x.data; p.xs = x.scales; p.xb = x.col_blocks; p.dy = dy.data; p.ds = dy.scales; p.db = dy.col_blocks;
   p.dw = dw; p.ld = ld; p.M = x.cols; p.N = dy.cols; p.accumulate = accumulate;
   p.steps = x.steps; p.blocks = x.blocks;
   p.first_step = (long)x.slot * x.steps; p.first_block = (long)x.slot * x.blocks; p.total = n * x.steps;
-  if (0) return launch_dw<4, 2>(p, s);
-  return launch_dw<3, 3>(p, s);
+  const Stash8Plan plan = stash8_plan(x.cols, dy.cols, p.total, n * x.blocks);
+  p.shares = plan.shares; p.share = plan.share; p.part = part;
+  return plan.mb == 3 ? launch_dw<3, 3, 1>(p, s) : launch_dw<2, 2, 2>(p, s);
 }
 
 }  // namespace tbp
