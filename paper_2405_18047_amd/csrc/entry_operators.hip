@@ -356,7 +356,7 @@ tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int hea
 
 int tbp_qk_norm_partial_rows(int rows, int n_heads, int n_kv_heads, int head_dim) {
   if (rows < 1 || n_heads < 0 || n_kv_heads < 0 || n_heads + (long)n_kv_heads < 1 || head_dim < 2) return 0;
-  return tbp::qk_norm_partial_rows(rows, (long)n_heads + n_kv_heads, head_dim);
+  return tbp::qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim);
 }
 
 tbp_status tbp_qk_norm_p1(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
@@ -375,7 +375,6 @@ tbp_status tbp_qk_norm_p1(int dtype, int rows, int n_heads, int n_kv_heads, int 
   if (dx == x) return fail(TBP_EINVAL, "dx may be dy, not x");
   tbp::QkNormParams p = qk_norm_params(rows, n_heads, n_kv_heads, head_dim, eps, gq, gk, rot_dim, layout, table, n_pos, positions, seq);
   p.x = x; p.ld_x = ld_x; p.dy = dy; p.ld_dy = ld_dy; p.y = dx; p.ld_y = ld_dx; p.partials = partials_out;
-  p.n_partials = tbp_qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim);
   TBP_HIP(tbp::qk_norm_p1(dtype, p, stream_of(stream)));
   return TBP_OK;
 }
@@ -410,7 +409,7 @@ static tbp_status check_packed(int dtype, int n_seqs, int rows, int n_heads, int
   if (check_heads(n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
   if (n_seqs < 0 || rows < 0) return fail(TBP_EINVAL, "negative size");
   if (rows > (1 << 22) || n_seqs > (1 << 20)) return fail(TBP_EINVAL, "rows above 2^22 or n_seqs above 2^20");
-  if ((long)n_heads * (rows / 64 + n_seqs + 1) >= (1L << 27)) return fail(TBP_EINVAL, "n_heads * (rows / 64 + n_seqs + 1) must be below 2^27");
+  if ((long)n_heads * (rows / 32 + n_seqs + 1) >= (1L << 27)) return fail(TBP_EINVAL, "n_heads * (rows / 32 + n_seqs + 1) must be below 2^27");
   return TBP_OK;
 }
 

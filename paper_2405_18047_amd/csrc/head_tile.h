@@ -23,6 +23,15 @@ struct HeadTile {
     const int G = (p % GPRW) ^ swz(row);
     goff = (unsigned)((long)row * ld * 2 + G * 16);
   }
+  // The same for an image whose rows are 32 rows of one head after the other: row r of the image is source row 32 (r / 32 / HEADS) + r % 32, head r / 32 % HEADS.
+  template <int HEADS> static __device__ __forceinline__ void plan_heads(int c, int p, long ld, int& row, unsigned& goff) {
+    plan(c, p, HEADS == 1 ? ld : 0, row, goff);
+    if constexpr (HEADS > 1) {
+      const int head = row / 32 % HEADS;
+      row = 32 * (row / 32 / HEADS) + row % 32;
+      goff += (unsigned)((long)row * ld * 2 + head * RB);
+    }
+  }
   // Per-lane byte offsets of the fragment reads, computed once per kernel (the swizzle makes them non-affine in the
   // k-step, so they are kept in registers; everything else - image, 32-row block, k-step pair - is an immediate).
   //   rows[s]: A-operand fragment of MFMA rows 0..31 of the image, contraction = columns 16 s .. 16 s + 15.

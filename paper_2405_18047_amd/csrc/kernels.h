@@ -302,14 +302,14 @@ struct QkNormParams {
   const float2* table; int n_pos;                    // half 0: none
   const int* positions; int seq;                     // position of row r: positions[r], or r % seq
   int rows, q_heads, kv_heads, dh, half, interleaved;
-  float* partials; int n_partials;                   // p1: [n_partials][2][dh]
+  float* partials; int n_partials, q_parts;          // p1: [n_partials][2][dh], the first q_parts of the query heads (set by the launch)
   // append only: x's heads are q_heads of q, kv_heads of k, kv_heads of v
   const int* lengths; int tokens_new;
   void* cache_k; void* cache_v; long ld_c; int capacity, sinks;
   int units, lanes, q_groups, kv_groups, row0; long items;      // set by the launch
 };
 constexpr int kQkNormMaxHead = 512, kQkNormPartials = 512;
-int qk_norm_partial_rows(int rows, int heads, int head_dim);
+int qk_norm_partial_rows(int rows, int q_heads, int kv_heads, int head_dim);
 hipError_t qk_norm(int dtype, const QkNormParams& p, hipStream_t s);
 hipError_t qk_norm_p1(int dtype, const QkNormParams& p, hipStream_t s);
 hipError_t qk_norm_append(int dtype, const QkNormParams& p, hipStream_t s);

@@ -5,10 +5,11 @@
 //   n = x r, r = 1 / sqrt(mean(x^2) + eps);  z = n g;  y = R z
 //   dz = R^T dy;  dn = dz g;  dx = r (dn - n mean(dn n)) = r dn - x r^3 mean(dn x);  dg = sum over tokens and heads of dz n
 //
-// A unit is 2 W columns of a head: of the rotated ones W and the W that they are paired with (half-split), or 2 W that hold whole pairs (interleaved); of
-// the others 2 W as they lie.  A group of lanes (a power of two) has one unit each (NU, one element at a time: up to NU) of one head, so that a head's sums are
-// a few lane exchanges, and takes HPT consecutive heads of one kind, which share angles and gains; all of them are loaded before the first is stored, so
-// that results may go where the operands came from.
+// A unit is two pieces of W columns, of the rotated ones or of the others, half of them apart: half-split positions pair the two, interleaved ones the columns within
+// each (W 1: the two columns of a pair).  A group of lanes (a power of two) has one unit each (W 1: up to NU) of one head, so that a head's sums are a few lane
+// exchanges, and takes HPT consecutive heads of one kind, which share angles and gains; all of them are loaded before the first is stored, so that
+// results may go where the operands came from.
+// Bound by memory: 8192 rows of 32 + 8 heads of 128, bf16, half-split, positions given: 33 us forward, 168 MB, 5.1 TB/s; 50 us backward, 252 MB, 5.0 TB/s.
 #include "kernels.h"
 #include "rows.h"
 
@@ -19,6 +20,7 @@ namespace tbp {
 // Columns and angles of a lane's units.
 template <typename T, int W, int NU, bool INTERLEAVED>
 struct Units {
+  static constexpr bool PAIRS = INTERLEAVED && W == 1;      // a pair is the unit's two columns side by side
   int first[NU], second[NU];                       // columns of the two pieces
   bool there[NU], turns[NU];
   float cs[NU][W], sn[NU][W];
@@ -29,8 +31,9 @@ struct Units {
       const int u = l + i * p.lanes;
       there[i] = u < p.units;
       turns[i] = u < rot;
-      first[i] = !INTERLEAVED && turns[i] ? u * W : 2 * u * W;
-      second[i] = !INTERLEAVED && turns[i] ? p.half + u * W : first[i] + W;
+      const int start = turns[i] ? 0 : 2 * p.half, apart = turns[i] ? p.half : p.dh / 2 - p.half, at = (turns[i] ? u : u - rot) * W;
+      first[i] = PAIRS ? 2 * u : start + at;
+      second[i] = PAIRS ? 2 * u + 1 : start + apart + at;
     }
   }
   __device__ __forceinline__ void angles(const QkNormParams& p, int l, int pos) {
@@ -38,12 +41,21 @@ struct Units {
 #pragma unroll
     for (int i = 0; i < NU; i++) {
       if (!turns[i]) continue;
-      const float2* const tb = p.table + (known ? (long)pos * p.half + (l + i * p.lanes) * W : 0);
+      const float2* const tb = p.table + (known ? (long)pos * p.half : 0);
+      const int u = l + i * p.lanes;
+      if constexpr (W > 1) {                       // (whole pieces: 16-byte aligned)
 #pragma unroll
-      for (int k = 0; k < W; k++) {
-        const float2 t = tb[k];
-        cs[i][k] = known ? t.x : __builtin_nanf("");
-        sn[i][k] = known ? t.y : __builtin_nanf("");
+        for (int k = 0; k < W; k += 2) {
+          const f32x4 t = *reinterpret_cast<const f32x4*>(tb + (!INTERLEAVED ? u * W + k : (k < W / 2 ? first[i] : second[i] - W) / 2 + k));
+          cs[i][k] = t[0]; sn[i][k] = t[1]; cs[i][k + 1] = t[2]; sn[i][k + 1] = t[3];
+        }
+      } else {
+        cs[i][0] = tb[u].x;
+        sn[i][0] = tb[u].y;
+      }
+      if (!known) {
+#pragma unroll
+        for (int k = 0; k < W; k++) cs[i][k] = sn[i][k] = __builtin_nanf("");
       }
     }
   }
@@ -152,24 +164,29 @@ __global__ __launch_bounds__(256) void qk_norm_kernel(QkNormParams p) {
     for (int i = 0; i < NU; i++) if (k < hn && un.there[i]) x[k][i].store(dst + (long)k * p.dh, un.first[i], un.second[i]);
 }
 
-// backward-p1: a workgroup walks (row, heads) items and leaves one partial row of the gains' gradient, [2][dh]: summed over a lane's items first, then over
-// the lanes of a wave that have the same columns, then over the waves in order: the same result every time.
+// backward-p1: the first q_parts workgroups walk (row, query heads) items, the others (row, key heads), and each leaves one partial row of the gains' gradient,
+// [2][dh], zeros for the other kind: summed over a lane's items first, then over the lanes of a wave that have the same columns, then over the waves
+// in order: the same result every time.
 template <typename T, int W, int NU, int HPT, bool INTERLEAVED>
-__global__ __launch_bounds__(512) void qk_norm_p1_kernel(QkNormParams p) {
-  extern __shared__ float sums[];                  // [8 waves][2][dh]
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void qk_norm_p1_kernel(QkNormParams p) {
+  extern __shared__ float sums[];                  // [8 waves][dh]
   const int l = (int)threadIdx.x & (p.lanes - 1), per = 512 / p.lanes;
-  const int groups = p.q_groups + p.kv_groups;
+  const bool kind = (int)blockIdx.x >= p.q_parts;
+  const int groups = kind ? p.kv_groups : p.q_groups, heads = kind ? p.kv_heads : p.q_heads;
+  const int parts = kind ? (int)gridDim.x - p.q_parts : p.q_parts, part = (int)blockIdx.x - (kind ? p.q_parts : 0);
   Units<T, W, NU, INTERLEAVED> un(p, l);
-  float dg[2][NU][2 * W];
+  const T* const gain = (const T*)(kind ? p.gk : p.gq);
+  float g[NU][2 * W], dg[NU][2 * W];
 #pragma unroll
-  for (int i = 0; i < NU; i++)
+  for (int i = 0; i < NU; i++) {
+    if (un.there[i]) load_gain<T, W>(gain, un.first[i], un.second[i], g[i]);
 #pragma unroll
-    for (int c = 0; c < 2 * W; c++) dg[0][i][c] = dg[1][i][c] = 0.f;
+    for (int c = 0; c < 2 * W; c++) dg[i][c] = 0.f;
+  }
   const float over = 1.f / (float)p.dh;
-  for (long at = (long)blockIdx.x * per + threadIdx.x / p.lanes; at < p.items; at += (long)gridDim.x * per) {
-    const int row = (int)(at / groups), hg = (int)(at - (long)row * groups);
-    const int kind = hg >= p.q_groups;
-    const int h0 = (hg - (kind ? p.q_groups : 0)) * HPT, heads = kind ? p.kv_heads : p.q_heads;
+  const long items = (long)p.rows * groups;
+  for (long at = (long)part * per + threadIdx.x / p.lanes; at < items; at += (long)parts * per) {
+    const int row = (int)(at / groups), h0 = (int)(at - (long)row * groups) * HPT;
     const int hn = heads - h0 < HPT ? heads - h0 : HPT;
     const int column = ((kind ? p.q_heads : 0) + h0) * p.dh;
     Unit<T, W> x[HPT][NU], d[HPT][NU];
@@ -182,16 +199,7 @@ __global__ __launch_bounds__(512) void qk_norm_p1_kernel(QkNormParams p) {
         x[k][i].load(src + (long)k * p.dh, un.first[i], un.second[i]);
         d[k][i].load(dsrc + (long)k * p.dh, un.first[i], un.second[i]);
       }
-    const T* const gain = (const T*)(kind ? p.gk : p.gq);
-    float g[NU][2 * W];
-#pragma unroll
-    for (int i = 0; i < NU; i++) if (un.there[i]) load_gain<T, W>(gain, un.first[i], un.second[i], g[i]);
     un.angles(p, l, p.positions ? p.positions[row] : row % p.seq);
-    float sum[NU][2 * W];                          // of dz n over this item's heads
-#pragma unroll
-    for (int i = 0; i < NU; i++)
-#pragma unroll
-      for (int c = 0; c < 2 * W; c++) sum[i][c] = 0.f;
 #pragma unroll
     for (int k = 0; k < HPT; k++) {
       if (k >= hn) break;
@@ -211,18 +219,12 @@ __global__ __launch_bounds__(512) void qk_norm_p1_kernel(QkNormParams p) {
         float o[2 * W];
 #pragma unroll
         for (int c = 0; c < 2 * W; c++) {
-          sum[i][c] += dz[i][c] * (v[i][c] * r);
+          dg[i][c] += dz[i][c] * (v[i][c] * r);
           o[c] = r * (dz[i][c] * g[i][c] - v[i][c] * back);
         }
         d[k][i].set(o);
       }
     }
-#pragma unroll
-    for (int i = 0; i < NU; i++)
-#pragma unroll
-      for (int c = 0; c < 2 * W; c++) {
-        if (kind) dg[1][i][c] += sum[i][c]; else dg[0][i][c] += sum[i][c];
-      }
     T* const dst = (T*)p.y + (long)row * p.ld_y + column;
 #pragma unroll
     for (int k = 0; k < HPT; k++)
@@ -231,20 +233,21 @@ __global__ __launch_bounds__(512) void qk_norm_p1_kernel(QkNormParams p) {
   }
   const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
 #pragma unroll
-  for (int kind = 0; kind < 2; kind++)
+  for (int i = 0; i < NU; i++)
 #pragma unroll
-    for (int i = 0; i < NU; i++)
-#pragma unroll
-      for (int c = 0; c < 2 * W; c++) {
-        float s = dg[kind][i][c];
-        for (int o = p.lanes; o < 64; o *= 2) s += __shfl_xor(s, o);
-        if (lane < p.lanes && un.there[i]) sums[(wave * 2 + kind) * p.dh + (c < W ? un.first[i] + c : un.second[i] + c - W)] = s;
-      }
+    for (int c = 0; c < 2 * W; c++) {
+      float s = dg[i][c];
+      for (int o = p.lanes; o < 64; o *= 2) s += __shfl_xor(s, o);
+      if (lane < p.lanes && un.there[i]) sums[wave * p.dh + (c < W ? un.first[i] + c : un.second[i] + c - W)] = s;
+    }
   __syncthreads();
   for (int c = (int)threadIdx.x; c < 2 * p.dh; c += 512) {
+    const bool k = c >= p.dh;
     float s = 0.f;
+    if (k == kind) {
 #pragma unroll
-    for (int w = 0; w < 8; w++) s += sums[w * 2 * p.dh + c];
+      for (int w = 0; w < 8; w++) s += sums[w * p.dh + (k ? c - p.dh : c)];
+    }
     p.partials[(long)blockIdx.x * 2 * p.dh + c] = s;
   }
 }
@@ -261,7 +264,7 @@ template <typename T>
 static bool wide(const QkNormParams& p) {
   constexpr int W = 16 / sizeof(T);
   const uintptr_t bits = (uintptr_t)p.x | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.cache_k | (uintptr_t)p.cache_v |
-                         (uintptr_t)p.gq | (uintptr_t)p.gk | (uintptr_t)((p.ld_x | p.ld_y | p.ld_dy | p.ld_c) * sizeof(T));
+                         (uintptr_t)p.gq | (uintptr_t)p.gk | (uintptr_t)p.table | (uintptr_t)((p.ld_x | p.ld_y | p.ld_dy | p.ld_c) * sizeof(T));
   return bits % 16 == 0 && p.half % W == 0 && (p.dh - 2 * p.half) % (2 * W) == 0;
 }
 
@@ -282,14 +285,24 @@ static hipError_t launch_fwd(QkNormParams p, hipStream_t s) {
   return hipSuccess;
 }
 
+int qk_norm_partial_rows(int rows, int q_heads, int kv_heads, int head_dim) {
+  const long n = ((long)rows * ((long)q_heads + kv_heads) * head_dim + 4095) / 4096, least = q_heads && kv_heads ? 2 : 1;
+  return (int)(n < least ? least : n < kQkNormPartials ? n : kQkNormPartials);
+}
+
 template <typename T, int W, int NU, int HPT, bool INTERLEAVED>
 static hipError_t launch_p1(QkNormParams p, hipStream_t s) {
   p.units = p.dh / (2 * W);
   p.lanes = lanes_of(p.units);
   p.q_groups = (p.q_heads + HPT - 1) / HPT;
   p.kv_groups = (p.kv_heads + HPT - 1) / HPT;
-  p.items = (long)p.rows * (p.q_groups + p.kv_groups);
-  hipLaunchKernelGGL((qk_norm_p1_kernel<T, W, NU, HPT, INTERLEAVED>), dim3((unsigned)p.n_partials), dim3(512), 16 * p.dh * sizeof(float), s, p);
+  p.n_partials = qk_norm_partial_rows(p.rows, p.q_heads, p.kv_heads, p.dh);
+  p.q_parts = p.n_partials;
+  if (p.kv_heads) {
+    const long share = ((long)p.n_partials * p.q_groups + (p.q_groups + p.kv_groups) / 2) / (p.q_groups + p.kv_groups);
+    p.q_parts = !p.q_heads ? 0 : share < 1 ? 1 : share < p.n_partials ? (int)share : p.n_partials - 1;
+  }
+  hipLaunchKernelGGL((qk_norm_p1_kernel<T, W, NU, HPT, INTERLEAVED>), dim3((unsigned)p.n_partials), dim3(512), 8 * p.dh * sizeof(float), s, p);
   return hipGetLastError();
 }
 
@@ -308,13 +321,7 @@ template <typename T>
 static hipError_t backward(const QkNormParams& p, hipStream_t s) {
   constexpr int W = 16 / sizeof(T);
   if (!wide<T>(p)) return p.interleaved ? launch_p1<T, 1, 4, 1, true>(p, s) : launch_p1<T, 1, 4, 1, false>(p, s);
-  if (four_heads(p, W)) return p.interleaved ? launch_p1<T, W, 1, 4, true>(p, s) : launch_p1<T, W, 1, 4, false>(p, s);
   return p.interleaved ? launch_p1<T, W, 1, 1, true>(p, s) : launch_p1<T, W, 1, 1, false>(p, s);
-}
-
-int qk_norm_partial_rows(int rows, int heads, int head_dim) {
-  const long n = ((long)rows * heads * head_dim + 8191) / 8192;
-  return (int)(n < kQkNormPartials ? n : kQkNormPartials);
 }
 
 hipError_t qk_norm(int dtype, const QkNormParams& p, hipStream_t s) { return dtype ? forward<bf16_t, false>(p, s) : forward<float, false>(p, s); }

@@ -41,10 +41,10 @@ struct KeyBlocks {
 };
 
 // Sequences that lie one behind the other (PACKED): sequence b has the rows starts[b] .. starts[b + 1] - 1 of `rows`, all causal; lse and delta are [H][rows].
-// Blocks of BQ queries (or keys) are numbered without a look at all lengths: sequence b's are those from starts[b] / BQ + b on, whose places do not
-// overlap since a sequence of n tokens has at most (starts[b + 1] / BQ - starts[b] / BQ) + 1 blocks.  Numbers that no block has end at once; the rows behind
-// the last sequence are a sequence without tokens, whose results are zeros.  Starts are taken as 0 .. rows and the first as 0.
+// The rows behind the last sequence are one without tokens, whose results are zeros.  Starts are taken as 0 .. rows and the first as 0.
+// A launch has as many numbers of blocks (of queries, or of keys) as any lengths may need; those that no block has end at once.
 struct Packed { const int* starts; int seqs, rows; };
+constexpr int kMostFirst = 16;
 inline __host__ __device__ long packed_blocks(const Packed& p, int block) { return (long)p.rows / block + p.seqs + 1; }
 
 __device__ __forceinline__ int packed_start(const Packed& p, int b) {
@@ -53,11 +53,15 @@ __device__ __forceinline__ int packed_start(const Packed& p, int b) {
 }
 
 // The sequence of a workgroup and its block in it.  n: tokens; S: rows to be written.
+// LAST: query blocks, whose last ones have the most to do and come first; else key blocks, and their first ones.
 struct SeqOf {
   long tok0; int n, S, block;
-  template <int BLOCK> __device__ __forceinline__ static SeqOf packed(const Packed& p, int number) {
-    // the last of the sequences 0 .. seqs (the rows behind them) whose numbers begin at or before this one, 64 at a time
+  // Sequence b's blocks are the numbers from starts[b] / BLOCK + b on, whose places do not overlap since a sequence has at most
+  // (starts[b + 1] / BLOCK - starts[b] / BLOCK) + 1 blocks.
+  template <int BLOCK, bool LAST> __device__ __forceinline__ static SeqOf in_order(const Packed& p, int number) {
     const int lane = threadIdx.x & 63;
+    if (LAST) number = (int)packed_blocks(p, BLOCK) - 1 - number;
+    // the last of the sequences 0 .. seqs (the rows behind them) that begins at or before this number, 64 at a time
     int lo = 0, size = p.seqs + 1;
     while (size > 1) {
       const int step = (size + 63) / 64, b = lo + lane * step;
@@ -71,6 +75,57 @@ struct SeqOf {
     const int first = packed_start(p, lo), end = lo < p.seqs ? packed_start(p, lo + 1) : p.rows;
     const int S = end > first ? end - first : 0;
     return SeqOf{first, lo < p.seqs ? S : 0, S, number - first / BLOCK - lo};
+  }
+  // Key blocks by what they have to do, the most first, for up to 64 sequences, a lane each.
+  template <int BLOCK> __device__ __forceinline__ static SeqOf most_first(const Packed& p, int number) {
+    const int lane = threadIdx.x & 63;
+    const int first = lane < p.seqs ? packed_start(p, lane) : 0, end = lane < p.seqs ? packed_start(p, lane + 1) : 0;
+    const int blocks = end > first ? (end - first + BLOCK - 1) / BLOCK : 0;
+    int all = 0, who = 0, block = 0;
+    if (p.seqs <= kMostFirst) {
+      // whatever sequence they are of: F(j) of them have more than j blocks of their sequence from them on, and those of one j go by their
+      // sequence; 64 values of F at a time, a lane each
+      int lo = 0, step = 1, beyond = 0;            // F(lo) > number >= F(lo + 1) = beyond
+      while (64 * step <= p.rows / BLOCK + 1) step *= 32;
+      for (bool top = true;; top = false) {
+        const int j = lo + lane * step;
+        int f = 0;
+        for (int s = 0; s < p.seqs; s++) {
+          const int over = __builtin_amdgcn_readlane(blocks, s) - j;
+          f += over > 0 ? over : 0;
+        }
+        if (top) all = __builtin_amdgcn_readfirstlane(f);
+        if (number >= all) break;
+        const int last = 63 - __builtin_clzll(__ballot(f > number));      // (below 63: F of the 64th is 0)
+        lo += last * step;
+        beyond = __builtin_amdgcn_readlane(f, last + 1);
+        if (step == 1) break;
+        step /= 32;
+      }
+      const unsigned long long has = __ballot(blocks > lo);
+      const bool mine = blocks > lo && __builtin_amdgcn_mbcnt_hi((unsigned)(has >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)has, 0)) == (unsigned)(number - beyond);
+      who = __builtin_ctzll(__ballot(mine) | 1ull << 63);
+      block = __builtin_amdgcn_readlane(blocks, who) - 1 - lo;
+    } else {
+      // by their sequence, the longest first
+      int at = 0;
+      for (int s = 0; s < p.seqs; s++) {
+        const int b = __builtin_amdgcn_readlane(blocks, s);
+        at += b > blocks || (b == blocks && s < lane) ? b : 0;
+        all += b;
+      }
+      who = __builtin_ctzll(__ballot(number >= at && number < at + blocks) | 1ull << 63);
+      block = number - __builtin_amdgcn_readlane(at, who);
+    }
+    if (number >= all) {
+      const int behind = p.seqs ? packed_start(p, p.seqs) : 0;
+      return SeqOf{behind, 0, p.rows - behind, number - all};
+    }
+    const int at = __builtin_amdgcn_readlane(first, who), n = __builtin_amdgcn_readlane(end, who) - at;
+    return SeqOf{at, n, n, block};
+  }
+  template <int BLOCK> __device__ __forceinline__ static SeqOf keys(const Packed& p, int number) {
+    return p.seqs <= 64 ? most_first<BLOCK>(p, number) : in_order<BLOCK, false>(p, number);
   }
 };
 
@@ -87,12 +142,12 @@ struct WinParams {
 // Workgroup ids run over (sequence, key head) fastest, then over the query heads of the key head, query blocks slowest: the heads
 // that read the same keys then sit on one XCD (ids go round the 8 XCDs) wherever the number of key heads is a multiple of 8.
 struct HeadOf {
-  int b, h, hk;
-  __device__ __forceinline__ HeadOf(int x, int B, int KV, int G) {
-    const int u = x % (B * KV), gq = x / (B * KV);
+  int b, hk, gq;                       // gq: of the key head's query heads (or groups of them)
+  __device__ __forceinline__ HeadOf(int x, int B, int KV) {
+    const int u = x % (B * KV);
+    gq = x / (B * KV);
     b = u / KV;
     hk = u - b * KV;
-    h = hk * G + gq;
   }
 };
 
@@ -107,10 +162,13 @@ struct HeadOf {
 // edges).  Left out of it again: tiles of 32 keys that a wave's queries do not see, one by one (two copies of the block's code, 165 us for 152).  No more than
 // the registers bounds the workgroups of a compute unit: head_dim 64, window 256, 4 sequences of 2048, 32 heads
 // 49.1 us with two, 38.4 with four.
-template <int DH, bool AHEAD, int SPLIT, bool PACKED>
+// HW: query heads of one key head that a workgroup has (PACKED), 128 / SPLIT / HW queries of each: short sequences then leave less of a block empty,
+// and less of what a block computes lies behind its queries.
+template <int DH, bool AHEAD, int SPLIT, int HW, bool PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
-  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT, NT = 2 / SPLIT;
+  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, QW = 4 / SPLIT, NT = 2 / SPLIT;
+  constexpr int ROWS = 128 / SPLIT, BQ = ROWS / HW;   // (query, head) rows and queries of the workgroup
   constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
   constexpr int NCH = IMG / 1024 / 4;                 // copies per wave per operand per block
 
@@ -120,15 +178,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 
   const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int x = PACKED ? (int)blockIdx.x % p.H : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / p.H : (int)blockIdx.y;
-  int qb = (PACKED ? (int)gridDim.x / p.H : (int)gridDim.y) - 1 - y;             // last query blocks first: the first ones may have short windows
-  const HeadOf at(x, p.B, p.KV, p.G);
-  const int b = at.b, h = at.h;
-  SeqOf seq{(long)b * p.S, 0, p.S, qb};
-  if constexpr (PACKED) { seq = SeqOf::packed<BQ>(p.packed, qb); qb = seq.block; }
-  const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
+  const int x = PACKED ? (int)blockIdx.x % (p.H / HW) : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / (p.H / HW) : (int)blockIdx.y;
+  int qb = PACKED ? y : (int)gridDim.y - 1 - y;                     // last query blocks first: the first ones may have short windows
+  const HeadOf at(x, p.B, p.KV);
   const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
-  const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
+  const int b = at.b, h0 = (at.hk * (p.G / HW) + at.gq) * HW, h = h0 + wq % HW;       // the workgroup's first query head, the wave's
+  SeqOf seq{(long)b * p.S, 0, p.S, qb};
+  if constexpr (PACKED) { seq = SeqOf::in_order<BQ, true>(p.packed, qb); qb = seq.block; }
+  const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
+  const int q0 = qb * BQ, qw0 = q0 + 32 * (wq / HW), query = qw0 + ql;
   const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
   const int n = PACKED ? seq.n : seq_end(p.lengths, b, p.S);
   constexpr int LPR = DH / 8, RPI = 64 / LPR;                       // lanes per row and rows per wave-wide store
@@ -153,11 +211,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   };
   // ---- the block's query rows: copied (coalesced) into the second slot, which nothing else uses until they have been read
   {
-    const u32x4 dq = rows_desc(q0, BQ, (long)h * DH);
+    const u32x4 dq = rows_desc(q0, BQ, (long)h0 * DH);
 #pragma unroll
     for (int i = 0; i < 2 * NCH / SPLIT; i++) {
       int row; unsigned go;
-      HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
+      HT::template plan_heads<HW>(wave + 4 * i, lane, p.ld_qkv, row, go);
       dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dq, q0 + row < n ? go : kOob);
     }
   }
@@ -315,14 +373,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   // ---- o = O^T / l, transposed back through LDS (rows padded against bank conflicts) and written as whole rows
   __syncthreads();
   constexpr int EROW = DH * 2 + 16;
-  static_assert(BQ * EROW <= 2 * SLOT, "the output tile must fit in the ring");
+  static_assert(ROWS * EROW <= 2 * SLOT, "the output tile must fit in the ring");
   lds_u8* const erow = lds + 32 * wq * EROW;
   float lq = (l[0] + l[1]) + xor32(l[0] + l[1]);
   if constexpr (SPLIT == 2) {
     // the two waves of a query: what the second one summed, brought to the common reference point, joins the first one's
-    static_assert(BQ * EROW + 1024 <= SLOT && QW * DT * 4096 <= SLOT, "output tile, statistics and partial sums side by side");
+    static_assert(ROWS * EROW + 1024 <= SLOT && QW * DT * 4096 <= SLOT, "output tile, statistics and partial sums side by side");
     LDS_AS float* const part = reinterpret_cast<LDS_AS float*>(lds + SLOT) + wq * (DT * 1024);
-    LDS_AS float* const stat = reinterpret_cast<LDS_AS float*>(lds + BQ * EROW) + wq * 128;
+    LDS_AS float* const stat = reinterpret_cast<LDS_AS float*>(lds + ROWS * EROW) + wq * 128;
     if (wk == 1) {
 #pragma unroll
       for (int t = 0; t < DT; t++)
@@ -384,10 +442,11 @@ struct WinDqParams {
   float scale, scale_log2e;
 };
 
-template <int DH, int SPLIT, bool PACKED>
+template <int DH, int SPLIT, int HW, bool PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_bwd_dq_kernel(WinDqParams p) {
   using HT = HeadTile<DH>;
-  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, BQ = 128 / SPLIT, QW = 4 / SPLIT;
+  constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, QW = 4 / SPLIT;
+  constexpr int ROWS = 128 / SPLIT, BQ = ROWS / HW;
   constexpr int IMG = BKV * HT::RB, SLOT = 2 * IMG;
   constexpr int NCH = IMG / 1024 / 4;
 
@@ -397,15 +456,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 
   const int lane = threadIdx.x & 63, ql = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int x = PACKED ? (int)blockIdx.x % p.H : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / p.H : (int)blockIdx.y;
-  int qb = (PACKED ? (int)gridDim.x / p.H : (int)gridDim.y) - 1 - y;
-  const HeadOf at(x, p.B, p.KV, p.G);
-  const int b = at.b, h = at.h;
+  const int x = PACKED ? (int)blockIdx.x % (p.H / HW) : (int)blockIdx.x, y = PACKED ? (int)blockIdx.x / (p.H / HW) : (int)blockIdx.y;
+  int qb = PACKED ? y : (int)gridDim.y - 1 - y;
+  const HeadOf at(x, p.B, p.KV);
+  const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
+  const int b = at.b, h0 = (at.hk * (p.G / HW) + at.gq) * HW, h = h0 + wq % HW;       // the workgroup's first query head, the wave's
   SeqOf seq{(long)b * p.S, 0, p.S, qb};
-  if constexpr (PACKED) { seq = SeqOf::packed<BQ>(p.packed, qb); qb = seq.block; }
+  if constexpr (PACKED) { seq = SeqOf::in_order<BQ, true>(p.packed, qb); qb = seq.block; }
   const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
-  const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;
-  const int q0 = qb * BQ, qw0 = q0 + 32 * wq, query = qw0 + ql;
+  const int q0 = qb * BQ, qw0 = q0 + 32 * (wq / HW), query = qw0 + ql;
   const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
   const int n = PACKED ? seq.n : seq_end(p.lengths, b, p.S);
   constexpr int LPR = DH / 8, RPI = 64 / LPR;
@@ -427,12 +486,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   };
   // ---- the block's query rows into the second slot and their output derivatives into the first (coalesced copies)
   {
-    const u32x4 dq = rows_desc(p.qkv, p.ld_qkv, q0, BQ, (long)h * DH), dd = rows_desc(p.dout, p.ld_do, q0, BQ, (long)h * DH);
+    const u32x4 dq = rows_desc(p.qkv, p.ld_qkv, q0, BQ, (long)h0 * DH), dd = rows_desc(p.dout, p.ld_do, q0, BQ, (long)h0 * DH);
 #pragma unroll
     for (int i = 0; i < 2 * NCH / SPLIT; i++) {
       int row; unsigned go, gd;
-      HT::plan(wave + 4 * i, lane, p.ld_qkv, row, go);
-      HT::plan(wave + 4 * i, lane, p.ld_do, row, gd);
+      HT::template plan_heads<HW>(wave + 4 * i, lane, p.ld_qkv, row, go);
+      HT::template plan_heads<HW>(wave + 4 * i, lane, p.ld_do, row, gd);
       const bool ok = q0 + row < n;
       dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dq, ok ? go : kOob);
       dma16(lds0 + (wave + 4 * i) * 1024, dd, ok ? gd : kOob);
@@ -476,11 +535,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   issue(0);
   // ---- delta: the block's rows of the output arrive in the second slot beside the first key block
   {
-    const u32x4 dr = rows_desc(p.out, p.ld_do, q0, BQ, (long)h * DH);
+    const u32x4 dr = rows_desc(p.out, p.ld_do, q0, BQ, (long)h0 * DH);
 #pragma unroll
     for (int i = 0; i < 2 * NCH / SPLIT; i++) {
       int row; unsigned go;
-      HT::plan(wave + 4 * i, lane, p.ld_do, row, go);
+      HT::template plan_heads<HW>(wave + 4 * i, lane, p.ld_do, row, go);
       dma16(lds0 + SLOT + (wave + 4 * i) * 1024, dr, q0 + row < n ? go : kOob);
     }
   }
@@ -571,7 +630,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     if (wk == 1) return;
   }
   constexpr int EROW = DH * 2 + 16;
-  static_assert(BQ * EROW <= 2 * SLOT, "the output tile must fit in the ring");
+  static_assert(ROWS * EROW <= 2 * SLOT, "the output tile must fit in the ring");
   lds_u8* const erow = lds + 32 * wq * EROW;
 #pragma unroll
   for (int t = 0; t < DT; t++)
@@ -655,7 +714,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
   const int yy = sink_block ? y : y - (PACKED ? 0 : p.parts.sink_blocks * p.parts.sink_parts);
   const int number = yy / np + (PACKED || sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::packed<KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::keys<KEYS>(p.packed, number);
   const int kb = seq.block, S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int kv0 = kb * KEYS, kw0 = kv0 + 32 * kblk, key = kw0 + kl;
   const long tok0 = seq.tok0;
@@ -960,7 +1019,7 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   const int number = !PACKED && p.parts.sink_parts == 1 ? cut + p.parts.sink_blocks : cut;       // (blocks that are cut: the sinks', the others', or all)
   const int b = PACKED ? 0 : (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::packed<KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::keys<KEYS>(p.packed, number);
   const int kb = seq.block;
   const int which = (int)threadIdx.x / (ROWS * LPR), t = (int)threadIdx.x % (ROWS * LPR);
   const int row = ((PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) % per) * ROWS + t / LPR, col = 8 * (t % LPR);
@@ -1222,13 +1281,13 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <int DH, bool AHEAD, int SPLIT, bool PACKED = false>
+template <int DH, bool AHEAD, int SPLIT, int HW = 1, bool PACKED = false>
 static hipError_t launch_fwd(const WinParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
-  auto kern = window_fwd_kernel<DH, AHEAD, SPLIT, PACKED>;
+  auto kern = window_fwd_kernel<DH, AHEAD, SPLIT, HW, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  const dim3 grid = PACKED ? dim3((unsigned)(p.H * packed_blocks(p.packed, 128 / SPLIT))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  const dim3 grid = PACKED ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
   hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
@@ -1251,13 +1310,13 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
   return w.seq <= 256 || w.window <= 512 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<128, true, 1>(p, s);
 }
 
-template <int DH, int SPLIT, bool PACKED = false>
+template <int DH, int SPLIT, int HW = 1, bool PACKED = false>
 static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
-  auto kern = window_bwd_dq_kernel<DH, SPLIT, PACKED>;
+  auto kern = window_bwd_dq_kernel<DH, SPLIT, HW, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  const dim3 grid = PACKED ? dim3((unsigned)(p.H * packed_blocks(p.packed, 128 / SPLIT))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  const dim3 grid = PACKED ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
   hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
@@ -1344,16 +1403,29 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
 // ---- packed sequences: the same kernels, by rules on the mean length, since the lengths are on the device
 static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, w.rows}; }
 
+template <int N> using Int = std::integral_constant<int, N>;
+// run(head_dim, query heads of a workgroup): as many as their number allows
+template <typename F> static hipError_t by_heads(const PackedShape& w, F run) {
+  const int G = w.heads / w.kv_heads;
+  if (w.head_dim == 64) return G % 4 == 0 ? run(Int<64>(), Int<4>()) : G % 2 == 0 ? run(Int<64>(), Int<2>()) : run(Int<64>(), Int<1>());
+  return G % 4 == 0 ? run(Int<128>(), Int<4>()) : G % 2 == 0 ? run(Int<128>(), Int<2>()) : run(Int<128>(), Int<1>());
+}
+
 hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s) {
   WinParams p{};
   p.qkv = (const bf16_t*)qkv; p.ld_qkv = ld_qkv; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.packed = packed_of(w);
   p.B = 1; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.rows;
   p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
-  const long blocks = w.rows / 128 + w.seqs, groups = w.heads * blocks;
-  const bool few = groups <= (w.head_dim == 64 ? 512 : 256);
-  if (few) return w.head_dim == 128 ? launch_fwd<128, false, 2, true>(p, s) : launch_fwd<64, false, 2, true>(p, s);
-  if (w.head_dim == 64) return launch_fwd<64, false, 1, true>(p, s);
-  return w.rows / (w.seqs > 0 ? w.seqs : 1) <= 256 ? launch_fwd<128, false, 1, true>(p, s) : launch_fwd<128, true, 1, true>(p, s);
+  const long groups = w.heads * ((long)w.rows / 128 + w.seqs);
+  const int mean = w.rows / (w.seqs > 0 ? w.seqs : 1);
+  const bool few = groups <= (w.head_dim == 64 ? 512 : 256), ahead = w.head_dim == 128 && mean > 256;
+  auto run = [&](auto dh, auto hw) {
+    constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
+    if (few) return launch_fwd<DH, false, 2, HW < 2 ? 1 : 2, true>(p, s);
+    if constexpr (DH == 128) if (ahead) return launch_fwd<DH, true, 1, HW, true>(p, s);
+    return launch_fwd<DH, false, 1, HW, true>(p, s);
+  };
+  return by_heads(w, run);
 }
 
 // Keys to a block and parts of a block's list of (query head, query step) pairs.
@@ -1381,10 +1453,11 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
   q.B = 1; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.rows;
   q.scale = 1.f / sqrtf((float)w.head_dim);
   q.scale_log2e = 1.4426950408889634f * q.scale;
-  const long groups = (long)w.heads * (w.rows / 128 + w.seqs);
-  hipError_t e;
-  if (groups <= (w.head_dim == 64 ? 512 : 256)) e = w.head_dim == 128 ? launch_dq<128, 2, true>(q, s) : launch_dq<64, 2, true>(q, s);
-  else e = w.head_dim == 128 ? launch_dq<128, 1, true>(q, s) : launch_dq<64, 1, true>(q, s);
+  const bool few = (long)w.heads * (w.rows / 128 + w.seqs) <= (w.head_dim == 64 ? 512 : 256);
+  hipError_t e = by_heads(w, [&](auto dh, auto hw) {
+    constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
+    return few ? launch_dq<DH, 2, HW < 2 ? 1 : 2, true>(q, s) : launch_dq<DH, 1, HW, true>(q, s);
+  });
   if (e != hipSuccess) return e;
   WinKvParams p{};
   p.qkv = q.qkv; p.ld_qkv = ld_qkv; p.dout = q.dout; p.ld_do = ld_out; p.lse = lse; p.delta = delta; p.packed = q.packed;
