@@ -30,8 +30,15 @@ constexpr int kTopExponent = 121;                // of a scale: 127 2^121 is the
 // Magnitudes are compared as bit patterns, in which NaN is above infinity (bf16: two to an instruction).
 template <typename T> struct Rows8;              // 8 columns of a row as they lie in memory
 template <> struct Rows8<bf16_t> {
+  typedef u32x4 Raw __attribute__((aligned(2)));      // (the memory instructions take any alignment)
   u32x4 q;
-  __device__ __forceinline__ void load(const bf16_t* p) { q = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+  __device__ __forceinline__ void load(const bf16_t* p) { q = *reinterpret_cast<const Raw*>(p); }
+  // the first n columns without, zeros behind them
+  __device__ __forceinline__ void drop(int n) {
+    if (n & 4) q = u32x4{q[2], q[3], 0, 0};
+    if (n & 2) q = u32x4{q[1], q[2], q[3], 0};
+    if (n & 1) q = u32x4{__builtin_amdgcn_alignbit(q[1], q[0], 16), __builtin_amdgcn_alignbit(q[2], q[1], 16), __builtin_amdgcn_alignbit(q[3], q[2], 16), q[3] >> 16};
+  }
   __device__ __forceinline__ void set(int c, bf16_t v) {
     const unsigned b = (unsigned)__builtin_bit_cast(unsigned short, v);
     q[c / 2] = c % 2 ? (q[c / 2] & 0xffffu) | (b << 16) : (q[c / 2] & 0xffff0000u) | b;
@@ -56,10 +63,16 @@ template <> struct Rows8<bf16_t> {
   };
 };
 template <> struct Rows8<float> {
+  typedef u32x4 Raw __attribute__((aligned(4)));
   u32x4 q[2];
   __device__ __forceinline__ void load(const float* p) {
 #pragma unroll
-    for (int i = 0; i < 2; i++) q[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+    for (int i = 0; i < 2; i++) q[i] = *reinterpret_cast<const Raw*>(p + 4 * i);
+  }
+  __device__ __forceinline__ void drop(int n) {
+    if (n & 4) { q[0] = q[1]; q[1] = u32x4{0, 0, 0, 0}; }
+    if (n & 2) { q[0] = u32x4{q[0][2], q[0][3], q[1][0], q[1][1]}; q[1] = u32x4{q[1][2], q[1][3], 0, 0}; }
+    if (n & 1) { q[0] = u32x4{q[0][1], q[0][2], q[0][3], q[1][0]}; q[1] = u32x4{q[1][1], q[1][2], q[1][3], 0}; }
   }
   __device__ __forceinline__ void set(int c, float v) { q[c / 4][c % 4] = __float_as_uint(v); }
   __device__ __forceinline__ void clear() { q[0] = q[1] = u32x4{0, 0, 0, 0}; }
@@ -84,7 +97,7 @@ template <> struct Rows8<float> {
   };
 };
 
-template <typename T, bool WIDE>
+template <typename T>
 __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* __restrict__ x, long ld) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];      // per wave 8 KiB of units; magnitudes and scales of the columns
   unsigned (*const top)[64] = reinterpret_cast<unsigned (*)[64]>(smem_raw + 8 * 8192);
@@ -97,21 +110,24 @@ __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* 
   for (int r = 0; r < 16; r++) v[r].clear();
   if (cn > 0 && tn > 0) {
     // (all loads before the first use of one, from the last row where there are no more: a load under a condition is waited for there)
-    const T* const at = x + (long)t0 * ld + c0;
-    if (WIDE && cn >= 8) {
+    const int past = cn < 8 && p.cols >= 8 ? 8 - cn : 0;      // a row's last columns: the 8 that end there, without the first of them
+    const T* const at = x + (long)t0 * ld + c0 - past;
+    if (p.cols >= 8) {
 #pragma unroll
       for (int r = 0; r < 16; r++) v[r].load(at + (long)(r < tn ? r : tn - 1) * ld);
+      if (past) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) v[r].drop(past);
+      }
     } else {
 #pragma unroll
       for (int r = 0; r < 16; r++)
 #pragma unroll
         for (int c = 0; c < 8; c++) v[r].set(c, at[(long)(r < tn ? r : tn - 1) * ld + (c < cn ? c : cn - 1)]);
-      if (cn < 8) {
 #pragma unroll
-        for (int r = 0; r < 16; r++)
+      for (int r = 0; r < 16; r++)
 #pragma unroll
-          for (int c = 0; c < 8; c++) if (c >= cn) v[r].set(c, (T)0.f);
-      }
+        for (int c = 0; c < 8; c++) if (c >= cn) v[r].set(c, (T)0.f);
     }
     if (tn < 16) {
 #pragma unroll
@@ -181,7 +197,7 @@ __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* 
 }
 
 // The way back: one thread = 16 tokens of 8 columns.
-template <typename T, bool WIDE>
+template <typename T>
 __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __restrict__ y, long ld) {
   const int cg = threadIdx.x & 7, rg = (int)blockIdx.y * 32 + ((int)threadIdx.x >> 3);
   const int c0 = (int)blockIdx.x * 64 + 8 * cg, t0 = 16 * rg;
@@ -201,13 +217,28 @@ __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __rest
 #pragma unroll
     for (int c = 0; c < 8; c++) v[c] = (float)((int)(q[c][r / 4] << (24 - 8 * (r % 4))) >> 24) * s[c];
     T* const row = y + (long)t * ld + c0;
-    if (WIDE && p.cols - c0 >= 8) {
-      if constexpr (sizeof(T) == 2) Vec<bf16_t>::store(row, v);
-      else { Vec<float>::store(row, v); Vec<float>::store(row + 4, v + 4); }
-    } else {
+    if (p.cols - c0 >= 8) {
+      typedef T Out __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));      // (any alignment, as above)
+      constexpr int N = 16 / sizeof(T);
 #pragma unroll
-      for (int c = 0; c < 8; c++)
-        if (c < p.cols - c0) row[c] = (T)v[c];
+      for (int i = 0; i < 8; i += N) {
+        Out o;
+#pragma unroll
+        for (int c = 0; c < N; c++) o[c] = (T)v[i + c];
+        *reinterpret_cast<Out*>(row + i) = o;
+      }
+    } else {
+      // a row's last columns: 4, 2 and 1 of them
+      const int n = p.cols - c0;
+      T* at = row;
+      if (n & 4) {
+        typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        *reinterpret_cast<Four*>(at) = Four{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        at += 4;
+      }
+      const float a = n & 4 ? v[4] : v[0], b = n & 4 ? v[5] : v[1], c = n & 4 ? v[6] : v[2];
+      if (n & 2) { at[0] = (T)a; at[1] = (T)b; at += 2; }
+      if (n & 1) at[0] = (T)(n & 2 ? c : a);
     }
   }
 }
@@ -463,10 +494,10 @@ __global__ __launch_bounds__(256) void stash8_join_kernel(Stash8Dw p) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <typename T, bool WIDE>
+template <typename T>
 static hipError_t launch_put(const Stash8Slot& p, const void* x, long ld, hipStream_t s) {
   constexpr size_t smem = 8 * 8192 + 8 * 256 + 256;
-  auto kern = stash8_put_kernel<T, WIDE>;
+  auto kern = stash8_put_kernel<T>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3((unsigned)((p.cols + 63) / 64), (unsigned)p.blocks), dim3(512), smem, s, p, (const T*)x, ld);
@@ -474,21 +505,13 @@ static hipError_t launch_put(const Stash8Slot& p, const void* x, long ld, hipStr
 }
 
 hipError_t stash8_put(int dtype, const Stash8Slot& p, const void* x, long ld, hipStream_t s) {
-  const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % (dtype ? 8 : 4) == 0;
-  if (dtype) return wide ? launch_put<bf16_t, true>(p, x, ld, s) : launch_put<bf16_t, false>(p, x, ld, s);
-  return wide ? launch_put<float, true>(p, x, ld, s) : launch_put<float, false>(p, x, ld, s);
+  return dtype ? launch_put<bf16_t>(p, x, ld, s) : launch_put<float>(p, x, ld, s);
 }
 
 hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStream_t s) {
   const dim3 grid((unsigned)((p.cols + 63) / 64), (unsigned)((p.tokens + 511) / 512)), block(256);
-  const bool wide = reinterpret_cast<uintptr_t>(y) % 16 == 0 && ld % (dtype ? 8 : 4) == 0;
-  if (dtype) {
-    if (wide) hipLaunchKernelGGL((stash8_get_kernel<bf16_t, true>), grid, block, 0, s, p, (bf16_t*)y, ld);
-    else hipLaunchKernelGGL((stash8_get_kernel<bf16_t, false>), grid, block, 0, s, p, (bf16_t*)y, ld);
-  } else {
-    if (wide) hipLaunchKernelGGL((stash8_get_kernel<float, true>), grid, block, 0, s, p, (float*)y, ld);
-    else hipLaunchKernelGGL((stash8_get_kernel<float, false>), grid, block, 0, s, p, (float*)y, ld);
-  }
+  if (dtype) hipLaunchKernelGGL(stash8_get_kernel<bf16_t>, grid, block, 0, s, p, (bf16_t*)y, ld);
+  else hipLaunchKernelGGL(stash8_get_kernel<float>, grid, block, 0, s, p, (float*)y, ld);
   return hipGetLastError();
 }
 

@@ -315,6 +315,7 @@ def test_starts_that_do_not_ascend_touch_nothing_else(starts):
 STASH_CASES = [  # tokens, cols, slots, dtype
     (1, 1, 1, "bf16"), (1, 8, 2, "f32"), (63, 33, 1, "bf16"), (64, 32, 3, "f32"), (65, 31, 2, "bf16"), (129, 72, 1, "f32"), (1024, 40, 2, "bf16"), (1025, 97, 2, "bf16"),
     (2500, 130, 1, "f32"), (333, 520, 3, "bf16"),
+    *[(70, n, 1, t) for n in (9, 10, 11, 12, 13, 14, 15, 71, 5) for t in ("bf16", "f32")],
 ]
 
 
