@@ -582,3 +582,55 @@ def test_answering_goes_on_from_a_packed_prompt():
         out, _ = tbp.tbp_window_decode(q, ck, cv, _ints([i + 1]), H, KV, dh, 1024)
         # (two roundings of P and of the result on either side)
         assert (out[0].float() - want[i].float()).norm() <= 1e-2 * want[i].float().norm()
+
+
+# ------------------------------------------------------------------------------------------------- past 32 bits
+def test_packed_attention_and_norms_past_four_gigabytes():
+    """Rows whose offsets pass 2^32 bytes, in 1801 sequences: the last ones as in a tensor of their own."""
+    H, KV, dh, n = 32, 8, 128, 200
+    seqs = 1801
+    rows, w, qk = n * seqs, (H + 2 * KV) * dh, (H + KV) * dh
+    assert rows * w * 2 > 1 << 32
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    qkv = torch.empty((rows, w), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    do = torch.empty((rows, H * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    starts = torch.arange(0, rows + 1, n, dtype=torch.int32, device=DEV)
+    gain = 1 + 0.1 * torch.randn((2, dh), generator=g, device=DEV)
+    gq, gk = gain.to(torch.bfloat16)
+    table = tbp.tbp_rotary_table(n, dh, 1e4, device=DEV)
+    last = slice(rows - 3 * n, rows)
+    few = _ints([0, n, 2 * n, 3 * n])
+
+    def step(x, d, s):
+        q = x.clone()
+        tbp.tbp_qk_norm(x, gq, gk, H, KV, dh, 1e-5, table, seq=n, out=q)
+        out, lse = tbp.tbp_packed_attention_fwd(q, s, H, KV, dh)
+        dq = tbp.tbp_packed_attention_p1(q, out, d, lse, s, H, KV, dh)
+        dx, _ = tbp.tbp_qk_norm_p1(dq, x, gq, gk, H, KV, dh, 1e-5, table, seq=n)
+        return q, out, lse, dq, dx
+
+    large = [t[:, last].clone() if i == 2 else t[last].clone() for i, t in enumerate(step(qkv, do, starts))]
+    small = step(qkv[last].clone(), do[last].clone(), few)
+    for name, a, b in zip(("norm", "out", "lse", "dqkv", "dx"), large, small):
+        # (the two may cut the work differently, which changes the order of sums: of the result two roundings to bf16, in the norms' derivative three)
+        assert (a.float() - b.float()).norm() <= 8e-3 * b.float().norm(), name
+
+
+def test_a_stash_past_four_gigabytes():
+    tokens, cols, slots = 4096, 11008, 100
+    kept, d = tbp.Stash8(tokens, cols, slots, device=DEV), tbp.Stash8(tokens, 64, slots, device=DEV)
+    assert kept.memory.nbytes > 1 << 32
+    one, d1 = tbp.Stash8(tokens, cols, 1, device=DEV), tbp.Stash8(tokens, 64, 1, device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    x, dy = torch.randn((tokens, cols), generator=g, device=DEV), torch.randn((tokens, 64), generator=g, device=DEV)
+    for k, t in ((kept, x), (d, dy)):
+        k.put(slots - 1, t)
+    one.put(0, x), d1.put(0, dy)
+    assert torch.equal(kept.get(slots - 1), one.get(0)) and not kept.get(slots - 2).any()
+    want = tbp.tbp_stash8_dw(one, d1)
+    assert torch.equal(tbp.tbp_stash8_dw(kept, d, first=slots - 1), want)
+    # (the other slots are zeros; blocks are added in another order: 4 of them, 2^-24 of what they add up to)
+    whole = tbp.tbp_stash8_dw(kept, d)
+    assert (whole - want).abs().max() <= 4 * 2.0 ** -24 * 4 * want.abs().max()
