@@ -44,7 +44,6 @@ struct KeyBlocks {
 // The rows behind the last sequence are one without tokens, whose results are zeros.  Starts are taken as 0 .. rows and the first as 0.
 // A launch has as many numbers of blocks (of queries, or of keys) as any lengths may need; those that no block has end at once.
 struct Packed { const int* starts; int seqs, rows; };
-constexpr int kMostFirst = 16;
 inline __host__ __device__ long packed_blocks(const Packed& p, int block) { return (long)p.rows / block + p.seqs + 1; }
 
 __device__ __forceinline__ int packed_start(const Packed& p, int b) {
@@ -83,56 +82,42 @@ struct SeqOf {
     const int S = end > first ? end - first : 0;
     return SeqOf{first, lo < p.seqs ? S : 0, S, number - first / BLOCK - lo};
   }
-  // Key blocks by what they have to do, the most first, for up to 64 sequences, a lane each.
+  // Key blocks by what they have to do, the most first, whatever sequence they are of, for up to 64 sequences, a lane each: F(j) blocks have more than j blocks of
+  // their sequence from them on, and those of one j go by their sequence.
   template <int BLOCK> __device__ __forceinline__ static SeqOf most_first(const Packed& p, int number) {
     const int lane = threadIdx.x & 63;
     const int first = lane < p.seqs ? packed_start(p, lane) : 0, end = lane < p.seqs ? packed_start(p, lane + 1) : 0;
     const int blocks = end > first ? (end - first + BLOCK - 1) / BLOCK : 0;
-    int all = 0, who = 0, block = 0;
-    if (p.seqs <= kMostFirst) {
-      // whatever sequence they are of: F(j) of them have more than j blocks of their sequence from them on, and those of one j go by their
-      // sequence; 64 values of F at a time, a lane each
-      int lo = 0, step = 1, beyond = 0;            // F(lo) > number >= F(lo + 1) = beyond
-      while (64 * step <= p.rows / BLOCK + 1) step *= 32;
-      for (bool top = true;; top = false) {
-        const int j = lo + lane * step;
-        int f = 0;
-        for (int s = 0; s < p.seqs; s++) {
-          const int over = __builtin_amdgcn_readlane(blocks, s) - j;
-          f += over > 0 ? over : 0;
-        }
-        if (top) all = __builtin_amdgcn_readfirstlane(f);
-        if (number >= all) break;
-        const int last = 63 - __builtin_clzll(__ballot(f > number));      // (below 63: F of the 64th is 0)
-        lo += last * step;
-        beyond = __builtin_amdgcn_readlane(f, last + 1);
-        if (step == 1) break;
-        step /= 32;
-      }
-      const unsigned long long has = __ballot(blocks > lo);
-      const bool mine = blocks > lo && __builtin_amdgcn_mbcnt_hi((unsigned)(has >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)has, 0)) == (unsigned)(number - beyond);
-      who = __builtin_ctzll(__ballot(mine) | 1ull << 63);
-      block = __builtin_amdgcn_readlane(blocks, who) - 1 - lo;
-    } else {
-      // by their sequence, the longest first
-      int at = 0;
+    int all = 0, lo = 0, step = 1, beyond = 0;     // F(lo) > number >= F(lo + 1) = beyond
+    while (64 * step <= p.rows / BLOCK + 1) step *= 32;
+    for (bool top = true;; top = false) {          // 64 values of F at a time, a lane each
+      const int j = lo + lane * step;
+      int f = 0;
       for (int s = 0; s < p.seqs; s++) {
-        const int b = __builtin_amdgcn_readlane(blocks, s);
-        at += b > blocks || (b == blocks && s < lane) ? b : 0;
-        all += b;
+        const int over = __builtin_amdgcn_readlane(blocks, s) - j;
+        f += over > 0 ? over : 0;
       }
-      who = __builtin_ctzll(__ballot(number >= at && number < at + blocks) | 1ull << 63);
-      block = number - __builtin_amdgcn_readlane(at, who);
+      if (top) all = __builtin_amdgcn_readfirstlane(f);
+      if (number >= all) {
+        const int behind = p.seqs ? packed_start(p, p.seqs) : 0;
+        return SeqOf{behind, 0, p.rows - behind, number - all};
+      }
+      const int last = 63 - __builtin_clzll(__ballot(f > number));      // (the first one is among them; at step 1 below 63: F is 0 at the 64th)
+      lo += last * step;
+      beyond = __builtin_amdgcn_readlane(f, last + 1);
+      if (step == 1) break;
+      step /= 32;
     }
-    if (number >= all) {
-      const int behind = p.seqs ? packed_start(p, p.seqs) : 0;
-      return SeqOf{behind, 0, p.rows - behind, number - all};
-    }
+    const unsigned long long has = __ballot(blocks > lo);
+    const bool mine = blocks > lo && __builtin_amdgcn_mbcnt_hi((unsigned)(has >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)has, 0)) == (unsigned)(number - beyond);
+    const int who = __builtin_ctzll(__ballot(mine) | 1ull << 63);
     const int at = __builtin_amdgcn_readlane(first, who), n = __builtin_amdgcn_readlane(end, who) - at;
-    return SeqOf{at, n, n, block};
+    return SeqOf{at, n, n, __builtin_amdgcn_readlane(blocks, who) - 1 - lo};
   }
-  template <int BLOCK> __device__ __forceinline__ static SeqOf keys(const Packed& p, int number) {
-    return p.seqs <= 64 ? most_first<BLOCK>(p, number) : in_order<BLOCK, false>(p, number);
+  // us of the backward, in order / the most first: 32 heads on 8 of 128, 5 sequences of 1639 529 / 484, 16 and 24 of 8192 in all 311 / 286 and 298 / 291, 64 of 4000 91 / 81,
+  // but 30 of 16384 847 / 864; 12 on 4 of 64, 61 of 4096 32 / 36 (looking through 64 of them takes as long as a block's work there)
+  template <int DH, int BLOCK> __device__ __forceinline__ static SeqOf keys(const Packed& p, int number) {
+    return p.seqs <= (DH == 128 ? 64 : 16) ? most_first<BLOCK>(p, number) : in_order<BLOCK, false>(p, number);
   }
 };
 
@@ -721,7 +706,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
   const int yy = sink_block ? y : y - (PACKED ? 0 : p.parts.sink_blocks * p.parts.sink_parts);
   const int number = yy / np + (PACKED || sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::keys<KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::keys<DH, KEYS>(p.packed, number);
   const int kb = seq.block, S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int kv0 = kb * KEYS, kw0 = kv0 + 32 * kblk, key = kw0 + kl;
   const long tok0 = seq.tok0;
@@ -1026,7 +1011,7 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   const int number = !PACKED && p.parts.sink_parts == 1 ? cut + p.parts.sink_blocks : cut;       // (blocks that are cut: the sinks', the others', or all)
   const int b = PACKED ? 0 : (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::keys<KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::keys<DH, KEYS>(p.packed, number);
   const int kb = seq.block;
   const int which = (int)threadIdx.x / (ROWS * LPR), t = (int)threadIdx.x % (ROWS * LPR);
   const int row = ((PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) % per) * ROWS + t / LPR, col = 8 * (t % LPR);

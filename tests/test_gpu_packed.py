@@ -198,7 +198,8 @@ PACKED_CASES = [  # lengths, rows behind, H, KV, dh
     ([1], 0, 1, 1, 64), ([], 5, 2, 1, 128), ([0, 0, 3, 0], 0, 4, 2, 128), ([1, 1, 1, 2], 1, 2, 2, 64), ([64, 63, 65], 0, 3, 1, 64), ([128, 127, 129, 1], 3, 4, 2, 128),
     ([300], 0, 8, 2, 128), ([37, 500, 1, 0, 211], 130, 6, 2, 64), ([5] * 70 + [0] * 70 + [9] * 3, 2, 4, 4, 64), ([700, 650], 0, 16, 4, 128), ([1100], 200, 4, 1, 64),
     ([257, 1, 400, 1, 256], 0, 40, 8, 128), ([33] * 40, 0, 32, 8, 128), ([1500, 3, 800], 5, 8, 8, 128), ([900, 40, 1200, 7, 300], 0, 24, 8, 64), ([2100, 30], 0, 16, 16, 128),
-    ([3] * 4200, 1, 2, 1, 64), ([1200, 900, 1000], 64, 32, 8, 128),
+    ([3] * 4200, 1, 2, 1, 64), ([1200, 900, 1000], 64, 32, 8, 128), ([4500, 300, 1], 10, 2, 1, 64), ([1, 0, 900] * 21 + [70], 0, 4, 1, 128), ([17] * 62, 3, 6, 2, 64),
+    ([17] * 63, 3, 6, 2, 64), ([200, 0, 1, 900, 65, 129, 64, 128, 300, 2, 31, 33, 500, 7, 90, 10], 0, 3, 1, 64),
 ]
 
 
@@ -256,6 +257,22 @@ def test_packed_attention_of_one_sequence_is_window_attention():
     g = tbp.tbp_packed_attention_p1(qkv, out, do, lse, _ints([0, n]), H, KV, dh)
     wg = tbp.tbp_window_attention_p1(qkv, want, do, wlse, n, H, KV, dh, n)
     for a, b in ((out, want), (lse, wlse[0]), (g, wg)):          # (the two may cut the work differently)
+        assert (a.float() - b.float()).norm() <= 4e-3 * b.float().norm()
+
+
+def test_packed_attention_of_very_long_sequences():
+    """More blocks than are looked through at once, at either level."""
+    n, H, KV, dh = 70000, 1, 1, 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    qkv = torch.empty((2 * n, 3 * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    do = torch.empty((2 * n, dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    s = _ints([0, n, 2 * n])
+    out, lse = tbp.tbp_packed_attention_fwd(qkv, s, H, KV, dh)
+    want, wlse = tbp.tbp_window_attention_fwd(qkv, n, H, KV, dh, n)
+    d = tbp.tbp_packed_attention_p1(qkv, out, do, lse, s, H, KV, dh)
+    wd = tbp.tbp_window_attention_p1(qkv, want, do, wlse, n, H, KV, dh, n)
+    for a, b in ((out, want), (lse, wlse.permute(1, 0, 2).reshape(H, 2 * n)), (d, wd)):      # (the two may cut the work differently)
         assert (a.float() - b.float()).norm() <= 4e-3 * b.float().norm()
 
 
