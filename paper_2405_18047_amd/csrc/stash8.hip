@@ -27,6 +27,8 @@ constexpr int kTopExponent = 121;                // of a scale: 127 2^121 is the
 // ------------------------------------------------------------------------------------------ into the stash, and out of it
 // One workgroup = 64 columns of one block of tokens, 8 threads side by side with 8 columns each (128 bytes of a row, bf16) and 64 of them below each other
 // with 16 tokens each, which stay in registers as they were loaded between the two looks at them: the largest magnitude of every column, then the rounding.
+// Bound by memory: 4096 x 11008 of bf16, 135 MB read and written, 22.4 us, 6.0 TB/s (of new inputs, out of no cache, 27 to 32); few tokens by a workgroup's chain of a load,
+// two barriers and a store: 129 x 256 5 us.
 // Magnitudes are compared as bit patterns, in which NaN is above infinity (bf16: two to an instruction).
 template <typename T> struct Rows8;              // 8 columns of a row as they lie in memory
 template <> struct Rows8<bf16_t> {
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(512) void stash8_put_kernel(Stash8Slot p, const T* 
   }
 }
 
-// The way back: one thread = 16 tokens of 8 columns.
+// The way back: one thread = 16 tokens of 8 columns.  Bound by memory: 4096 x 11008 into bf16 21.9 us, 6.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __restrict__ y, long ld) {
   const int cg = threadIdx.x & 7, rg = (int)blockIdx.y * 32 + ((int)threadIdx.x >> 3);
@@ -244,11 +246,16 @@ __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __rest
 }
 
 // ------------------------------------------------------------------------------------------ dW = X^T dY
-// One workgroup = 4 waves, 2 x 2, each 128 x 32 NB of the output; the contraction in steps of 64 tokens through a ring of slots in LDS, filled by
+// Integers rather than 8-bit floats: on gfx950 the sums of 8-bit float products keep 13 bits below the largest of their group (1.5e-5 of the sums of N(0,1)
+// products, measured), integer sums are whole; and a block's rounding of N(0,1) values is 1.0 % of them where e4m3 with the same kind of scale has 2.7 %.
+// One workgroup = 4 waves, 2 x 2, each 32 MB x 32 NB of the output; the contraction in steps of 64 tokens through a ring of slots in LDS, filled by
 // asynchronous copies all but one of them ahead.  The units are copied as they are: every fragment is 64 lanes x 16 bytes in a row.
 // The integer sums of a block of tokens are exact: 1024 x 127^2 is below 2^24, so that they are exact in fp32 as well, in which the blocks are added
 // up, each with the product of the two columns' scales.  That takes three vector instructions per element and block, done tile by tile in front of the tile's first
-// product of the next block, and a second set of accumulators, which one wave per SIMD has the registers for.
+// product of the next block (5 % of the time), and a second set of accumulators: 96 x 96 to a wave, one wave to a SIMD, or 64 x 64 and two.
+// Bound by power on large outputs: 11008 x 4096 over 8 x 4096 tokens 1450 to 1720 us over cards, 1.72 to 2.04 PFLOP/s (at the rate of the bf16 weight gradients, 1.29, 2283), at 1.5 to 1.9 GHz with
+// the matrix pipes busy 52 %; the same instructions on zeros take 7 % fewer cycles, at 2.27 GHz.  Rounds of few steps by their start and end (8 us): 4096 x 4096 over 4096
+// tokens 80 us, 1.7 PFLOP/s.  Tried without gain: copies spread over all of a step's products; tiles of 128 x 96 and 128 x 64 to a wave (1594 and 1653 us for 1588).
 constexpr int dw_slots(int mb, int nb, int per_cu) { return (160 * 1024 / per_cu - 8 * 2048) / (2 * (mb + nb) * kUnit); }
 struct Stash8Dw {
   const unsigned char* x; const float* xs; int xb;     // units, scales, column blocks
@@ -515,8 +522,11 @@ hipError_t stash8_get(int dtype, const Stash8Slot& p, void* y, long ld, hipStrea
   return hipGetLastError();
 }
 
-// Tiles of 96 x 96 to a wave and one workgroup to a compute unit, or of 64 x 64 and two, by the time that their rounds of workgroups take.  Shares of the
-// contraction where there are few tiles, each of whole blocks.
+// Tiles of 96 x 96 to a wave and one workgroup to a compute unit, or of 64 x 64 and two, by the time that their rounds of workgroups take: us per step and
+// per round.  Measured, 96 / 64: 11008 x 4096 over 8 x 4096 tokens 1702 / 1780, 5120 x 13824 over 4 x 4096 1204 / 1259, 8 x 1024 4096 x 11008 398 / 393, 4096 x 4096 over 8 x
+// 4096 570 / 560, 12288 x 4096 over 2 x 1024 173 / 134.
+// Shares of the contraction where there are few tiles, each of whole blocks, three at least.  us, one / shares: 512 x 512 over 8 x 2048 tokens 75 / 20, 1536 x 1536 over 8 x 4096 143 /
+// 98, 2048 x 1024 over 4 x 4096 77 / 50, but 2048 x 2048 over 8 x 1024 in two 48 / 51.
 Stash8Plan stash8_plan(int m, int n, int steps, int blocks) {
   const long mb = (m + 31) / 32, nb = (n + 31) / 32;
   const long large = ((mb + 5) / 6) * ((nb + 5) / 6), small = ((mb + 3) / 4) * ((nb + 3) / 4);
