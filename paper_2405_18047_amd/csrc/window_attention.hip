@@ -1,5 +1,5 @@
 // Sliding-window attention with sinks for gfx950 (bf16 storage, fp32 accumulation, head_dim 64 or 128, grouped heads): forward,
-// backward-p1, and the form for one new token per sequence over a cache.
+// backward-p1, and the form for one new token per sequence over a cache; forward and backward-p1 also over packed sequences, causal without a window.
 //
 // Query i of a sequence of n tokens sees key j when j <= i and (j > i - window or j < sinks); tokens n .. S - 1 of a row of the
 // batch are padding: never read, zeros in every result (lse: -inf).  H query heads share KV key heads, H / KV = G each.
@@ -43,6 +43,7 @@ struct KeyBlocks {
 // Sequences that lie one behind the other (PACKED): sequence b has the rows starts[b] .. starts[b + 1] - 1 of `rows`, all causal; lse and delta are [H][rows].
 // The rows behind the last sequence are one without tokens, whose results are zeros.  Starts are taken as 0 .. rows and the first as 0.
 // A launch has as many numbers of blocks (of queries, or of keys) as any lengths may need; those that no block has end at once.
+enum { kInOrder = 1, kMostFirst };     // values of PACKED: whose block a number is
 struct Packed { const int* starts; int seqs, rows; };
 inline __host__ __device__ long packed_blocks(const Packed& p, int block) { return (long)p.rows / block + p.seqs + 1; }
 
@@ -82,21 +83,23 @@ struct SeqOf {
     const int S = end > first ? end - first : 0;
     return SeqOf{first, lo < p.seqs ? S : 0, S, number - first / BLOCK - lo};
   }
-  // Key blocks by what they have to do, the most first, whatever sequence they are of, for up to 64 sequences, a lane each: F(j) blocks have more than j blocks of
-  // their sequence from them on, and those of one j go by their sequence.
-  template <int BLOCK> __device__ __forceinline__ static SeqOf most_first(const Packed& p, int number) {
+  // Blocks by what they have to do, the most first, whatever sequence they are of, for up to 64 sequences, a lane each: F(j) blocks have more than j blocks of
+  // their sequence from them on (of keys; of queries up to them), and those of one j go by their sequence.
+  template <int BLOCK, bool LAST> __device__ __forceinline__ static SeqOf most_first(const Packed& p, int number) {
     const int lane = threadIdx.x & 63;
     const int first = lane < p.seqs ? packed_start(p, lane) : 0, end = lane < p.seqs ? packed_start(p, lane + 1) : 0;
     const int blocks = end > first ? (end - first + BLOCK - 1) / BLOCK : 0;
     int all = 0, lo = 0, step = 1, beyond = 0;     // F(lo) > number >= F(lo + 1) = beyond
-    while (64 * step <= p.rows / BLOCK + 1) step *= 32;
+    while (__any(blocks >= 64 * step)) step *= 32;         // (one look at 64 values for sequences of up to 63 blocks)
     for (bool top = true;; top = false) {          // 64 values of F at a time, a lane each
       const int j = lo + lane * step;
       int f = 0;
-      for (int s = 0; s < p.seqs; s++) {
-        const int over = __builtin_amdgcn_readlane(blocks, s) - j;
-        f += over > 0 ? over : 0;
-      }
+      for (int s = 0; s < p.seqs; s += 4)          // (lanes without a sequence have no blocks)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const int over = __builtin_amdgcn_readlane(blocks, s + i) - j;
+          f += over > 0 ? over : 0;
+        }
       if (top) all = __builtin_amdgcn_readfirstlane(f);
       if (number >= all) {
         const int behind = p.seqs ? packed_start(p, p.seqs) : 0;
@@ -112,12 +115,10 @@ struct SeqOf {
     const bool mine = blocks > lo && __builtin_amdgcn_mbcnt_hi((unsigned)(has >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)has, 0)) == (unsigned)(number - beyond);
     const int who = __builtin_ctzll(__ballot(mine) | 1ull << 63);
     const int at = __builtin_amdgcn_readlane(first, who), n = __builtin_amdgcn_readlane(end, who) - at;
-    return SeqOf{at, n, n, __builtin_amdgcn_readlane(blocks, who) - 1 - lo};
+    return SeqOf{at, n, n, LAST ? lo : __builtin_amdgcn_readlane(blocks, who) - 1 - lo};
   }
-  // us of the backward, in order / the most first: 32 heads on 8 of 128, 5 sequences of 1639 529 / 484, 16 and 24 of 8192 in all 311 / 286 and 298 / 291, 64 of 4000 91 / 81,
-  // but 30 of 16384 847 / 864; 12 on 4 of 64, 61 of 4096 32 / 36 (looking through 64 of them takes as long as a block's work there)
-  template <int DH, int BLOCK> __device__ __forceinline__ static SeqOf keys(const Packed& p, int number) {
-    return p.seqs <= (DH == 128 ? 64 : 16) ? most_first<BLOCK>(p, number) : in_order<BLOCK, false>(p, number);
+  template <int PACKED, int BLOCK, bool LAST> __device__ __forceinline__ static SeqOf of(const Packed& p, int number) {
+    return PACKED == kMostFirst ? most_first<BLOCK, LAST>(p, number) : in_order<BLOCK, LAST>(p, number);
   }
 };
 
@@ -156,7 +157,7 @@ struct HeadOf {
 // 49.1 us with two, 38.4 with four.
 // HW: query heads of one key head that a workgroup has (PACKED), 128 / SPLIT / HW queries of each: short sequences then leave less of a block empty,
 // and less of what a block computes lies behind its queries.
-template <int DH, bool AHEAD, int SPLIT, int HW, bool PACKED>
+template <int DH, bool AHEAD, int SPLIT, int HW, int PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WinParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, QW = 4 / SPLIT, NT = 2 / SPLIT;
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
   const int b = at.b, h0 = (at.hk * (p.G / HW) + at.gq) * HW, h = h0 + wq % HW;       // the workgroup's first query head, the wave's
   SeqOf seq{(long)b * p.S, 0, p.S, qb};
-  if constexpr (PACKED) { seq = SeqOf::in_order<BQ, true>(p.packed, qb); qb = seq.block; }
+  if constexpr (PACKED) { seq = SeqOf::of<PACKED, BQ, true>(p.packed, qb); qb = seq.block; }
   const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int q0 = qb * BQ, qw0 = q0 + 32 * (wq / HW), query = qw0 + ql;
   const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 #pragma unroll
         for (int e = 0; e < 16; e++) {
           const int r = 32 * kt + 8 * (e >> 2) + (e & 3);
-          st[kt][e] = (r > hi || (r <= lo && r >= sk)) ? -INFINITY : st[kt][e];
+          st[kt][e] = (r > hi || (!PACKED && r <= lo && r >= sk)) ? -INFINITY : st[kt][e];
         }
     }
     // The reference point m of the exponentials has to stay within a safe distance of the running maximum, not on it: it is moved
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
       for (int e = 0; e < 16; e++) ot[t][e] = ot[t][e] * f0 + part[(t * 16 + e) * 64 + lane] * f1;
   }
   {
-    const bool live = query < n;                        // (padding: zeros, whatever the lane holds)
+    const bool live = PACKED || query < n;              // (padding: zeros, whatever the lane holds)
     const float inv = 1.f / lq;
 #pragma unroll
     for (int t = 0; t < DT; t++)
@@ -434,7 +435,7 @@ struct WinDqParams {
   float scale, scale_log2e;
 };
 
-template <int DH, int SPLIT, int HW, bool PACKED>
+template <int DH, int SPLIT, int HW, int PACKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void window_bwd_dq_kernel(WinDqParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BKV = 64, QW = 4 / SPLIT;
@@ -454,7 +455,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
   const int wq = SPLIT == 1 ? wave : wave % QW, wk = SPLIT == 1 ? 0 : wave / QW;      // which 32 queries, which 32-key tile of every block (SPLIT 2)
   const int b = at.b, h0 = (at.hk * (p.G / HW) + at.gq) * HW, h = h0 + wq % HW;       // the workgroup's first query head, the wave's
   SeqOf seq{(long)b * p.S, 0, p.S, qb};
-  if constexpr (PACKED) { seq = SeqOf::in_order<BQ, true>(p.packed, qb); qb = seq.block; }
+  if constexpr (PACKED) { seq = SeqOf::of<PACKED, BQ, true>(p.packed, qb); qb = seq.block; }
   const int S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int q0 = qb * BQ, qw0 = q0 + 32 * (wq / HW), query = qw0 + ql;
   const long tok0 = seq.tok0, stat0 = PACKED ? (long)h * p.S + tok0 : ((long)b * p.H + h) * p.S;
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 #pragma unroll
         for (int e = 0; e < 16; e++) {
           const int r = 32 * kt + 8 * (e >> 2) + (e & 3);
-          st[e] = (r > hi || (r <= lo && r >= sk)) ? 0.f : st[e];
+          st[e] = (r > hi || (!PACKED && r <= lo && r >= sk)) ? 0.f : st[e];
         }
       }
 #pragma unroll
@@ -630,7 +631,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     for (int e4 = 0; e4 < 4; e4++) {
       bf16x4 v;
 #pragma unroll
-      for (int r = 0; r < 4; r++) v[r] = (bf16_t)(qlive ? dqt[t][4 * e4 + r] * p.scale : 0.f);
+      for (int r = 0; r < 4; r++) v[r] = (bf16_t)(PACKED || qlive ? dqt[t][4 * e4 + r] * p.scale : 0.f);
       *reinterpret_cast<LDS_AS bf16x4*>(erow + ql * EROW + (32 * t + 8 * e4 + 4 * g) * 2) = v;
     }
   // (LDS operations of a wave execute in order: the reads below see this wave's own writes above)
@@ -678,7 +679,7 @@ template <typename F, int... I> __device__ __forceinline__ void each(F f, std::i
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-template <int DH, int KEYS, bool PACKED>
+template <int DH, int KEYS, int PACKED>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 4 : 2))) void window_bwd_kv_kernel(WinKvParams p) {
   using HT = HeadTile<DH>;
   constexpr int KS = DH / 16, DT = DH / 32, BQ = 64;
@@ -706,7 +707,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
   const int yy = sink_block ? y : y - (PACKED ? 0 : p.parts.sink_blocks * p.parts.sink_parts);
   const int number = yy / np + (PACKED || sink_block ? 0 : p.parts.sink_blocks), part = yy % np;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::keys<DH, KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::of<PACKED, KEYS, false>(p.packed, number);
   const int kb = seq.block, S = seq.S, window = PACKED ? 1 << 30 : p.window, sinks = PACKED ? 0 : p.sinks;
   const int kv0 = kb * KEYS, kw0 = kv0 + 32 * kblk, key = kw0 + kl;
   const long tok0 = seq.tok0;
@@ -805,7 +806,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
 #pragma unroll
           for (int e = 0; e < 16; e++) {
             const int r = 8 * (e >> 2) + (e & 3);
-            pv[e] = (r < lo || r >= hi) ? 0.f : pv[e];
+            pv[e] = (r < lo || (!PACKED && r >= hi)) ? 0.f : pv[e];
           }
         }
 #pragma unroll
@@ -1004,14 +1005,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 
 
 // dk and dv of the key blocks that were cut: the parts added up in order.  One workgroup = 8 or 16 key rows of one of them; a thread has 8
 // columns of one row of dK or dV.  Bound by the latency of the parts: 38 of them 13.4 us one at a time, 7.6 eight at a time.
-template <int DH, int KEYS, bool PACKED>
+template <int DH, int KEYS, int PACKED>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinKvParams p) {
   constexpr int LPR = DH / 8, ROWS = 256 / (2 * LPR);
   const int per = KEYS / ROWS, cut = (PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) / per;
   const int number = !PACKED && p.parts.sink_parts == 1 ? cut + p.parts.sink_blocks : cut;       // (blocks that are cut: the sinks', the others', or all)
   const int b = PACKED ? 0 : (int)blockIdx.x / p.KV, hk = (int)blockIdx.x % p.KV;
   SeqOf seq{(long)b * p.S, 0, p.S, number};
-  if constexpr (PACKED) seq = SeqOf::keys<DH, KEYS>(p.packed, number);
+  if constexpr (PACKED) seq = SeqOf::of<PACKED, KEYS, false>(p.packed, number);
   const int kb = seq.block;
   const int which = (int)threadIdx.x / (ROWS * LPR), t = (int)threadIdx.x % (ROWS * LPR);
   const int row = ((PACKED ? (int)blockIdx.x / p.KV : (int)blockIdx.y) % per) * ROWS + t / LPR, col = 8 * (t % LPR);
@@ -1273,13 +1274,13 @@ __global__ __launch_bounds__(256) void window_decode_kernel(WinDecodeParams p) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <int DH, bool AHEAD, int SPLIT, int HW = 1, bool PACKED = false>
+template <int DH, bool AHEAD, int SPLIT, int HW = 1, int PACKED = 0>
 static hipError_t launch_fwd(const WinParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
   auto kern = window_fwd_kernel<DH, AHEAD, SPLIT, HW, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  const dim3 grid = PACKED ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  const dim3 grid = PACKED != 0 ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
   hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
@@ -1302,34 +1303,34 @@ hipError_t window_attention_fwd(const WindowShape& w, const int* lengths, const 
   return w.seq <= 256 || w.window <= 512 ? launch_fwd<128, false, 1>(p, s) : launch_fwd<128, true, 1>(p, s);
 }
 
-template <int DH, int SPLIT, int HW = 1, bool PACKED = false>
+template <int DH, int SPLIT, int HW = 1, int PACKED = 0>
 static hipError_t launch_dq(const WinDqParams& p, hipStream_t s) {
   constexpr size_t smem = 2 * 2 * 64 * DH * 2;
   auto kern = window_bwd_dq_kernel<DH, SPLIT, HW, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  const dim3 grid = PACKED ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
+  const dim3 grid = PACKED != 0 ? dim3((unsigned)(p.H / HW * packed_blocks(p.packed, 128 / SPLIT / HW))) : dim3((unsigned)(p.H * p.B), (unsigned)((p.S * SPLIT + 127) / 128));
   hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, p);
   return hipGetLastError();
 }
 
-template <int DH, int KEYS, bool PACKED = false>
+template <int DH, int KEYS, int PACKED = 0>
 static hipError_t launch_kv(const WinKvParams& p, hipStream_t s) {
   constexpr size_t smem = 3 * (2 * 64 * DH * 2 + (DH == 64 ? 0 : 1024)) + 2 * 4 * 4096;       // three slots, two hand-over buffers
   auto kern = window_bwd_kv_kernel<DH, KEYS, PACKED>;
   static AttrOnce once;
   if (hipError_t e = once.set(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
   constexpr int per = KEYS / (256 / (2 * (DH / 8)));
-  if constexpr (PACKED) {
+  if constexpr (PACKED != 0) {
     const long blocks = p.KV * packed_blocks(p.packed, KEYS);
     hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.parts.other_parts)), dim3(512), smem, s, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.parts.other_parts == 1) return e;
-    hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, true>), dim3((unsigned)(blocks * per)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, PACKED>), dim3((unsigned)(blocks * per)), dim3(256), 0, s, p);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.KV * p.B), (unsigned)p.parts.workgroups()), dim3(512), smem, s, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.parts.cut_blocks()) return e;
-  hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, false>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((window_bwd_join_kernel<DH, KEYS, 0>), dim3((unsigned)(p.KV * p.B), (unsigned)(p.parts.cut_blocks() * per)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -1395,6 +1396,18 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
 // ---- packed sequences: the same kernels, by rules on the mean length, since the lengths are on the device
 static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, w.rows}; }
 
+// Whether blocks come the most work first whatever their sequence, or by their rows.  The last workgroups then are short ones: by rows, of 5 sequences of 1639 tokens
+// the forward's last sixth ran with half of the places empty.  The most first costs the finding of a block among its sequences (a third of a us of each), and keys and values
+// that are met again later, so not where those of the heads that an L2 works on exceed its 4 MiB.  A rule of the launch: with both orders in one kernel it was 4 % slower.
+// us of the forward, in order / the most first, of 128: 32 heads on 8, 3 sequences of 1365 66.0 / 60.1, 5 of 1639 139 / 136, 24 of 8192 in all 76 / 74, but 24 of 16384 174 / 183, 32 of
+// 8192 70.8 / 73.1; 16 on 8, 5 of 1639 77 / 66, 24 of 8192 52.7 / 48.7; 16 on 16, 6 of 4096 49 / 51; of 64: 32 on 8, 24 of 8192 41.5 / 36.7, but 64 of 128 19.7 / 20.3.
+static bool queries_by_work(const PackedShape& w) {
+  return w.seqs > 1 && w.seqs <= 24 && w.heads / w.kv_heads % 2 == 0 && (long)w.kv_heads * w.rows * w.head_dim <= 1 << 23;
+}
+// us of the backward, in order / the most first: 32 heads on 8 of 128, 5 sequences of 1639 529 / 484, 16 and 24 of 8192 in all 311 / 286 and 298 / 291, 64 of 4000 91 / 80, but 32 of 128
+// 59.7 / 61.4; 32 on 8 of 64, 24 of 8192 144 / 124, 40 of 16384 297 / 279, 20 of 200 33.5 / 30.5, but 64 of 128 60.1 / 64.9, 30 of 67 24.4 / 26.2
+static bool keys_by_work(const PackedShape& w) { return w.seqs <= 64 && (w.head_dim == 128 || w.rows >= 192 * w.seqs); }
+
 template <int N> using Int = std::integral_constant<int, N>;
 // run(head_dim, query heads of a workgroup): as many as their number allows
 template <typename F> static hipError_t by_heads(const PackedShape& w, F run) {
@@ -1412,12 +1425,12 @@ hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_q
   const int mean = w.rows / (w.seqs > 0 ? w.seqs : 1);
   // scores ahead where sequences have several blocks of keys: us, ahead / not, 32 heads on 8 of 128: 5 sequences of 1639 141 / 149, 16 on 16, 6 of 683 on average 48 / 53,
   // 60 of 130 67 / 67
-  const bool few = groups <= (w.head_dim == 64 ? 512 : 256), ahead = w.head_dim == 128 && mean > 256;
+  const bool few = groups <= (w.head_dim == 64 ? 512 : 256), ahead = w.head_dim == 128 && mean > 256, by_work = queries_by_work(w);
   auto run = [&](auto dh, auto hw) {
     constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
-    if (few) return launch_fwd<DH, false, 2, HW < 2 ? 1 : 2, true>(p, s);
-    if constexpr (DH == 128) if (ahead) return launch_fwd<DH, true, 1, HW, true>(p, s);
-    return launch_fwd<DH, false, 1, HW, true>(p, s);
+    if (few) return launch_fwd<DH, false, 2, HW < 2 ? 1 : 2, kInOrder>(p, s);
+    if constexpr (DH == 128) if (ahead) return by_work ? launch_fwd<DH, true, 1, HW, kMostFirst>(p, s) : launch_fwd<DH, true, 1, HW, kInOrder>(p, s);
+    return by_work ? launch_fwd<DH, false, 1, HW, kMostFirst>(p, s) : launch_fwd<DH, false, 1, HW, kInOrder>(p, s);
   };
   return by_heads(w, run);
 }
@@ -1452,10 +1465,11 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
   q.B = 1; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.rows;
   q.scale = 1.f / sqrtf((float)w.head_dim);
   q.scale_log2e = 1.4426950408889634f * q.scale;
-  const bool few = (long)w.heads * (w.rows / 128 + w.seqs) <= (w.head_dim == 64 ? 512 : 256);
+  const bool few = (long)w.heads * (w.rows / 128 + w.seqs) <= (w.head_dim == 64 ? 512 : 256), by_work = queries_by_work(w);
   hipError_t e = by_heads(w, [&](auto dh, auto hw) {
     constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
-    return few ? launch_dq<DH, 2, HW < 2 ? 1 : 2, true>(q, s) : launch_dq<DH, 1, HW, true>(q, s);
+    if (few) return launch_dq<DH, 2, HW < 2 ? 1 : 2, kInOrder>(q, s);
+    return by_work ? launch_dq<DH, 1, HW, kMostFirst>(q, s) : launch_dq<DH, 1, HW, kInOrder>(q, s);
   });
   if (e != hipSuccess) return e;
   WinKvParams p{};
@@ -1464,8 +1478,12 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
   p.B = 1; p.H = q.H; p.KV = q.KV; p.G = q.G; p.S = q.S;
   p.parts = packed_parts(w);
   p.scale = q.scale; p.scale_log2e = q.scale_log2e;
-  if (w.head_dim == 64) return launch_kv<64, 64, true>(p, s);
-  return p.parts.keys == 64 ? launch_kv<128, 64, true>(p, s) : launch_kv<128, 128, true>(p, s);
+  auto run = [&](auto order) {
+    constexpr int PACKED = decltype(order)::value;
+    if (w.head_dim == 64) return launch_kv<64, 64, PACKED>(p, s);
+    return p.parts.keys == 64 ? launch_kv<128, 64, PACKED>(p, s) : launch_kv<128, 128, PACKED>(p, s);
+  };
+  return keys_by_work(w) ? run(Int<kMostFirst>()) : run(Int<kInOrder>());
 }
 
 // Shares of a head's keys, at most: as many as make the rounds of workgroups (one per compute unit at head_dim 128, two at 64) short by this model, whose

@@ -249,6 +249,36 @@ def test_packed_attention_matches_oracle(case):
             assert np.all(err <= t), (name, a, b, float((err / t).max()))
 
 
+# few sequences, query heads that share keys: query blocks in the order of their work
+BY_WORK_CASES = [
+    ([300, 1, 0, 129, 128, 127, 640, 33, 32, 31, 64, 65, 2], 7, 16, 8, 128), ([2600, 2048, 2016, 1], 2, 8, 2, 128), ([130, 4200], 1, 8, 4, 128), ([2500, 40, 700], 0, 32, 16, 64),
+    ([3000, 1, 0, 1, 2000], 3, 16, 4, 64), ([0, 0, 1030, 0], 0, 32, 8, 128), ([90 + 7 * i for i in range(24)], 0, 16, 2, 64), ([90 + 7 * i for i in range(25)], 0, 16, 2, 64),
+]
+
+
+@pytest.mark.parametrize("case", BY_WORK_CASES, ids=lambda c: f"{len(c[0])}x{max(c[0], default=0)}+{c[1]}-{c[2]}-{c[3]}-{c[4]}")
+def test_packed_attention_in_the_order_of_the_work_matches_oracle(case):
+    test_packed_attention_matches_oracle(case)
+
+
+def test_packed_attention_of_heads_that_share_keys_over_a_very_long_sequence():
+    """More query blocks of a sequence than are looked through at once, at any level."""
+    n, m, H, KV, dh = 70000, 600, 4, 1, 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    qkv = torch.empty((n + m, 6 * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    do = torch.empty((n + m, 4 * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    s = _ints([0, m, n + m])
+    out, lse = tbp.tbp_packed_attention_fwd(qkv, s, H, KV, dh)
+    d = tbp.tbp_packed_attention_p1(qkv, out, do, lse, s, H, KV, dh)
+    for at, k in ((0, m), (m, n)):
+        x = qkv[at:at + k].contiguous()
+        want, wlse = tbp.tbp_window_attention_fwd(x, k, H, KV, dh, k)
+        wd = tbp.tbp_window_attention_p1(x, want, do[at:at + k].contiguous(), wlse, k, H, KV, dh, k)
+        for a, b in ((out[at:at + k], want), (lse[:, at:at + k], wlse[0]), (d[at:at + k], wd)):     # (the two may cut the work differently)
+            assert (a.float() - b.float()).norm() <= 4e-3 * b.float().norm()
+
+
 def test_packed_attention_of_one_sequence_is_window_attention():
     n, H, KV, dh = 777, 8, 2, 128
     _, _, _, _, qkv, do = _packed_inputs(([n], 0, H, KV, dh))
