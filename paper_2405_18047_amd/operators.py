@@ -483,7 +483,7 @@ def tbp_packed_attention_p1(qkv, out, d_out, lse, starts, n_heads, n_kv_heads, h
 class Stash8:
     """`slots` micro-batches [tokens, cols] of one tensor, held in 8 bits with a power of two as scale for every 1024 tokens of a column: a linear layer's inputs or
     output derivatives between backward-p1 and backward-p2 (tbp_stash8_dw), or what a functional operation needs again (get).  A slot that nothing
-    was put into holds zeros.  dtype: of the tensors that get returns."""
+    was put into holds zeros (the memory is zeroed on the stream that is current now).  dtype: of the tensors that get returns."""
 
     def __init__(self, tokens, cols, slots=1, dtype=torch.bfloat16, device="cuda"):
         nbytes = lib().tbp_stash8_bytes(slots, tokens, cols)
