@@ -103,7 +103,7 @@ def _good_calls():
     attn = dict(n_heads=4, n_kv_heads=2, head_dim=64)
     return {
         "norm": (tbp.tbp_qk_norm, dict(qk=_bf(6, 384), **heads, table=table, positions=_i32(6), out=_bf(6, 384))),
-        "norm_p1": (tbp.tbp_qk_norm_p1, dict(d_out=_bf(6, 384), qk=_bf(6, 384), **heads, table=table, positions=_i32(6), out=_bf(6, 384), partials=torch.zeros((1, 128)))),
+        "norm_p1": (tbp.tbp_qk_norm_p1, dict(d_out=_bf(6, 384), qk=_bf(6, 384), **heads, table=table, positions=_i32(6), out=_bf(6, 384), partials=torch.zeros((tbp.lib().tbp_qk_norm_partial_rows(6, 4, 2, 64), 128)))),
         "append": (tbp.tbp_qk_norm_append, dict(qkv=_bf(6, 512), **heads, table=table, lengths=_i32(2), cache_k=_bf(2, 8, 128), cache_v=_bf(2, 8, 128), q_out=_bf(6, 256))),
         "packed_fwd": (tbp.tbp_packed_attention_fwd, dict(qkv=_bf(6, 512), starts=_i32(3), **attn, out=_bf(6, 256), lse=torch.zeros((4, 6)))),
         "packed_p1": (tbp.tbp_packed_attention_p1, dict(qkv=_bf(6, 512), out=_bf(6, 256), d_out=_bf(6, 256), lse=torch.zeros((4, 6)), starts=_i32(3), **attn, dqkv=_bf(6, 512),
