@@ -426,7 +426,7 @@ tbp_status tbp_qk_norm_append(int dtype, int batch, int n_new, int n_heads, int 
  * j <= i.  Rows behind the last sequence (from starts[n_seqs] on) are padding: never read, zeros in every result, lse -infinity.  Entries
  * outside 0 .. rows are taken as the nearest of these and starts[0] as 0; where they do not ascend, results are undefined (nothing outside the
  * tensors is touched).  lse: device [n_heads, rows] fp32.  Types, head rules, layouts, alignment and finite rows as for tbp_window_attention_fwd.
- * Limits: 0 <= rows <= 2^22, 0 <= n_seqs <= 2^20, n_heads * (rows / 32 + n_seqs + 1) below 2^27. */
+ * Limits: 0 <= rows <= 2^22, 0 <= n_seqs <= 2^20, n_heads * (rows / 32 + n_seqs + 1) below 2^23. */
 tbp_status tbp_packed_attention_fwd(int dtype, int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, const int32_t* starts,
                                     const void* qkv, int ld_qkv, void* out, int ld_out, float* lse, void* stream);
 /* Its backward-p1, as tbp_window_attention_p1.  scratch: device, 256-byte aligned, >= tbp_packed_attention_p1_scratch_bytes of the same sizes. */

@@ -409,7 +409,7 @@ static tbp_status check_packed(int dtype, int n_seqs, int rows, int n_heads, int
   if (check_heads(n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
   if (n_seqs < 0 || rows < 0) return fail(TBP_EINVAL, "negative size");
   if (rows > (1 << 22) || n_seqs > (1 << 20)) return fail(TBP_EINVAL, "rows above 2^22 or n_seqs above 2^20");
-  if ((long)n_heads * (rows / 32 + n_seqs + 1) >= (1L << 27)) return fail(TBP_EINVAL, "n_heads * (rows / 32 + n_seqs + 1) must be below 2^27");
+  if ((long)n_heads * (rows / 32 + n_seqs + 1) >= (1L << 23)) return fail(TBP_EINVAL, "n_heads * (rows / 32 + n_seqs + 1) must be below 2^23");      // (threads of a launch are counted in 32 bits)
   return TBP_OK;
 }
 

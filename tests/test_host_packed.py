@@ -165,3 +165,11 @@ def test_other_bad_calls_are_refused():
     with pytest.raises(ValueError, match="whole"):
         call, good = _good_calls()["append"]
         call(**{**good, "qkv": _bf(5, 512)})
+
+
+def test_packed_attention_takes_no_more_blocks_than_a_launch_has_threads_for():
+    """A launch has up to 512 threads for every (key head, 64 rows or sequence), counted in 32 bits."""
+    assert tbp.lib().tbp_packed_attention_p1_scratch_bytes(3, 1 << 22, 64, 64, 64) == 0
+    assert b"2^23" in tbp.lib().tbp_last_error()
+    assert tbp.lib().tbp_packed_attention_p1_scratch_bytes(1 << 20, 1 << 20, 8, 8, 128) == 0
+    assert tbp.lib().tbp_packed_attention_p1_scratch_bytes(3, 1 << 22, 32, 8, 128) > 0
