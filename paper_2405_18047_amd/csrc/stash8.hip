@@ -445,7 +445,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER
     left = left == n ? p.steps : left - n;
   }
   wait_vmem<0>();                                      // (copies past the end: zeros)
-  if (p.shares > 1) {
+  if (MB == 2 && p.shares > 1) {                       // (only the small tiles are so few)
     f32x4* const part = reinterpret_cast<f32x4*>(p.part) + (((long)share * p.tiles_m * p.tiles_n + (long)tm * p.tiles_n + tn) * 4 + wave) * (MB * NB * 256) + lane;
 #pragma unroll
     for (int i = 0; i < MB; i++) {
@@ -555,8 +555,8 @@ static hipError_t launch_dw(Stash8Dw p, hipStream_t s) {
   p.tiles_n = (p.db + 2 * NB - 1) / (2 * NB);
   const long tiles = (long)p.tiles_m * p.tiles_n;
   hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * p.shares)), dim3(256), smem, s, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.shares == 1) return e;
-  hipLaunchKernelGGL((stash8_join_kernel<MB, NB>), dim3((unsigned)(tiles * MB * NB * 4)), dim3(256), 0, s, p);
+  if constexpr (MB == 2)
+    if (p.shares > 1) hipLaunchKernelGGL((stash8_join_kernel<MB, NB>), dim3((unsigned)(tiles * MB * NB * 4)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
