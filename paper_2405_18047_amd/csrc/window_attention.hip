@@ -1429,8 +1429,10 @@ hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_q
   auto run = [&](auto dh, auto hw) {
     constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
     if (few) return launch_fwd<DH, false, 2, HW < 2 ? 1 : 2, kInOrder>(p, s);
-    if constexpr (DH == 128) if (ahead) return by_work ? launch_fwd<DH, true, 1, HW, kMostFirst>(p, s) : launch_fwd<DH, true, 1, HW, kInOrder>(p, s);
-    return by_work ? launch_fwd<DH, false, 1, HW, kMostFirst>(p, s) : launch_fwd<DH, false, 1, HW, kInOrder>(p, s);
+    if constexpr (DH == 128 && HW > 1) if (ahead && by_work) return launch_fwd<DH, true, 1, HW, kMostFirst>(p, s);
+    if constexpr (DH == 128) if (ahead) return launch_fwd<DH, true, 1, HW, kInOrder>(p, s);
+    if constexpr (HW > 1) if (by_work) return launch_fwd<DH, false, 1, HW, kMostFirst>(p, s);
+    return launch_fwd<DH, false, 1, HW, kInOrder>(p, s);
   };
   return by_heads(w, run);
 }
@@ -1469,7 +1471,8 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
   hipError_t e = by_heads(w, [&](auto dh, auto hw) {
     constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
     if (few) return launch_dq<DH, 2, HW < 2 ? 1 : 2, kInOrder>(q, s);
-    return by_work ? launch_dq<DH, 1, HW, kMostFirst>(q, s) : launch_dq<DH, 1, HW, kInOrder>(q, s);
+    if constexpr (HW > 1) if (by_work) return launch_dq<DH, 1, HW, kMostFirst>(q, s);
+    return launch_dq<DH, 1, HW, kInOrder>(q, s);
   });
   if (e != hipSuccess) return e;
   WinKvParams p{};
