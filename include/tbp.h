@@ -446,7 +446,7 @@ tbp_status tbp_stash8_put(int dtype, int slots, int tokens, int cols, int slot, 
 tbp_status tbp_stash8_get(int dtype, int slots, int tokens, int cols, int slot, const void* stash, void* y, int ld_y, void* stream);
 /* backward-p2 of a linear layer from two such stashes (Section 3.1; Section 3.2: the slots are one contraction length, without a copy): dw [m, ld_dw]
  * fp32 (= or +=) X^T dY, X [n * tokens, m] and dY [n * tokens, cols n_out] the n slots from `first` on.  The sums over a block of 1024 tokens are
- * exact integers, those over the blocks fp32 (of a block less than fp32's smallest normal number may be lost), in an order that does not depend on timing.  n == 0 writes zeros (or leaves an accumulated dw alone).
+ * exact integers, whatever the two scales (0 stays 0), those over the blocks fp32, one rounding a block, in an order that does not depend on timing.  n == 0 writes zeros (or leaves an accumulated dw alone).
  * workspace: device, 256-byte aligned, >= tbp_stash8_dw_workspace_bytes of the same sizes (may be 0: NULL); calls that share one must not overlap. */
 size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n);
 tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,

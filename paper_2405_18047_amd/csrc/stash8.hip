@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __rest
 // One workgroup = 4 waves, 2 x 2, each 32 MB x 32 NB of the output; the contraction in steps of 64 tokens through a ring of slots in LDS, filled by
 // asynchronous copies all but one of them ahead.  The units are copied as they are: every fragment is 64 lanes x 16 bytes in a row.
 // The integer sums of a block of tokens are exact: 1024 x 127^2 is below 2^24, so that they are exact in fp32 as well, in which the blocks are added
-// up, each with the product of the two columns' scales.  That takes three vector instructions per element and block, done tile by tile in front of the tile's first
+// up, each times the two columns' scales.  That takes three vector instructions per element and block, done tile by tile in front of the tile's first
 // product of the next block (5 % of the time), and a second set of accumulators: 96 x 96 to a wave, one wave to a SIMD, or 64 x 64 and two.
 // Bound by power on large outputs: 11008 x 4096 over 8 x 4096 tokens 1450 to 1720 us over cards, 1.72 to 2.04 PFLOP/s (at the rate of the bf16 weight gradients, 1.29, 2283), at 1.5 to 1.9 GHz with
 // the matrix pipes busy 52 %; the same instructions on zeros take 7 % fewer cycles, at 2.27 GHz.  Rounds of few steps by their start and end (8 us): 4096 x 4096 over 4096
@@ -369,21 +369,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER
     else if (k < NB + 1) frb[to][k - 1] = *reinterpret_cast<LDS_AS const i32x4*>(from + (UA + wn * NB + k - 1) * kUnit);
     else fra[to][k - NB] = *reinterpret_cast<LDS_AS const i32x4*>(from + (wm * MB + k - NB) * kUnit);
   };
-  // what the block's integer sums add to the result: a tile, by the scales of its rows and of the lane's column
+  // What the block's integer sums add to the result: a tile, by the scales of its rows and of the lane's column.  The integer takes the column's first and the row's
+  // as the rounded sum is formed: the product of the two scales may be infinite where the integer is 0, or too small for fp32 where the result is not.  Below 2^24,
+  // the integer times a scale up to 2^103 is exact and finite.  Of a larger one (`high`: some column of the wave's has one) 2^24 goes to the rows, but for
+  // those above 2^103 themselves, with which the result is 0 or infinite all the same.
+  constexpr float HIGH = 0x1p103f;
   f32x4 sa[4];
   float sb[NB];
-  auto scales_of = [&](int i, int block) {
+  bool high = false, moved[NB];
+  auto rows_of = [&](int i, int block) {
     const LDS_AS float* const s = reinterpret_cast<const LDS_AS float*>(sc + (block & (RING - 1)) * SCALES);
 #pragma unroll
     for (int q = 0; q < 4; q++) sa[q] = *reinterpret_cast<const LDS_AS f32x4*>(s + 32 * (wm * MB + i) + 8 * q + 4 * g);
-    if (i == 0) {
-#pragma unroll
-      for (int j = 0; j < NB; j++) sb[j] = s[256 + 32 * (wn * NB + j) + (lane & 31)];
-    }
   };
-  auto add_tile = [&](int i, int j) {
+  auto scales_of = [&](int i, int block) {
+    if (i == 0) {
+      const LDS_AS float* const s = reinterpret_cast<const LDS_AS float*>(sc + (block & (RING - 1)) * SCALES);
+      bool any = false;
 #pragma unroll
-    for (int e = 0; e < 16; e++) fa[i][j][e] = __builtin_fmaf((float)ia[i][j][e], sa[e >> 2][e & 3] * sb[j], fa[i][j][e]);
+      for (int j = 0; j < NB; j++) {
+        const float b = s[256 + 32 * (wn * NB + j) + (lane & 31)];
+        moved[j] = b > HIGH;
+        sb[j] = moved[j] ? b * 0x1p-24f : b;
+        any |= moved[j];
+      }
+      high = __any(any);
+    }
+    rows_of(i, block);
+  };
+  auto add_tile = [&](int i, int j, int block) {
+    if (__builtin_expect(high, 0)) {
+      rows_of(i, block);
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const float row = sa[e >> 2][e & 3];
+        sa[e >> 2][e & 3] = moved[j] && !(row > HIGH) ? row * 0x1p24f : row;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e++) fa[i][j][e] = __builtin_fmaf((float)ia[i][j][e] * sb[j], sa[e >> 2][e & 3], fa[i][j][e]);
     asm volatile("" : "+v"(fa[i][j]));                // (here and now: the compiler would keep all the integers for later)
   };
 
@@ -405,7 +429,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER
       const int i = k / NB, j = k % NB;
       if constexpr (BEGIN) {
         if (j == 0) scales_of(i, before);
-        add_tile(i, j);
+        add_tile(i, j, before);
 #pragma unroll
         for (int e = 0; e < 16; e++) ia[i][j][e] = 0;
       }
@@ -452,7 +476,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER
       scales_of(i, block - 1);
 #pragma unroll
       for (int j = 0; j < NB; j++) {
-        add_tile(i, j);
+        add_tile(i, j, block - 1);
 #pragma unroll
         for (int q = 0; q < 4; q++) part[((i * NB + j) * 4 + q) * 64] = f32x4{fa[i][j][4 * q], fa[i][j][4 * q + 1], fa[i][j][4 * q + 2], fa[i][j][4 * q + 3]};
       }
@@ -464,7 +488,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(PER_CU, PER
     scales_of(i, block - 1);
 #pragma unroll
     for (int j = 0; j < NB; j++) {
-      add_tile(i, j);
+      add_tile(i, j, block - 1);
       const int n = 32 * (ub_b + wn * NB + j) + (lane & 31);
       if (n < p.N) {
 #pragma unroll

@@ -485,6 +485,59 @@ def test_integer_sums_at_their_largest():
     assert torch.all(dw[4:] == -1024 * 127 * 127) and torch.all(dw[3] == -1024 * 127 * 127 + 127)
 
 
+def _any_magnitude(tokens, cols, seed, share, signed=True):
+    """Whole multiples of powers of two of every size that a scale has, a column each; a share of the tokens has a value."""
+    u = np.abs(si.standard_normal(seed, "u", (tokens, cols)))
+    q = np.clip(np.rint(40 * u), 1, 127) * (u - np.floor(u) < share)
+    if signed:
+        q *= np.sign(si.standard_normal(seed, "sign", (tokens, cols)))
+    e = (np.arange(cols) * 89 + 31 * seed) % 248 - 126               # (neighbours far apart)
+    return (q * 2.0 ** e[None, :]).astype(np.float32)
+
+
+@pytest.mark.parametrize("case", [(64, 40, 50, 0.03), (1000, 200, 260, 0.002), (1024, 130, 300, 1.0), (65, 3070, 3050, 0.05)], ids=str)
+def test_weight_gradients_of_any_magnitudes(case):
+    """One block: the sums of integers are exact, so that a gradient is the exact one rounded to fp32 once: 0 where the integers add up to 0, whatever
+    the scales; infinite beyond fp32's range; the nearest multiple of 2^-149 below its smallest normal number."""
+    tokens, m, n_out, share = case
+    _say(f"dw of any magnitudes {case}")
+    x, d = _any_magnitude(tokens, m, 1, share), _any_magnitude(tokens, n_out, 2, share)
+    kx, kd = tbp.Stash8(tokens, m, device=DEV), tbp.Stash8(tokens, n_out, device=DEV)
+    kx.put(0, to_dev(x, "f32")), kd.put(0, to_dev(d, "f32"))
+    exact, _ = ref.stash8_dw([x], [d])
+    with np.errstate(over="ignore"):
+        want = exact.astype(np.float32)
+    assert np.isinf(want).any() and np.isfinite(want).any()
+    got = tbp.tbp_stash8_dw(kx, kd)
+    assert np.array_equal(got.cpu().numpy(), want)
+    base = torch.full((m, n_out), 0.5, device=DEV)
+    tbp.tbp_stash8_dw(kx, kd, dw=base, accumulate=True)
+    assert np.array_equal(base.cpu().numpy(), np.float32(0.5) + want)
+    # nothing in common
+    x, d = torch.zeros((tokens, m), device=DEV), torch.zeros((tokens, n_out), device=DEV)
+    x[0], d[1] = 1e38, 1e10
+    kx.put(0, x), kd.put(0, d)
+    assert not tbp.tbp_stash8_dw(kx, kd).any()
+    tbp.tbp_stash8_dw(kx, kd, dw=base.fill_(0.5), accumulate=True)
+    assert torch.all(base == 0.5)
+
+
+def test_weight_gradients_of_any_magnitudes_over_many_blocks():
+    """In shares of the contraction, of values that are not negative: what fp32 loses of the sums (as above), infinite beyond its range, never NaN."""
+    tokens, m, n_out, slots = 1100, 150, 130, 8
+    xs, ds = [_any_magnitude(tokens, m, 3, 0.01 * i, False) for i in range(slots)], [_any_magnitude(tokens, n_out, 4, 0.01, False) for _ in range(slots)]
+    kx, kd = tbp.Stash8(tokens, m, slots, device=DEV), tbp.Stash8(tokens, n_out, slots, device=DEV)
+    for i in range(slots):
+        kx.put(i, to_dev(xs[i], "f32")), kd.put(i, to_dev(ds[i], "f32"))
+    assert tbp.lib().tbp_stash8_dw_workspace_bytes(tokens, m, n_out, slots) > 0
+    want, _ = ref.stash8_dw(xs, ds)
+    got = to_np(tbp.tbp_stash8_dw(kx, kd))
+    lost = 2 * slots * (2.0 ** -24 * want + 2.0 ** -150)
+    beyond, within = want - lost >= 2.0 ** 128, want + lost < 2.0 ** 128 - 2.0 ** 103
+    assert beyond.any() and within.any()
+    assert np.all(np.isposinf(got[beyond])) and np.all(np.abs(got - want)[within] <= lost[within]) and np.all(got >= 0)
+
+
 # ------------------------------------------------------------------------------------- together, captured, on other streams
 def _layer(seed, starts, H, KV, dh, d):
     """What a layer of packed documents has: hidden rows, weights of its projections, gains, the output's derivative, positions in the documents."""
