@@ -467,7 +467,8 @@ static tbp::Stash8Slot stash8_slot(int slots, int tokens, int cols, int slot, co
 }
 
 size_t tbp_stash8_bytes(int slots, int tokens, int cols) {
-  if (slots < 1 || check_stash8(slots, tokens, cols) != TBP_OK) return 0;
+  if (check_stash8(slots, tokens, cols) != TBP_OK) return 0;
+  if (slots == 0) { fail(TBP_EINVAL, "a stash must have slots, at least 1"); return 0; }
   return stash8_data_bytes(slots, tokens, cols) + (size_t)slots * ((tokens + tbp::kStash8Block - 1) / tbp::kStash8Block) * ((cols + 31) / 32) * 32 * sizeof(float);
 }
 

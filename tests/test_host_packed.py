@@ -173,3 +173,11 @@ def test_packed_attention_takes_no_more_blocks_than_a_launch_has_threads_for():
     assert b"2^23" in tbp.lib().tbp_last_error()
     assert tbp.lib().tbp_packed_attention_p1_scratch_bytes(1 << 20, 1 << 20, 8, 8, 128) == 0
     assert tbp.lib().tbp_packed_attention_p1_scratch_bytes(3, 1 << 22, 32, 8, 128) > 0
+
+
+@pytest.mark.parametrize("size", [{"slots": 0}, {"slots": -1}, {"tokens": 0}, {"cols": 1 << 22}, {"tokens": 1 << 22, "slots": 1 << 15}], ids=str)
+def test_a_stash_that_cannot_be_says_why(size):
+    """The text is this refusal's, not that of a failure before it."""
+    _refused(tbp.lib().tbp_packed_attention_fwd(*{**PACKED, "head_dim": 96}.values()), "head_dim")
+    with pytest.raises(ValueError, match="no stash of .*(slots|tokens)[^:]*(at least|above|too large)"):
+        tbp.Stash8(**{"tokens": 5, "cols": 4, "slots": 1, **size}, device="cpu")
