@@ -451,6 +451,8 @@ tbp_status tbp_stash8_get(int dtype, int slots, int tokens, int cols, int slot, 
 size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n);
 tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,
                          int ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+/* How it runs over n slots: rows and columns of a workgroup's output tile, and shares of the contraction (host only; for tests and measurements). */
+tbp_status tbp_stash8_dw_plan(int tokens, int m, int n_out, int n, int* tile, int* shares);
 
 /* Measurement aid (no paper passage: it prices the hardware, not the method): a register-resident loop of
  * 32x32x16 bf16 MFMAs, blocks x 4 wavefronts x iters x 16 instructions = blocks*iters*2^21 FLOP, touching no memory

@@ -138,6 +138,7 @@ def lib() -> C.CDLL:
         L.tbp_stash8_put.argtypes = [i32] * 5 + [ptr, i32, ptr, ptr]
         L.tbp_stash8_get.argtypes = [i32] * 5 + [ptr, ptr, i32, ptr]
         L.tbp_stash8_dw_workspace_bytes.argtypes, L.tbp_stash8_dw_workspace_bytes.restype = [i32] * 4, size
+        L.tbp_stash8_dw_plan.argtypes = [i32] * 4 + [C.POINTER(i32)] * 2
         L.tbp_stash8_dw.argtypes = [i32] * 6 + [ptr, ptr, ptr, i32, i32, ptr, size, ptr]
         _lib = L
     return _lib

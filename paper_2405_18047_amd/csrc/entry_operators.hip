@@ -498,6 +498,14 @@ size_t tbp_stash8_dw_workspace_bytes(int tokens, int m, int n_out, int n) {
   return tbp::stash8_plan(m, n_out, n * ((tokens + 63) / 64), n * ((tokens + tbp::kStash8Block - 1) / tbp::kStash8Block)).bytes;
 }
 
+tbp_status tbp_stash8_dw_plan(int tokens, int m, int n_out, int n, int* tile, int* shares) {
+  if (!tile || !shares) return fail(TBP_EINVAL, "outputs must be non-null");
+  if (check_stash8(n, tokens, m) != TBP_OK || check_stash8(n, tokens, n_out) != TBP_OK) return TBP_EINVAL;
+  const tbp::Stash8Plan plan = tbp::stash8_plan(m, n_out, n * ((tokens + 63) / 64), n * ((tokens + tbp::kStash8Block - 1) / tbp::kStash8Block));
+  *tile = 64 * plan.mb; *shares = plan.shares;
+  return TBP_OK;
+}
+
 tbp_status tbp_stash8_dw(int slots, int tokens, int m, int n_out, int first, int n, const void* x_stash, const void* dy_stash, float* dw,
                          int ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
   if (check_stash8(slots, tokens, m) != TBP_OK || check_stash8(slots, tokens, n_out) != TBP_OK) return TBP_EINVAL;

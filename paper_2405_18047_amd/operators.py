@@ -19,7 +19,7 @@ __all__ = [
     "TBP_ROTARY_HALF", "TBP_ROTARY_INTERLEAVED", "TBP_ROTARY_PLAIN", "TBP_ROTARY_LINEAR", "TBP_ROTARY_BASE", "TBP_ROTARY_RAMP",
     "tbp_rotary_scale", "tbp_rotary_table", "tbp_rotary", "tbp_rotary_append", "tbp_window_attention_fwd", "tbp_window_attention_p1",
     "tbp_window_decode_workspace", "tbp_window_decode", "tbp_logprobs", "tbp_logprobs_p1", "tbp_logprobs_step", "GradList",
-    "tbp_qk_norm", "tbp_qk_norm_p1", "tbp_qk_norm_append", "tbp_packed_attention_fwd", "tbp_packed_attention_p1", "Stash8", "tbp_stash8_dw",
+    "tbp_qk_norm", "tbp_qk_norm_p1", "tbp_qk_norm_append", "tbp_packed_attention_fwd", "tbp_packed_attention_p1", "Stash8", "tbp_stash8_dw", "tbp_stash8_dw_plan",
 ]
 
 TBP_ROTARY_HALF, TBP_ROTARY_INTERLEAVED = 0, 1
@@ -534,3 +534,10 @@ def tbp_stash8_dw(x, dy, first=0, n=None, dw=None, accumulate=False, workspace=N
     _check(L.tbp_stash8_dw(x.slots, x.tokens, x.cols, dy.cols, first, n, x.memory.data_ptr(), dy.memory.data_ptr(), dw.data_ptr(), ld, 1 if accumulate else 0,
                            at, nbytes, _stream_of(x.memory.get_device(), dy.memory, *given)))
     return dw
+
+
+def tbp_stash8_dw_plan(tokens, m, n_out, n):
+    """(rows and columns of a workgroup's output tile, shares of the contraction) of tbp_stash8_dw over n slots."""
+    out = [C.c_int() for _ in range(2)]
+    _check(lib().tbp_stash8_dw_plan(tokens, m, n_out, n, *(C.byref(o) for o in out)))
+    return tuple(o.value for o in out)

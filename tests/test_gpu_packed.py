@@ -475,6 +475,24 @@ def test_weight_gradients_from_the_stash(case):
     assert not base[:m, :n_out].any() and torch.all(base[m:] == 0.5) and torch.all(base[:, n_out:] == 0.5)
 
 
+# tokens and columns that end inside a tile, several slots, blocks of one step and of many
+LARGE_TILE_CASES = [(65, 3070, 3050, 2, "bf16"), (1100, 3010, 2990, 3, "bf16"), (40, 2900, 3040, 9, "f32"), (1024, 3071, 2881, 2, "f32"), (150, 6100, 1500, 4, "bf16"), (65, 4400, 4201, 2, "bf16")]
+
+
+@pytest.mark.parametrize("case", LARGE_TILE_CASES, ids=str)
+def test_weight_gradients_in_the_large_tiles(case):
+    tokens, m, n_out, slots, _ = case
+    for n in (slots, slots - slots // 2, 1):
+        assert tbp.tbp_stash8_dw_plan(tokens, m, n_out, n) == (192, 1)
+    test_weight_gradients_from_the_stash(case)
+
+
+def test_the_cases_of_weight_gradients_run_every_way():
+    plans = {tbp.tbp_stash8_dw_plan(*c[:4]) for c in DW_CASES + LARGE_TILE_CASES}
+    assert {(tile, shares > 1) for tile, shares in plans} == {(128, False), (128, True), (192, False)}
+    assert tbp.tbp_stash8_dw_plan(65, 3070, 3050, 1) == (192, 1)      # (test_weight_gradients_of_any_magnitudes)
+
+
 def test_integer_sums_at_their_largest():
     """1024 products of 127 * 127 and their signs: the integers' range, and fp32's whole numbers."""
     kx, kd = tbp.Stash8(1024, 40, 1, device=DEV), tbp.Stash8(1024, 50, 1, device=DEV)

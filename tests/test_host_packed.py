@@ -181,3 +181,13 @@ def test_a_stash_that_cannot_be_says_why(size):
     _refused(tbp.lib().tbp_packed_attention_fwd(*{**PACKED, "head_dim": 96}.values()), "head_dim")
     with pytest.raises(ValueError, match="no stash of .*(slots|tokens)[^:]*(at least|above|too large)"):
         tbp.Stash8(**{"tokens": 5, "cols": 4, "slots": 1, **size}, device="cpu")
+
+
+def test_how_a_weight_gradient_from_the_stash_runs():
+    assert tbp.tbp_stash8_dw_plan(4096, 11008, 4096, 8) == (192, 1) and tbp.tbp_stash8_dw_plan(100, 50, 60, 0) == (128, 1)
+    tile, shares = tbp.tbp_stash8_dw_plan(2048, 512, 512, 8)
+    assert tile == 128 and shares > 1 and tbp.lib().tbp_stash8_dw_workspace_bytes(2048, 512, 512, 8) == shares * 512 * 512 * 4
+    for bad in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1, 1, 1, -1), (1, 1 << 22, 1, 1)):
+        with pytest.raises(tbp.TbpError):
+            tbp.tbp_stash8_dw_plan(*bad)
+    _refused(tbp.lib().tbp_stash8_dw_plan(1, 1, 1, 1, None, C.byref(C.c_int())), "null")
