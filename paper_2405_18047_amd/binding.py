@@ -128,6 +128,7 @@ def lib() -> C.CDLL:
         L.tbp_grad_sumsq.argtypes = [i32, i32] + [ptr] * 5
         L.tbp_grad_clip.argtypes = [i32] * 3 + [ptr] * 4 + [f32, ptr, ptr, ptr]
         L.tbp_qk_norm.argtypes = [i32] * 5 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr]
+        L.tbp_qk_norm_heads_per_thread.argtypes = [i32] * 5
         L.tbp_qk_norm_partial_rows.argtypes = [i32] * 4
         L.tbp_qk_norm_p1.argtypes = [i32] * 5 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, ptr]
         L.tbp_qk_norm_append.argtypes = [i32] * 6 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]

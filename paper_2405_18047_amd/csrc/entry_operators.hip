@@ -354,6 +354,11 @@ tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int hea
   return TBP_OK;
 }
 
+int tbp_qk_norm_heads_per_thread(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim) {
+  if (rows < 0 || n_heads < 0 || n_kv_heads < 0 || head_dim < 2) return 0;
+  return tbp::qk_norm_heads_per_thread(dtype, rows, n_heads, n_kv_heads, head_dim);
+}
+
 int tbp_qk_norm_partial_rows(int rows, int n_heads, int n_kv_heads, int head_dim) {
   if (rows < 1 || n_heads < 0 || n_kv_heads < 0 || n_heads + (long)n_kv_heads < 1 || head_dim < 2) return 0;
   return tbp::qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim);

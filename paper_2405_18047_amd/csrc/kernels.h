@@ -309,6 +309,7 @@ struct QkNormParams {
   int units, lanes, q_groups, kv_groups, row0; long items;      // set by the launch
 };
 constexpr int kQkNormMaxHead = 512, kQkNormPartials = 512;
+int qk_norm_heads_per_thread(int dtype, int rows, int q_heads, int kv_heads, int head_dim);
 int qk_norm_partial_rows(int rows, int q_heads, int kv_heads, int head_dim);
 hipError_t qk_norm(int dtype, const QkNormParams& p, hipStream_t s);
 hipError_t qk_norm_p1(int dtype, const QkNormParams& p, hipStream_t s);

@@ -309,13 +309,16 @@ static hipError_t launch_p1(QkNormParams p, hipStream_t s) {
 // heads per thread in the forward: four share angles and gains and load more at a time; one, where four leave compute units short of workgroups.  us, one / four, 40 heads of 128,
 // bf16: 1024 rows 7.7 / 7.5, 2048 11.0 / 9.1, 8192 32.0 / 32.6; 16 of 64: 8192 rows 11.3 / 8.7; fp32, 40 of 128: 1024 9.7 / 7.9.  In backward-p1 always one: four take 220 registers of
 // the 128 that four waves per SIMD have: 8192 rows of 40 heads of 128 70 us for 50.
-static bool four_heads(const QkNormParams& p, int w) { return (long)p.rows * ((p.q_heads + p.kv_heads + 3) / 4) * (p.dh / (2 * w)) >= 384 * 256; }
+int qk_norm_heads_per_thread(int dtype, int rows, int q_heads, int kv_heads, int head_dim) {
+  const int w = dtype ? 8 : 4;
+  return (long)rows * (((long)q_heads + kv_heads + 3) / 4) * (head_dim / (2 * w)) >= 384 * 256 ? 4 : 1;
+}
 
 template <typename T, bool APPEND>
 static hipError_t forward(const QkNormParams& p, hipStream_t s) {
   constexpr int W = 16 / sizeof(T);
   if (!wide<T>(p)) return p.interleaved ? launch_fwd<T, 1, 4, 1, true, APPEND>(p, s) : launch_fwd<T, 1, 4, 1, false, APPEND>(p, s);
-  if (four_heads(p, W)) return p.interleaved ? launch_fwd<T, W, 1, 4, true, APPEND>(p, s) : launch_fwd<T, W, 1, 4, false, APPEND>(p, s);
+  if (qk_norm_heads_per_thread(sizeof(T) == 2, p.rows, p.q_heads, p.kv_heads, p.dh) == 4) return p.interleaved ? launch_fwd<T, W, 1, 4, true, APPEND>(p, s) : launch_fwd<T, W, 1, 4, false, APPEND>(p, s);
   return p.interleaved ? launch_fwd<T, W, 1, 1, true, APPEND>(p, s) : launch_fwd<T, W, 1, 1, false, APPEND>(p, s);
 }
 

@@ -113,6 +113,21 @@ def test_norms_match_oracle(case, ld):
     assert np.all(np.abs(to_np(dg).reshape(2, dh) - dg_ref) <= 2.0 ** -16 * size + 1e-30)
 
 
+# the same with four heads to a thread, the last ones fewer
+FOUR_HEADS_CASES = [
+    (8200, 7, 3, 64, 64, 0, "bf16", True), (8200, 7, 3, 64, 32, 1, "bf16", False), (4100, 7, 3, 64, 64, 1, "f32", True), (4100, 7, 3, 64, 32, 0, "f32", False), (3300, 13, 2, 128, 128, 0, "bf16", True),
+    (4200, 2, 9, 128, 96, 1, "bf16", True), (4100, 5, 1, 96, 0, 0, "f32", False), (1030, 12, 0, 512, 512, 0, "bf16", True), (3000, 0, 9, 128, 64, 0, "f32", True),
+]
+
+
+@pytest.mark.parametrize("ld", [0, 8])
+@pytest.mark.parametrize("case", FOUR_HEADS_CASES, ids=str)
+def test_norms_of_four_heads_to_a_thread_match_oracle(case, ld):
+    rows, H, KV, dh, _, _, dtype, _ = case
+    assert tbp.lib().tbp_qk_norm_heads_per_thread(tbp.TBP_BF16 if dtype == "bf16" else tbp.TBP_F32, rows, H, KV, dh) == 4
+    test_norms_match_oracle(case, ld)
+
+
 def test_norms_of_misaligned_rows():
     rows, H, KV, dh = 21, 3, 1, 64
     x, dy, gq, gk, ang, where = _norm_inputs((rows, H, KV, dh, 64, 0, "bf16", True))
@@ -187,6 +202,39 @@ def test_norm_append_is_the_norm_and_the_cache_s_rule(case):
             at = ops.cache_row(int(p), capacity, sinks)
             wk[r // n, at], wv[r // n, at] = y[r, wq:], qkv[r, wq + wkv:]
     assert torch.allclose(ck.float(), wk.float(), **same) and torch.equal(cv, wv)
+
+
+FOUR_HEADS_APPEND_CASES = [
+    (5, 1700, 6, 3, 64, 64, 0, "bf16", 1000, 3, [1700, 1699, 5000, 1701, -2]), (5, 1700, 6, 3, 64, 32, 1, "bf16", 1000, 0, [1700, 0, 5000, 1701, 3400]),
+    (3, 1400, 6, 3, 64, 64, 1, "f32", 1400, 0, [1400, 1399, 2800]), (2, 3100, 5, 1, 64, 0, 0, "f32", 30, 4, [3100, 3400]), (2, 1100, 13, 13, 128, 128, 0, "bf16", 1200, 1, [1100, 2300]),
+]
+
+
+@pytest.mark.parametrize("case", FOUR_HEADS_APPEND_CASES, ids=str)
+def test_norm_append_of_four_heads_to_a_thread_matches_oracle(case):
+    """q and the caches against the definition: normed and rotated, zeros for tokens before a sequence's first, what later tokens take over left out."""
+    nb, n, H, KV, dh, rot, layout, dtype, capacity, sinks, lengths = case
+    _say(f"append {case}")
+    assert tbp.lib().tbp_qk_norm_heads_per_thread(tbp.TBP_BF16 if dtype == "bf16" else tbp.TBP_F32, nb * n, H, KV, dh) == 4
+    wq, wkv, eps, n_pos = H * dh, KV * dh, 1e-3, 5000
+    qkv = _rnd(3, "qkv", (nb * n, wq + 2 * wkv), dtype)
+    gq, gk = (si.store_round(1 + 0.2 * si.standard_normal(3, k, (dh,)), dtype) for k in ("gq", "gk"))
+    table = tbp.tbp_rotary_table(n_pos, rot, 1e4, device=DEV) if rot else None
+    dev = to_dev(qkv, dtype)
+    ck, cv = (torch.full((nb, capacity, wkv), 77.0, dtype=dev.dtype, device=DEV) for _ in range(2))
+    q = tbp.tbp_qk_norm_append(dev, to_dev(gq, dtype), to_dev(gk, dtype), H, KV, dh, eps, table, _ints(lengths), ck, cv, sinks=sinks, layout=layout)
+    pos = np.concatenate([np.arange(m - n, m) for m in lengths])
+    ang = np.maximum(pos, 0)[:, None] * 1e4 ** (-np.arange(rot // 2) * 2.0 / max(rot, 1))[None, :]
+    want = ref.qk_norm(qkv[:, :wq + wkv], gq, gk, H, KV, eps, ang, layout)
+    off = HALF_STEP[dtype] * np.abs(want) + 2.0 ** -20 * _heads_top(want, H + KV)      # (as for the norms)
+    there = pos >= 0
+    got = to_np(q)
+    assert np.all(np.abs(got - want[:, :wq])[there] <= off[there, :wq]) and not got[~there].any()
+    wk, tol, wv = np.full((nb, capacity, wkv), 77.0), np.zeros((nb, capacity, wkv)), np.full((nb, capacity, wkv), 77.0)
+    for r in np.flatnonzero(there):
+        at = r // n, ops.cache_row(int(pos[r]), capacity, sinks)
+        wk[at], tol[at], wv[at] = want[r, wq:], off[r, wq:], qkv[r, wq + wkv:]
+    assert np.all(np.abs(to_np(ck) - wk) <= tol) and np.array_equal(to_np(cv), wv)
 
 
 # ------------------------------------------------------------------------------------------------- packed sequences

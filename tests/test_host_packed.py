@@ -191,3 +191,9 @@ def test_how_a_weight_gradient_from_the_stash_runs():
         with pytest.raises(tbp.TbpError):
             tbp.tbp_stash8_dw_plan(*bad)
     _refused(tbp.lib().tbp_stash8_dw_plan(1, 1, 1, 1, None, C.byref(C.c_int())), "null")
+
+
+def test_heads_that_a_thread_of_the_norms_takes():
+    per = tbp.lib().tbp_qk_norm_heads_per_thread
+    assert per(BF16, 8192, 32, 8, 128) == 4 == per(F32, 1 << 22, 1, 0, 512) and per(BF16, 16, 32, 8, 128) == 1 == per(F32, 0, 4, 2, 64)
+    assert per(BF16, -1, 4, 2, 64) == 0 == per(BF16, 4, 4, 2, 0)
