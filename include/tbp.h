@@ -437,6 +437,16 @@ tbp_status tbp_packed_attention_p1(int dtype, int n_seqs, int rows, int n_heads,
                                    const void* qkv, int ld_qkv, const void* out, const void* d_out, int ld_out, const float* lse,
                                    void* dqkv, int ld_dqkv, void* scratch, void* stream);
 
+/* How the two run (host only; for tests and measurements). */
+typedef struct {
+  int32_t query_heads, key_shares; /* forward and dq: query heads of a key head that share a workgroup; waves that share a query's keys, 1 or 2 */
+  int32_t scores_ahead;            /* forward: scores of the next block of keys ahead of its turn */
+  int32_t queries_most_first;      /* forward and dq: blocks of queries the most work first, 0: in the order of the rows */
+  int32_t keys, parts;             /* dk and dv: keys of a workgroup, parts that its queries are cut into */
+  int32_t keys_most_first;         /* dk and dv: blocks of keys the most work first */
+} tbp_packed_plan;
+tbp_status tbp_packed_attention_plan(int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, tbp_packed_plan* plan);
+
 /* A stash in 8 bits of one tensor (a linear layer's input or output derivative, kept from backward-p1 to backward-p2): `slots` micro-batches of
  * [tokens, cols] each.  Of every 1024 tokens of a column, counted from a slot's first, the values are held as q 2^e: q = -127 .. 127 an
  * 8-bit integer, rounded to the nearest, halves to even; e the smallest exponent, -126 .. 121, with which the largest of them is in that range (values above 127 2^121 are held as that).

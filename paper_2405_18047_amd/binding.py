@@ -133,6 +133,7 @@ def lib() -> C.CDLL:
         L.tbp_qk_norm_p1.argtypes = [i32] * 5 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, i32, ptr, ptr]
         L.tbp_qk_norm_append.argtypes = [i32] * 6 + [f32, ptr, ptr, i32, i32, ptr, i32, ptr, ptr, i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]
         L.tbp_packed_attention_fwd.argtypes = [i32] * 6 + [ptr, ptr, i32, ptr, i32, ptr, ptr]
+        L.tbp_packed_attention_plan.argtypes = [i32] * 5 + [ptr]
         L.tbp_packed_attention_p1_scratch_bytes.argtypes, L.tbp_packed_attention_p1_scratch_bytes.restype = [i32] * 5, size
         L.tbp_packed_attention_p1.argtypes = [i32] * 6 + [ptr, ptr, i32, ptr, ptr, i32, ptr, ptr, i32, ptr, ptr]
         L.tbp_stash8_bytes.argtypes, L.tbp_stash8_bytes.restype = [i32] * 3, size

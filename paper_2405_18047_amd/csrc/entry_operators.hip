@@ -430,6 +430,14 @@ tbp_status tbp_packed_attention_fwd(int dtype, int n_seqs, int rows, int n_heads
   return TBP_OK;
 }
 
+tbp_status tbp_packed_attention_plan(int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim, tbp_packed_plan* plan) {
+  if (!plan) return fail(TBP_EINVAL, "plan must be non-null");
+  if (check_packed(TBP_BF16, n_seqs, rows, n_heads, n_kv_heads, head_dim) != TBP_OK) return TBP_EINVAL;
+  const tbp::PackedPlan p = tbp::packed_plan(tbp::PackedShape{nullptr, n_seqs, rows, n_heads, n_kv_heads, head_dim});
+  *plan = tbp_packed_plan{p.query_heads, p.key_shares, p.scores_ahead, p.queries_most_first, p.keys, p.parts, p.keys_most_first};
+  return TBP_OK;
+}
+
 size_t tbp_packed_attention_p1_scratch_bytes(int n_seqs, int rows, int n_heads, int n_kv_heads, int head_dim) {
   if (rows < 1 || check_packed(TBP_BF16, n_seqs, rows, n_heads, n_kv_heads, head_dim) != TBP_OK) return 0;
   return delta_bytes(1, n_heads, rows) + tbp::packed_attention_p1_partial_bytes(tbp::PackedShape{nullptr, n_seqs, rows, n_heads, n_kv_heads, head_dim});

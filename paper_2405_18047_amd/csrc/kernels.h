@@ -249,6 +249,8 @@ hipError_t window_decode(const WindowShape& w, int capacity, const int* lengths,
 
 // ---- causal attention over packed sequences (the same kernels), see include/tbp.h ------------------------------------------------
 struct PackedShape { const int* starts; int seqs, rows, heads, kv_heads, head_dim; };
+struct PackedPlan { int query_heads, key_shares, scores_ahead, queries_most_first, keys, parts, keys_most_first; };      // tbp_packed_plan
+PackedPlan packed_plan(const PackedShape& w);
 size_t packed_attention_p1_partial_bytes(const PackedShape& w);
 hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s);
 hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qkv, const void* out, const void* d_out, long ld_out, const float* lse,

@@ -1409,33 +1409,6 @@ static bool queries_by_work(const PackedShape& w) {
 static bool keys_by_work(const PackedShape& w) { return w.seqs <= 64 && (w.head_dim == 128 || w.rows >= 192 * w.seqs); }
 
 template <int N> using Int = std::integral_constant<int, N>;
-// run(head_dim, query heads of a workgroup): as many as their number allows
-template <typename F> static hipError_t by_heads(const PackedShape& w, F run) {
-  const int G = w.heads / w.kv_heads;
-  if (w.head_dim == 64) return G % 4 == 0 ? run(Int<64>(), Int<4>()) : G % 2 == 0 ? run(Int<64>(), Int<2>()) : run(Int<64>(), Int<1>());
-  return G % 4 == 0 ? run(Int<128>(), Int<4>()) : G % 2 == 0 ? run(Int<128>(), Int<2>()) : run(Int<128>(), Int<1>());
-}
-
-hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s) {
-  WinParams p{};
-  p.qkv = (const bf16_t*)qkv; p.ld_qkv = ld_qkv; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.packed = packed_of(w);
-  p.B = 1; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.rows;
-  p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
-  const long groups = w.heads * ((long)w.rows / 128 + w.seqs);
-  const int mean = w.rows / (w.seqs > 0 ? w.seqs : 1);
-  // scores ahead where sequences have several blocks of keys: us, ahead / not, 32 heads on 8 of 128: 5 sequences of 1639 141 / 149, 16 on 16, 6 of 683 on average 48 / 53,
-  // 60 of 130 67 / 67
-  const bool few = groups <= (w.head_dim == 64 ? 512 : 256), ahead = w.head_dim == 128 && mean > 256, by_work = queries_by_work(w);
-  auto run = [&](auto dh, auto hw) {
-    constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
-    if (few) return launch_fwd<DH, false, 2, HW < 2 ? 1 : 2, kInOrder>(p, s);
-    if constexpr (DH == 128 && HW > 1) if (ahead && by_work) return launch_fwd<DH, true, 1, HW, kMostFirst>(p, s);
-    if constexpr (DH == 128) if (ahead) return launch_fwd<DH, true, 1, HW, kInOrder>(p, s);
-    if constexpr (HW > 1) if (by_work) return launch_fwd<DH, false, 1, HW, kMostFirst>(p, s);
-    return launch_fwd<DH, false, 1, HW, kInOrder>(p, s);
-  };
-  return by_heads(w, run);
-}
 
 // Keys to a block and parts of a block's list of (query head, query step) pairs.
 static WindowParts packed_parts(const PackedShape& w) {
@@ -1454,9 +1427,48 @@ static WindowParts packed_parts(const PackedShape& w) {
   return r;
 }
 
+PackedPlan packed_plan(const PackedShape& w) {
+  const int G = w.heads / w.kv_heads, heads = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1, mean = w.rows / (w.seqs > 0 ? w.seqs : 1);
+  const WindowParts keys = packed_parts(w);
+  PackedPlan p{heads, 1, 0, 0, keys.keys, keys.other_parts, keys_by_work(w)};
+  // 64 (query, head) rows to a workgroup where those of 128 leave compute units short of work, as for windows
+  if (w.heads * ((long)w.rows / 128 + w.seqs) <= (w.head_dim == 64 ? 512 : 256)) {
+    p.query_heads = heads < 2 ? 1 : 2;
+    p.key_shares = 2;
+    return p;
+  }
+  // scores ahead where sequences have several blocks of keys: us, ahead / not, 32 heads on 8 of 128: 5 sequences of 1639 141 / 149, 16 on 16, 6 of 683 on average 48 / 53,
+  // 60 of 130 67 / 67
+  p.scores_ahead = w.head_dim == 128 && mean > 256;
+  p.queries_most_first = queries_by_work(w);
+  return p;
+}
+
 size_t packed_attention_p1_partial_bytes(const PackedShape& w) {
   const WindowParts r = packed_parts(w);
   return r.other_parts == 1 ? 0 : (size_t)w.kv_heads * packed_blocks(packed_of(w), r.keys) * r.other_parts * 2 * r.keys * w.head_dim * sizeof(float);
+}
+
+// run(head_dim, query heads of a workgroup)
+template <typename F> static hipError_t by_heads(const PackedShape& w, const PackedPlan& plan, F run) {
+  if (w.head_dim == 64) return plan.query_heads == 4 ? run(Int<64>(), Int<4>()) : plan.query_heads == 2 ? run(Int<64>(), Int<2>()) : run(Int<64>(), Int<1>());
+  return plan.query_heads == 4 ? run(Int<128>(), Int<4>()) : plan.query_heads == 2 ? run(Int<128>(), Int<2>()) : run(Int<128>(), Int<1>());
+}
+
+hipError_t packed_attention_fwd(const PackedShape& w, const void* qkv, long ld_qkv, void* out, long ld_out, float* lse, hipStream_t s) {
+  WinParams p{};
+  p.qkv = (const bf16_t*)qkv; p.ld_qkv = ld_qkv; p.out = (bf16_t*)out; p.ld_out = ld_out; p.lse = lse; p.packed = packed_of(w);
+  p.B = 1; p.H = w.heads; p.KV = w.kv_heads; p.G = w.heads / w.kv_heads; p.S = w.rows;
+  p.scale_log2e = 1.4426950408889634f / sqrtf((float)w.head_dim);
+  const PackedPlan plan = packed_plan(w);
+  return by_heads(w, plan, [&](auto dh, auto hw) {
+    constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
+    if constexpr (HW < 4) if (plan.key_shares == 2) return launch_fwd<DH, false, 2, HW, kInOrder>(p, s);
+    if constexpr (DH == 128 && HW > 1) if (plan.scores_ahead && plan.queries_most_first) return launch_fwd<DH, true, 1, HW, kMostFirst>(p, s);
+    if constexpr (DH == 128) if (plan.scores_ahead) return launch_fwd<DH, true, 1, HW, kInOrder>(p, s);
+    if constexpr (HW > 1) if (plan.queries_most_first) return launch_fwd<DH, false, 1, HW, kMostFirst>(p, s);
+    return launch_fwd<DH, false, 1, HW, kInOrder>(p, s);
+  });
 }
 
 hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qkv, const void* out, const void* d_out, long ld_out, const float* lse,
@@ -1467,11 +1479,11 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
   q.B = 1; q.H = w.heads; q.KV = w.kv_heads; q.G = w.heads / w.kv_heads; q.S = w.rows;
   q.scale = 1.f / sqrtf((float)w.head_dim);
   q.scale_log2e = 1.4426950408889634f * q.scale;
-  const bool few = (long)w.heads * (w.rows / 128 + w.seqs) <= (w.head_dim == 64 ? 512 : 256), by_work = queries_by_work(w);
-  hipError_t e = by_heads(w, [&](auto dh, auto hw) {
+  const PackedPlan plan = packed_plan(w);
+  hipError_t e = by_heads(w, plan, [&](auto dh, auto hw) {
     constexpr int DH = decltype(dh)::value, HW = decltype(hw)::value;
-    if (few) return launch_dq<DH, 2, HW < 2 ? 1 : 2, kInOrder>(q, s);
-    if constexpr (HW > 1) if (by_work) return launch_dq<DH, 1, HW, kMostFirst>(q, s);
+    if constexpr (HW < 4) if (plan.key_shares == 2) return launch_dq<DH, 2, HW, kInOrder>(q, s);
+    if constexpr (HW > 1) if (plan.queries_most_first) return launch_dq<DH, 1, HW, kMostFirst>(q, s);
     return launch_dq<DH, 1, HW, kInOrder>(q, s);
   });
   if (e != hipSuccess) return e;
@@ -1486,7 +1498,7 @@ hipError_t packed_attention_p1(const PackedShape& w, const void* qkv, long ld_qk
     if (w.head_dim == 64) return launch_kv<64, 64, PACKED>(p, s);
     return p.parts.keys == 64 ? launch_kv<128, 64, PACKED>(p, s) : launch_kv<128, 128, PACKED>(p, s);
   };
-  return keys_by_work(w) ? run(Int<kMostFirst>()) : run(Int<kInOrder>());
+  return plan.keys_most_first ? run(Int<kMostFirst>()) : run(Int<kInOrder>());
 }
 
 // Shares of a head's keys, at most: as many as make the rounds of workgroups (one per compute unit at head_dim 128, two at 64) short by this model, whose

@@ -19,7 +19,7 @@ __all__ = [
     "TBP_ROTARY_HALF", "TBP_ROTARY_INTERLEAVED", "TBP_ROTARY_PLAIN", "TBP_ROTARY_LINEAR", "TBP_ROTARY_BASE", "TBP_ROTARY_RAMP",
     "tbp_rotary_scale", "tbp_rotary_table", "tbp_rotary", "tbp_rotary_append", "tbp_window_attention_fwd", "tbp_window_attention_p1",
     "tbp_window_decode_workspace", "tbp_window_decode", "tbp_logprobs", "tbp_logprobs_p1", "tbp_logprobs_step", "GradList",
-    "tbp_qk_norm", "tbp_qk_norm_p1", "tbp_qk_norm_append", "tbp_packed_attention_fwd", "tbp_packed_attention_p1", "Stash8", "tbp_stash8_dw", "tbp_stash8_dw_plan",
+    "tbp_qk_norm", "tbp_qk_norm_p1", "tbp_qk_norm_append", "tbp_packed_attention_fwd", "tbp_packed_attention_p1", "tbp_packed_plan", "tbp_packed_attention_plan", "Stash8", "tbp_stash8_dw", "tbp_stash8_dw_plan",
 ]
 
 TBP_ROTARY_HALF, TBP_ROTARY_INTERLEAVED = 0, 1
@@ -32,6 +32,10 @@ _CODE = {torch.bfloat16: TBP_BF16, torch.float32: TBP_F32}
 class tbp_rotary_scale(C.Structure):
     _fields_ = [("scaling", C.c_int32), ("factor", C.c_float), ("low", C.c_float), ("high", C.c_float), ("original", C.c_float),
                 ("magnitude", C.c_float)]
+
+
+class tbp_packed_plan(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("query_heads", "key_shares", "scores_ahead", "queries_most_first", "keys", "parts", "keys_most_first")]
 
 
 def _dt(t):
@@ -477,6 +481,13 @@ def tbp_packed_attention_p1(qkv, out, d_out, lse, starts, n_heads, n_kv_heads, h
                                      _vector(lse, n_heads * rows, _F32, "lse"), dqkv.data_ptr(), ld_dqkv, at,
                                      _stream_of(qkv.get_device(), starts, out, d_out, lse, *given)))
     return dqkv
+
+
+def tbp_packed_attention_plan(n_seqs, rows, n_heads, n_kv_heads, head_dim):
+    """How forward and backward-p1 run: a tbp_packed_plan."""
+    plan = tbp_packed_plan()
+    _check(lib().tbp_packed_attention_plan(n_seqs, rows, n_heads, n_kv_heads, head_dim, C.byref(plan)))
+    return plan
 
 
 # ---- a stash in 8 bits -----------------------------------------------------------------------------------------------------------

@@ -309,6 +309,41 @@ def test_packed_attention_in_the_order_of_the_work_matches_oracle(case):
     test_packed_attention_matches_oracle(case)
 
 
+def _ways(case):
+    """How the launches of a case run: (kernel, head_dim, ..) as tbp_packed_plan says."""
+    lengths, behind, H, KV, dh = case
+    p = tbp.tbp_packed_attention_plan(len(lengths), sum(lengths) + behind, H, KV, dh)
+    queries = dh, p.query_heads, p.key_shares, p.queries_most_first
+    return {("fwd", *queries, p.scores_ahead), ("dq", *queries), ("kv", dh, p.keys, p.parts > 1, p.keys_most_first)}
+
+
+# one way each that the cases above do not take
+WAYS = [
+    (([37, 1, 0, 130, 200, 64, 31, 33, 65, 2, 129, 128] * 3, 3, 16, 8, 128), ("fwd", 128, 2, 1, 0, 0)),
+    (([400, 1, 420, 260, 390, 301, 64] * 5, 1, 4, 2, 128), ("fwd", 128, 2, 1, 0, 1)),
+    (([200, 1, 0, 129, 64, 33, 170, 250, 31, 65, 220], 5, 16, 4, 128), ("fwd", 128, 4, 1, 1, 0)),
+    (([37, 130, 1, 0, 64, 65, 31] * 10, 2, 4, 4, 128), ("kv", 128, 64, False, 0)),
+    (([200, 129, 260, 1, 300, 310] * 11, 7, 8, 1, 128), ("kv", 128, 64, True, 0)),
+    (([800, 1100, 640, 129, 1400] * 13, 2, 2, 1, 128), ("kv", 128, 128, False, 0)),
+    (([800, 1100, 640, 129, 1400] * 13, 2, 4, 1, 128), ("kv", 128, 128, True, 0)),
+    (([1400, 1300, 1396], 0, 32, 8, 128), ("kv", 128, 128, True, 1)),
+]
+
+
+@pytest.mark.parametrize("case,way", WAYS, ids=lambda c: "-".join(map(str, c)) if isinstance(c[0], str) else "")
+def test_packed_attention_runs_every_way(case, way):
+    assert way in _ways(case)
+    test_packed_attention_matches_oracle(case)
+
+
+def test_the_cases_of_packed_attention_run_every_way():
+    each = [(dh, hw) for dh in (64, 128) for hw in (1, 2, 4)]
+    queries = {(dh, hw, 2, 0) for dh, hw in each if hw < 4} | {(dh, hw, 1, most) for dh, hw in each for most in (0, 1) if hw > 1 or not most}
+    every = {("dq", *q) for q in queries} | {("fwd", *q, 0) for q in queries} | {("fwd", *q, 1) for q in queries if q[0] == 128 and q[2] == 1}
+    every |= {("kv", *k, cut, most) for k in ((64, 64), (128, 64), (128, 128)) for cut in (False, True) for most in (0, 1)}
+    assert set.union(*(_ways(c) for c in PACKED_CASES + BY_WORK_CASES + [c for c, _ in WAYS])) == every
+
+
 def test_packed_attention_of_heads_that_share_keys_over_a_very_long_sequence():
     """More query blocks of a sequence than are looked through at once, at any level."""
     n, m, H, KV, dh = 70000, 600, 4, 1, 64

@@ -197,3 +197,13 @@ def test_heads_that_a_thread_of_the_norms_takes():
     per = tbp.lib().tbp_qk_norm_heads_per_thread
     assert per(BF16, 8192, 32, 8, 128) == 4 == per(F32, 1 << 22, 1, 0, 512) and per(BF16, 16, 32, 8, 128) == 1 == per(F32, 0, 4, 2, 64)
     assert per(BF16, -1, 4, 2, 64) == 0 == per(BF16, 4, 4, 2, 0)
+
+
+def test_how_packed_attention_runs():
+    p = tbp.tbp_packed_attention_plan(1, 200, 32, 8, 128)
+    assert (p.query_heads, p.key_shares, p.scores_ahead, p.queries_most_first, p.keys) == (2, 2, 0, 0, 64) and p.parts > 1
+    p = tbp.tbp_packed_attention_plan(1000, 1 << 17, 6, 2, 64)
+    assert (p.query_heads, p.key_shares, p.scores_ahead, p.queries_most_first, p.keys, p.parts, p.keys_most_first) == (1, 1, 0, 0, 64, 1, 0)
+    with pytest.raises(tbp.TbpError, match="head_dim"):
+        tbp.tbp_packed_attention_plan(1, 200, 32, 8, 96)
+    _refused(tbp.lib().tbp_packed_attention_plan(1, 200, 32, 8, 128, None), "null")
