@@ -1396,17 +1396,28 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
 // ---- packed sequences: the same kernels, by rules on the mean length, since the lengths are on the device
 static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, w.rows}; }
 
-// Whether blocks come the most work first whatever their sequence, or by their rows.  The last workgroups then are short ones: by rows, of 5 sequences of 1639 tokens
-// the forward's last sixth ran with half of the places empty.  The most first costs the finding of a block among its sequences (a third of a us of each), and keys and values
-// that are met again later, so not where those of the heads that an L2 works on exceed its 4 MiB.  A rule of the launch: with both orders in one kernel it was 4 % slower.
-// us of the forward, in order / the most first, of 128: 32 heads on 8, 3 sequences of 1365 66.0 / 60.1, 5 of 1639 139 / 136, 24 of 8192 in all 76 / 74, but 24 of 16384 174 / 183, 32 of
-// 8192 70.8 / 73.1; 16 on 8, 5 of 1639 77 / 66, 24 of 8192 52.7 / 48.7; 16 on 16, 6 of 4096 49 / 51; of 64: 32 on 8, 24 of 8192 41.5 / 36.7, but 64 of 128 19.7 / 20.3.
-static bool queries_by_work(const PackedShape& w) {
-  return w.seqs > 1 && w.seqs <= 24 && w.heads / w.kv_heads % 2 == 0 && (long)w.kv_heads * w.rows * w.head_dim <= 1 << 23;
+// Whether blocks come the most work first whatever their sequence, or by their rows.  The last workgroups then are short ones; but a block has to be found among its
+// sequences (a third of a us of each), and keys and values are met again later.  A rule of the launch, which does not know the lengths: with both orders in one kernel
+// it was 4 % slower.
+// Blocks of queries, `hw` heads to a workgroup: where an XCD has one group of heads (ids go round the 8 of them), keys and values are 32 MiB at most, and sequences few: up to 24 where
+// the workgroups are two and a half rounds of the card's places, else up to 8.  us of the forward, in order / the most first, lengths all alike and up to 30 times apart.
+// Of 128, 16 heads on 8, 8192 rows: 8 sequences 55 / 48 and 77 / 67, 24 34 / 36 and 43 / 39; 16 on 4: 12 42 / 38 and 63 / 55; 32 on 8, 4096 rows: 5 45 / 41 and
+// 75 / 73, 12 29 / 30 and 40 / 39; more rounds: 32 on 8, 8192 rows: 5 131 / 129 and 260 / 257, 8 94 / 93 and 134 / 132, but 12 75 / 79 and 84 / 89, 24 54 / 62 and 71 / 74.
+// More groups: 64 on 8, 4096 rows: 5 80 / 85 and 91 / 96; 64 on 16: 8 63 / 73 and 84 / 86.  At 32 MiB, lengths apart: 8 on 1, 65536 rows, 5 and 20 1947 / 1948 and
+// 972 / 987; 32 on 4, 16384 651 / 656 and 221 / 227.  Of 64, 32 on 8, 8192 rows: 8 52 / 47 and 91 / 82, 24 27 / 29 and 43 / 39; 16384 rows: 8 173 / 161 and 215 / 200, 32 63 / 66 and 84 / 88.
+static bool queries_by_work(const PackedShape& w, int hw) {
+  const long groups = w.heads / hw, workgroups = groups * ((long)w.rows * hw / 128 + w.seqs), places = w.head_dim == 64 ? 1024 : 512;
+  return hw > 1 && w.seqs > 1 && groups <= 8 && (long)w.kv_heads * w.rows * w.head_dim <= 1 << 23 && w.seqs <= (2 * workgroups <= 5 * places ? 24 : 8);
 }
-// us of the backward, in order / the most first: 32 heads on 8 of 128, 5 sequences of 1639 529 / 484, 16 and 24 of 8192 in all 311 / 286 and 298 / 291, 64 of 4000 91 / 80, but 32 of 128
-// 59.7 / 61.4; 32 on 8 of 64, 24 of 8192 144 / 124, 40 of 16384 297 / 279, 20 of 200 33.5 / 30.5, but 64 of 128 60.1 / 64.9, 30 of 67 24.4 / 26.2
-static bool keys_by_work(const PackedShape& w) { return w.seqs <= 64 && (w.head_dim == 128 || w.rows >= 192 * w.seqs); }
+// Blocks of keys.  us of the backward, in order / the most first, lengths as above.  Of 128, 32 heads on 8: 8 sequences of 4096 rows in all 111 / 97 alike, 16 of 4000 80 / 75 and 107 / 98, 64 of
+// 12800 262 / 247 and 288 / 277, but 64 of 8192 120 / 130 and 165 / 159 (alike, of 128 tokens, the slower side at every number: accepted for the others); 24 on 8: 48 of 8192
+// 135 / 130 and 158 / 149, but 64 110 / 118 and 150 / 151; 8 on 8: 6 of 8192 136 / 123 and 189 / 177, but 16 75 / 78 and 101 / 104, 64 66 / 77 and 85 / 87; 16 on 16:
+// 4 of 4096 103 / 96 and 136 / 133, but 16 of 8192 136 / 152 and 188 / 199; 32 on 16: 48 of 8192 159 / 183 and 192 / 206.  Of 64, 32 on 8: 32 of 8192 84 / 81 and 141 / 114, 64 of 16384
+// 151 / 152 and 245 / 224; 16 on 8: 48 113 / 115 and 144 / 141, but 64 96 / 104 and 142 / 137; below 192 tokens on average 32 on 8, 64 of 8192 68 / 71 alike; 12 on 4, 30 of 67 24.4 / 26.2.
+static bool keys_by_work(const PackedShape& w) {
+  const int G = w.heads / w.kv_heads, most = G == 1 || w.kv_heads > 8 ? 8 : G < 4 ? 48 : 64;
+  return w.seqs <= most && (w.head_dim == 128 || w.rows >= 192 * w.seqs);
+}
 
 template <int N> using Int = std::integral_constant<int, N>;
 
@@ -1440,7 +1451,7 @@ PackedPlan packed_plan(const PackedShape& w) {
   // scores ahead where sequences have several blocks of keys: us, ahead / not, 32 heads on 8 of 128: 5 sequences of 1639 141 / 149, 16 on 16, 6 of 683 on average 48 / 53,
   // 60 of 130 67 / 67
   p.scores_ahead = w.head_dim == 128 && mean > 256;
-  p.queries_most_first = queries_by_work(w);
+  p.queries_most_first = queries_by_work(w, heads);
   return p;
 }
 

@@ -327,6 +327,7 @@ WAYS = [
     (([800, 1100, 640, 129, 1400] * 13, 2, 2, 1, 128), ("kv", 128, 128, False, 0)),
     (([800, 1100, 640, 129, 1400] * 13, 2, 4, 1, 128), ("kv", 128, 128, True, 0)),
     (([1400, 1300, 1396], 0, 32, 8, 128), ("kv", 128, 128, True, 1)),
+    (([1300, 1, 40, 700, 65, 1000, 0, 330], 3, 16, 8, 64), ("fwd", 64, 2, 1, 1, 0)),
 ]
 
 
