@@ -400,7 +400,8 @@ tbp_status tbp_grad_clip(int dtype, int out_dtype, int n, const void* const* gra
 
 /* Norms of the query and key heads, and the rotary positions in the same pass: of every head y = R (x / sqrt(mean(x^2) + eps) * g),
  * g the gains gq (query heads) or gk (key heads), device [head_dim] in the storage type, R the rotation of the first rot_dim columns as
- * for tbp_rotary (rot_dim 0: none, table not read).  x [rows, ld_x]: column blocks q [n_heads*head_dim] | k [n_kv_heads*head_dim];
+ * for tbp_rotary (rot_dim 0: none, table not read).  The squares are added up in fp32: a head whose sum passes its range (values of about 1e18 and more) norms to
+ * zeros, and its dx is zeros.  x [rows, ld_x]: column blocks q [n_heads*head_dim] | k [n_kv_heads*head_dim];
  * y [rows, ld_y] likewise; y may be x itself (other overlaps not; backward-p1 needs x).  head_dim even, at most 512.  positions, seq,
  * table, layout and positions outside the table as for tbp_rotary.  Any alignment of the element type; 16-byte alignment of rows,
  * pieces and gains is faster. */

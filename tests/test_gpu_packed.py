@@ -172,6 +172,16 @@ def test_a_norm_of_values_that_are_not_finite_stays_in_its_head():
     assert torch.all(torch.isnan(y[1, 64:128])) and torch.all(torch.isnan(dx[1, 64:128]))
 
 
+def test_heads_whose_squares_pass_the_range_norm_to_zeros():
+    H, KV, dh = 3, 1, 64
+    x, dy = (to_dev(_rnd(9, k, (4, 256), "bf16"), "bf16") for k in ("x", "dy"))
+    g = torch.ones(dh, dtype=torch.bfloat16, device=DEV)
+    x[1, 64:128] *= 2.0 ** 70
+    y, dx = tbp.tbp_qk_norm(x, g, g, H, KV, dh, 1e-5), tbp.tbp_qk_norm_p1(dy, x, g, g, H, KV, dh, 1e-5)[0]
+    for t in (y, dx):
+        assert not t[1, 64:128].any() and torch.all(torch.isfinite(t)) and torch.all(t[0] != 0)
+
+
 APPEND_CASES = [  # batch, n_new, H, KV, dh, rot, layout, dtype, capacity, sinks, lengths
     (1, 1, 1, 1, 64, 64, 0, "bf16", 3, 0, [1]), (3, 1, 4, 2, 128, 128, 0, "bf16", 9, 2, [1, 40, 0]), (2, 5, 2, 1, 96, 32, 1, "f32", 4, 1, [3, 17]),
     (4, 3, 3, 3, 62, 30, 1, "bf16", 7, 0, [3, 2, 30, -5]), (2, 40, 8, 2, 64, 0, 0, "bf16", 16, 4, [40, 60]), (16, 1, 32, 8, 128, 128, 0, "bf16", 30, 4, list(range(20, 36))),
