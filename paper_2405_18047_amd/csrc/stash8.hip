@@ -3,7 +3,8 @@
 //
 // Of every kStash8Block tokens of a column (counted from a slot's first token) the values are q 2^e with q = -127 .. 127 and e the smallest exponent,
 // -126 at least, with which the largest of them is in that range (121 at most: beyond, q ends at 127); q is the nearest integer, halves to even.  Powers of two, so that scaling is exact and
-// the one rounding is q's: at most half of 2^e, which is at most 2^-6 of the block's largest value.
+// the one rounding is q's: at most half of 2^e.  For e above -126 the largest value is above 127 2^(e - 1), so that 2^e is below 1/63.5 of it; at -126 the half step is 2^-127,
+// whatever the values; at 121 a value above 127 2^121 is off by what it is above that.
 // A block that holds an infinity or a NaN has no such scale: its scale is NaN, and with it all that it stands for.
 //
 // Layout: the matrix instructions want, per column, consecutive tokens.  A unit of 32 columns x 64 tokens is 2 KiB: two halves of 32 tokens, in each the
@@ -253,8 +254,8 @@ __global__ __launch_bounds__(256) void stash8_get_kernel(Stash8Slot p, T* __rest
 // The integer sums of a block of tokens are exact: 1024 x 127^2 is below 2^24, so that they are exact in fp32 as well, in which the blocks are added
 // up, each times the two columns' scales.  That takes three vector instructions per element and block, done tile by tile in front of the tile's first
 // product of the next block (5 % of the time), and a second set of accumulators: 96 x 96 to a wave, one wave to a SIMD, or 64 x 64 and two.
-// Bound by power on large outputs: 11008 x 4096 over 8 x 4096 tokens 1450 to 1720 us over cards, 1.72 to 2.04 PFLOP/s (at the rate of the bf16 weight gradients, 1.29, 2283), at 1.5 to 1.9 GHz with
-// the matrix pipes busy 52 %; the same instructions on zeros take 7 % fewer cycles, at 2.27 GHz.  Rounds of few steps by their start and end (8 us): 4096 x 4096 over 4096
+// Bound by power on large outputs: 11008 x 4096 over 8 x 4096 tokens 1440 to 1720 us over cards, 1.72 to 2.05 PFLOP/s (at the rate of the bf16 weight gradients, 1.29, 2283), at 1.5 to 1.9 GHz with
+// the matrix pipes busy 54 %; the same instructions on zeros take 7 % fewer cycles, at 2.27 GHz.  Rounds of few steps by their start and end (8 us): 4096 x 4096 over 4096
 // tokens 80 us, 1.7 PFLOP/s.  Tried without gain: copies spread over all of a step's products; tiles of 128 x 96 and 128 x 64 to a wave (1594 and 1653 us for 1588).
 constexpr int dw_slots(int mb, int nb, int per_cu) { return (160 * 1024 / per_cu - 8 * 2048) / (2 * (mb + nb) * kUnit); }
 struct Stash8Dw {

@@ -1397,7 +1397,7 @@ hipError_t window_attention_p1(const WindowShape& w, const int* lengths, const v
 static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, w.rows}; }
 
 // Whether blocks come the most work first whatever their sequence, or by their rows.  The last workgroups then are short ones; but a block has to be found among its
-// sequences (a third of a us of each), and keys and values are met again later.  A rule of the launch, which does not know the lengths: with both orders in one kernel
+// sequences (0.95 us of each, of 5 sequences, by rows 0.5), and keys and values are met again later.  A rule of the launch, which does not know the lengths: with both orders in one kernel
 // it was 4 % slower.
 // Blocks of queries, `hw` heads to a workgroup: where an XCD has one group of heads (ids go round the 8 of them), keys and values are 32 MiB at most, and sequences few: up to 24 where
 // the workgroups are two and a half rounds of the card's places, else up to 8.  us of the forward, in order / the most first, lengths all alike and up to 30 times apart.
