@@ -327,7 +327,7 @@ def _ways(case):
     return {("fwd", *queries, p.scores_ahead), ("dq", *queries), ("kv", dh, p.keys, p.parts > 1, p.keys_most_first)}
 
 
-# one way each that the cases above do not take
+# one way each that the cases above do not take, or, of keys in the order of the rows, not in few sequences
 WAYS = [
     (([37, 1, 0, 130, 200, 64, 31, 33, 65, 2, 129, 128] * 3, 3, 16, 8, 128), ("fwd", 128, 2, 1, 0, 0)),
     (([400, 1, 420, 260, 390, 301, 64] * 5, 1, 4, 2, 128), ("fwd", 128, 2, 1, 0, 1)),
@@ -337,6 +337,7 @@ WAYS = [
     (([800, 1100, 640, 129, 1400] * 13, 2, 2, 1, 128), ("kv", 128, 128, False, 0)),
     (([800, 1100, 640, 129, 1400] * 13, 2, 4, 1, 128), ("kv", 128, 128, True, 0)),
     (([1400, 1300, 1396], 0, 32, 8, 128), ("kv", 128, 128, True, 1)),
+    (([300, 1, 0, 129, 128, 640, 33, 257, 64, 65, 500, 31], 3, 4, 4, 128), ("kv", 128, 64, False, 0)), (([900, 1200, 129, 1000, 700, 1, 1100, 800, 1400], 2, 4, 4, 128), ("kv", 128, 128, False, 0)),
     (([1300, 1, 40, 700, 65, 1000, 0, 330], 3, 16, 8, 64), ("fwd", 64, 2, 1, 1, 0)),
 ]
 

@@ -212,7 +212,7 @@ def test_how_packed_attention_runs():
 def test_packed_attention_takes_the_order_that_measured_faster():
     order = lambda *size: (lambda p: (p.queries_most_first, p.keys_most_first))(tbp.tbp_packed_attention_plan(*size))
     # sequences, rows, heads, key heads, head_dim: 4 and more percent between the two, whether lengths are alike or far apart (queries), or both
-    for size, queries in (((8, 8192, 16, 8, 128), 1), ((12, 8192, 16, 4, 128), 1), ((5, 4096, 32, 8, 128), 1), ((12, 8192, 32, 8, 128), 0), ((24, 8192, 32, 8, 128), 0), ((5, 4096, 64, 8, 128), 0),
+    for size, queries in (((8, 8192, 16, 8, 128), 1), ((12, 8192, 16, 4, 128), 1), ((12, 32768, 8, 1, 128), 1), ((24, 32768, 8, 2, 64), 1), ((24, 8192, 32, 4, 128), 0), ((5, 4096, 32, 8, 128), 1), ((12, 8192, 32, 8, 128), 0), ((24, 8192, 32, 8, 128), 0), ((5, 4096, 64, 8, 128), 0),
                           ((8, 4096, 64, 16, 128), 0), ((8, 8192, 32, 8, 64), 1), ((8, 16384, 32, 8, 64), 1), ((32, 16384, 32, 8, 64), 0), ((24, 8192, 64, 16, 64), 0)):
         assert order(*size)[0] == queries, size
     for size, keys in (((8, 4096, 32, 8, 128), 1), ((16, 4000, 32, 8, 128), 1), ((64, 12800, 32, 8, 128), 1), ((6, 8192, 8, 8, 128), 1), ((64, 8192, 8, 8, 128), 0), ((16, 8192, 16, 16, 128), 0),
