@@ -408,7 +408,7 @@ tbp_status tbp_grad_clip(int dtype, int out_dtype, int n, const void* const* gra
 tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim, float eps, const void* gq, const void* gk,
                        int rot_dim, int layout, const void* table, int n_pos, const int32_t* positions, int seq, const void* x,
                        int ld_x, void* y, int ld_y, void* stream);
-/* Heads that a thread of it, or of tbp_qk_norm_append, takes in 16-byte pieces (host only; for tests and measurements); other rows: one. */
+/* Heads that a thread of it, or of tbp_qk_norm_append, takes in 16-byte pieces (host only; for tests and measurements; 0 where there is no such call); other rows: one. */
 int tbp_qk_norm_heads_per_thread(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim);
 /* Its backward-p1 (Section 3.1): dx [rows, ld_dx] from dy [rows, ld_dy] and the forward's x; dx may be dy itself.  The gains' gradient
  * is backward-p2 work and is left, as by tbp_rmsnorm_p1_partials, as tbp_qk_norm_partial_rows(rows, n_heads, n_kv_heads, head_dim) partial

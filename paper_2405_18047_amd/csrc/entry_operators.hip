@@ -355,7 +355,8 @@ tbp_status tbp_qk_norm(int dtype, int rows, int n_heads, int n_kv_heads, int hea
 }
 
 int tbp_qk_norm_heads_per_thread(int dtype, int rows, int n_heads, int n_kv_heads, int head_dim) {
-  if (rows < 0 || n_heads < 0 || n_kv_heads < 0 || head_dim < 2) return 0;
+  if (check_storage(dtype) != TBP_OK || rows < 0 || n_heads < 0 || n_kv_heads < 0 || head_dim < 2 || head_dim > tbp::kQkNormMaxHead ||
+      ((long)n_heads + 2L * n_kv_heads) * head_dim >= (1L << 30)) return 0;      // (no such call)
   return tbp::qk_norm_heads_per_thread(dtype, rows, n_heads, n_kv_heads, head_dim);
 }
 

@@ -196,7 +196,7 @@ def test_how_a_weight_gradient_from_the_stash_runs():
 def test_heads_that_a_thread_of_the_norms_takes():
     per = tbp.lib().tbp_qk_norm_heads_per_thread
     assert per(BF16, 8192, 32, 8, 128) == 4 == per(F32, 1 << 22, 1, 0, 512) and per(BF16, 16, 32, 8, 128) == 1 == per(F32, 0, 4, 2, 64)
-    assert per(BF16, -1, 4, 2, 64) == 0 == per(BF16, 4, 4, 2, 0)
+    assert per(BF16, -1, 4, 2, 64) == 0 == per(BF16, 4, 4, 2, 0) and per(7, 4, 4, 2, 64) == 0 == per(BF16, 4, 1 << 25, 2, 64) and per(F32, 4, 4, 2, 514) == 0
 
 
 def test_how_packed_attention_runs():
