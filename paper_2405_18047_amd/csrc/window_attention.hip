@@ -1402,7 +1402,7 @@ static Packed packed_of(const PackedShape& w) { return Packed{w.starts, w.seqs, 
 // Blocks of queries, `hw` heads to a workgroup: where an XCD has one group of heads (ids go round the 8 of them), keys and values are 32 MiB at most, and sequences few: up to 24 where
 // two XCDs share a group or the workgroups are two and a half rounds of the card's places, else up to 8.  us of the forward, in order / the most first, lengths all alike and up to 30 times apart.
 // Of 128, 16 heads on 8, 8192 rows: 8 sequences 55 / 48 and 77 / 67, 24 34 / 36 and 43 / 39; 16 on 4: 12 42 / 38 and 63 / 55; 32 on 8, 4096 rows: 5 45 / 41 and
-// 75 / 73, 12 29 / 30 and 40 / 39; more rounds: 32 on 8, 8192 rows: 5 131 / 129 and 260 / 257, 8 94 / 93 and 134 / 132, but 12 75 / 79 and 84 / 89, 24 54 / 62 and 71 / 74; 32 on 4 alike; two XCDs to a group: 16 on 2,
+// 75 / 73, 12 29 / 30 and 40 / 39; more rounds: 32 on 8, 8192 rows: 5 131 / 129 and 260 / 257, 8 94 / 93 and 134 / 132, but 12 75 / 79 and 84 / 89, 24 54 / 62 and 71 / 74; 32 on 4: 24 56 / 64 and 71 / 74; two XCDs to a group: 16 on 2,
 // 16384 rows, 24 77 / 80 and 126 / 119; 8 on 1, 32768 rows: 12 209 / 193 and 317 / 295, 24 119 / 117 and 184 / 175.
 // More groups: 64 on 8, 4096 rows: 5 80 / 85 and 91 / 96; 64 on 16: 8 63 / 73 and 84 / 86.  At 32 MiB, lengths apart: 8 on 1, 65536 rows, 5 and 20 1947 / 1948 and
 // 972 / 987; 32 on 4, 16384 651 / 656 and 221 / 227.  Of 64, 32 on 8, 8192 rows: 8 52 / 47 and 91 / 82, 24 27 / 29 and 43 / 39; 16384 rows: 8 173 / 161 and 215 / 200, 32 63 / 66 and 84 / 88.
@@ -1411,7 +1411,7 @@ static bool queries_by_work(const PackedShape& w, int hw) {
   return hw > 1 && w.seqs > 1 && groups <= 8 && (long)w.kv_heads * w.rows * w.head_dim <= 1 << 23 && w.seqs <= (groups <= 4 || 2 * workgroups <= 5 * places ? 24 : 8);
 }
 // Blocks of keys.  us of the backward, in order / the most first, lengths as above.  Of 128, 32 heads on 8: 8 sequences of 4096 rows in all 111 / 97 alike, 16 of 4000 80 / 75 and 107 / 98, 64 of
-// 12800 262 / 247 and 288 / 277, but 64 of 8192 120 / 130 and 165 / 159 (alike, of 128 tokens, the slower side at every number: accepted for the others); 24 on 8: 48 of 8192
+// 12800 262 / 247 and 288 / 277, but 64 of 8192 120 / 130 and 165 / 159 (alike and of 128 tokens the slower side, accepted for the others); 24 on 8: 48 of 8192
 // 135 / 130 and 158 / 149, but 64 110 / 118 and 150 / 151; 8 on 8: 6 of 8192 136 / 123 and 189 / 177, but 16 75 / 78 and 101 / 104, 64 66 / 77 and 85 / 87; 16 on 16:
 // 4 of 4096 103 / 96 and 136 / 133, but 16 of 8192 136 / 152 and 188 / 199; 32 on 16: 48 of 8192 159 / 183 and 192 / 206.  Of 64, 32 on 8: 32 of 8192 84 / 81 and 141 / 114, 64 of 16384
 // 151 / 152 and 245 / 224; 16 on 8: 48 113 / 115 and 144 / 141, but 64 96 / 104 and 142 / 137; below 192 tokens on average 32 on 8, 64 of 8192 68 / 71 alike; 12 on 4, 30 of 67 24.4 / 26.2.
